@@ -267,6 +267,168 @@ int sys_conv1d_has(int projection, int k);
 int sys_conv2d_has(int projection, int kh, int kw);
 
 /*
+ * ---- Operators of a state-space mixer layer ------------------------------------------------
+ *
+ * The recurrences above with data of many channels, as layers of sequence models use them: a
+ * short causal convolution of every channel, a scan whose coefficients depend on the data, and
+ * the group norm behind them.  Tensors are channels last, [batch, length, channels] with the
+ * channels of a row next to each other; batch and row strides are the caller's (in elements), so
+ * that a tensor may be a part of the columns of a wider projection.  Inputs may have any strides
+ * (0 for a row or batch that is used again); rows and batches of an output must not overlap.
+ * Elements are fp32, fp16 or bf16 (sys_dtype_t); sums, statistics, exponentials and states are
+ * fp32, and each result is rounded once, where it is stored.  Results do not depend on the run:
+ * there are no atomic sums.
+ *
+ * As everywhere in this library a call validates its arguments before the first HIP call, only
+ * enqueues kernels on `stream`, allocates nothing and keeps nothing.  Some of these operators
+ * combine parts of a long axis in device memory of the caller's: *_workspace gives the bytes for
+ * a call (0: none needed, pass NULL), 4-byte aligned, contents of no matter before or after, not
+ * to be used by calls that may run at the same time.  Optional pointers may be NULL.  Outputs must
+ * not overlap inputs or each other (SYS_ERR_ALIAS; whole ranges from the first to the last element
+ * are compared), except where a state is updated in place.
+ *
+ * d_lengths (optional, device, one int per sequence): only the first lengths[b] positions of
+ * sequence b exist (values are held within 0 .. length).  What lies behind them is not read
+ * into any result, whatever it is, and outputs there are 0; a sequence of length 0 passes its
+ * state on as it is.
+ */
+typedef enum { SYS_F32 = 0, SYS_F16 = 1, SYS_BF16 = 2 } sys_dtype_t;
+
+/* x; x / (1 + e^-x); max(x, 0) */
+typedef enum { SYS_ACT_NONE = 0, SYS_ACT_SILU = 1, SYS_ACT_RELU = 2 } sys_activation_t;
+
+#define SYS_MAX_CAUSAL_WIDTH 8   /* taps of the causal convolution: 2 .. 8 */
+#define SYS_MAX_STATES 64        /* states a channel of the selective scan: 1 .. 64 */
+
+typedef struct {
+    int dtype;                   /* of x, y, states and their gradients */
+    int param_dtype;             /* of w, bias and their gradients: dtype or SYS_F32 */
+    int activation;              /* SYS_ACT_NONE or SYS_ACT_SILU */
+    int width;                   /* taps a channel */
+    int batch, length, channels; /* batch, length >= 0 */
+    int slots;                   /* sys_causal_conv1d_update: states in d_state; else ignored */
+    long long x_batch, x_row;    /* strides of x */
+    long long y_batch, y_row;    /* strides of y (backward: of dy) */
+} sys_causal_conv1d_t;
+
+/*
+ * Causal convolution of every channel with taps of its own:
+ *   d_y[b,t,c] = act(bias[c] + sum_{j<width} w[c,j] * x[b, t-(width-1)+j, c])
+ *   d_x      [batch, length, channels]
+ *   d_w      [channels, width], d_bias [channels] (optional)
+ *   d_state  [batch, width-1, channels], contiguous (optional): x at t = -(width-1) .. -1; zeros without it
+ *   d_state_out  like d_state (optional, written): the last width-1 rows of state and x
+ *   SYS_ERR_UNSUPPORTED  a width, type or activation that is not listed, pointers off their element's alignment
+ *   SYS_ERR_SIZE  negative sizes, no channels, strides of y that make rows overlap
+ */
+int sys_causal_conv1d(const sys_causal_conv1d_t *p, const void *d_x, const void *d_w, const void *d_bias,
+                      const void *d_state, const int *d_lengths, void *d_y, void *d_state_out, hipStream_t stream);
+
+/*
+ * Its gradients.  d_dy [batch, length, channels]; d_dstate_out (optional): gradient of state_out.
+ * Written: d_dx [batch, length, channels] contiguous, d_dw like w, d_dbias like bias (optional; it
+ * needs d_bias), d_dstate like state (optional; it needs d_state).
+ */
+int sys_causal_conv1d_backward(const sys_causal_conv1d_t *p, const void *d_dy, const void *d_x, const void *d_w,
+                               const void *d_bias, const void *d_state, const int *d_lengths, const void *d_dstate_out,
+                               void *d_dx, void *d_dw, void *d_dbias, void *d_dstate, void *d_workspace, hipStream_t stream);
+size_t sys_causal_conv1d_backward_workspace(const sys_causal_conv1d_t *p);
+
+/*
+ * One token for each of `batch` requests (length is ignored; x_row, y_row too):
+ *   d_x [batch, channels], d_y [batch, channels]
+ *   d_state  [slots, width-1, channels]: the states of all requests in service
+ *   d_slots  (optional) [batch]: the slot of each request, every one at most once; without it request i has
+ *            slot i (slots >= batch).  A slot outside 0 .. slots-1 marks a request that is not there: its row of
+ *            y is 0 and no state is touched.
+ *   d_state_out  d_state itself (update in place), or another cache of the same shape, whose rows of
+ *            the slots named are written and whose other rows are left alone
+ */
+int sys_causal_conv1d_update(const sys_causal_conv1d_t *p, const void *d_x, const void *d_w, const void *d_bias,
+                             const void *d_state, const int *d_slots, void *d_y, void *d_state_out, hipStream_t stream);
+
+typedef struct {
+    int dtype;                          /* of u, delta, z, B, C, y and their gradients */
+    int softplus;                       /* 1: step sizes are softplus(delta + bias); 0: delta + bias */
+    int batch, length, channels;        /* batch, length >= 0 */
+    int states;                         /* states a channel */
+    int groups;                         /* of B and C; channel d uses group d / (channels / groups) */
+    int slots;                          /* sys_selective_scan_update: states in d_state; else ignored */
+    long long u_batch, u_row, delta_batch, delta_row, z_batch, z_row;
+    long long b_batch, b_row, c_batch, c_row;   /* a row of B or C: [groups, states], contiguous */
+    long long y_batch, y_row;           /* strides of y (backward: of dy) */
+} sys_selective_scan_t;
+
+/*
+ * Selective scan: for every sequence and channel
+ *   s_t = softplus(delta_t + delta_bias),   h_t[n] = e^(s_t A[n]) h_{t-1}[n] + s_t u_t B_t[n],
+ *   y_t = (sum_n C_t[n] h_t[n] + D u_t) * z_t / (1 + e^-z_t)
+ *   d_u, d_delta, d_z (optional)  [batch, length, channels]
+ *   d_A  [channels, states] fp32;  d_B, d_C  [batch, length, groups, states]
+ *   d_D, d_delta_bias (optional)  [channels] fp32
+ *   d_state  [batch, channels, states] fp32 (optional): h before the first position; zeros without it
+ *   d_state_out  like d_state (optional, written): h behind the last one
+ */
+int sys_selective_scan(const sys_selective_scan_t *p, const void *d_u, const void *d_delta, const float *d_A,
+                       const void *d_B, const void *d_C, const float *d_D, const void *d_z, const float *d_delta_bias,
+                       const float *d_state, const int *d_lengths, void *d_y, float *d_state_out, void *d_workspace,
+                       hipStream_t stream);
+size_t sys_selective_scan_workspace(const sys_selective_scan_t *p);
+
+/*
+ * Its gradients.  d_dy [batch, length, channels]; d_dstate_out (optional): gradient of state_out.
+ * Written, all contiguous: d_du, d_ddelta, d_dz (optional; with d_z it is required)
+ * [batch, length, channels]; d_dB, d_dC [batch, length, groups, states], summed over the channels of a
+ * group; d_dA [channels, states], d_dD, d_ddelta_bias [channels] fp32 (each optional where its input is),
+ * d_dstate like d_state (optional).
+ */
+int sys_selective_scan_backward(const sys_selective_scan_t *p, const void *d_dy, const void *d_u, const void *d_delta,
+                                const float *d_A, const void *d_B, const void *d_C, const float *d_D, const void *d_z,
+                                const float *d_delta_bias, const float *d_state, const int *d_lengths,
+                                const float *d_dstate_out, void *d_du, void *d_ddelta, float *d_dA, void *d_dB, void *d_dC,
+                                float *d_dD, void *d_dz, float *d_ddelta_bias, float *d_dstate, void *d_workspace,
+                                hipStream_t stream);
+size_t sys_selective_scan_backward_workspace(const sys_selective_scan_t *p);
+
+/*
+ * One token for each of `batch` requests (length and the row strides are ignored): u, delta, z, y
+ * [batch, channels], B, C [batch, groups, states], d_state [slots, channels, states] fp32; slots as
+ * sys_causal_conv1d_update.
+ */
+int sys_selective_scan_update(const sys_selective_scan_t *p, const void *d_u, const void *d_delta, const float *d_A,
+                              const void *d_B, const void *d_C, const float *d_D, const void *d_z, const float *d_delta_bias,
+                              const float *d_state, const int *d_slots, void *d_y, float *d_state_out, hipStream_t stream);
+
+typedef struct {
+    int dtype;                   /* of x, y and their gradients */
+    int param_dtype;             /* of w, b and their gradients: dtype or SYS_F32 */
+    int activation;              /* a sys_activation_t */
+    int groups;                  /* of channels / groups neighbouring channels */
+    int batch, channels;         /* batch >= 0 */
+    float eps;                   /* >= 0 */
+    int reserved;                /* 0 */
+    long long rows;              /* positions of an image, or 1 for tokens that are normalised one by one */
+    long long x_batch, x_row;    /* strides of x */
+    long long y_batch, y_row;    /* strides of y (backward: of dy) */
+} sys_group_norm_t;
+
+/*
+ * Group norm with an activation, channels last: over the rows of a batch entry and the channels of a group
+ *   mean = E[x],  rstd = 1 / sqrt(E[(x - mean)^2] + eps),  d_y = act((x - mean) * rstd * w[c] + b[c])
+ *   d_x, d_y  [batch, rows, channels];  d_w, d_b (optional)  [channels]
+ *   d_mean, d_rstd (optional, written)  [batch, groups] fp32: what the backward call needs
+ */
+int sys_group_norm(const sys_group_norm_t *p, const void *d_x, const void *d_w, const void *d_b, void *d_y,
+                   float *d_mean, float *d_rstd, void *d_workspace, hipStream_t stream);
+size_t sys_group_norm_workspace(const sys_group_norm_t *p);
+
+/* Its gradients: d_dx [batch, rows, channels] contiguous; d_dw, d_db like w and b (optional; d_dw needs d_w, d_db needs d_b). */
+int sys_group_norm_backward(const sys_group_norm_t *p, const void *d_dy, const void *d_x, const void *d_w, const void *d_b,
+                            const float *d_mean, const float *d_rstd, void *d_dx, void *d_dw, void *d_db, void *d_workspace,
+                            hipStream_t stream);
+size_t sys_group_norm_backward_workspace(const sys_group_norm_t *p);
+
+/*
  * Plain device-to-device copy of n floats with 16-byte accesses.  It is the
  * yard-stick the benchmark prints beside every convolution ("what the memory
  * system gives a streaming kernel of this footprint") and the kernel of known

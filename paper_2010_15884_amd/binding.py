@@ -356,3 +356,13 @@ def sys_alu_yardstick_f32(d_out, workgroups: int, trips: int, stream=None) -> in
 
 def sys_version() -> int:
     return int(lib().sys_version())
+
+
+# the operators on channels-last sequences
+from .sequence import (ACTIVATIONS, SYS_ACT_NONE, SYS_ACT_RELU, SYS_ACT_SILU, SYS_BF16, SYS_F16, SYS_F32,  # noqa: E402, F401
+                       SYS_MAX_CAUSAL_WIDTH, SYS_MAX_STATES, ScanGradients, sys_causal_conv1d, sys_causal_conv1d_backward,
+                       sys_causal_conv1d_update, sys_group_norm, sys_group_norm_backward, sys_selective_scan,
+                       sys_selective_scan_backward, sys_selective_scan_update)
+from .sequence import EXPORTS as _SEQUENCE_EXPORTS  # noqa: E402
+
+EXPORTS += _SEQUENCE_EXPORTS

@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsysconv.so")
-SOURCES = ["api.hip", "conv1d.hip", "conv1d_arrays.hip", "conv1d_split.hip", "conv1d_stride2.hip", "conv1d_stt.hip", "conv2d.hip", "conv2d_mfma.hip", "conv2d_split.hip", "conv2d_stride2.hip", "copy.hip"]
+SOURCES = ["api.hip", "causal_conv.hip", "conv1d.hip", "conv1d_arrays.hip", "conv1d_split.hip", "conv1d_stride2.hip", "conv1d_stt.hip", "conv2d.hip", "conv2d_mfma.hip", "conv2d_split.hip", "conv2d_stride2.hip", "copy.hip",
+           "group_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -68,20 +69,25 @@ def build_c_demo(verbose: bool = True) -> str:
 
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
-HOST_LOGIC = ["api.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip"]      # argument checks, the design planner, the tap scaling
+# argument checks, the design planner, the tap scaling, the shapes of launches and workspaces
+HOST_LOGIC = ["api.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip", "group_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
 
 
-def build_host_sanitized(verbose: bool = True) -> str:
+def build_host_sanitized(verbose: bool = True, driver: str = "abi_san_driver") -> str:
     """Host code of the library under AddressSanitizer + UndefinedBehaviorSanitizer (the device code is
     compiled as always): the translation units that hold host logic are rebuilt with the sanitizers on the
-    host pass only, linked with the ordinary objects of the rest and with tests/abi_san_driver.cpp into an
+    host pass only, linked with the ordinary objects of the rest and with a driver of tests/ into an
     executable that needs no GPU."""
     san_dir = os.path.join(OBJ, "san")
+    newest = max(os.path.getmtime(os.path.join(d, f)) for d in (CSRC, os.path.join(ROOT, "include")) for f in os.listdir(d) if f.endswith(".h"))
     os.makedirs(san_dir, exist_ok=True)
     objs = []
     for src in SOURCES:
         if src in HOST_LOGIC:
             obj = os.path.join(san_dir, src.replace(".hip", ".o"))
+            objs.append(obj)
+            if os.path.exists(obj) and os.path.getmtime(obj) > max(newest, os.path.getmtime(os.path.join(CSRC, src)), os.path.getmtime(__file__)):
+                continue                           # built for another driver
             cmd = ["hipcc", *[f for f in FLAGS if f != "-O3"], "-O1", *SAN_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
             res = subprocess.run(cmd, capture_output=True, text=True)
             if res.returncode != 0:
@@ -90,9 +96,9 @@ def build_host_sanitized(verbose: bool = True) -> str:
             obj = os.path.join(OBJ, src.replace(".hip", ".o"))
             if not os.path.exists(obj):
                 _compile(src)
-        objs.append(obj)
-    exe = os.path.join(san_dir, "abi_san_driver")
-    driver = os.path.join(ROOT, "tests", "abi_san_driver.cpp")
+            objs.append(obj)
+    exe = os.path.join(san_dir, driver)
+    driver = os.path.join(ROOT, "tests", driver + ".cpp")
     cmd = ["hipcc", "--offload-arch=gfx950", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined",
            "-fno-sanitize-recover=all", "-fno-gpu-sanitize", "-I", os.path.join(ROOT, "include"), "-x", "c++", driver,
            "-x", "none", *objs, "-o", exe]

@@ -12,12 +12,7 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-int hip_status(hipError_t e)
-{
-    if (e == hipSuccess) return SYS_OK;
-    g_last_hip_error = (int)e;
-    return SYS_ERR_HIP;
-}
+using sysconv::hip_status;
 
 bool ranges_overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
 {
@@ -52,6 +47,13 @@ bool too_wide(int w) { return w > INT_MAX - 2048; }
 // (4000x100 10x10, 3991 of them, 7.2 / 6.8), SBM above; 8x8: SBM at every size (FBS gains a third of a
 // microsecond on 300x400, and loses from 600^2 on: 800^2 5.8 / 5.4).  The rest: FBS.
 namespace sysconv {
+int hip_status(hipError_t e)
+{
+    if (e == hipSuccess) return SYS_OK;
+    g_last_hip_error = (int)e;
+    return SYS_ERR_HIP;
+}
+
 int conv2d_vector_projection(int oh, int ow, size_t x_pitch, int kh, int kw)
 {
     const size_t pitch_bytes = x_pitch * sizeof(float);
@@ -274,9 +276,9 @@ const char* sys_status_string(int status)
     switch (status) {
     case SYS_OK: return "ok";
     case SYS_ERR_NULL: return "null pointer argument";
-    case SYS_ERR_SIZE: return "invalid size (need 1 <= taps <= extent, pitch >= width)";
+    case SYS_ERR_SIZE: return "invalid size (need 1 <= taps <= extent, pitch >= width, whole groups)";
     case SYS_ERR_ALIAS: return "input and output ranges overlap";
-    case SYS_ERR_UNSUPPORTED: return "unsupported size, alignment or projection";
+    case SYS_ERR_UNSUPPORTED: return "unsupported size, alignment, type or projection";
     case SYS_ERR_HIP: return "HIP runtime error (see sys_last_hip_error)";
     case SYS_ERR_DESIGN: return "not a valid systolic design (dependence, singular transform or causality)";
     default: return "unknown status";

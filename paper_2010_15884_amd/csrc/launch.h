@@ -31,6 +31,8 @@ struct TapsOf {
     }
 };
 
+// The status of a HIP call (sysconv.h), remembered for sys_last_hip_error.
+int hip_status(hipError_t e);
 
 hipError_t launch_conv1d_fbs(const float* x, size_t n, const float* w, int k, float* y, hipStream_t s);
 hipError_t launch_conv1d_sbm(const float* x, size_t n, const float* w, int k, float* y, hipStream_t s);
