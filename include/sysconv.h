@@ -299,6 +299,7 @@ typedef enum { SYS_ACT_NONE = 0, SYS_ACT_SILU = 1, SYS_ACT_RELU = 2 } sys_activa
 
 #define SYS_MAX_CAUSAL_WIDTH 8   /* taps of the causal convolution: 2 .. 8 */
 #define SYS_MAX_STATES 64        /* states a channel of the selective scan: 1 .. 64 */
+#define SYS_MAX_SCAN_ROW ((1LL << 26) - 1)   /* elements from row to row of the selective scan's tensors */
 
 typedef struct {
     int dtype;                   /* of x, y, states and their gradients */

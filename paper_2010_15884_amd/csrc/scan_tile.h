@@ -15,6 +15,7 @@ namespace sysconv {
 constexpr int kScanThreads = 256;
 constexpr int kScanChannels = kScanThreads / 4;     // a workgroup
 constexpr int kScanTile = 16;                       // positions a tile
+static_assert(15 * SYS_MAX_SCAN_ROW + (1LL << 24) < (1LL << 30), "a tile's offsets in bytes fit 32 bits (up to 2^24 channels)");
 
 struct ScanShape {
     int channels_a_group, blocks_a_group, channel_blocks;   // of 64 channels
@@ -52,28 +53,83 @@ __device__ __forceinline__ ScanPlace scan_place(const sys_selective_scan_t& p, c
     return at;
 }
 
+// A tile of rows of a strided tensor, addressed as a buffer that ends with the last row that exists: a lane's offset within a tile is worked
+// out once, the tile's place is uniform, and rows past the end give zeros (or are not written) without a branch, which would make
+// every load wait for the one before it.  Rows are at most SYS_MAX_SCAN_ROW elements apart, so that a tile's offsets fit 32 bits.
+template <typename T>
+struct RowBuffer {
+    T* at;                             // row 0 of the present tile, column 0
+    long long left;                    // bytes from there to the end of the last row that exists; none left: every load gives 0
+    long long row;
+    __device__ __forceinline__ RowBuffer(const void* base, long long row_stride, int columns, int t0, int end)
+        : at((T*)base + t0 * row_stride), left(((long long)(end - 1 - t0) * row_stride + columns) * (long long)sizeof(T)), row(row_stride)
+    {
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile() const
+    {
+        const int high = (int)(left >> 32);
+        return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, high < 0 ? 0u : high ? 0xffffffffu : (unsigned)left, 0x00027000);
+    }
+    __device__ __forceinline__ void next() { at += kScanTile * row, left -= kScanTile * row * (long long)sizeof(T); }
+    __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }
+};
+
+// An element as it was loaded, 32 bits a value: 16-bit values in a register each, or the compiler packs pairs and waits for the loads to do so.
+template <typename T>
+__device__ __forceinline__ unsigned buffer_load(__amdgpu_buffer_rsrc_t b, unsigned offset)
+{
+    if constexpr (sizeof(T) == 4) return __builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b16(b, offset, 0, 0);
+}
+
+template <typename T>
+__device__ __forceinline__ float loaded(unsigned v)
+{
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, v);
+    else return (float)__builtin_bit_cast(T, (unsigned short)v);
+}
+
+template <typename T>
+__device__ __forceinline__ void buffer_store(__amdgpu_buffer_rsrc_t b, unsigned offset, T v)
+{
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), b, offset, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), b, offset, 0, 0);
+}
+
+constexpr unsigned kNowhere = 0xfffffff0u;          // an offset that is never written
+
 // B or C of kScanTile positions for LDS, [position][4 * NS], zeros past the last state and the sequence's end: first into registers ...
 template <typename T, int NS>
 struct StateTile {
     static constexpr int kWidth = 4 * NS;
     static constexpr int kEach = (kScanTile * kWidth + kScanThreads - 1) / kScanThreads;
-    float v[kEach];
-    __device__ __forceinline__ void load(const T* rows, long long row, int states, int t0, int length)
+    static constexpr int kRowStep = kScanThreads / kWidth;             // rows from one of a lane's elements to the next
+    static_assert(kScanThreads % kWidth == 0, "a lane keeps its state");
+    RowBuffer<T> rows;
+    unsigned v[kEach], offset[kEach];
+    int end;
+    bool is;
+    __device__ __forceinline__ StateTile(const T* base, long long row, int states, int t0, int end_row)
+        : rows(base, row, states, t0, end_row), end(end_row), is((int)threadIdx.x % kWidth < states)
     {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int k = i * kScanThreads + (int)threadIdx.x;
-            const int t = t0 + k / kWidth, n = k % kWidth;
-            v[i] = k < kScanTile * kWidth && t < length && n < states ? (float)rows[t * row + n] : 0.0f;
-        }
+        for (int i = 0; i < kEach; ++i) offset[i] = rows.offset((int)threadIdx.x / kWidth + i * kRowStep, (int)threadIdx.x % kWidth);
+    }
+    __device__ __forceinline__ void load()
+    {
+        const __amdgpu_buffer_rsrc_t b = rows.tile();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = buffer_load<T>(b, offset[i]);
+        rows.next();
     }
     // ... and from there into LDS
-    __device__ __forceinline__ void store(float* lds) const
+    __device__ __forceinline__ void store(float* lds, int t0) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int k = i * kScanThreads + (int)threadIdx.x;
-            if (k < kScanTile * kWidth) lds[k] = v[i];
+            const int r = (int)threadIdx.x / kWidth + i * kRowStep;
+            if (kEach * kRowStep <= kScanTile || r < kScanTile)
+                lds[r * kWidth + (int)threadIdx.x % kWidth] = is && t0 + r < end ? loaded<T>(v[i]) : 0.0f;
         }
     }
 };

@@ -46,49 +46,75 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(sys_selective_scan_t
     }
     const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f;
     const float skip = OUTPUTS && a.d ? a.d[at.channel] : 0.0f;
-    const T* u = (const T*)a.u + at.batch * p.u_batch + at.channel;
-    const T* delta = (const T*)a.delta + at.batch * p.delta_batch + at.channel;
-    const T* z = OUTPUTS && a.z ? (const T*)a.z + at.batch * p.z_batch + at.channel : nullptr;
-    const T* b = (const T*)a.b + at.batch * p.b_batch + (size_t)at.group * p.states;
-    const T* c = (const T*)a.c + at.batch * p.c_batch + (size_t)at.group * p.states;
-    T* y = OUTPUTS ? (T*)a.y + at.batch * p.y_batch + at.channel : nullptr;
-
+    const int last = at.length < at.end ? at.length : at.end;      // positions that exist in this chunk end here
+    const bool gated = OUTPUTS && a.z;
+    RowBuffer<T> u((const T*)a.u + at.batch * p.u_batch, p.u_row, p.channels, at.begin, last);
+    RowBuffer<T> delta((const T*)a.delta + at.batch * p.delta_batch, p.delta_row, p.channels, at.begin, last);
+    RowBuffer<T> z(gated ? (const T*)a.z + at.batch * p.z_batch : nullptr, p.z_row, p.channels, at.begin, last);
+    if (!gated) z.left = -1;
+    RowBuffer<T> y(OUTPUTS ? (const T*)a.y + at.batch * p.y_batch : nullptr, p.y_row, p.channels, at.begin, last);
+    unsigned u_at[kOwn], delta_at[kOwn], z_at[kOwn], y_at[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        u_at[k] = u.offset(4 * k + part, at.channel);
+        delta_at[k] = delta.offset(4 * k + part, at.channel);
+        z_at[k] = z.offset(4 * k + part, at.channel);
+        y_at[k] = at.there ? y.offset(4 * k + part, at.channel) : kNowhere;
+    }
     __shared__ __attribute__((aligned(16))) float tile_b[2][kScanTile * 4 * NS], tile_c[OUTPUTS ? 2 : 1][kScanTile * 4 * NS];
-    StateTile<T, NS> next_b, next_c;
-    float next_u[kOwn], next_delta[kOwn], next_z[kOwn];
-    auto fetch = [&](int t0) {
-        next_b.load(b, p.b_row, p.states, t0, at.length);
-        if (OUTPUTS) next_c.load(c, p.c_row, p.states, t0, at.length);
+    StateTile<T, NS> next_b((const T*)a.b + at.batch * p.b_batch + (size_t)at.group * p.states, p.b_row, p.states, at.begin, last);
+    StateTile<T, NS> next_c((const T*)a.c + at.batch * p.c_batch + (size_t)at.group * p.states, p.c_row, p.states, at.begin, last);
+    unsigned next_u[kOwn], next_delta[kOwn], next_z[kOwn];
+    auto fetch = [&] {
+        next_b.load();
+        if (OUTPUTS) next_c.load();
+        const __amdgpu_buffer_rsrc_t u_tile = u.tile(), delta_tile = delta.tile();
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            const int t = t0 + 4 * k + part;
-            const bool on = t < at.length && t < at.end;
-            next_u[k] = on ? (float)u[t * p.u_row] : 0.0f;
-            next_delta[k] = on ? (float)delta[t * p.delta_row] : 0.0f;
-            next_z[k] = on && z ? (float)z[t * p.z_row] : 0.0f;
+            next_u[k] = buffer_load<T>(u_tile, u_at[k]);
+            next_delta[k] = buffer_load<T>(delta_tile, delta_at[k]);
         }
+        if (OUTPUTS) {
+            const __amdgpu_buffer_rsrc_t z_tile = z.tile();
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) next_z[k] = buffer_load<T>(z_tile, z_at[k]);
+        }
+        u.next(), delta.next(), z.next();
     };
-    const int last = at.length < at.end ? at.length : at.end;      // positions that exist in this chunk end here
     float s_sum = 0.0f;
-    fetch(at.begin);
+    fetch();
     for (int t0 = at.begin, turn = 0; t0 < last; t0 += kScanTile, turn ^= 1) {
         float own_u[kOwn], own_s[kOwn], own_z[kOwn], own_y[kOwn];
-        next_b.store(tile_b[turn]);
-        if (OUTPUTS) next_c.store(tile_c[turn]);
+        next_b.store(tile_b[turn], t0);
+        if (OUTPUTS) next_c.store(tile_c[turn], t0);
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            own_u[k] = next_u[k];
-            own_z[k] = next_z[k];
-            const float s = p.softplus ? softplus(next_delta[k] + bias) : next_delta[k] + bias;
-            own_s[k] = t0 + 4 * k + part < last ? s : 0.0f;        // a position that is not there leaves the state as it is
-            s_sum += own_s[k];
+            own_u[k] = loaded<T>(next_u[k]);
+            own_z[k] = loaded<T>(next_z[k]);
+            own_s[k] = loaded<T>(next_delta[k]) + bias;
+        }
+        if (p.softplus) {
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) own_s[k] = softplus(own_s[k]);
+        }
+        if (t0 + kScanTile > last) {
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                const bool on = t0 + 4 * k + part < last;             // a position that is not there leaves the state as it is
+                own_s[k] = on ? own_s[k] : 0.0f;
+                own_u[k] = on ? own_u[k] : 0.0f;
+            }
+        }
+        if (!OUTPUTS) {
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) s_sum += own_s[k];
         }
         __syncthreads();
-        if (t0 + kScanTile < last) fetch(t0 + kScanTile);
+        fetch();                                                       // (past the end: zeros)
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             const float s_own = own_s[k], x_own = own_s[k] * own_u[k];
-            own_y[k] = 0.0f;
+            float sums_of[4];
             auto step = [&](auto lane) {
                 constexpr int j = decltype(lane)::value;
                 const float s = quad_take<j>(s_own), x = quad_take<j>(x_own);
@@ -100,30 +126,30 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(sys_selective_scan_t
                     h[i] = __builtin_fmaf(fast_exp2(s * decay[i]), h[i], x * bt[i]);
                     if (OUTPUTS) sum = __builtin_fmaf(ct[i], h[i], sum);
                 }
-                if (OUTPUTS) {
-                    sum = quad_sum(sum);
-                    own_y[k] = part == j ? sum : own_y[k];
-                }
+                sums_of[j] = sum;
             };
             step(std::integral_constant<int, 0>());
             step(std::integral_constant<int, 1>());
             step(std::integral_constant<int, 2>());
             step(std::integral_constant<int, 3>());
+            if (OUTPUTS) own_y[k] = quad_sums(sums_of);
         }
         if (OUTPUTS) {
+            const __amdgpu_buffer_rsrc_t y_tile = y.tile();
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
-                const int t = t0 + 4 * k + part;
                 float out = __builtin_fmaf(skip, own_u[k], own_y[k]);
-                if (z) out *= silu(own_z[k]);
-                if (at.there && t < last) y[t * p.y_row] = (T)out;
+                if (gated) out *= silu(own_z[k]);
+                buffer_store<T>(y_tile, y_at[k], (T)out);
             }
+            y.next();
         }
         // the other buffer is written next; every wavefront has passed the barrier of this tile when it has read the one before
     }
     if (OUTPUTS) {
+        T* rest = (T*)a.y + at.batch * p.y_batch + at.channel;
         for (int t = (at.begin > last ? at.begin : last) + part; t < at.end; t += 4)
-            if (at.there) y[t * p.y_row] = (T)0.0f;
+            if (at.there) rest[t * p.y_row] = (T)0.0f;
         if (a.state_out && at.there && at.chunk == shape.chunks - 1) {
 #pragma unroll
             for (int i = 0; i < NS; ++i)
@@ -188,7 +214,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(sys_selective_s
 
 // ---------------------------------------------------------------- launches
 
-ScanShape forward_shape(const sys_selective_scan_t& p)
+ScanShape forward_shape(const sys_selective_scan_t& p, bool ragged)
 {
     ScanShape s;
     s.channels_a_group = p.channels / p.groups;
@@ -196,9 +222,11 @@ ScanShape forward_shape(const sys_selective_scan_t& p)
     s.channel_blocks = s.blocks_a_group * p.groups;
     const long long workgroups = (long long)s.channel_blocks * p.batch;
     const int tiles = (p.length + kScanTile - 1) / kScanTile;
-    // eight wavefronts a CU, in chunks of at least four tiles
-    long long chunks = workgroups >= 256 ? 1 : 512 / (workgroups ? workgroups : 1);
-    if (chunks > tiles / 4) chunks = tiles / 4;
+    // Chunks cost 1.65 times the work, so they begin where a wavefront a SIMD is not there; then sixteen wavefronts a CU, in chunks of at
+    // least two tiles (one sequence of 4096 positions and channels, eight / sixteen / thirty-two a CU: 161 / 149 / 153 us).  With lengths some
+    // chunks will be empty (seven sequences of 0 .. 517 positions: 49 / 37 / 31).
+    long long chunks = workgroups >= 256 ? 1 : (ragged ? 2048 : 1024) / (workgroups ? workgroups : 1);
+    if (chunks > tiles / 2) chunks = tiles / 2;
     if (chunks > 64) chunks = 64;
     if (chunks < 1) chunks = 1;
     const int tiles_a_chunk = tiles ? (int)((tiles + chunks - 1) / chunks) : 1;
@@ -210,7 +238,7 @@ ScanShape forward_shape(const sys_selective_scan_t& p)
 template <typename T, int NS>
 hipError_t launch_forward(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s)
 {
-    const ScanShape shape = forward_shape(p);
+    const ScanShape shape = forward_shape(p, a.lengths != nullptr);
     const long long blocks = (long long)shape.channel_blocks * shape.chunks * p.batch;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     if (shape.chunks > 1) {
@@ -258,12 +286,17 @@ hipError_t launch(bool step, const sys_selective_scan_t& p, const ScanArgs& a, h
 
 }  // namespace
 
-hipError_t launch_scan(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s) { return launch(false, p, a, s); }
+hipError_t launch_scan(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s)
+{
+    sys_selective_scan_t q = p;
+    if (q.length == 1) q.y_row = q.channels;           // (a stride of no meaning; rows that are not there must lie behind this one)
+    return launch(false, q, a, s);
+}
 hipError_t launch_scan_step(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s) { return launch(true, p, a, s); }
 
 size_t scan_workspace(const sys_selective_scan_t& p)
 {
-    const ScanShape s = forward_shape(p);
+    const ScanShape s = forward_shape(p, true);         // (more chunks than without lengths)
     if (s.chunks == 1) return 0;
     return (size_t)p.batch * s.chunks * p.channels * (4 * scan_states_a_lane(p.states) + 1) * sizeof(float);
 }

@@ -80,9 +80,8 @@ __device__ __forceinline__ float softplus(float x)
 {
     const float e = fast_exp2(-kLog2e * __builtin_fabsf(x));
     const float w = 1.0f + e;
-    const float lost = e - (w - 1.0f);
-    // fmaxf would drop a NaN
-    return (x > 0.0f ? x : (x != x ? x : 0.0f)) + __builtin_fmaf(__builtin_amdgcn_logf(w), kLn2, lost);
+    // (fmaxf drops a NaN, which comes back with e)
+    return __builtin_fmaxf(x, 0.0f) + __builtin_fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.0f));
 }
 
 // Sum of v over the 4 lanes of a quad (every lane gets it).
@@ -91,6 +90,21 @@ __device__ __forceinline__ float quad_sum(float v)
     v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
     v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
     return v;
+}
+
+template <int CONTROL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xF, 0xF, true));
+}
+
+// Sums over the quad of four values a lane; lane j gets that of v[j].  Each step sends half of what a lane has to its neighbour.
+__device__ __forceinline__ float quad_sums(const float (&v)[4])
+{
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    const float a = (odd ? v[1] : v[0]) + dpp<0xB1>(odd ? v[0] : v[1]);
+    const float b = (odd ? v[3] : v[2]) + dpp<0xB1>(odd ? v[2] : v[3]);
+    return (high ? b : a) + dpp<0x4E>(high ? a : b);
 }
 
 // v of lane J of the quad.

@@ -5,6 +5,8 @@
 #include "launch.h"
 #include "sequence.h"
 
+#include <initializer_list>
+
 namespace {
 
 using sysconv::hip_status;
@@ -90,6 +92,9 @@ int check(const sys_selective_scan_t& p, bool step, bool writes_y)
     if (writes_y && (step ? rows_meet(1, p.batch, p.channels, 0, p.y_batch) : rows_meet(p.batch, p.length, p.channels, p.y_batch, p.y_row))) return SYS_ERR_SIZE;
     if (!known_dtype(p.dtype) || (p.softplus != 0 && p.softplus != 1) || p.states > SYS_MAX_STATES) return SYS_ERR_UNSUPPORTED;
     if (p.length > kMostRows || p.channels > kMostChannels) return SYS_ERR_UNSUPPORTED;
+    if (!step && p.length > 1)
+        for (long long s : {p.u_row, p.delta_row, p.z_row, p.b_row, p.c_row, p.y_row})
+            if (s > SYS_MAX_SCAN_ROW) return SYS_ERR_UNSUPPORTED;
     return SYS_OK;
 }
 

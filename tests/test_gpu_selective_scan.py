@@ -166,7 +166,7 @@ def test_offsets_beyond_32_bits():
     c = _make(6, 2, 20, 70, 16, BF16)
     want = _forward(c)[0]
     far = torch.empty(1 << 32, dtype=BF16, device="cuda")
-    u = far.as_strided((2, 20, 70), ((1 << 31) + 5, (1 << 26) + 3, 1))
+    u = far.as_strided((2, 20, 70), ((1 << 31) + 5, (1 << 25) + 3, 1))
     u.copy_(c["u"])
     assert torch.equal(_forward(dict(c, u=u))[0], want)
     grads, far_grads = (B.sys_selective_scan_backward(c["dy"], v, *_inputs(c)[1:], softplus=True) for v in (c["u"], u))
