@@ -6,6 +6,9 @@ one is given, and what is wrong with the arguments is refused before anything ru
 torch.  With ``stream`` (a hipStream_t) outputs and workspaces are allocated on that stream; the inputs must be ready on it and live until it
 is done with them.
 
+Types, shapes and strides are checked and packed once for every combination that a program calls with (a "plan": what the C entry point is
+told, and the workspace's size); a later call with the same ones finds it by them, which leaves a third of the host time of a small call.
+
 The functions are reached through ``binding`` (``binding.sys_causal_conv1d`` and so on).
 """
 from __future__ import annotations
@@ -51,6 +54,7 @@ class _EntryPoints:
             f.argtypes, f.restype = [ctypes.c_char_p], ctypes.c_size_t
             setattr(self, name, f)
         self.empty, self.float32 = torch.empty, torch.float32
+        self.stream, self.external = torch.cuda.stream, torch.cuda.ExternalStream
         self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -141,24 +145,52 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _on(t, stream):
-    """Where outputs and workspaces of a call are allocated: on its stream."""
+_plans = {}
+
+
+def _planned(make, options, *tensors):
+    """make(*tensors, *options), kept by what it depends on: the types, devices, shapes and strides of the tensors, and the options."""
+    try:
+        key = (make, options, *[None if t is None else (t.dtype, t.get_device(), t.shape, t.stride()) for t in tensors])
+        plan = _plans.get(key)
+    except (AttributeError, TypeError, RuntimeError):          # what is no tensor is refused by make
+        key = plan = None
+    if plan is None:
+        plan = make(*tensors, *options)
+        if key is not None:
+            if len(_plans) >= 4096:
+                _plans.clear()
+            _plans[key] = plan
+    return plan
+
+
+def _allocated(t, stream, make):
+    """Outputs and workspace of a call, allocated on its stream."""
     if t.get_device() != _calls.device():
         raise ValueError("the tensors must be on the current device")
     if stream is None:
-        return contextlib.nullcontext()
-    import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=t.device))
+        return make(_calls.empty, t.device)
+    with _calls.stream(_calls.external(int(stream), device=t.device)):
+        return make(_calls.empty, t.device)
 
 
-def _workspace(size, t):
-    return _calls.empty((size + 3) // 4, dtype=_calls.float32, device=t.device) if size else None
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _run(name, packed, stream, *pointers):
     status = getattr(_calls, name)(packed, *pointers, _b._stream_handle(stream))
     if status:
         _b._check(status)
+
+
+def _floats(size):
+    return (size + 3) // 4
+
+
+def _packed_strides(shape):
+    """Batch and row strides of a contiguous tensor of this shape."""
+    return shape[1] * shape[2], shape[2]
 
 
 # ---------------------------------------------------------------- causal convolution
@@ -179,22 +211,26 @@ def _conv_arguments(d_x, d_w, d_bias, activation, rows):
     return code, params, channels, d_w.shape[1], _activation(activation)
 
 
-def sys_causal_conv1d(d_x, d_w, d_bias=None, d_y=None, activation="NONE", d_state=None, d_state_out=None, d_lengths=None, stream=None):
-    """y[b,t,c] = act(bias[c] + sum_j w[c,j] x[b, t-(width-1)+j, c]).  d_x: [batch, length, channels] (any batch and row strides);
-    d_w: [channels, width]; d_state, d_state_out: [batch, width-1, channels]; d_lengths: int32 [batch].  Returns d_y."""
+def _conv_plan(d_x, d_w, d_bias, d_state, d_lengths, d_other, d_state_out, activation, backward):
     code, params, channels, width, act = _conv_arguments(d_x, d_w, d_bias, activation, 2)
     batch, length = d_x.shape[0], d_x.shape[1]
     states = (batch, width - 1, channels)
     _packed(d_state, d_x, "d_state", states)
-    _packed(d_state_out, d_x, "d_state_out", states)
+    _packed(d_state_out, d_x, "d_dstate_out" if backward else "d_state_out", states)
     _ints(d_lengths, d_x, "d_lengths", batch)
+    if d_other is not None or backward:
+        _like(d_other, d_x, "d_dy" if backward else "d_y", d_x.shape)
     c = _calls or _entry_points()
-    with _on(d_x, stream):
-        if d_y is None:
-            d_y = c.empty((batch, length, channels), dtype=d_x.dtype, device=d_x.device)
-        else:
-            _like(d_y, d_x, "d_y", d_x.shape)
-    packed = _CONV.pack(code, params, act, width, batch, length, channels, 0, d_x.stride(0), d_x.stride(1), d_y.stride(0), d_y.stride(1))
+    other = _packed_strides(d_x.shape) if d_other is None else (d_other.stride(0), d_other.stride(1))
+    packed = _CONV.pack(code, params, act, width, batch, length, channels, 0, d_x.stride(0), d_x.stride(1), *other)
+    return packed, _floats(c.sys_causal_conv1d_backward_workspace(packed)) if backward else 0
+
+
+def sys_causal_conv1d(d_x, d_w, d_bias=None, d_y=None, activation="NONE", d_state=None, d_state_out=None, d_lengths=None, stream=None):
+    """y[b,t,c] = act(bias[c] + sum_j w[c,j] x[b, t-(width-1)+j, c]).  d_x: [batch, length, channels] (any batch and row strides);
+    d_w: [channels, width]; d_state, d_state_out: [batch, width-1, channels]; d_lengths: int32 [batch].  Returns d_y."""
+    packed, _ = _planned(_conv_plan, (activation, False), d_x, d_w, d_bias, d_state, d_lengths, d_y, d_state_out)
+    d_y = _allocated(d_x, stream, lambda empty, device: empty(d_x.shape, dtype=d_x.dtype, device=device) if d_y is None else d_y)
     _run("sys_causal_conv1d", packed, stream, d_x.data_ptr(), d_w.data_ptr(), _ptr(d_bias), _ptr(d_state), _ptr(d_lengths), d_y.data_ptr(),
          _ptr(d_state_out))
     return d_y
@@ -202,29 +238,18 @@ def sys_causal_conv1d(d_x, d_w, d_bias=None, d_y=None, activation="NONE", d_stat
 
 def sys_causal_conv1d_backward(d_dy, d_x, d_w, d_bias=None, activation="NONE", d_state=None, d_lengths=None, d_dstate_out=None, stream=None):
     """Gradients of sys_causal_conv1d: (dx, dw, dbias, dstate), the last two None where the call had no bias or state."""
-    code, params, channels, width, act = _conv_arguments(d_x, d_w, d_bias, activation, 2)
-    batch, length = d_x.shape[0], d_x.shape[1]
-    states = (batch, width - 1, channels)
-    _like(d_dy, d_x, "d_dy", d_x.shape)
-    _packed(d_state, d_x, "d_state", states)
-    _packed(d_dstate_out, d_x, "d_dstate_out", states)
-    _ints(d_lengths, d_x, "d_lengths", batch)
-    c = _calls or _entry_points()
-    packed = _CONV.pack(code, params, act, width, batch, length, channels, 0, d_x.stride(0), d_x.stride(1), d_dy.stride(0), d_dy.stride(1))
-    with _on(d_x, stream):
-        dx = c.empty((batch, length, channels), dtype=d_x.dtype, device=d_x.device)
-        dw = c.empty((channels, width), dtype=d_w.dtype, device=d_x.device)
-        dbias = None if d_bias is None else c.empty((channels,), dtype=d_w.dtype, device=d_x.device)
-        dstate = None if d_state is None else c.empty(states, dtype=d_x.dtype, device=d_x.device)
-        workspace = _workspace(c.sys_causal_conv1d_backward_workspace(packed), d_x)
+    packed, floats = _planned(_conv_plan, (activation, True), d_x, d_w, d_bias, d_state, d_lengths, d_dy, d_dstate_out)
+
+    def make(empty, device):
+        like = lambda t: None if t is None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
+        return like(d_x), like(d_w), like(d_bias), like(d_state), empty(floats, dtype=_calls.float32, device=device) if floats else None
+    dx, dw, dbias, dstate, workspace = _allocated(d_x, stream, make)
     _run("sys_causal_conv1d_backward", packed, stream, d_dy.data_ptr(), d_x.data_ptr(), d_w.data_ptr(), _ptr(d_bias), _ptr(d_state),
          _ptr(d_lengths), _ptr(d_dstate_out), dx.data_ptr(), dw.data_ptr(), _ptr(dbias), _ptr(dstate), _ptr(workspace))
     return dx, dw, dbias, dstate
 
 
-def sys_causal_conv1d_update(d_x, d_w, d_bias, d_state, d_y=None, activation="NONE", d_slots=None, d_state_out=None, stream=None):
-    """One token a request: d_x [requests, channels], d_state [slots, width-1, channels], updated in place (or into d_state_out) at
-    the slots of d_slots (int32; request i has slot i without it; a slot that is not there skips its request).  Returns d_y."""
+def _conv_step_plan(d_x, d_w, d_bias, d_state, d_slots, d_y, d_state_out, activation):
     code, params, channels, width, act = _conv_arguments(d_x, d_w, d_bias, activation, 1)
     requests = d_x.shape[0]
     _code(d_state, "d_state")
@@ -232,13 +257,17 @@ def sys_causal_conv1d_update(d_x, d_w, d_bias, d_state, d_y=None, activation="NO
     _packed(d_state, d_x, "d_state", (slots, width - 1, channels))
     _packed(d_state_out, d_x, "d_state_out", d_state.shape)
     _ints(d_slots, d_x, "d_slots", requests)
-    c = _calls or _entry_points()
-    with _on(d_x, stream):
-        if d_y is None:
-            d_y = c.empty((requests, channels), dtype=d_x.dtype, device=d_x.device)
-        else:
-            _like(d_y, d_x, "d_y", d_x.shape)
-    packed = _CONV.pack(code, params, act, width, requests, 1, channels, slots, d_x.stride(0), 0, d_y.stride(0), 0)
+    if d_y is not None:
+        _like(d_y, d_x, "d_y", d_x.shape)
+    _calls or _entry_points()
+    return _CONV.pack(code, params, act, width, requests, 1, channels, slots, d_x.stride(0), 0, channels if d_y is None else d_y.stride(0), 0)
+
+
+def sys_causal_conv1d_update(d_x, d_w, d_bias, d_state, d_y=None, activation="NONE", d_slots=None, d_state_out=None, stream=None):
+    """One token a request: d_x [requests, channels], d_state [slots, width-1, channels], updated in place (or into d_state_out) at
+    the slots of d_slots (int32; request i has slot i without it; a slot that is not there skips its request).  Returns d_y."""
+    packed = _planned(_conv_step_plan, (activation,), d_x, d_w, d_bias, d_state, d_slots, d_y, d_state_out)
+    d_y = _allocated(d_x, stream, lambda empty, device: empty(d_x.shape, dtype=d_x.dtype, device=device) if d_y is None else d_y)
     _run("sys_causal_conv1d_update", packed, stream, d_x.data_ptr(), d_w.data_ptr(), _ptr(d_bias), d_state.data_ptr(), _ptr(d_slots),
          d_y.data_ptr(), _ptr(d_state if d_state_out is None else d_state_out))
     return d_y
@@ -250,7 +279,8 @@ def _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, rows):
     code = _code(d_u, "d_u")
     if d_u.dim() != rows + 1:
         raise ValueError("d_u must be [batch, length, channels]" if rows == 2 else "d_u must be [requests, channels]")
-    f32, channels = _entry_f32(), d_u.shape[-1]
+    import torch
+    f32, channels = torch.float32, d_u.shape[-1]
     _like(d_u, d_u, "d_u", d_u.shape)
     _like(d_delta, d_u, "d_delta", d_u.shape)
     if d_z is not None:
@@ -270,16 +300,25 @@ def _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, rows):
         _like(t, d_u, what, (*d_u.shape[:-1], groups, states))
         if groups > 1 and t.stride(-2) != states:
             raise ValueError(f"the groups of a row of {what} must be contiguous")
-    return code, channels, states, groups
-
-
-def _entry_f32():
-    import torch
-    return torch.float32
+    return code, channels, states, groups, f32
 
 
 def _strides(t):
     return (t.stride(0), t.stride(1)) if t is not None else (0, 0)
+
+
+def _scan_plan(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, d_state, d_lengths, d_other, d_state_out, softplus, backward):
+    code, channels, states, groups, f32 = _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, 2)
+    batch, length = d_u.shape[0], d_u.shape[1]
+    _packed(d_state, d_u, "d_state", (batch, channels, states), f32)
+    _packed(d_state_out, d_u, "d_dstate_out" if backward else "d_state_out", (batch, channels, states), f32)
+    _ints(d_lengths, d_u, "d_lengths", batch)
+    if d_other is not None or backward:
+        _like(d_other, d_u, "d_dy" if backward else "d_y", d_u.shape)
+    c = _calls or _entry_points()
+    packed = _SCAN.pack(code, bool(softplus), batch, length, channels, states, groups, 0, *_strides(d_u), *_strides(d_delta), *_strides(d_z),
+                        *_strides(d_B), *_strides(d_C), *(_packed_strides(d_u.shape) if d_other is None else _strides(d_other)))
+    return packed, _floats(c.sys_selective_scan_backward_workspace(packed) if backward else c.sys_selective_scan_workspace(packed))
 
 
 def sys_selective_scan(d_u, d_delta, d_A, d_B, d_C, d_D=None, d_z=None, d_delta_bias=None, d_y=None, softplus=False, d_state=None,
@@ -287,20 +326,9 @@ def sys_selective_scan(d_u, d_delta, d_A, d_B, d_C, d_D=None, d_z=None, d_delta_
     """h_t = e^(s_t A) h_{t-1} + s_t u_t B_t, y_t = (C_t . h_t + D u_t) silu(z_t), s_t = delta_t + delta_bias (its softplus with
     ``softplus``).  d_u, d_delta, d_z: [batch, length, channels]; d_B, d_C: [batch, length, groups, states]; d_A [channels,
     states], d_D, d_delta_bias [channels] and the states [batch, channels, states] are float32.  Returns d_y."""
-    code, channels, states, groups = _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, 2)
-    batch, length = d_u.shape[0], d_u.shape[1]
-    c = _calls or _entry_points()
-    _packed(d_state, d_u, "d_state", (batch, channels, states), c.float32)
-    _packed(d_state_out, d_u, "d_state_out", (batch, channels, states), c.float32)
-    _ints(d_lengths, d_u, "d_lengths", batch)
-    with _on(d_u, stream):
-        if d_y is None:
-            d_y = c.empty((batch, length, channels), dtype=d_u.dtype, device=d_u.device)
-        else:
-            _like(d_y, d_u, "d_y", d_u.shape)
-        packed = _SCAN.pack(code, bool(softplus), batch, length, channels, states, groups, 0, *_strides(d_u), *_strides(d_delta),
-                            *_strides(d_z), *_strides(d_B), *_strides(d_C), *_strides(d_y))
-        workspace = _workspace(c.sys_selective_scan_workspace(packed), d_u)
+    packed, floats = _planned(_scan_plan, (softplus, False), d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, d_state, d_lengths, d_y, d_state_out)
+    d_y, workspace = _allocated(d_u, stream, lambda empty, device: (empty(d_u.shape, dtype=d_u.dtype, device=device) if d_y is None else d_y,
+                                                                    empty(floats, dtype=_calls.float32, device=device) if floats else None))
     _run("sys_selective_scan", packed, stream, d_u.data_ptr(), d_delta.data_ptr(), d_A.data_ptr(), d_B.data_ptr(), d_C.data_ptr(), _ptr(d_D),
          _ptr(d_z), _ptr(d_delta_bias), _ptr(d_state), _ptr(d_lengths), d_y.data_ptr(), _ptr(d_state_out), _ptr(workspace))
     return d_y
@@ -309,49 +337,41 @@ def sys_selective_scan(d_u, d_delta, d_A, d_B, d_C, d_D=None, d_z=None, d_delta_
 def sys_selective_scan_backward(d_dy, d_u, d_delta, d_A, d_B, d_C, d_D=None, d_z=None, d_delta_bias=None, softplus=False, d_state=None,
                                 d_lengths=None, d_dstate_out=None, stream=None) -> ScanGradients:
     """Gradients of sys_selective_scan, computed from its inputs; those of B and C are summed over the channels of a group."""
-    code, channels, states, groups = _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, 2)
-    batch, length = d_u.shape[0], d_u.shape[1]
-    c = _calls or _entry_points()
-    _like(d_dy, d_u, "d_dy", d_u.shape)
-    _packed(d_state, d_u, "d_state", (batch, channels, states), c.float32)
-    _packed(d_dstate_out, d_u, "d_dstate_out", (batch, channels, states), c.float32)
-    _ints(d_lengths, d_u, "d_lengths", batch)
-    packed = _SCAN.pack(code, bool(softplus), batch, length, channels, states, groups, 0, *_strides(d_u), *_strides(d_delta), *_strides(d_z),
-                        *_strides(d_B), *_strides(d_C), *_strides(d_dy))
-    with _on(d_u, stream):
-        def make(shape, dtype):
-            return c.empty(shape, dtype=dtype, device=d_u.device)
-        values, pairs = (batch, length, channels), (batch, length, groups, states)
-        g = ScanGradients(make(values, d_u.dtype), make(values, d_u.dtype), make((channels, states), c.float32), make(pairs, d_u.dtype),
-                          make(pairs, d_u.dtype), None if d_D is None else make((channels,), c.float32),
-                          None if d_z is None else make(values, d_u.dtype), None if d_delta_bias is None else make((channels,), c.float32),
-                          None if d_state is None else make((batch, channels, states), c.float32))
-        workspace = _workspace(c.sys_selective_scan_backward_workspace(packed), d_u)
+    packed, floats = _planned(_scan_plan, (softplus, True), d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, d_state, d_lengths, d_dy, d_dstate_out)
+
+    def make(empty, device):
+        like = lambda t: None if t is None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
+        return (ScanGradients(like(d_u), like(d_u), like(d_A), like(d_B), like(d_B), like(d_D), like(d_z), like(d_delta_bias), like(d_state)),
+                empty(floats, dtype=_calls.float32, device=device) if floats else None)
+    g, workspace = _allocated(d_u, stream, make)
     _run("sys_selective_scan_backward", packed, stream, d_dy.data_ptr(), d_u.data_ptr(), d_delta.data_ptr(), d_A.data_ptr(), d_B.data_ptr(),
-         d_C.data_ptr(), _ptr(d_D), _ptr(d_z), _ptr(d_delta_bias), _ptr(d_state), _ptr(d_lengths), _ptr(d_dstate_out), _ptr(g.du), _ptr(g.ddelta),
-         _ptr(g.dA), _ptr(g.dB), _ptr(g.dC), _ptr(g.dD), _ptr(g.dz), _ptr(g.ddelta_bias), _ptr(g.dstate), _ptr(workspace))
+         d_C.data_ptr(), _ptr(d_D), _ptr(d_z), _ptr(d_delta_bias), _ptr(d_state), _ptr(d_lengths), _ptr(d_dstate_out), g.du.data_ptr(),
+         g.ddelta.data_ptr(), g.dA.data_ptr(), g.dB.data_ptr(), g.dC.data_ptr(), _ptr(g.dD), _ptr(g.dz), _ptr(g.ddelta_bias), _ptr(g.dstate),
+         _ptr(workspace))
     return g
+
+
+def _scan_step_plan(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, d_state, d_slots, d_y, d_state_out, softplus):
+    code, channels, states, groups, f32 = _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, 1)
+    requests = d_u.shape[0]
+    _code(d_state, "d_state")
+    slots = d_state.shape[0] if d_state.dim() else 0
+    _packed(d_state, d_u, "d_state", (slots, channels, states), f32)
+    _packed(d_state_out, d_u, "d_state_out", d_state.shape, f32)
+    _ints(d_slots, d_u, "d_slots", requests)
+    if d_y is not None:
+        _like(d_y, d_u, "d_y", d_u.shape)
+    _calls or _entry_points()
+    return _SCAN.pack(code, bool(softplus), requests, 1, channels, states, groups, slots, d_u.stride(0), 0, d_delta.stride(0), 0,
+                      0 if d_z is None else d_z.stride(0), 0, d_B.stride(0), 0, d_C.stride(0), 0, channels if d_y is None else d_y.stride(0), 0)
 
 
 def sys_selective_scan_update(d_u, d_delta, d_A, d_B, d_C, d_state, d_D=None, d_z=None, d_delta_bias=None, d_y=None, softplus=False,
                               d_slots=None, d_state_out=None, stream=None):
     """One token a request: d_u, d_delta, d_z [requests, channels], d_B, d_C [requests, groups, states], d_state float32 [slots,
     channels, states], updated in place (or into d_state_out); slots as sys_causal_conv1d_update.  Returns d_y."""
-    code, channels, states, groups = _scan_arguments(d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, 1)
-    requests = d_u.shape[0]
-    c = _calls or _entry_points()
-    _code(d_state, "d_state")
-    slots = d_state.shape[0] if d_state.dim() else 0
-    _packed(d_state, d_u, "d_state", (slots, channels, states), c.float32)
-    _packed(d_state_out, d_u, "d_state_out", d_state.shape, c.float32)
-    _ints(d_slots, d_u, "d_slots", requests)
-    with _on(d_u, stream):
-        if d_y is None:
-            d_y = c.empty((requests, channels), dtype=d_u.dtype, device=d_u.device)
-        else:
-            _like(d_y, d_u, "d_y", d_u.shape)
-    packed = _SCAN.pack(code, bool(softplus), requests, 1, channels, states, groups, slots, d_u.stride(0), 0, d_delta.stride(0), 0,
-                        0 if d_z is None else d_z.stride(0), 0, d_B.stride(0), 0, d_C.stride(0), 0, d_y.stride(0), 0)
+    packed = _planned(_scan_step_plan, (softplus,), d_u, d_delta, d_A, d_B, d_C, d_D, d_z, d_delta_bias, d_state, d_slots, d_y, d_state_out)
+    d_y = _allocated(d_u, stream, lambda empty, device: empty(d_u.shape, dtype=d_u.dtype, device=device) if d_y is None else d_y)
     _run("sys_selective_scan_update", packed, stream, d_u.data_ptr(), d_delta.data_ptr(), d_A.data_ptr(), d_B.data_ptr(), d_C.data_ptr(),
          _ptr(d_D), _ptr(d_z), _ptr(d_delta_bias), d_state.data_ptr(), _ptr(d_slots), d_y.data_ptr(),
          _ptr(d_state if d_state_out is None else d_state_out))
@@ -360,11 +380,12 @@ def sys_selective_scan_update(d_u, d_delta, d_A, d_B, d_C, d_state, d_D=None, d_
 
 # ---------------------------------------------------------------- group norm
 
-def _norm_arguments(d_x, groups, d_w, d_b, eps, activation):
+def _norm_plan(d_x, d_w, d_b, d_mean, d_rstd, d_other, groups, eps, activation, backward):
     code = _code(d_x, "d_x")
     if d_x.dim() != 3:
         raise ValueError("d_x must be [batch, rows, channels]")
     batch, rows, channels = d_x.shape
+    groups = int(groups)
     _like(d_x, d_x, "d_x", d_x.shape)
     params = code
     if d_w is not None:
@@ -374,45 +395,37 @@ def _norm_arguments(d_x, groups, d_w, d_b, eps, activation):
         if d_w is not None and got != params:
             raise TypeError("d_w and d_b must have one type")
         params = got
-
-    def pack(y):
-        return _NORM.pack(code, params, _activation(activation), int(groups), batch, channels, float(eps), 0, rows, d_x.stride(0), d_x.stride(1),
-                          y.stride(0), y.stride(1))
-    return batch, rows, channels, pack
+    import torch
+    for t, what in ((d_mean, "d_mean"), (d_rstd, "d_rstd")):
+        if backward:
+            _code(t, what)
+        _packed(t, d_x, what, (batch, groups), torch.float32)
+    if d_other is not None or backward:
+        _like(d_other, d_x, "d_dy" if backward else "d_y", d_x.shape)
+    c = _calls or _entry_points()
+    packed = _NORM.pack(code, params, _activation(activation), groups, batch, channels, float(eps), 0, rows, d_x.stride(0), d_x.stride(1),
+                        *(_packed_strides(d_x.shape) if d_other is None else _strides(d_other)))
+    return packed, _floats(c.sys_group_norm_backward_workspace(packed) if backward else c.sys_group_norm_workspace(packed))
 
 
 def sys_group_norm(d_x, groups, d_w=None, d_b=None, eps=1e-5, activation="NONE", d_y=None, d_mean=None, d_rstd=None, stream=None):
     """y = act((x - mean) * rstd * w + b), statistics over the rows of a batch entry and the channels of a group.  d_x: [batch, rows,
     channels] (rows = 1: token by token); d_mean, d_rstd: float32 [batch, groups], written where given.  Returns d_y."""
-    batch, rows, channels, pack = _norm_arguments(d_x, groups, d_w, d_b, eps, activation)
-    c = _calls or _entry_points()
-    _packed(d_mean, d_x, "d_mean", (batch, int(groups)), c.float32)
-    _packed(d_rstd, d_x, "d_rstd", (batch, int(groups)), c.float32)
-    with _on(d_x, stream):
-        if d_y is None:
-            d_y = c.empty((batch, rows, channels), dtype=d_x.dtype, device=d_x.device)
-        else:
-            _like(d_y, d_x, "d_y", d_x.shape)
-        packed = pack(d_y)
-        workspace = _workspace(c.sys_group_norm_workspace(packed), d_x)
+    packed, floats = _planned(_norm_plan, (groups, eps, activation, False), d_x, d_w, d_b, d_mean, d_rstd, d_y)
+    d_y, workspace = _allocated(d_x, stream, lambda empty, device: (empty(d_x.shape, dtype=d_x.dtype, device=device) if d_y is None else d_y,
+                                                                    empty(floats, dtype=_calls.float32, device=device) if floats else None))
     _run("sys_group_norm", packed, stream, d_x.data_ptr(), _ptr(d_w), _ptr(d_b), d_y.data_ptr(), _ptr(d_mean), _ptr(d_rstd), _ptr(workspace))
     return d_y
 
 
 def sys_group_norm_backward(d_dy, d_x, groups, d_mean, d_rstd, d_w=None, d_b=None, activation="NONE", stream=None):
     """Gradients of sys_group_norm from its inputs and statistics: (dx, dw, db), the last two None without w or b."""
-    batch, rows, channels, pack = _norm_arguments(d_x, groups, d_w, d_b, 0.0, activation)
-    c = _calls or _entry_points()
-    _like(d_dy, d_x, "d_dy", d_x.shape)
-    for t, what in ((d_mean, "d_mean"), (d_rstd, "d_rstd")):
-        _code(t, what)
-        _packed(t, d_x, what, (batch, int(groups)), c.float32)
-    packed = pack(d_dy)
-    with _on(d_x, stream):
-        dx = c.empty((batch, rows, channels), dtype=d_x.dtype, device=d_x.device)
-        dw = None if d_w is None else c.empty((channels,), dtype=d_w.dtype, device=d_x.device)
-        db = None if d_b is None else c.empty((channels,), dtype=d_b.dtype, device=d_x.device)
-        workspace = _workspace(c.sys_group_norm_backward_workspace(packed), d_x)
+    packed, floats = _planned(_norm_plan, (groups, 0.0, activation, True), d_x, d_w, d_b, d_mean, d_rstd, d_dy)
+
+    def make(empty, device):
+        like = lambda t: None if t is None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
+        return like(d_x), like(d_w), like(d_b), empty(floats, dtype=_calls.float32, device=device) if floats else None
+    dx, dw, db, workspace = _allocated(d_x, stream, make)
     _run("sys_group_norm_backward", packed, stream, d_dy.data_ptr(), d_x.data_ptr(), _ptr(d_w), _ptr(d_b), d_mean.data_ptr(), d_rstd.data_ptr(),
          dx.data_ptr(), _ptr(dw), _ptr(db), _ptr(workspace))
     return dx, dw, db
