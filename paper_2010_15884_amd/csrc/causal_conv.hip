@@ -13,21 +13,24 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The taps of V channels.  w is [channels][K].
-template <int K, int V>
+// The taps of V channels: V * K values in a row of w, [channels][K].
+template <typename T, int K, int V>
 __device__ __forceinline__ void load_taps(const sys_causal_conv1d_t& p, const void* w, int c0, float (&tap)[K][V])
 {
+    float flat[V * K];
+    load_params<T, V * K>(w, (size_t)c0 * K, p.param_dtype, flat);
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int j = 0; j < K; ++j) tap[j][i] = load_param(w, (size_t)(c0 + i) * K + j, p.param_dtype);
+        for (int j = 0; j < K; ++j) tap[j][i] = flat[i * K + j];
 }
 
-template <int V>
+template <typename T, int V>
 __device__ __forceinline__ void load_bias(const sys_causal_conv1d_t& p, const void* bias, int c0, float (&b)[V])
 {
 #pragma unroll
-    for (int i = 0; i < V; ++i) b[i] = bias ? load_param(bias, (size_t)c0 + i, p.param_dtype) : 0.0f;
+    for (int i = 0; i < V; ++i) b[i] = 0.0f;
+    if (bias) load_params<T, V>(bias, (size_t)c0, p.param_dtype, b);
 }
 
 // The lanes of a row hold V channels each; the last one begins earlier where the channels are no multiple of V, and both lanes
@@ -41,25 +44,27 @@ __device__ __forceinline__ int first_channel(int lane, int channels)
 
 // Row e of state ++ x (e = t + K-1), zeros where there is none.
 template <typename T, int K, int V>
-__device__ __forceinline__ void load_row(const T* x, const T* state, long long x_row, int channels, int e, int len, int c0, float (&out)[V])
+__device__ __forceinline__ typename Channels<T, V>::Raw raw_row(const T* x, const T* state, long long x_row, int channels, int e, int len, int c0)
 {
     const int t = e - (K - 1);
-    if (t >= 0 && t < len) Channels<T, V>::load(x + t * x_row + c0, out);
-    else if (t < 0 && e >= 0 && state) Channels<T, V>::load(state + (size_t)e * channels + c0, out);
-    else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = 0.0f;
-    }
+    if (t >= 0 && t < len) return Channels<T, V>::raw(x + t * x_row + c0);
+    if (t < 0 && e >= 0 && state) return Channels<T, V>::raw(state + (size_t)e * channels + c0);
+    return typename Channels<T, V>::Raw{};
 }
 
-constexpr int kRows = 8;           // rows a lane in the forward kernel
-
 template <typename T, int K, int V>
+__device__ __forceinline__ void load_row(const T* x, const T* state, long long x_row, int channels, int e, int len, int c0, float (&out)[V])
+{
+    Channels<T, V>::values(raw_row<T, K, V>(x, state, x_row, channels, e, len, c0), out);
+}
+
+template <typename T, int K, int V, int ROWS>
 __global__ __launch_bounds__(kThreads) void causal_conv_kernel(sys_causal_conv1d_t p, CausalConvArgs a, int blocks_a_sequence, int lanes_a_row)
 {
-    const int b = blockIdx.x / blocks_a_sequence;
-    const int at = (blockIdx.x - b * blocks_a_sequence) * kThreads + threadIdx.x;
-    const int chunk = at / lanes_a_row, t0 = chunk * kRows;
+    const unsigned block = xcd_place(blockIdx.x, gridDim.x);
+    const int b = block / blocks_a_sequence;
+    const int at = (block - b * blocks_a_sequence) * kThreads + threadIdx.x;
+    const int chunk = at / lanes_a_row, t0 = chunk * ROWS;
     // the rows past the last one are there for the state behind the sequence
     if (t0 >= p.length && !(t0 == 0 && p.length == 0)) return;
     const int c0 = first_channel<V>(at - chunk * lanes_a_row, p.channels);
@@ -68,32 +73,48 @@ __global__ __launch_bounds__(kThreads) void causal_conv_kernel(sys_causal_conv1d
     const T* state = a.state ? (const T*)a.state + (size_t)b * (K - 1) * p.channels : nullptr;
     T* y = (T*)a.y + b * p.y_batch + c0;
 
-    float rows[K - 1 + kRows][V];
-    if (t0 >= K - 1 && t0 + kRows <= len) {
+    typename Channels<T, V>::Raw raw[K - 1 + ROWS];
+    if (t0 >= K - 1 && t0 + ROWS <= len) {
+        const T* from = x + (t0 - (K - 1)) * p.x_row + c0;
 #pragma unroll
-        for (int r = 0; r < K - 1 + kRows; ++r) Channels<T, V>::load(x + (t0 - (K - 1) + r) * p.x_row + c0, rows[r]);
+        for (int r = 0; r < K - 1 + ROWS; ++r) raw[r] = Channels<T, V>::raw(from + r * p.x_row);
     } else {
 #pragma unroll
-        for (int r = 0; r < K - 1 + kRows; ++r) load_row<T, K, V>(x, state, p.x_row, p.channels, t0 + r, len, c0, rows[r]);
+        for (int r = 0; r < K - 1 + ROWS; ++r) raw[r] = raw_row<T, K, V>(x, state, p.x_row, p.channels, t0 + r, len, c0);
     }
-    float tap[K][V], bias[V];
-    load_taps<K, V>(p, a.w, c0, tap);
-    load_bias<V>(p, a.bias, c0, bias);
+    float tap[K][V], bias[V], rows[K][V];
+    load_taps<T, K, V>(p, a.w, c0, tap);
+    load_bias<T, V>(p, a.bias, c0, bias);
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
+    for (int j = 0; j + 1 < K; ++j) Channels<T, V>::values(raw[j], rows[j + 1]);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
         if (t0 + r >= p.length) break;
+#pragma unroll
+        for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) rows[j][i] = rows[j + 1][i];
+        Channels<T, V>::values(raw[r + K - 1], rows[K - 1]);
         float out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float pre = bias[i];
 #pragma unroll
-            for (int j = 0; j < K; ++j) pre = __builtin_fmaf(tap[j][i], rows[r + j][i], pre);
-            out[i] = t0 + r < len ? (p.activation == SYS_ACT_SILU ? silu(pre) : pre) : 0.0f;
+            for (int j = 0; j < K; ++j) pre = __builtin_fmaf(tap[j][i], rows[j][i], pre);
+            out[i] = pre;
         }
-        Channels<T, V>::store(y + (t0 + r) * p.y_row, out);
+        if (p.activation == SYS_ACT_SILU) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) out[i] = silu(out[i]);
+        }
+        if (t0 + r >= len) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) out[i] = 0.0f;
+        }
+        Channels<T, V>::store_nt(y + (t0 + r) * p.y_row, out);
     }
     // the chunk that holds the last position (the first one of an empty sequence) leaves the state
-    const int last = len > 0 ? (len - 1) / kRows : 0;
+    const int last = len > 0 ? (len - 1) / ROWS : 0;
     if (a.state_out && chunk == last) {
         T* s = (T*)a.state_out + (size_t)b * (K - 1) * p.channels + c0;
         for (int j = 0; j < K - 1; ++j) {
@@ -106,20 +127,142 @@ __global__ __launch_bounds__(kThreads) void causal_conv_kernel(sys_causal_conv1d
 
 // ---------------------------------------------------------------- gradients
 
-constexpr int kRun = 64;           // rows a lane in the backward kernel
+constexpr int kRun = 32;           // rows a lane in the backward kernel
 constexpr int kRunWaves = 4;       // runs a workgroup: a wavefront each, whose sums for the taps are added in LDS
+constexpr int kAhead = 4;          // rows whose loads are in flight while as many are worked on
 
-// In rows e of state ++ x, e = 0 .. len+K-2: dext[e] = sum_j w[j] dpre[e-j] (dpre is 0 outside 0 .. len-1), plus the gradient of
-// the state behind the sequence in its last K-1 rows; the first K-1 rows are the gradient of the state before it.  Going down
-// the rows, dpre[e] needs rows e .. e+K-1 of state ++ x, and dext[e] the last K values of dpre, so one window of each moves
-// along.  A run begins K-1 rows early to fill the window of dpre.
+// What a lane of the backward kernel carries down the rows.  In rows e of state ++ x, e = 0 .. len+K-2: dext[e] = sum_j w[j] dpre[e-j]
+// (dpre is 0 outside 0 .. len-1), plus the gradient of the state behind the sequence in its last K-1 rows; the first K-1 rows are the
+// gradient of the state before it.  Going down the rows, dpre[e] needs rows e .. e+K-1 of state ++ x, and dext[e] the last K values of
+// dpre, so one window of each moves along.  A run begins K-1 rows early to fill the window of dpre.
+template <typename T, int K, int V>
+struct GradWindow {
+    float tap[K][V], bias[V];
+    float rows[K][V], dpre[K][V];      // rows e .. e+K-1; dpre[e-(K-1)] .. dpre[e]
+    float sums[K + 1][V];              // of the taps and the bias
+    bool silu_there;
+
+    // the windows move on by a row: next is row e+K-1 of state ++ x
+    __device__ __forceinline__ void move(typename Channels<T, V>::Raw next)
+    {
+#pragma unroll
+        for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) rows[j][i] = rows[j + 1][i], dpre[j][i] = dpre[j + 1][i];
+        Channels<T, V>::values(next, rows[K - 1]);
+    }
+    __device__ __forceinline__ void differentiate(typename Channels<T, V>::Raw dy)
+    {
+        Channels<T, V>::values(dy, dpre[K - 1]);
+        if (!silu_there) return;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float pre = bias[i];
+#pragma unroll
+            for (int j = 0; j < K; ++j) pre = __builtin_fmaf(tap[j][i], rows[j][i], pre);
+            dpre[K - 1][i] *= silu_grad(pre);
+        }
+    }
+    __device__ __forceinline__ void nothing()
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) dpre[K - 1][i] = 0.0f;
+    }
+    __device__ __forceinline__ void add()
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int j = 0; j < K; ++j) sums[j][i] = __builtin_fmaf(dpre[K - 1][i], rows[j][i], sums[j][i]);
+            sums[K][i] += dpre[K - 1][i];
+        }
+    }
+    __device__ __forceinline__ void output(float (&out)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            out[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < K; ++j) out[i] = __builtin_fmaf(tap[j][i], dpre[K - 1 - j][i], out[i]);
+        }
+    }
+};
+
+// Rows begin .. end-1 of dext.  WHOLE: every row of x and dy that they need exists, and none is a state's; else each is asked for (the
+// same for all lanes of a wavefront).  Either way kAhead rows are in flight while as many are worked on.
+template <typename T, int K, int V, bool WHOLE>
+__device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const CausalConvArgs& a, GradWindow<T, K, V>& w, const T* x, const T* dy, const T* state,
+                                         int b, int c0, int len, int begin, int end)
+{
+    typedef Channels<T, V> C;
+    const T* dstate_out = a.dstate_out ? (const T*)a.dstate_out + (size_t)b * (K - 1) * p.channels + c0 : nullptr;
+    T* dstate = a.dstate ? (T*)a.dstate + (size_t)b * (K - 1) * p.channels + c0 : nullptr;
+    T* dx = (T*)a.dx + (size_t)b * p.length * p.channels + c0;
+    const T* whole_x = x + (begin - (K - 1)) * p.x_row + c0;           // row `begin` of state ++ x
+    const T* whole_dy = dy + begin * p.y_row;
+    auto load_x = [&](int e) { return WHOLE ? C::raw(whole_x + (e - begin) * p.x_row) : raw_row<T, K, V>(x, state, p.x_row, p.channels, e, len, c0); };
+    auto load_dy = [&](int e) { return WHOLE || (e >= 0 && e < len) ? C::raw(WHOLE ? whole_dy + (e - begin) * p.y_row : dy + e * p.y_row) : typename C::Raw{}; };
+    typename C::Raw first[K - 1], more[K - 1], more_dy[K - 1], ahead[kAhead], ahead_dy[kAhead];
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+        first[j] = load_x(begin - (K - 1) + j);
+        more[j] = load_x(begin + j);
+        more_dy[j] = load_dy(begin - (K - 1) + j);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ahead[k] = load_x(begin + K - 1 + k), ahead_dy[k] = load_dy(begin + k);
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) C::values(first[j], w.rows[j + 1]);
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+        w.move(more[j]);
+        if (WHOLE || begin - (K - 1) + j >= 0) w.differentiate(more_dy[j]);      // (zeros where there is no dy)
+        else w.nothing();
+    }
+    for (int e0 = begin; e0 < end; e0 += kAhead) {
+        typename C::Raw now[kAhead], now_dy[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) now[k] = ahead[k], now_dy[k] = ahead_dy[k];
+        const int next = !WHOLE || e0 + kAhead < end ? e0 + kAhead : e0;            // (the last round loads its own rows once more)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) ahead[k] = load_x(next + K - 1 + k), ahead_dy[k] = load_dy(next + k);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int e = e0 + k;
+            w.move(now[k]);
+            float out[V];
+            if (WHOLE || (e >= 0 && e < len)) {
+                w.differentiate(now_dy[k]);
+                w.add();               // (0 * a row that holds a NaN would be one)
+            } else {
+                w.nothing();
+            }
+            w.output(out);
+            if (WHOLE) {
+                C::store_nt(dx + (size_t)(e - (K - 1)) * p.channels, out);
+                continue;
+            }
+            if (e >= end) break;
+            if (dstate_out && e >= len && e < len + K - 1) {
+                float tail[V];
+                C::load(dstate_out + (size_t)(e - len) * p.channels, tail);
+#pragma unroll
+                for (int i = 0; i < V; ++i) out[i] += tail[i];
+            }
+            if (e >= K - 1) C::store_nt(dx + (size_t)(e - (K - 1)) * p.channels, out);
+            else if (dstate) C::store(dstate + (size_t)e * p.channels, out);
+        }
+    }
+}
+
 template <typename T, int K, int V>
 __global__ __launch_bounds__(kRunWaves * 64) void causal_conv_grad_kernel(sys_causal_conv1d_t p, CausalConvArgs a, int runs, int groups_a_sequence, int lane_blocks)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lanes_a_row = (p.channels + V - 1) / V;
-    const int lane_block = blockIdx.x % lane_blocks;
-    const int rest = blockIdx.x / lane_blocks;
+    const unsigned block = xcd_place(blockIdx.x, gridDim.x);
+    const int lane_block = block % lane_blocks;
+    const int rest = block / lane_blocks;
     const int b = rest / groups_a_sequence, group = rest - b * groups_a_sequence;
     const int run = group * kRunWaves + wave;
     const int channel_lane = lane_block * 64 + lane;
@@ -129,73 +272,24 @@ __global__ __launch_bounds__(kRunWaves * 64) void causal_conv_grad_kernel(sys_ca
     const T* x = (const T*)a.x + b * p.x_batch;
     const T* dy = (const T*)a.dy + b * p.y_batch + c0;
     const T* state = a.state ? (const T*)a.state + (size_t)b * (K - 1) * p.channels : nullptr;
-    const T* dstate_out = a.dstate_out ? (const T*)a.dstate_out + (size_t)b * (K - 1) * p.channels + c0 : nullptr;
-    T* dstate = a.dstate ? (T*)a.dstate + (size_t)b * (K - 1) * p.channels + c0 : nullptr;
-    T* dx = (T*)a.dx + (size_t)b * p.length * p.channels + c0;
 
-    float sums[K + 1][V];              // of the taps and the bias
+    GradWindow<T, K, V> w;
 #pragma unroll
     for (int j = 0; j <= K; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sums[j][i] = 0.0f;
-
+        for (int i = 0; i < V; ++i) w.sums[j][i] = 0.0f;
     if (there) {
-        float tap[K][V], bias[V];
-        load_taps<K, V>(p, a.w, c0, tap);
-        load_bias<V>(p, a.bias, c0, bias);
-        const int begin = run * kRun, total = p.length + K - 1;
-        const int end = begin + kRun < total ? begin + kRun : total;
-        float rows[K][V], dpre[K][V];  // rows e .. e+K-1; dpre[e-(K-1)] .. dpre[e]
+        load_taps<T, K, V>(p, a.w, c0, w.tap);
+        load_bias<T, V>(p, a.bias, c0, w.bias);
+        w.silu_there = p.activation == SYS_ACT_SILU;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) dpre[j][i] = rows[j][i] = 0.0f;
-#pragma unroll
-        for (int j = 1; j < K; ++j) load_row<T, K, V>(x, state, p.x_row, p.channels, begin - (K - 1) + j - 1, len, c0, rows[j]);
-        for (int e = begin - (K - 1); e < end; ++e) {
-            float g[V];
-#pragma unroll
-            for (int j = 0; j + 1 < K; ++j)
-#pragma unroll
-                for (int i = 0; i < V; ++i) { rows[j][i] = rows[j + 1][i]; dpre[j][i] = dpre[j + 1][i]; }
-            load_row<T, K, V>(x, state, p.x_row, p.channels, e + K - 1, len, c0, rows[K - 1]);
-            const bool on = e >= 0 && e < len;
-            if (on) Channels<T, V>::load(dy + e * p.y_row, g);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float pre = bias[i];
-#pragma unroll
-                for (int j = 0; j < K; ++j) pre = __builtin_fmaf(tap[j][i], rows[j][i], pre);
-                dpre[K - 1][i] = on ? (p.activation == SYS_ACT_SILU ? g[i] * silu_grad(pre) : g[i]) : 0.0f;
-            }
-            if (e < begin) continue;
-            float out[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                out[i] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < K; ++j) out[i] = __builtin_fmaf(tap[j][i], dpre[K - 1 - j][i], out[i]);
-            }
-            if (on) {                  // (0 * a row that holds a NaN would be one)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-#pragma unroll
-                    for (int j = 0; j < K; ++j) sums[j][i] = __builtin_fmaf(dpre[K - 1][i], rows[j][i], sums[j][i]);
-                    sums[K][i] += dpre[K - 1][i];
-                }
-            }
-            if (dstate_out && e >= len && e < len + K - 1) {
-                float more[V];
-                Channels<T, V>::load(dstate_out + (size_t)(e - len) * p.channels, more);
-#pragma unroll
-                for (int i = 0; i < V; ++i) out[i] += more[i];
-            }
-            if (e < K - 1) {
-                if (dstate) Channels<T, V>::store(dstate + (size_t)e * p.channels, out);
-            } else {
-                Channels<T, V>::store(dx + (size_t)(e - (K - 1)) * p.channels, out);
-            }
-        }
+            for (int i = 0; i < V; ++i) w.dpre[j][i] = w.rows[j][i] = 0.0f;
+        // the last run goes on through the K-1 rows behind the sequence
+        const int begin = run * kRun;
+        if (begin >= 2 * (K - 1) && begin + kRun <= len && run != runs - 1) grad_run<T, K, V, true>(p, a, w, x, dy, state, b, c0, len, begin, begin + kRun);
+        else grad_run<T, K, V, false>(p, a, w, x, dy, state, b, c0, len, begin, run == runs - 1 ? p.length + K - 1 : begin + kRun);
     }
 
     // the workgroup's sums, [K+1][channels] a workgroup
@@ -205,7 +299,7 @@ __global__ __launch_bounds__(kRunWaves * 64) void causal_conv_grad_kernel(sys_ca
     for (int j = 0; j <= K; ++j) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) shared[wave][i * 64 + lane] = sums[j][i];
+        for (int i = 0; i < V; ++i) shared[wave][i * 64 + lane] = w.sums[j][i];
         __syncthreads();
         if (wave == 0 && channel_lane < lanes_a_row) {
 #pragma unroll
@@ -261,8 +355,8 @@ __global__ __launch_bounds__(kThreads) void causal_conv_step_kernel(sys_causal_c
 #pragma unroll
     for (int j = 0; j + 1 < K; ++j) Channels<T, V>::load((const T*)a.state + base + (size_t)j * p.channels, rows[j]);
     Channels<T, V>::load((const T*)a.x + r * p.x_batch + c0, rows[K - 1]);
-    load_taps<K, V>(p, a.w, c0, tap);
-    load_bias<V>(p, a.bias, c0, bias);
+    load_taps<T, K, V>(p, a.w, c0, tap);
+    load_bias<T, V>(p, a.bias, c0, bias);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         float pre = bias[i];
@@ -277,18 +371,27 @@ __global__ __launch_bounds__(kThreads) void causal_conv_step_kernel(sys_causal_c
 
 // ---------------------------------------------------------------- launches
 
-int runs_of(const sys_causal_conv1d_t& p) { return (p.length + p.width - 1 + kRun - 1) / kRun; }
+int runs_of(const sys_causal_conv1d_t& p) { return p.length ? (p.length + kRun - 1) / kRun : 1; }
 int run_groups_of(const sys_causal_conv1d_t& p) { return (runs_of(p) + kRunWaves - 1) / kRunWaves; }
+
+template <typename T, int K, int V, int ROWS>
+hipError_t launch_rows(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s)
+{
+    const int lanes = (p.channels + V - 1) / V;
+    const long long chunks = p.length ? (p.length + ROWS - 1) / ROWS : 1;
+    const long long blocks = (chunks * lanes + kThreads - 1) / kThreads;
+    if (chunks * lanes > 0x7fffffffLL - kThreads || blocks * p.batch > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((causal_conv_kernel<T, K, V, ROWS>), dim3((unsigned)(blocks * p.batch)), dim3(kThreads), 0, s, p, a, (int)blocks, lanes);
+    return hipGetLastError();
+}
 
 template <typename T, int K, int V>
 hipError_t launch_forward(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s)
 {
-    const int lanes = (p.channels + V - 1) / V;
-    const long long chunks = p.length ? (p.length + kRows - 1) / kRows : 1;
-    const long long blocks = (chunks * lanes + kThreads - 1) / kThreads;
-    if (chunks * lanes > 0x7fffffffLL - kThreads || blocks * p.batch > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((causal_conv_kernel<T, K, V>), dim3((unsigned)(blocks * p.batch)), dim3(kThreads), 0, s, p, a, (int)blocks, lanes);
-    return hipGetLastError();
+    // Rows a lane: 16 read the K-1 rows above a chunk the least often, 4 leave the most wavefronts (K = 4 in bf16, 4 / 8 / 16 rows: 1 x 2048 x 1024
+    // 3.8 / 4.8 / 6.8 us, 4 x 1024 x 2048 8.0 / 8.8 / 9.1, 8 x 2048 x 1024 14.2 / 14.1 / 14.6, 4 x 4096 x 2048 26.6 / 25.3 / 24.3).
+    const double waves = (double)p.batch * p.length * ((p.channels + V - 1) / V) / (16 * 64);
+    return waves >= 3072 ? launch_rows<T, K, V, 16>(p, a, s) : launch_rows<T, K, V, 4>(p, a, s);
 }
 
 template <typename T, int K, int V>
@@ -325,7 +428,8 @@ hipError_t launch_width(Form form, const sys_causal_conv1d_t& p, const CausalCon
     constexpr int V = kLaneChannels<T>;
     switch (form) {
     case kForward: return p.channels >= V ? launch_forward<T, K, V>(p, a, s) : launch_forward<T, K, 1>(p, a, s);
-    case kBackward: return p.channels >= V ? launch_backward<T, K, V>(p, a, s) : launch_backward<T, K, 1>(p, a, s);
+    // half as wide: the windows, taps and sums of 16 bytes take 230 registers (4 taps; 53.7 / 53.9 us, level) or more than there are (8)
+    case kBackward: return p.channels >= V / 2 ? launch_backward<T, K, V / 2>(p, a, s) : launch_backward<T, K, 1>(p, a, s);
     // lanes that share channels would read states that others have moved on
     default: return p.channels % V == 0 ? launch_step<T, K, V>(p, a, s) : launch_step<T, K, 1>(p, a, s);
     }

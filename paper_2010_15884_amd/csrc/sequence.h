@@ -22,12 +22,16 @@ template <typename T, int V>
 struct Channels {
     typedef T Vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     typedef float F __attribute__((ext_vector_type(V)));
-    static __device__ __forceinline__ void load(const T* p, float (&out)[V])
+    // as they lie in memory: half the registers of their values, for loads that are far ahead of their use
+    typedef T Raw __attribute__((ext_vector_type(V)));
+    static __device__ __forceinline__ Raw raw(const T* p) { return *(const Vec*)p; }
+    static __device__ __forceinline__ void values(Raw v, float (&out)[V])
     {
-        const F f = __builtin_convertvector(*(const Vec*)p, F);
+        const F f = __builtin_convertvector(v, F);
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = f[i];
     }
+    static __device__ __forceinline__ void load(const T* p, float (&out)[V]) { values(raw(p), out); }
     static __device__ __forceinline__ void store(T* p, const float (&in)[V])
     {
         F f;
@@ -35,12 +39,23 @@ struct Channels {
         for (int i = 0; i < V; ++i) f[i] = in[i];
         *(Vec*)p = __builtin_convertvector(f, Vec);
     }
+    static __device__ __forceinline__ void store_nt(T* p, const float (&in)[V])
+    {
+        F f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = in[i];
+        __builtin_nontemporal_store(__builtin_convertvector(f, Vec), (Vec*)p);
+    }
 };
 
 template <typename T>
 struct Channels<T, 1> {
+    typedef T Raw;
+    static __device__ __forceinline__ Raw raw(const T* p) { return *p; }
+    static __device__ __forceinline__ void values(Raw v, float (&out)[1]) { out[0] = (float)v; }
     static __device__ __forceinline__ void load(const T* p, float (&out)[1]) { out[0] = (float)*p; }
     static __device__ __forceinline__ void store(T* p, const float (&in)[1]) { *p = (T)in[0]; }
+    static __device__ __forceinline__ void store_nt(T* p, const float (&in)[1]) { *p = (T)in[0]; }
 };
 
 // Channels of 16 bytes: what a lane loads at once.
@@ -52,6 +67,24 @@ __device__ __forceinline__ float load_param(const void* p, size_t i, int dtype)
     if (dtype == SYS_F32) return ((const float*)p)[i];
     if (dtype == SYS_F16) return (float)((const f16_t*)p)[i];
     return (float)((const bf16_t*)p)[i];
+}
+
+// N neighbouring parameters from the i-th on, of T or fp32: one branch for all of them, loads of up to 16 bytes.
+template <typename T, int N>
+__device__ __forceinline__ void load_params(const void* p, size_t i, int dtype, float (&out)[N])
+{
+    constexpr int kMost = kLaneChannels<T>;
+    if (sizeof(T) == 4 || dtype == SYS_F32) {
+#pragma unroll
+        for (int k = 0; k + 4 <= N; k += 4) Channels<float, 4>::load((const float*)p + i + k, *(float(*)[4])(out + k));
+#pragma unroll
+        for (int k = N / 4 * 4; k < N; ++k) out[k] = ((const float*)p)[i + k];
+    } else {
+#pragma unroll
+        for (int k = 0; k + kMost <= N; k += kMost) Channels<T, kMost>::load((const T*)p + i + k, *(float(*)[kMost])(out + k));
+#pragma unroll
+        for (int k = N / kMost * kMost; k < N; ++k) out[k] = (float)((const T*)p)[i + k];
+    }
 }
 
 __device__ __forceinline__ void store_param(void* p, size_t i, int dtype, float v)
@@ -112,6 +145,13 @@ template <int J>
 __device__ __forceinline__ float quad_take(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), J * 0x55, 0xF, 0xF, true));
+}
+
+// Workgroups go round the eight XCDs, each with an L2 of its own: workgroup i of n works at place(i), so that an XCD gets neighbouring places.
+__device__ __forceinline__ unsigned xcd_place(unsigned i, unsigned n)
+{
+    const unsigned each = n / 8;
+    return i < each * 8 ? (i & 7) * each + (i >> 3) : i;
 }
 
 // The positions of sequence b that exist: its length, held within the rows that there are.
