@@ -1,9 +1,12 @@
 // Group norm with an activation, channels last: y = act((x - mean) rstd w + b), statistics over the rows of a batch entry and the
 // channels of a group.  Bound by memory: some ten operations a value beside its bytes.
 //
-// A lane holds V neighbouring channels of one group (16 bytes, or what divides a group's channels) and walks down the rows.
+// Two ways.  Where a group's rows fit the registers of a workgroup (or of a part of a wavefront: a token, a small image) they are
+// read once, wait there for the group's sums, and are written once (norm_resident_kernel, norm_grad_resident_kernel).  Else a first
+// launch sums up chunks of rows channel by channel, a small one combines them, and a last one reads the rows again.
+//
 // Values and squares are never summed as they come, so a mean far from zero costs no digits of the variance: the group's first
-// value is taken off every other one, eight differences at a time give their own mean and sum of squared distances, and
+// value is taken off every other one, some differences at a time give their own mean and sum of squared distances, and
 // (count, mean, distances) are merged pairwise, n = n1 + n2, mean = mean1 + d n2/n, M2 = M2_1 + M2_2 + d^2 n1 n2/n with
 // d = mean2 - mean1 (the first value may be far from all others).
 #include "launch.h"
@@ -13,13 +16,6 @@ namespace sysconv {
 namespace {
 
 constexpr int kThreads = 256;
-
-struct NormShape {
-    int columns;                   // lanes a row: channels / V
-    int columns_a_group;
-    int chunks;                    // of the rows, a workgroup each
-    long long chunk_rows;
-};
 
 struct Moments {
     float n, mean, m2;
@@ -32,11 +28,7 @@ __device__ __forceinline__ Moments merged(Moments a, Moments b)
     return {n, b.n > 0.0f ? __builtin_fmaf(d, share, a.mean) : a.mean, b.n > 0.0f ? a.m2 + b.m2 + d * d * a.n * share : a.m2};
 }
 
-__device__ __forceinline__ Moments over_wave(Moments m)
-{
-    for (int k = 1; k < 64; k <<= 1) m = merged(m, Moments{__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.m2, k)});
-    return m;
-}
+__device__ __forceinline__ Moments from_lane(Moments m, int k) { return {__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.m2, k)}; }
 
 __device__ __forceinline__ float activated(float v, int activation)
 {
@@ -49,6 +41,290 @@ __device__ __forceinline__ float activated_grad(float v, int activation)
     if (activation == SYS_ACT_SILU) return silu_grad(v);
     return activation == SYS_ACT_RELU ? (v > 0.0f ? 1.0f : 0.0f) : 1.0f;
 }
+
+// What is taken off a group's values: the first one of the batch entry.
+template <typename T>
+__device__ __forceinline__ float group_first(const sys_group_norm_t& p, const T* x, int group)
+{
+    return (float)x[(long long)group * (p.channels / p.groups)];
+}
+
+// w and b of V channels, 1 and 0 without them.
+template <typename T, int V>
+__device__ __forceinline__ void load_affine(const sys_group_norm_t& p, const NormArgs& a, int channel, float (&w)[V], float (&b)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = 1.0f, b[i] = 0.0f;
+    if (a.w) load_params<T, V>(a.w, (size_t)channel, p.param_dtype, w);
+    if (a.b) load_params<T, V>(a.b, (size_t)channel, p.param_dtype, b);
+}
+
+// ================================================================ rows that stay in registers
+
+// A unit -- a batch entry and `tile` neighbouring groups -- has 2^log_unit lanes, 1 to 1024: a part of a wavefront or a whole workgroup.
+// From the lowest bits of the lane up: lane of the group (V channels each, rounded up to a power of two), group of the tile, row.
+// A lane has its channels in `items` rows.
+struct ResidentShape {
+    int log_group, log_tile, log_unit, threads;     // lanes a group; groups a tile; lanes a unit; lanes a workgroup
+    int items, tiles;                               // tiles: of a batch entry
+    int columns_a_group;                            // lanes of a group that hold channels
+    int slices;                                     // gradients: batch entries are dealt out to so many units of a tile
+};
+
+struct ResidentLane {
+    int unit, tile_group, group, row, tall, channel;
+    bool there;
+    __device__ __forceinline__ ResidentLane(const sys_group_norm_t& p, const ResidentShape& s, int units, unsigned place)
+    {
+        const int in_unit = threadIdx.x & ((1 << s.log_unit) - 1), in_group = in_unit & ((1 << s.log_group) - 1);
+        const int index = place * (blockDim.x >> s.log_unit) + (threadIdx.x >> s.log_unit);
+        unit = index < units ? index : units - 1;
+        tile_group = (in_unit >> s.log_group) & ((1 << s.log_tile) - 1);
+        row = in_unit >> (s.log_group + s.log_tile);
+        tall = 1 << (s.log_unit - s.log_group - s.log_tile);
+        const int g = unit % s.tiles * (1 << s.log_tile) + tile_group;
+        there = index < units && in_group < s.columns_a_group && g < p.groups;
+        group = g < p.groups ? g : p.groups - 1;
+        const int channels = p.channels / p.groups, v = channels / s.columns_a_group;
+        channel = group * channels + (in_group < s.columns_a_group ? in_group : 0) * v;
+    }
+};
+
+// Rows of a lane: those past the last one repeat it, and their values are not used.
+template <typename T, int V, int ITEMS>
+struct ResidentRows {
+    typename Channels<T, V>::Raw raw[ITEMS];
+    __device__ __forceinline__ void load(const T* from, long long row_stride, long long rows, int row, int tall, int items)
+    {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (ITEMS > 1 && i >= items) continue;
+            const long long r = row + (long long)i * tall;
+            raw[i] = Channels<T, V>::raw(from + (r < rows ? r : rows - 1) * row_stride);
+        }
+    }
+};
+
+// The same rows, to be worked on once more: without this the compiler keeps what it made of them the first time, in registers that are not there.
+template <typename Raw>
+__device__ __forceinline__ void forget(Raw& raw)
+{
+    if constexpr (sizeof(Raw) == 2) {
+        unsigned v = __builtin_bit_cast(unsigned short, raw);
+        asm volatile("" : "+v"(v));
+        raw = __builtin_bit_cast(Raw, (unsigned short)v);
+    } else if constexpr (sizeof(Raw) == 4) {
+        unsigned v = __builtin_bit_cast(unsigned, raw);
+        asm volatile("" : "+v"(v));
+        raw = __builtin_bit_cast(Raw, v);
+    } else {
+        typedef unsigned Words __attribute__((ext_vector_type(sizeof(Raw) / 4)));
+        Words v = __builtin_bit_cast(Words, raw);
+        asm volatile("" : "+v"(v));
+        raw = __builtin_bit_cast(Raw, v);
+    }
+}
+
+// Adds up over the lanes of a unit that share a group: F merges two values, in an order that depends on the shape alone.
+// Units of more than a wavefront go through LDS, [wavefront][group of the tile]; every wavefront of the workgroup has to come here.
+template <typename M, typename FromLane, typename Merge>
+__device__ __forceinline__ M over_unit(const ResidentShape& s, int tile_group, M m, M* shared, FromLane from, Merge merge)
+{
+    for (int bit = 0; bit < s.log_unit && bit < 6; ++bit)
+        if (bit < s.log_group || bit >= s.log_group + s.log_tile) m = merge(m, from(m, 1 << bit));
+    if (s.log_unit <= 6) return m;
+    const int waves = 1 << (s.log_unit - 6), first = (threadIdx.x >> s.log_unit) * waves;
+    __syncthreads();                                // (what a call before this one left has been read)
+    const unsigned lane = threadIdx.x & 63;
+    if (lane < (1u << (s.log_group + s.log_tile)) && (lane & ((1u << s.log_group) - 1)) == 0)
+        shared[((threadIdx.x >> 6) << s.log_tile) + tile_group] = m;
+    __syncthreads();
+    m = shared[(first << s.log_tile) + tile_group];
+    for (int k = 1; k < waves; ++k) m = merge(m, shared[((first + k) << s.log_tile) + tile_group]);
+    return m;
+}
+
+constexpr int kMostTile = 32;                       // groups a tile, and entries of `shared` a wavefront
+
+template <typename T, int V, int ITEMS>
+__global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
+{
+    __shared__ Moments shared[16 * kMostTile];
+    const ResidentLane at(p, s, p.batch * s.tiles, xcd_place(blockIdx.x, gridDim.x));
+    const int b = at.unit / s.tiles;
+    const T* x = (const T*)a.x + b * p.x_batch;
+    ResidentRows<T, V, ITEMS> rows;
+    rows.load(x + at.channel, p.x_row, p.rows, at.row, at.tall, s.items);
+    const float first = group_first<T>(p, x, at.group);
+    float w[V], shift[V];
+    load_affine<T, V>(p, a, at.channel, w, shift);
+    Moments m = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (ITEMS > 1 && i >= s.items) continue;
+        float v[V], sum = 0.0f, square = 0.0f;
+        Channels<T, V>::values(rows.raw[i], v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum += v[k] - first;
+        const float mean = sum * (1.0f / V);
+#pragma unroll
+        for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - first) - mean, (v[k] - first) - mean, square);
+        const bool on = at.there && at.row + (long long)i * at.tall < p.rows;
+        // (what is not there gives no count; a NaN in a row that is repeated is in its group already)
+        m = merged(m, Moments{on ? (float)V : 0.0f, on ? mean : 0.0f, on ? square : 0.0f});
+    }
+    m = over_unit(s, at.tile_group, m, shared, [](Moments v, int k) { return from_lane(v, k); }, [](Moments l, Moments r) { return merged(l, r); });
+    if (!at.there) return;
+    const float mean = m.mean + first, rstd = 1.0f / __builtin_sqrtf(m.m2 / m.n + p.eps);
+    if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
+        if (a.mean) a.mean[(size_t)b * p.groups + at.group] = mean;
+        if (a.rstd) a.rstd[(size_t)b * p.groups + at.group] = rstd;
+    }
+    T* y = (T*)a.y + b * p.y_batch + at.channel;
+#pragma unroll
+    for (int k = 0; k < V; ++k) w[k] *= rstd;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (ITEMS > 1 && i >= s.items) continue;
+        const long long r = at.row + (long long)i * at.tall;
+        if (r >= p.rows) continue;
+        float v[V];
+        Channels<T, V>::values(rows.raw[i], v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf(v[k] - mean, w[k], shift[k]);
+        if (p.activation != SYS_ACT_NONE) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = activated(v[k], p.activation);
+        }
+        Channels<T, V>::store_nt(y + r * p.y_row, v);
+    }
+}
+
+// Gradients: with hat = (x - mean) rstd and f = dy act'(hat w + b): dw = sum f hat, db = sum f over batch and rows, and
+// dx = rstd (f w - m1 - hat m2), m1 = E[f w], m2 = E[f w hat] over the group.
+
+struct Pair {
+    float a, b;
+};
+
+// f and hat of V channels of a row.
+template <int V>
+__device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[V], const float (&mean)[V], const float (&rstd)[V], const float (&w)[V], const float (&shift)[V], int activation,
+                                         float (&f)[V], float (&hat)[V])
+{
+#pragma unroll
+    for (int k = 0; k < V; ++k) hat[k] = (x[k] - mean[k]) * rstd[k], f[k] = dy[k];
+    if (activation == SYS_ACT_NONE) return;
+#pragma unroll
+    for (int k = 0; k < V; ++k) f[k] *= activated_grad(__builtin_fmaf(hat[k], w[k], shift[k]), activation);
+}
+
+// A unit goes through the batch entries of its slice (one row a lane: with the next one's on their way) and adds up dw and db of its channels:
+// [slice][f | f hat][channel] in the workspace.
+template <typename T, int V, int ITEMS>
+__global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
+{
+    __shared__ Pair shared[8 * kMostTile];
+    __shared__ float sums[512];
+    const ResidentLane at(p, s, s.slices * s.tiles, xcd_place(blockIdx.x, gridDim.x));
+    const int slice = at.unit / s.tiles;
+    const T *x = (const T*)a.x + at.channel, *dy = (const T*)a.dy + at.channel;
+    float w[V], shift[V], f_sum[V], hat_sum[V];
+    load_affine<T, V>(p, a, at.channel, w, shift);
+#pragma unroll
+    for (int k = 0; k < V; ++k) f_sum[k] = hat_sum[k] = 0.0f;
+    const float share = 1.0f / ((float)p.rows * (float)(p.channels / p.groups));
+    ResidentRows<T, V, ITEMS> rows_x, rows_dy, next_x, next_dy;
+    auto fetch = [&](ResidentRows<T, V, ITEMS>& to_x, ResidentRows<T, V, ITEMS>& to_dy, int b) {
+        if (b >= p.batch) b = p.batch - 1;
+        to_x.load(x + b * p.x_batch, p.x_row, p.rows, at.row, at.tall, s.items);
+        to_dy.load(dy + b * p.y_batch, p.y_row, p.rows, at.row, at.tall, s.items);
+    };
+    if (ITEMS == 1) fetch(next_x, next_dy, slice);
+    // as many rounds for every unit, so that all wavefronts of a workgroup meet at its barriers
+    for (int b0 = 0; b0 < p.batch; b0 += s.slices) {
+        const int b = b0 + slice;
+        const bool there = at.there && b < p.batch;
+        if (ITEMS == 1) {
+            rows_x = next_x, rows_dy = next_dy;
+            if (b0 + s.slices < p.batch) fetch(next_x, next_dy, b + s.slices);
+        } else {
+            fetch(rows_x, rows_dy, b);
+        }
+        const size_t group = (size_t)(b < p.batch ? b : p.batch - 1) * p.groups + at.group;
+        float mean[V], rstd[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) mean[k] = a.mean_in[group], rstd[k] = a.rstd_in[group];
+        Pair m = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (ITEMS > 1 && i >= s.items) continue;
+            float v[V], g[V], f[V], hat[V];
+            Channels<T, V>::values(rows_x.raw[i], v);
+            Channels<T, V>::values(rows_dy.raw[i], g);
+            row_grad<V>(v, g, mean, rstd, w, shift, p.activation, f, hat);
+            if (there && at.row + (long long)i * at.tall < p.rows) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    f_sum[k] += f[k];
+                    hat_sum[k] = __builtin_fmaf(f[k], hat[k], hat_sum[k]);
+                    m.a = __builtin_fmaf(f[k], w[k], m.a);
+                    m.b = __builtin_fmaf(f[k] * w[k], hat[k], m.b);
+                }
+            }
+        }
+        m = over_unit(s, at.tile_group, m, shared, [](Pair v, int k) { return Pair{__shfl_xor(v.a, k), __shfl_xor(v.b, k)}; },
+                      [](Pair l, Pair r) { return Pair{l.a + r.a, l.b + r.b}; });
+        const float m1 = m.a * share, m2 = m.b * share;
+        T* dx = (T*)a.dx + (size_t)(b < p.batch ? b : 0) * p.rows * p.channels + at.channel;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (ITEMS > 1 && i >= s.items) continue;
+            const long long r = at.row + (long long)i * at.tall;
+            if (!there || r >= p.rows) continue;
+            float v[V], g[V], f[V], hat[V];
+            if (ITEMS > 1) {
+                forget(rows_x.raw[i]);
+                forget(rows_dy.raw[i]);
+            }
+            Channels<T, V>::values(rows_x.raw[i], v);
+            Channels<T, V>::values(rows_dy.raw[i], g);
+            row_grad<V>(v, g, mean, rstd, w, shift, p.activation, f, hat);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = rstd[k] * (__builtin_fmaf(f[k], w[k], -m1) - hat[k] * m2);
+            Channels<T, V>::store_nt(dx + r * p.channels, v);
+        }
+    }
+    if (!a.dw && !a.db) return;
+    // over the rows of the unit: the upper bits of the lane
+    const int wide = s.log_group + s.log_tile;
+    float* to = a.workspace + (size_t)slice * 2 * p.channels + at.channel;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        for (int which = 0; which < 2; ++which) {
+            float v = which ? hat_sum[k] : f_sum[k];
+            for (int bit = wide; bit < s.log_unit && bit < 6; ++bit) v += __shfl_xor(v, 1 << bit);
+            if (s.log_unit > 6 && wide < s.log_unit) {
+                __syncthreads();
+                sums[threadIdx.x] = v;
+                __syncthreads();
+                const int step = wide < 6 ? 64 : 1 << wide, first = threadIdx.x & ~((1 << s.log_unit) - 1);
+                if (at.row == 0) {
+                    for (int t = step; t < (1 << s.log_unit); t += step) v += sums[first + (threadIdx.x & ((1 << wide) - 1)) + t];
+                }
+            }
+            if (at.there && at.row == 0) to[(size_t)which * p.channels + k] = v;
+        }
+    }
+}
+
+// ================================================================ rows that are read twice
+
+struct NormShape {
+    int columns;                   // lanes a row, of V channels (the last one begins earlier where channels are no multiple of V)
+    int chunks;                    // of the rows, a workgroup each
+    long long chunk_rows;
+};
 
 // Where a lane of a workgroup works: 256 lanes side by side in a row, or several rows of fewer.
 struct Lanes {
@@ -64,83 +340,123 @@ struct Lanes {
     }
 };
 
-// ---------------------------------------------------------------- forward
+// Rows of a lane that are on their way together.
+constexpr int kNormRows = 8;
 
-// What is taken off a group's values: the first one of the batch entry.
-template <typename T>
-__device__ __forceinline__ float group_first(const sys_group_norm_t& p, const T* x, int group)
-{
-    return (float)x[(long long)group * (p.channels / p.groups)];
-}
-
-// Moments of every column of a chunk of rows: [batch][chunk][column] Moments.
+// Mean (less the group's first value) and sum of squared distances of every channel in a chunk of rows: [batch][chunk][mean | m2][channel].
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
-    constexpr int kBatchRows = 8 / V;
     const int b = blockIdx.x / shape.chunks, chunk = blockIdx.x - b * shape.chunks;
     const Lanes at(shape.columns);
+    const int channels = p.channels / p.groups;
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
     const T* x = (const T*)a.x + b * p.x_batch;
-    Moments* to = (Moments*)a.workspace + ((size_t)b * shape.chunks + chunk) * shape.columns;
-    __shared__ Moments shared[kThreads];
+    float* to = a.workspace + ((size_t)b * shape.chunks + chunk) * 2 * p.channels;
+    __shared__ float shared_n[kThreads], shared_mean[V][kThreads], shared_m2[V][kThreads];
     for (int c0 = 0; c0 < shape.columns; c0 += at.wide) {
-        const int column = c0 + at.column;
-        Moments m = {0.0f, 0.0f, 0.0f};
-        if (at.there && column < shape.columns) {
-            const float first = group_first<T>(p, x, column / shape.columns_a_group);
-            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kBatchRows) {
-                float v[kBatchRows][V], sum = 0.0f, count = 0.0f, square = 0.0f;
+        const bool there = at.there && c0 + at.column < shape.columns;
+        const int column = c0 + at.column < shape.columns ? c0 + at.column : shape.columns - 1;
+        const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
+        float n = 0.0f, mean[V], m2[V], first[V];
 #pragma unroll
-                for (int k = 0; k < kBatchRows; ++k) {
-                    const bool on = r + (long long)k * at.tall < end;
-                    Channels<T, V>::load(x + (on ? r + (long long)k * at.tall : r) * p.x_row + (long long)column * V, v[k]);
-                    count += on ? (float)V : 0.0f;
+        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f, first[i] = group_first<T>(p, x, (channel + i) / channels);
+        if (there) {
+            const T* from = x + channel;
+            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
+                typename Channels<T, V>::Raw raw[kNormRows];
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) {
+                    const long long row = r + (long long)k * at.tall;
+                    raw[k] = Channels<T, V>::raw(from + (row < end ? row : r) * p.x_row);
+                }
+                float count = 0.0f, sum[V], square[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] = square[i] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) {
+                    const float on = r + (long long)k * at.tall < end ? 1.0f : 0.0f;
+                    float v[V];
+                    Channels<T, V>::values(raw[k], v);
+                    count += on;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(on, v[i] - first[i], sum[i]);      // (the row that stands in for one that is not there is in the sum)
+                }
+                const float inverse = fast_rcp(count);
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] *= inverse;
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) {
+                    const float on = r + (long long)k * at.tall < end ? 1.0f : 0.0f;
+                    float v[V];
+                    Channels<T, V>::values(raw[k], v);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        v[k][i] -= first;
-                        sum += on ? v[k][i] : 0.0f;
+                        const float d = (v[i] - first[i]) - sum[i];
+                        square[i] = __builtin_fmaf(on * d, d, square[i]);
                     }
                 }
-                const float mean = sum * fast_rcp(count);
+                const float all = n + count, share = count * fast_rcp(all);
 #pragma unroll
-                for (int k = 0; k < kBatchRows; ++k) {
-                    const bool on = r + (long long)k * at.tall < end;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) square += on ? (v[k][i] - mean) * (v[k][i] - mean) : 0.0f;
+                for (int i = 0; i < V; ++i) {
+                    const float d = sum[i] - mean[i];
+                    mean[i] = __builtin_fmaf(d, share, mean[i]);
+                    m2[i] += square[i] + d * d * n * share;
                 }
-                m = merged(m, Moments{count, mean, square});
+                n = all;
             }
         }
-        __syncthreads();
-        shared[threadIdx.x] = m;
-        __syncthreads();
-        if (at.row == 0 && column < shape.columns) {
-            for (int k = 1; k < at.tall; ++k) m = merged(m, shared[k * at.wide + at.column]);
-            to[column] = m;
+        // the rows of the workgroup, by halves
+        for (int tall = at.tall; tall > 1;) {
+            const int half = (tall + 1) / 2;
+            __syncthreads();
+            if (at.row >= half && at.row < tall) {
+                shared_n[threadIdx.x] = n;
+#pragma unroll
+                for (int i = 0; i < V; ++i) shared_mean[i][threadIdx.x] = mean[i], shared_m2[i][threadIdx.x] = m2[i];
+            }
+            __syncthreads();
+            if (at.row + half < tall) {
+                const int other = threadIdx.x + half * at.wide;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const Moments m = merged(Moments{n, mean[i], m2[i]}, Moments{shared_n[other], shared_mean[i][other], shared_m2[i][other]});
+                    mean[i] = m.mean;
+                    m2[i] = m.m2;
+                }
+                n += shared_n[other];
+            }
+            tall = half;
+        }
+        if (there && at.row == 0) {
+            Channels<float, V>::store(to + channel, mean);
+            Channels<float, V>::store(to + p.channels + channel, m2);
         }
     }
 }
 
-// mean and rstd of every group, a wavefront each: [batch][group] pairs behind the moments, and the caller's arrays.
+// mean and rstd of every group, a wavefront each: [batch][group] pairs behind the chunks' sums, and the caller's arrays.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_statistics_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
     const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 6;
     if (at >= (long long)p.batch * p.groups) return;
     const int b = (int)(at / p.groups), group = (int)(at - (long long)b * p.groups), lane = threadIdx.x & 63;
-    const Moments* from = (const Moments*)a.workspace + (size_t)b * shape.chunks * shape.columns + (size_t)group * shape.columns_a_group;
+    const int channels = p.channels / p.groups;
+    const float* from = a.workspace + (size_t)b * shape.chunks * 2 * p.channels + (size_t)group * channels;
     Moments m = {0.0f, 0.0f, 0.0f};
-    const long long all = (long long)shape.chunks * shape.columns_a_group;
+    const long long all = (long long)shape.chunks * channels;
     for (long long k = lane; k < all; k += 64) {
-        const long long chunk = k / shape.columns_a_group;
-        m = merged(m, from[chunk * shape.columns + (k - chunk * shape.columns_a_group)]);
+        const long long chunk = k / channels;
+        const long long rows = (chunk + 1) * shape.chunk_rows <= p.rows ? shape.chunk_rows : p.rows - chunk * shape.chunk_rows;
+        const float* entry = from + chunk * 2 * p.channels + (k - chunk * channels);
+        m = merged(m, Moments{(float)rows, entry[0], entry[p.channels]});
     }
-    m = over_wave(m);
+    for (int k = 1; k < 64; k <<= 1) m = merged(m, from_lane(m, k));
     if (lane) return;
     const float rstd = 1.0f / __builtin_sqrtf(m.m2 / m.n + p.eps);
-    float* to = (float*)((Moments*)a.workspace + (size_t)p.batch * shape.chunks * shape.columns) + 2 * at;
     const float mean = m.mean + group_first<T>(p, (const T*)a.x + b * p.x_batch, group);
+    float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * at;
     to[0] = mean;
     to[1] = rstd;
     if (a.mean) a.mean[at] = mean;
@@ -153,34 +469,47 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(sys_group_norm_t p
     const int b = blockIdx.x / shape.chunks, chunk = blockIdx.x - b * shape.chunks;
     const Lanes at(shape.columns);
     if (!at.there) return;
+    const int channels = p.channels / p.groups;
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
-    const T* x = (const T*)a.x + b * p.x_batch;
-    T* y = (T*)a.y + b * p.y_batch;
-    const float* statistics = (const float*)((const Moments*)a.workspace + (size_t)p.batch * shape.chunks * shape.columns) + 2 * (size_t)b * p.groups;
+    const float* statistics = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * (size_t)b * p.groups;
     for (int column = at.column; column < shape.columns; column += at.wide) {
-        const int group = column / shape.columns_a_group;
-        const float mean = statistics[2 * group], rstd = statistics[2 * group + 1];
-        float scale[V], shift[V];
+        const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
+        const T* x = (const T*)a.x + b * p.x_batch + channel;
+        T* y = (T*)a.y + b * p.y_batch + channel;
+        float mean[V], scale[V], shift[V];
+        load_affine<T, V>(p, a, channel, scale, shift);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            scale[i] = (a.w ? load_param(a.w, (size_t)column * V + i, p.param_dtype) : 1.0f) * rstd;
-            shift[i] = a.b ? load_param(a.b, (size_t)column * V + i, p.param_dtype) : 0.0f;
+            const int group = (channel + i) / channels;
+            mean[i] = statistics[2 * group];
+            scale[i] *= statistics[2 * group + 1];
         }
-        for (long long r = begin + at.row; r < end; r += at.tall) {
-            float v[V];
-            Channels<T, V>::load(x + r * p.x_row + (long long)column * V, v);
+        for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
+            typename Channels<T, V>::Raw raw[kNormRows];
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activated(__builtin_fmaf(v[i] - mean, scale[i], shift[i]), p.activation);
-            Channels<T, V>::store(y + r * p.y_row + (long long)column * V, v);
+            for (int k = 0; k < kNormRows; ++k) {
+                const long long row = r + (long long)k * at.tall;
+                raw[k] = Channels<T, V>::raw(x + (row < end ? row : r) * p.x_row);
+            }
+#pragma unroll
+            for (int k = 0; k < kNormRows; ++k) {
+                const long long row = r + (long long)k * at.tall;
+                if (row >= end) break;
+                float v[V];
+                Channels<T, V>::values(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(v[i] - mean[i], scale[i], shift[i]);
+                if (p.activation != SYS_ACT_NONE) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = activated(v[i], p.activation);
+                }
+                Channels<T, V>::store_nt(y + row * p.y_row, v);
+            }
         }
     }
 }
 
-// ---------------------------------------------------------------- gradients
-//
-// With hat = (x - mean) rstd and f = dy act'(hat w + b): dw = sum f hat, db = sum f over batch and rows, and
-// dx = rstd (f w - m1 - hat m2), m1 = E[f w], m2 = E[f w hat] over the group, which are sums over its channels of w times the entry's db and dw.
-
+// m1 and m2 are sums over a group's channels of w times the batch entry's sums of f and f hat, which dw and db are made of as well.
 // The workspace: where its parts begin, in floats.
 struct GradSpace {
     size_t sums;                   // [batch][f | f hat][channel], behind [batch][chunk][f | f hat][channel] at 0
@@ -197,41 +526,63 @@ __host__ __device__ GradSpace grad_space(const sys_group_norm_t& p, const NormSh
     return g;
 }
 
+constexpr int kGradRows = 4;       // rows of x and of dy on their way together
+
+// Constants of a lane's channels in the gradients.
+template <typename T, int V>
+struct GradLane {
+    float mean[V], rstd[V], w[V], shift[V];
+    __device__ __forceinline__ GradLane(const sys_group_norm_t& p, const NormArgs& a, int b, int channel)
+    {
+        load_affine<T, V>(p, a, channel, w, shift);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const size_t group = (size_t)b * p.groups + (channel + i) / (p.channels / p.groups);
+            mean[i] = a.mean_in[group];
+            rstd[i] = a.rstd_in[group];
+        }
+    }
+};
+
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
     const int b = blockIdx.x / shape.chunks, chunk = blockIdx.x - b * shape.chunks;
     const Lanes at(shape.columns);
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
-    const T* x = (const T*)a.x + b * p.x_batch;
-    const T* dy = (const T*)a.dy + b * p.y_batch;
     float* to = a.workspace + ((size_t)b * shape.chunks + chunk) * 2 * p.channels;
     __shared__ float shared[V][kThreads];
     for (int c0 = 0; c0 < shape.columns; c0 += at.wide) {
-        const int column = c0 + at.column;
-        const bool there = at.there && column < shape.columns;
+        const bool there = at.there && c0 + at.column < shape.columns;
+        const int column = c0 + at.column < shape.columns ? c0 + at.column : shape.columns - 1;
+        const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
         float f_sum[V], hat_sum[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) f_sum[i] = hat_sum[i] = 0.0f;
         if (there) {
-            const int group = column / shape.columns_a_group;
-            const float mean = a.mean_in[(size_t)b * p.groups + group], rstd = a.rstd_in[(size_t)b * p.groups + group];
-            float w[V], shift[V];
+            const GradLane<T, V> lane(p, a, b, channel);
+            const T* x = (const T*)a.x + b * p.x_batch + channel;
+            const T* dy = (const T*)a.dy + b * p.y_batch + channel;
+            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
+                typename Channels<T, V>::Raw raw_x[kGradRows], raw_dy[kGradRows];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                w[i] = a.w ? load_param(a.w, (size_t)column * V + i, p.param_dtype) : 1.0f;
-                shift[i] = a.b ? load_param(a.b, (size_t)column * V + i, p.param_dtype) : 0.0f;
-            }
-            for (long long r = begin + at.row; r < end; r += at.tall) {
-                float v[V], f[V];
-                Channels<T, V>::load(x + r * p.x_row + (long long)column * V, v);
-                Channels<T, V>::load(dy + r * p.y_row + (long long)column * V, f);
+                for (int k = 0; k < kGradRows; ++k) {
+                    const long long row = r + (long long)k * at.tall < end ? r + (long long)k * at.tall : r;
+                    raw_x[k] = Channels<T, V>::raw(x + row * p.x_row);
+                    raw_dy[k] = Channels<T, V>::raw(dy + row * p.y_row);
+                }
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float hat = (v[i] - mean) * rstd;
-                    f[i] *= activated_grad(__builtin_fmaf(hat, w[i], shift[i]), p.activation);
-                    f_sum[i] += f[i];
-                    hat_sum[i] = __builtin_fmaf(f[i], hat, hat_sum[i]);
+                for (int k = 0; k < kGradRows; ++k) {
+                    if (r + (long long)k * at.tall >= end) break;
+                    float v[V], g[V], f[V], hat[V];
+                    Channels<T, V>::values(raw_x[k], v);
+                    Channels<T, V>::values(raw_dy[k], g);
+                    row_grad<V>(v, g, lane.mean, lane.rstd, lane.w, lane.shift, p.activation, f, hat);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        f_sum[i] += f[i];
+                        hat_sum[i] = __builtin_fmaf(f[i], hat[i], hat_sum[i]);
+                    }
                 }
             }
         }
@@ -239,67 +590,73 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(sys_group_norm
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < V; ++i) shared[i][threadIdx.x] = which ? hat_sum[i] : f_sum[i];
-            __syncthreads();
-            if (at.row == 0 && there) {
+            // the rows of the workgroup, by halves
+            for (int tall = at.tall; tall > 1;) {
+                const int half = (tall + 1) / 2;
+                __syncthreads();
+                if (at.row + half < tall) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float s = shared[i][at.column];
-                    for (int k = 1; k < at.tall; ++k) s += shared[i][k * at.wide + at.column];
-                    to[(size_t)which * p.channels + (size_t)column * V + i] = s;
+                    for (int i = 0; i < V; ++i) shared[i][threadIdx.x] += shared[i][threadIdx.x + half * at.wide];
                 }
+                tall = half;
+            }
+            if (at.row == 0 && there) {
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = shared[i][threadIdx.x];
+                Channels<float, V>::store(to + (size_t)which * p.channels + channel, v);
             }
         }
     }
 }
 
-// Sums over the chunks: a lane an element of [batch][f | f hat][channel].
-__global__ __launch_bounds__(kThreads) void norm_grad_chunks_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
+// Sums over `parts` rows of [part][f | f hat][channel], for every one of `sets` such blocks: 16 columns x 16 shares a workgroup, in one order.
+// The sums go to `to` ([set][f | f hat][channel]) or, as the last step, to the gradients themselves.
+__global__ __launch_bounds__(kThreads) void norm_grad_parts_kernel(sys_group_norm_t p, NormArgs a, const float* from, float* to, int parts, int blocks_a_set)
 {
-    const long long at = (long long)blockIdx.x * kThreads + threadIdx.x, row = 2LL * p.channels;
-    if (at >= p.batch * row) return;
-    const long long b = at / row;
-    const float* from = a.workspace + b * shape.chunks * row + (at - b * row);
+    const int set = blockIdx.x / blocks_a_set, columns = 2 * p.channels;
+    const int column = (blockIdx.x - set * blocks_a_set) * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
+    from += (size_t)set * parts * columns;
     float s = 0.0f;
-    for (int k = 0; k < shape.chunks; ++k) s += from[k * row];
-    a.workspace[grad_space(p, shape).sums + at] = s;
-}
-
-// The first group_blocks workgroups: m1 and m2, a wavefront a group.  The others: dw and db, a lane a channel.
-__global__ __launch_bounds__(kThreads) void norm_grad_means_kernel(sys_group_norm_t p, NormArgs a, NormShape shape, unsigned group_blocks)
-{
-    const GradSpace g = grad_space(p, shape);
-    const float* sums = a.workspace + g.sums;
-    if (blockIdx.x < group_blocks) {
-        const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 6;
-        if (at >= (long long)p.batch * p.groups) return;
-        const long long b = at / p.groups;
-        const int channels = p.channels / p.groups, first = (int)(at - b * p.groups) * channels, lane = threadIdx.x & 63;
-        const float* from = sums + b * 2 * p.channels;
-        float m1 = 0.0f, m2 = 0.0f;
-        for (int k = lane; k < channels; k += 64) {
-            const float w = a.w ? load_param(a.w, first + k, p.param_dtype) : 1.0f;
-            m1 = __builtin_fmaf(w, from[first + k], m1);
-            m2 = __builtin_fmaf(w, from[p.channels + first + k], m2);
-        }
-        for (int k = 1; k < 64; k <<= 1) {
-            m1 += __shfl_xor(m1, k);
-            m2 += __shfl_xor(m2, k);
-        }
-        const float all = (float)((double)channels * (double)p.rows);
-        if (lane == 0) {
-            a.workspace[g.means + 2 * at] = m1 / all;
-            a.workspace[g.means + 2 * at + 1] = m2 / all;
-        }
+    if (column < columns)
+        for (int k = share; k < parts; k += 16) s += from[(size_t)k * columns + column];
+    __shared__ float shared[16][16];
+    shared[share][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (share || column >= columns) return;
+    for (int k = 1; k < 16; ++k) s += shared[k][threadIdx.x];
+    if (to) {
+        to[(size_t)set * columns + column] = s;
         return;
     }
-    const long long at = (long long)(blockIdx.x - group_blocks) * kThreads + threadIdx.x;
-    if (at >= 2LL * p.channels) return;
-    const bool is_w = at >= p.channels;
-    void* to = is_w ? a.dw : a.db;
-    if (!to) return;
-    float s = 0.0f;
-    for (int b = 0; b < p.batch; ++b) s += sums[b * 2LL * p.channels + at];
-    store_param(to, at - (is_w ? p.channels : 0), p.param_dtype, s);
+    void* out = column >= p.channels ? a.dw : a.db;
+    if (out) store_param(out, column >= p.channels ? column - p.channels : column, p.param_dtype, s);
+}
+
+// m1 and m2, a wavefront a group.
+__global__ __launch_bounds__(kThreads) void norm_grad_means_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
+{
+    const GradSpace g = grad_space(p, shape);
+    const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 6;
+    if (at >= (long long)p.batch * p.groups) return;
+    const long long b = at / p.groups;
+    const int channels = p.channels / p.groups, first = (int)(at - b * p.groups) * channels, lane = threadIdx.x & 63;
+    const float* from = a.workspace + g.sums + b * 2 * p.channels;
+    float m1 = 0.0f, m2 = 0.0f;
+    for (int k = lane; k < channels; k += 64) {
+        const float w = a.w ? load_param(a.w, first + k, p.param_dtype) : 1.0f;
+        m1 = __builtin_fmaf(w, from[first + k], m1);
+        m2 = __builtin_fmaf(w, from[p.channels + first + k], m2);
+    }
+    for (int k = 1; k < 64; k <<= 1) {
+        m1 += __shfl_xor(m1, k);
+        m2 += __shfl_xor(m2, k);
+    }
+    const float all = (float)channels * (float)p.rows;
+    if (lane == 0) {
+        a.workspace[g.means + 2 * at] = m1 / all;
+        a.workspace[g.means + 2 * at + 1] = m2 / all;
+    }
 }
 
 template <typename T, int V>
@@ -309,50 +666,114 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(sys_group_nor
     const Lanes at(shape.columns);
     if (!at.there) return;
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
-    const T* x = (const T*)a.x + b * p.x_batch;
-    const T* dy = (const T*)a.dy + b * p.y_batch;
-    T* dx = (T*)a.dx + (size_t)b * p.rows * p.channels;
     const float* means = a.workspace + grad_space(p, shape).means + 2 * (size_t)b * p.groups;
     for (int column = at.column; column < shape.columns; column += at.wide) {
-        const int group = column / shape.columns_a_group;
-        const float mean = a.mean_in[(size_t)b * p.groups + group], rstd = a.rstd_in[(size_t)b * p.groups + group];
-        const float m1 = means[2 * group], m2 = means[2 * group + 1];
-        float w[V], shift[V];
+        const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
+        const T* x = (const T*)a.x + b * p.x_batch + channel;
+        const T* dy = (const T*)a.dy + b * p.y_batch + channel;
+        T* dx = (T*)a.dx + (size_t)b * p.rows * p.channels + channel;
+        const GradLane<T, V> lane(p, a, b, channel);
+        float m1[V], m2[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            w[i] = a.w ? load_param(a.w, (size_t)column * V + i, p.param_dtype) : 1.0f;
-            shift[i] = a.b ? load_param(a.b, (size_t)column * V + i, p.param_dtype) : 0.0f;
+            const int group = (channel + i) / (p.channels / p.groups);
+            m1[i] = means[2 * group];
+            m2[i] = means[2 * group + 1];
         }
-        for (long long r = begin + at.row; r < end; r += at.tall) {
-            float v[V], f[V];
-            Channels<T, V>::load(x + r * p.x_row + (long long)column * V, v);
-            Channels<T, V>::load(dy + r * p.y_row + (long long)column * V, f);
+        for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
+            typename Channels<T, V>::Raw raw_x[kGradRows], raw_dy[kGradRows];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float hat = (v[i] - mean) * rstd;
-                f[i] *= activated_grad(__builtin_fmaf(hat, w[i], shift[i]), p.activation);
-                v[i] = rstd * (__builtin_fmaf(f[i], w[i], -m1) - hat * m2);
+            for (int k = 0; k < kGradRows; ++k) {
+                const long long row = r + (long long)k * at.tall < end ? r + (long long)k * at.tall : r;
+                raw_x[k] = Channels<T, V>::raw(x + row * p.x_row);
+                raw_dy[k] = Channels<T, V>::raw(dy + row * p.y_row);
             }
-            Channels<T, V>::store(dx + r * p.channels + (long long)column * V, v);
+#pragma unroll
+            for (int k = 0; k < kGradRows; ++k) {
+                const long long row = r + (long long)k * at.tall;
+                if (row >= end) break;
+                float v[V], g[V], f[V], hat[V];
+                Channels<T, V>::values(raw_x[k], v);
+                Channels<T, V>::values(raw_dy[k], g);
+                row_grad<V>(v, g, lane.mean, lane.rstd, lane.w, lane.shift, p.activation, f, hat);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = lane.rstd[i] * (__builtin_fmaf(f[i], lane.w[i], -m1[i]) - hat[i] * m2[i]);
+                Channels<T, V>::store_nt(dx + row * p.channels, v);
+            }
         }
     }
 }
 
-// ---------------------------------------------------------------- launches
+// ================================================================ launches
 
-int vector_of(const sys_group_norm_t& p)
+// Channels a lane: 16 bytes, or what divides the channels of a group.
+int group_vector(const sys_group_norm_t& p)
 {
     int v = p.dtype == SYS_F32 ? 4 : 8;
     while (p.channels / p.groups % v) v /= 2;
     return v;
 }
 
+int most_channels(const sys_group_norm_t& p) { return p.dtype == SYS_F32 ? 4 : 8; }
+
+int log2_up(long long n)
+{
+    int l = 0;
+    while ((1LL << l) < n) ++l;
+    return l;
+}
+
+// Rows of a lane that are held: at most 64 registers for x, 32 each for x and dy.
+template <typename T, int V, bool GRAD>
+constexpr int kMostItems = V * (int)sizeof(T) > 8 ? (GRAD ? 8 : 16) : (GRAD ? 16 : 32);
+
+int most_items(const sys_group_norm_t& p, int v, bool grad)
+{
+    return v * (p.dtype == SYS_F32 ? 4 : 2) > 8 ? (grad ? 8 : 16) : (grad ? 16 : 32);
+}
+
+// Whether a call's rows stay in registers, and how they lie there.
+bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
+{
+    ResidentShape s;
+    const int v = group_vector(p), element = p.dtype == SYS_F32 ? 4 : 2;
+    s.columns_a_group = p.channels / p.groups / v;
+    s.log_group = log2_up(s.columns_a_group);
+    const int most_log = grad ? 9 : 10;                    // 512 lanes leave 256 registers, 1024 leave 128
+    if (s.log_group > most_log) return false;
+    // a part of a row of at least 64 bytes, where the unit is more than a wavefront
+    s.log_tile = 0;
+    const long long lanes = p.rows << s.log_group;
+    const int most = most_items(p, v, grad);
+    if (lanes > 64) {
+        while (s.log_group + s.log_tile < 6 && s.log_tile < 5 && (p.channels / p.groups * element << s.log_tile) < 64 && (1 << s.log_tile) < p.groups) ++s.log_tile;
+    }
+    const int wide = s.log_group + s.log_tile;
+    // up to four rows a lane, then the whole workgroup, then as many rows as there are registers for
+    s.log_unit = wide + log2_up((p.rows + 3) / 4);
+    if (s.log_unit > most_log) s.log_unit = most_log;
+    const long long tall = 1LL << (s.log_unit - wide);
+    const long long items = (p.rows + tall - 1) / tall;
+    if (items > most) return false;
+    s.items = (int)items;
+    s.tiles = (p.groups + (1 << s.log_tile) - 1) >> s.log_tile;
+    s.threads = s.log_unit > 8 ? 1 << s.log_unit : kThreads;
+    s.slices = 1;
+    if (grad) {
+        // enough units for sixteen wavefronts a CU, but no more sums of dw and db than that
+        long long slices = (4096LL * 64 >> s.log_unit) / s.tiles;
+        slices = slices < 1 ? 1 : slices > p.batch ? p.batch : slices;
+        s.slices = (int)(slices < 1 ? 1 : slices);
+    }
+    *out = s;
+    return true;
+}
+
 NormShape shape_of(const sys_group_norm_t& p)
 {
     NormShape s;
-    const int v = vector_of(p);
-    s.columns = p.channels / v;
-    s.columns_a_group = s.columns / p.groups;
+    const int v = p.channels >= most_channels(p) ? most_channels(p) : 1;
+    s.columns = (p.channels + v - 1) / v;
     // some 2048 workgroups, each of at least 16 rows a lane
     const long long tall = s.columns < kThreads ? kThreads / s.columns : 1;
     const long long most = (p.rows + 16 * tall - 1) / (16 * tall);
@@ -366,62 +787,94 @@ NormShape shape_of(const sys_group_norm_t& p)
 
 unsigned blocks_for(long long lanes) { return (unsigned)((lanes + kThreads - 1) / kThreads); }
 
-template <typename T, int V>
-hipError_t launch_forward(const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
+unsigned resident_blocks(const ResidentShape& s, long long units) { return (unsigned)(((units << s.log_unit) + s.threads - 1) / s.threads); }
+
+template <typename T, int V, int ITEMS>
+hipError_t launch_resident(const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
 {
-    const NormShape shape = shape_of(p);
-    const dim3 grid((unsigned)(shape.chunks * p.batch)), block(kThreads);
-    hipLaunchKernelGGL((norm_moments_kernel<T, V>), grid, block, 0, s, p, a, shape);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((norm_statistics_kernel<T>), dim3(blocks_for(64LL * p.batch * p.groups)), block, 0, s, p, a, shape);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((norm_apply_kernel<T, V>), grid, block, 0, s, p, a, shape);
+    hipLaunchKernelGGL((norm_resident_kernel<T, V, ITEMS>), dim3(resident_blocks(s, (long long)p.batch * s.tiles)), dim3(s.threads), 0, stream, p, a, s);
+    return hipGetLastError();
+}
+
+template <typename T, int V, int ITEMS>
+hipError_t launch_grad_resident(const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
+{
+    hipLaunchKernelGGL((norm_grad_resident_kernel<T, V, ITEMS>), dim3(resident_blocks(s, (long long)s.slices * s.tiles)), dim3(s.threads), 0, stream, p, a, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!a.dw && !a.db)) return e;
+    const int blocks = (2 * p.channels + 15) / 16;
+    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, a, a.workspace, nullptr, s.slices, blocks);
     return hipGetLastError();
 }
 
 template <typename T, int V>
-hipError_t launch_backward(const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
+hipError_t launch_items(bool grad, const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
+{
+    if (s.items == 1) return grad ? launch_grad_resident<T, V, 1>(p, a, s, stream) : launch_resident<T, V, 1>(p, a, s, stream);
+    if (s.items <= 4) return grad ? launch_grad_resident<T, V, 4>(p, a, s, stream) : launch_resident<T, V, 4>(p, a, s, stream);
+    return grad ? launch_grad_resident<T, V, kMostItems<T, V, true>>(p, a, s, stream) : launch_resident<T, V, kMostItems<T, V, false>>(p, a, s, stream);
+}
+
+template <typename T, int V>
+hipError_t launch_chunks(bool grad, const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
 {
     const NormShape shape = shape_of(p);
     const dim3 grid((unsigned)(shape.chunks * p.batch)), block(kThreads);
     const unsigned group_blocks = blocks_for(64LL * p.batch * p.groups);
     hipError_t e;
-    if (p.batch) {
-        hipLaunchKernelGGL((norm_grad_sums_kernel<T, V>), grid, block, 0, s, p, a, shape);
+    if (!grad) {
+        hipLaunchKernelGGL((norm_moments_kernel<T, V>), grid, block, 0, s, p, a, shape);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        hipLaunchKernelGGL(norm_grad_chunks_kernel, dim3(blocks_for(2LL * p.batch * p.channels)), block, 0, s, p, a, shape);
+        hipLaunchKernelGGL((norm_statistics_kernel<T>), dim3(group_blocks), block, 0, s, p, a, shape);
         if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL((norm_apply_kernel<T, V>), grid, block, 0, s, p, a, shape);
+        return hipGetLastError();
     }
-    hipLaunchKernelGGL(norm_grad_means_kernel, dim3(group_blocks + blocks_for(2LL * p.channels)), block, 0, s, p, a, shape, group_blocks);
-    if ((e = hipGetLastError()) != hipSuccess || !p.batch) return e;
+    const int blocks = (2 * p.channels + 15) / 16;
+    float* sums = a.workspace + grad_space(p, shape).sums;
+    hipLaunchKernelGGL((norm_grad_sums_kernel<T, V>), grid, block, 0, s, p, a, shape);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3((unsigned)blocks * p.batch), block, 0, s, p, a, a.workspace, sums, shape.chunks, blocks);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(norm_grad_means_kernel, dim3(group_blocks), block, 0, s, p, a, shape);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((norm_grad_apply_kernel<T, V>), grid, block, 0, s, p, a, shape);
+    if ((e = hipGetLastError()) != hipSuccess || (!a.dw && !a.db)) return e;
+    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), block, 0, s, p, a, sums, nullptr, p.batch, blocks);
     return hipGetLastError();
-}
-
-template <typename T, int V>
-hipError_t launch_vector(bool grad, const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
-{
-    return grad ? launch_backward<T, V>(p, a, s) : launch_forward<T, V>(p, a, s);
 }
 
 template <typename T>
 hipError_t launch_type(bool grad, const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
 {
-    switch (vector_of(p)) {
-    case 1: return launch_vector<T, 1>(grad, p, a, s);
-    case 2: return launch_vector<T, 2>(grad, p, a, s);
-    case 4: return launch_vector<T, 4>(grad, p, a, s);
-    default:
-        if constexpr (sizeof(T) == 2) return launch_vector<T, 8>(grad, p, a, s);
-        return hipErrorInvalidValue;
+    ResidentShape r;
+    if (resident_shape(p, grad, &r)) {
+        switch (group_vector(p)) {
+        case 1: return launch_items<T, 1>(grad, p, a, r, s);
+        case 2: return launch_items<T, 2>(grad, p, a, r, s);
+        case 4: return launch_items<T, 4>(grad, p, a, r, s);
+        default:
+            if constexpr (sizeof(T) == 2) return launch_items<T, 8>(grad, p, a, r, s);
+            return hipErrorInvalidValue;
+        }
     }
+    return p.channels >= kLaneChannels<T> ? launch_chunks<T, kLaneChannels<T>>(grad, p, a, s) : launch_chunks<T, 1>(grad, p, a, s);
 }
 
 hipError_t launch(bool grad, const sys_group_norm_t& p, const NormArgs& a, hipStream_t s)
 {
-    // (blocks of the small kernels: a wavefront a group, a lane a channel of a batch entry)
-    if (64LL * p.batch * p.groups > 0x7fffffffLL * kThreads || (long long)shape_of(p).chunks * p.batch > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const long long most = 0x7fffffffLL;
+    if (!p.batch) {                                        // (only the gradients come here: sums of nothing)
+        if (!a.dw && !a.db) return hipSuccess;
+        const int blocks = (2 * p.channels + 15) / 16;
+        hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), dim3(kThreads), 0, s, p, a, (const float*)nullptr, nullptr, 0, blocks);
+        return hipGetLastError();
+    }
+    ResidentShape r;
+    if (resident_shape(p, grad, &r) ? ((long long)p.batch * r.tiles << r.log_unit) > most * kThreads || (long long)p.batch * r.tiles > most
+                                    : 64LL * p.batch * p.groups > most * kThreads || (long long)shape_of(p).chunks * p.batch > most
+                                          || (2LL * p.channels + 15) / 16 * p.batch > most)
+        return hipErrorInvalidConfiguration;
     switch (p.dtype) {
     case SYS_F32: return launch_type<float>(grad, p, a, s);
     case SYS_F16: return launch_type<f16_t>(grad, p, a, s);
@@ -436,10 +889,17 @@ hipError_t launch_group_norm_grad(const sys_group_norm_t& p, const NormArgs& a, 
 
 size_t group_norm_workspace(const sys_group_norm_t& p)
 {
-    const NormShape s = shape_of(p);
-    return (size_t)p.batch * s.chunks * s.columns * sizeof(Moments) + (size_t)p.batch * p.groups * 2 * sizeof(float);
+    ResidentShape r;
+    if (!p.batch || resident_shape(p, false, &r)) return 0;
+    return ((size_t)p.batch * shape_of(p).chunks * 2 * p.channels + (size_t)p.batch * p.groups * 2) * sizeof(float);
 }
 
-size_t group_norm_grad_workspace(const sys_group_norm_t& p) { return grad_space(p, shape_of(p)).floats * sizeof(float); }
+size_t group_norm_grad_workspace(const sys_group_norm_t& p)
+{
+    ResidentShape r;
+    if (!p.batch) return 0;
+    if (resident_shape(p, true, &r)) return (size_t)r.slices * 2 * p.channels * sizeof(float);
+    return grad_space(p, shape_of(p)).floats * sizeof(float);
+}
 
 }  // namespace sysconv
