@@ -49,6 +49,20 @@ __device__ __forceinline__ float group_first(const sys_group_norm_t& p, const T*
     return (float)x[(long long)group * (p.channels / p.groups)];
 }
 
+// The groups of V neighbouring channels, one division for all of them.
+template <int V>
+__device__ __forceinline__ void groups_of(int channel, int channels_a_group, int (&group)[V])
+{
+    int g = channel / channels_a_group, in_group = channel - g * channels_a_group;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        group[i] = g;
+        const bool next = ++in_group == channels_a_group;
+        g += next;
+        in_group = next ? 0 : in_group;
+    }
+}
+
 // w and b of V channels, 1 and 0 without them.
 template <typename T, int V>
 __device__ __forceinline__ void load_affine(const sys_group_norm_t& p, const NormArgs& a, int channel, float (&w)[V], float (&b)[V])
@@ -68,7 +82,8 @@ struct ResidentShape {
     int log_group, log_tile, log_unit, threads;     // lanes a group; groups a tile; lanes a unit; lanes a workgroup
     int items, tiles;                               // tiles: of a batch entry
     int columns_a_group;                            // lanes of a group that hold channels
-    int slices;                                     // gradients: batch entries are dealt out to so many units of a tile
+    int entries, units;                             // batch entries a unit has at a time; units of the launch
+    int slices, rounds;                             // gradients: units of a tile, and how often each takes its entries
 };
 
 struct ResidentLane {
@@ -90,17 +105,19 @@ struct ResidentLane {
     }
 };
 
-// Rows of a lane: those past the last one repeat it, and their values are not used.
+// Rows of a lane, `tall` apart; zeros, which are not used, past the last one.
 template <typename T, int V, int ITEMS>
 struct ResidentRows {
     typename Channels<T, V>::Raw raw[ITEMS];
-    __device__ __forceinline__ void load(const T* from, long long row_stride, long long rows, int row, int tall, int items)
+    __device__ __forceinline__ void load(const T* from, long long row_stride, int rows, int row, int tall, int items)
     {
+        from += row * row_stride;
+        const long long step = tall * row_stride;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            if (ITEMS > 1 && i >= items) continue;
-            const long long r = row + (long long)i * tall;
-            raw[i] = Channels<T, V>::raw(from + (r < rows ? r : rows - 1) * row_stride);
+            raw[i] = typename Channels<T, V>::Raw{};
+            if ((ITEMS == 1 || i < items) && row + i * tall < rows) raw[i] = Channels<T, V>::raw(from);
+            from += step;
         }
     }
 };
@@ -125,43 +142,40 @@ __device__ __forceinline__ void forget(Raw& raw)
     }
 }
 
-// Adds up over the lanes of a unit that share a group: F merges two values, in an order that depends on the shape alone.
+// Adds up over the lanes of a unit that share a group: merge(l, r) of two values, in an order that depends on the shape alone.
 // Units of more than a wavefront go through LDS, [wavefront][group of the tile]; every wavefront of the workgroup has to come here.
-template <typename M, typename FromLane, typename Merge>
-__device__ __forceinline__ M over_unit(const ResidentShape& s, int tile_group, M m, M* shared, FromLane from, Merge merge)
+template <int ENTRIES, typename M, typename FromLane, typename Merge>
+__device__ __forceinline__ void over_unit(const ResidentShape& s, int tile_group, M (&m)[ENTRIES], M* shared, FromLane from, Merge merge)
 {
-    for (int bit = 0; bit < s.log_unit && bit < 6; ++bit)
-        if (bit < s.log_group || bit >= s.log_group + s.log_tile) m = merge(m, from(m, 1 << bit));
-    if (s.log_unit <= 6) return m;
+    for (int bit = 0; bit < s.log_unit && bit < 6; ++bit) {
+        if (bit >= s.log_group && bit < s.log_group + s.log_tile) continue;
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) m[e] = merge(m[e], from(m[e], 1 << bit));
+    }
+    if (s.log_unit <= 6) return;
     const int waves = 1 << (s.log_unit - 6), first = (threadIdx.x >> s.log_unit) * waves;
-    __syncthreads();                                // (what a call before this one left has been read)
     const unsigned lane = threadIdx.x & 63;
-    if (lane < (1u << (s.log_group + s.log_tile)) && (lane & ((1u << s.log_group) - 1)) == 0)
-        shared[((threadIdx.x >> 6) << s.log_tile) + tile_group] = m;
-    __syncthreads();
-    m = shared[(first << s.log_tile) + tile_group];
-    for (int k = 1; k < waves; ++k) m = merge(m, shared[((first + k) << s.log_tile) + tile_group]);
-    return m;
+#pragma unroll
+    for (int e = 0; e < ENTRIES; ++e) {
+        __syncthreads();                            // (what the sum before this one left has been read)
+        if (lane < (1u << (s.log_group + s.log_tile)) && (lane & ((1u << s.log_group) - 1)) == 0)
+            shared[((threadIdx.x >> 6) << s.log_tile) + tile_group] = m[e];
+        __syncthreads();
+        m[e] = shared[(first << s.log_tile) + tile_group];
+        for (int k = 1; k < waves; ++k) m[e] = merge(m[e], shared[((first + k) << s.log_tile) + tile_group]);
+    }
 }
 
 constexpr int kMostTile = 32;                       // groups a tile, and entries of `shared` a wavefront
 
+// Moments of a lane's rows.
 template <typename T, int V, int ITEMS>
-__global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
+__device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>& rows, float first, bool there, int count, int row, int tall, int items)
 {
-    __shared__ Moments shared[16 * kMostTile];
-    const ResidentLane at(p, s, p.batch * s.tiles, xcd_place(blockIdx.x, gridDim.x));
-    const int b = at.unit / s.tiles;
-    const T* x = (const T*)a.x + b * p.x_batch;
-    ResidentRows<T, V, ITEMS> rows;
-    rows.load(x + at.channel, p.x_row, p.rows, at.row, at.tall, s.items);
-    const float first = group_first<T>(p, x, at.group);
-    float w[V], shift[V];
-    load_affine<T, V>(p, a, at.channel, w, shift);
     Moments m = {0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        if (ITEMS > 1 && i >= s.items) continue;
+        if (ITEMS > 1 && i >= items) continue;
         float v[V], sum = 0.0f, square = 0.0f;
         Channels<T, V>::values(rows.raw[i], v);
 #pragma unroll
@@ -169,34 +183,63 @@ __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p,
         const float mean = sum * (1.0f / V);
 #pragma unroll
         for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - first) - mean, (v[k] - first) - mean, square);
-        const bool on = at.there && at.row + (long long)i * at.tall < p.rows;
-        // (what is not there gives no count; a NaN in a row that is repeated is in its group already)
-        m = merged(m, Moments{on ? (float)V : 0.0f, on ? mean : 0.0f, on ? square : 0.0f});
+        const bool on = there && row + i * tall < count;
+        const Moments own = {on ? (float)V : 0.0f, on ? mean : 0.0f, on ? square : 0.0f};
+        m = i == 0 ? own : merged(m, own);
     }
-    m = over_unit(s, at.tile_group, m, shared, [](Moments v, int k) { return from_lane(v, k); }, [](Moments l, Moments r) { return merged(l, r); });
-    if (!at.there) return;
-    const float mean = m.mean + first, rstd = 1.0f / __builtin_sqrtf(m.m2 / m.n + p.eps);
-    if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
-        if (a.mean) a.mean[(size_t)b * p.groups + at.group] = mean;
-        if (a.rstd) a.rstd[(size_t)b * p.groups + at.group] = rstd;
+    return m;
+}
+
+// A unit has ENTRIES batch entries in a row; with one row a lane (ITEMS 1: tokens) several, whose loads and sums run side by side.
+template <typename T, int V, int ITEMS, int ENTRIES>
+__global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
+{
+    __shared__ Moments shared[16 * kMostTile];
+    const ResidentLane at(p, s, s.units, xcd_place(blockIdx.x, gridDim.x));
+    const int b0 = at.unit / s.tiles * ENTRIES;
+    ResidentRows<T, V, ITEMS> rows[ENTRIES];
+    float first[ENTRIES];
+#pragma unroll
+    for (int e = 0; e < ENTRIES; ++e) {
+        const T* x = (const T*)a.x + (b0 + e < p.batch ? b0 + e : p.batch - 1) * p.x_batch;
+        rows[e].load(x + at.channel, p.x_row, (int)p.rows, at.row, at.tall, s.items);
+        first[e] = group_first<T>(p, x, at.group);
     }
-    T* y = (T*)a.y + b * p.y_batch + at.channel;
+    float w[V], shift[V];
+    load_affine<T, V>(p, a, at.channel, w, shift);
+    Moments m[ENTRIES];
 #pragma unroll
-    for (int k = 0; k < V; ++k) w[k] *= rstd;
+    for (int e = 0; e < ENTRIES; ++e) m[e] = lane_moments<T, V, ITEMS>(rows[e], first[e], at.there, (int)p.rows, at.row, at.tall, s.items);
+    over_unit<ENTRIES>(s, at.tile_group, m, shared, [](Moments v, int k) { return from_lane(v, k); }, [](Moments l, Moments r) { return merged(l, r); });
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        if (ITEMS > 1 && i >= s.items) continue;
-        const long long r = at.row + (long long)i * at.tall;
-        if (r >= p.rows) continue;
-        float v[V];
-        Channels<T, V>::values(rows.raw[i], v);
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf(v[k] - mean, w[k], shift[k]);
-        if (p.activation != SYS_ACT_NONE) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = activated(v[k], p.activation);
+    for (int e = 0; e < ENTRIES; ++e) {
+        if (!at.there || b0 + e >= p.batch) continue;
+        const float mean = m[e].mean + first[e], rstd = 1.0f / __builtin_sqrtf(m[e].m2 / m[e].n + p.eps);
+        if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
+            const size_t group = (size_t)(b0 + e) * p.groups + at.group;
+            if (a.mean) a.mean[group] = mean;
+            if (a.rstd) a.rstd[group] = rstd;
         }
-        Channels<T, V>::store_nt(y + r * p.y_row, v);
+        T* y = (T*)a.y + (b0 + e) * p.y_batch + at.row * p.y_row + at.channel;
+        const long long step = at.tall * p.y_row;
+        float scale[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) scale[k] = w[k] * rstd;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (ITEMS > 1 && i >= s.items) continue;
+            if (at.row + i * at.tall >= (int)p.rows) continue;
+            float v[V];
+            if (ITEMS > 1) forget(rows[e].raw[i]);
+            Channels<T, V>::values(rows[e].raw[i], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf(v[k] - mean, scale[k], shift[k]);
+            if (p.activation != SYS_ACT_NONE) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] = activated(v[k], p.activation);
+            }
+            Channels<T, V>::store_nt(y + i * step, v);
+        }
     }
 }
 
@@ -207,26 +250,29 @@ struct Pair {
     float a, b;
 };
 
-// f and hat of V channels of a row.
-template <int V>
-__device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[V], const float (&mean)[V], const float (&rstd)[V], const float (&w)[V], const float (&shift)[V], int activation,
+// f and hat of V channels of a row, whose statistics are the channels' own or one group's.
+__device__ __forceinline__ float pick(const float* v, int k) { return v[k]; }
+__device__ __forceinline__ float pick(float v, int) { return v; }
+
+template <int V, typename Statistic>
+__device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[V], const Statistic& mean, const Statistic& rstd, const float (&w)[V], const float (&shift)[V], int activation,
                                          float (&f)[V], float (&hat)[V])
 {
 #pragma unroll
-    for (int k = 0; k < V; ++k) hat[k] = (x[k] - mean[k]) * rstd[k], f[k] = dy[k];
+    for (int k = 0; k < V; ++k) hat[k] = (x[k] - pick(mean, k)) * pick(rstd, k), f[k] = dy[k];
     if (activation == SYS_ACT_NONE) return;
 #pragma unroll
     for (int k = 0; k < V; ++k) f[k] *= activated_grad(__builtin_fmaf(hat[k], w[k], shift[k]), activation);
 }
 
-// A unit goes through the batch entries of its slice (one row a lane: with the next one's on their way) and adds up dw and db of its channels:
-// [slice][f | f hat][channel] in the workspace.
-template <typename T, int V, int ITEMS>
+// A unit goes through the batch entries of its slice, ENTRIES at a time, and adds up dw and db of its channels: [slice][f | f hat][channel] in the
+// workspace.
+template <typename T, int V, int ITEMS, int ENTRIES>
 __global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
 {
     __shared__ Pair shared[8 * kMostTile];
     __shared__ float sums[512];
-    const ResidentLane at(p, s, s.slices * s.tiles, xcd_place(blockIdx.x, gridDim.x));
+    const ResidentLane at(p, s, s.units, xcd_place(blockIdx.x, gridDim.x));
     const int slice = at.unit / s.tiles;
     const T *x = (const T*)a.x + at.channel, *dy = (const T*)a.dy + at.channel;
     float w[V], shift[V], f_sum[V], hat_sum[V];
@@ -234,65 +280,65 @@ __global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_
 #pragma unroll
     for (int k = 0; k < V; ++k) f_sum[k] = hat_sum[k] = 0.0f;
     const float share = 1.0f / ((float)p.rows * (float)(p.channels / p.groups));
-    ResidentRows<T, V, ITEMS> rows_x, rows_dy, next_x, next_dy;
-    auto fetch = [&](ResidentRows<T, V, ITEMS>& to_x, ResidentRows<T, V, ITEMS>& to_dy, int b) {
-        if (b >= p.batch) b = p.batch - 1;
-        to_x.load(x + b * p.x_batch, p.x_row, p.rows, at.row, at.tall, s.items);
-        to_dy.load(dy + b * p.y_batch, p.y_row, p.rows, at.row, at.tall, s.items);
-    };
-    if (ITEMS == 1) fetch(next_x, next_dy, slice);
     // as many rounds for every unit, so that all wavefronts of a workgroup meet at its barriers
-    for (int b0 = 0; b0 < p.batch; b0 += s.slices) {
-        const int b = b0 + slice;
-        const bool there = at.there && b < p.batch;
-        if (ITEMS == 1) {
-            rows_x = next_x, rows_dy = next_dy;
-            if (b0 + s.slices < p.batch) fetch(next_x, next_dy, b + s.slices);
-        } else {
-            fetch(rows_x, rows_dy, b);
+    for (int round = 0; round < s.rounds; ++round) {
+        const int b0 = (round * s.slices + slice) * ENTRIES;
+        ResidentRows<T, V, ITEMS> rows_x[ENTRIES], rows_dy[ENTRIES];
+        float mean[ENTRIES], rstd[ENTRIES];
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) {
+            const int b = b0 + e < p.batch ? b0 + e : p.batch - 1;
+            rows_x[e].load(x + b * p.x_batch, p.x_row, (int)p.rows, at.row, at.tall, s.items);
+            rows_dy[e].load(dy + b * p.y_batch, p.y_row, (int)p.rows, at.row, at.tall, s.items);
+            mean[e] = a.mean_in[(size_t)b * p.groups + at.group];
+            rstd[e] = a.rstd_in[(size_t)b * p.groups + at.group];
         }
-        const size_t group = (size_t)(b < p.batch ? b : p.batch - 1) * p.groups + at.group;
-        float mean[V], rstd[V];
+        Pair m[ENTRIES];
 #pragma unroll
-        for (int k = 0; k < V; ++k) mean[k] = a.mean_in[group], rstd[k] = a.rstd_in[group];
-        Pair m = {0.0f, 0.0f};
+        for (int e = 0; e < ENTRIES; ++e) {
+            m[e] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            if (ITEMS > 1 && i >= s.items) continue;
-            float v[V], g[V], f[V], hat[V];
-            Channels<T, V>::values(rows_x.raw[i], v);
-            Channels<T, V>::values(rows_dy.raw[i], g);
-            row_grad<V>(v, g, mean, rstd, w, shift, p.activation, f, hat);
-            if (there && at.row + (long long)i * at.tall < p.rows) {
+            for (int i = 0; i < ITEMS; ++i) {
+                if (ITEMS > 1 && i >= s.items) continue;
+                float v[V], g[V], f[V], hat[V];
+                Channels<T, V>::values(rows_x[e].raw[i], v);
+                Channels<T, V>::values(rows_dy[e].raw[i], g);
+                row_grad<V>(v, g, mean[e], rstd[e], w, shift, p.activation, f, hat);
+                if (at.there && b0 + e < p.batch && at.row + i * at.tall < (int)p.rows) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    f_sum[k] += f[k];
-                    hat_sum[k] = __builtin_fmaf(f[k], hat[k], hat_sum[k]);
-                    m.a = __builtin_fmaf(f[k], w[k], m.a);
-                    m.b = __builtin_fmaf(f[k] * w[k], hat[k], m.b);
+                    for (int k = 0; k < V; ++k) {
+                        f_sum[k] += f[k];
+                        hat_sum[k] = __builtin_fmaf(f[k], hat[k], hat_sum[k]);
+                        m[e].a = __builtin_fmaf(f[k], w[k], m[e].a);
+                        m[e].b = __builtin_fmaf(f[k] * w[k], hat[k], m[e].b);
+                    }
                 }
             }
         }
-        m = over_unit(s, at.tile_group, m, shared, [](Pair v, int k) { return Pair{__shfl_xor(v.a, k), __shfl_xor(v.b, k)}; },
-                      [](Pair l, Pair r) { return Pair{l.a + r.a, l.b + r.b}; });
-        const float m1 = m.a * share, m2 = m.b * share;
-        T* dx = (T*)a.dx + (size_t)(b < p.batch ? b : 0) * p.rows * p.channels + at.channel;
+        over_unit<ENTRIES>(s, at.tile_group, m, shared, [](Pair v, int k) { return Pair{__shfl_xor(v.a, k), __shfl_xor(v.b, k)}; },
+                           [](Pair l, Pair r) { return Pair{l.a + r.a, l.b + r.b}; });
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            if (ITEMS > 1 && i >= s.items) continue;
-            const long long r = at.row + (long long)i * at.tall;
-            if (!there || r >= p.rows) continue;
-            float v[V], g[V], f[V], hat[V];
-            if (ITEMS > 1) {
-                forget(rows_x.raw[i]);
-                forget(rows_dy.raw[i]);
+        for (int e = 0; e < ENTRIES; ++e) {
+            if (!at.there || b0 + e >= p.batch) continue;
+            const float m1 = m[e].a * share, m2 = m[e].b * share;
+            T* dx = (T*)a.dx + ((size_t)(b0 + e) * p.rows + at.row) * p.channels + at.channel;
+            const long long step = (long long)at.tall * p.channels;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                if (ITEMS > 1 && i >= s.items) continue;
+                if (at.row + i * at.tall >= (int)p.rows) continue;
+                float v[V], g[V], f[V], hat[V];
+                if (ITEMS * ENTRIES > 1) {
+                    forget(rows_x[e].raw[i]);
+                    forget(rows_dy[e].raw[i]);
+                }
+                Channels<T, V>::values(rows_x[e].raw[i], v);
+                Channels<T, V>::values(rows_dy[e].raw[i], g);
+                row_grad<V>(v, g, mean[e], rstd[e], w, shift, p.activation, f, hat);
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] = rstd[e] * (__builtin_fmaf(f[k], w[k], -m1) - hat[k] * m2);
+                Channels<T, V>::store_nt(dx + i * step, v);
             }
-            Channels<T, V>::values(rows_x.raw[i], v);
-            Channels<T, V>::values(rows_dy.raw[i], g);
-            row_grad<V>(v, g, mean, rstd, w, shift, p.activation, f, hat);
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = rstd[k] * (__builtin_fmaf(f[k], w[k], -m1) - hat[k] * m2);
-            Channels<T, V>::store_nt(dx + r * p.channels, v);
         }
     }
     if (!a.dw && !a.db) return;
@@ -359,8 +405,10 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
         const int column = c0 + at.column < shape.columns ? c0 + at.column : shape.columns - 1;
         const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
         float n = 0.0f, mean[V], m2[V], first[V];
+        int group[V];
+        groups_of<V>(channel, channels, group);
 #pragma unroll
-        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f, first[i] = group_first<T>(p, x, (channel + i) / channels);
+        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f, first[i] = group_first<T>(p, x, group[i]);
         if (there) {
             const T* from = x + channel;
             for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
@@ -435,32 +483,46 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
     }
 }
 
-// mean and rstd of every group, a wavefront each: [batch][group] pairs behind the chunks' sums, and the caller's arrays.
+// A group's entries in [chunk][channel], dealt out to the lanes of a workgroup: f(chunk, channel of the group).
+template <typename F>
+__device__ __forceinline__ void each_entry(int chunks, int channels, F&& f)
+{
+    if (channels >= kThreads) {
+        for (int chunk = 0; chunk < chunks; ++chunk)
+            for (int c = threadIdx.x; c < channels; c += kThreads) f(chunk, c);
+    } else {
+        const int tall = kThreads / channels, row = (int)threadIdx.x / channels, c = (int)threadIdx.x - row * channels;
+        if (row < tall)
+            for (int chunk = row; chunk < chunks; chunk += tall) f(chunk, c);
+    }
+}
+
+// mean and rstd of every group, a workgroup each: [batch][group] pairs behind the chunks' sums, and the caller's arrays.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_statistics_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
-    const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 6;
-    if (at >= (long long)p.batch * p.groups) return;
-    const int b = (int)(at / p.groups), group = (int)(at - (long long)b * p.groups), lane = threadIdx.x & 63;
+    const int b = blockIdx.x / p.groups, group = blockIdx.x - b * p.groups;
     const int channels = p.channels / p.groups;
     const float* from = a.workspace + (size_t)b * shape.chunks * 2 * p.channels + (size_t)group * channels;
+    const float last_rows = (float)(p.rows - (shape.chunks - 1) * shape.chunk_rows);
     Moments m = {0.0f, 0.0f, 0.0f};
-    const long long all = (long long)shape.chunks * channels;
-    for (long long k = lane; k < all; k += 64) {
-        const long long chunk = k / channels;
-        const long long rows = (chunk + 1) * shape.chunk_rows <= p.rows ? shape.chunk_rows : p.rows - chunk * shape.chunk_rows;
-        const float* entry = from + chunk * 2 * p.channels + (k - chunk * channels);
-        m = merged(m, Moments{(float)rows, entry[0], entry[p.channels]});
-    }
+    each_entry(shape.chunks, channels, [&](int chunk, int c) {
+        const float* entry = from + (size_t)chunk * 2 * p.channels + c;
+        m = merged(m, Moments{chunk + 1 < shape.chunks ? (float)shape.chunk_rows : last_rows, entry[0], entry[p.channels]});
+    });
     for (int k = 1; k < 64; k <<= 1) m = merged(m, from_lane(m, k));
-    if (lane) return;
+    __shared__ Moments shared[kThreads / 64];
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int k = 1; k < kThreads / 64; ++k) m = merged(m, shared[k]);
     const float rstd = 1.0f / __builtin_sqrtf(m.m2 / m.n + p.eps);
     const float mean = m.mean + group_first<T>(p, (const T*)a.x + b * p.x_batch, group);
-    float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * at;
+    float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * (size_t)blockIdx.x;
     to[0] = mean;
     to[1] = rstd;
-    if (a.mean) a.mean[at] = mean;
-    if (a.rstd) a.rstd[at] = rstd;
+    if (a.mean) a.mean[blockIdx.x] = mean;
+    if (a.rstd) a.rstd[blockIdx.x] = rstd;
 }
 
 template <typename T, int V>
@@ -478,11 +540,12 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(sys_group_norm_t p
         T* y = (T*)a.y + b * p.y_batch + channel;
         float mean[V], scale[V], shift[V];
         load_affine<T, V>(p, a, channel, scale, shift);
+        int group[V];
+        groups_of<V>(channel, channels, group);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int group = (channel + i) / channels;
-            mean[i] = statistics[2 * group];
-            scale[i] *= statistics[2 * group + 1];
+            mean[i] = statistics[2 * group[i]];
+            scale[i] *= statistics[2 * group[i] + 1];
         }
         for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
             typename Channels<T, V>::Raw raw[kNormRows];
@@ -532,14 +595,15 @@ constexpr int kGradRows = 4;       // rows of x and of dy on their way together
 template <typename T, int V>
 struct GradLane {
     float mean[V], rstd[V], w[V], shift[V];
+    int group[V];
     __device__ __forceinline__ GradLane(const sys_group_norm_t& p, const NormArgs& a, int b, int channel)
     {
         load_affine<T, V>(p, a, channel, w, shift);
+        groups_of<V>(channel, p.channels / p.groups, group);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const size_t group = (size_t)b * p.groups + (channel + i) / (p.channels / p.groups);
-            mean[i] = a.mean_in[group];
-            rstd[i] = a.rstd_in[group];
+            mean[i] = a.mean_in[(size_t)b * p.groups + group[i]];
+            rstd[i] = a.rstd_in[(size_t)b * p.groups + group[i]];
         }
     }
 };
@@ -610,38 +674,59 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(sys_group_norm
     }
 }
 
-// Sums over `parts` rows of [part][f | f hat][channel], for every one of `sets` such blocks: 16 columns x 16 shares a workgroup, in one order.
-// The sums go to `to` ([set][f | f hat][channel]) or, as the last step, to the gradients themselves.
-__global__ __launch_bounds__(kThreads) void norm_grad_parts_kernel(sys_group_norm_t p, NormArgs a, const float* from, float* to, int parts, int blocks_a_set)
+// Sums over `parts` rows of [part][f | f hat][channel] of 16 columns, 16 shares of the parts a workgroup, in one order; in the first 16 lanes.
+__device__ __forceinline__ float sum_parts(const float* from, int parts, int columns, int column)
 {
-    const int set = blockIdx.x / blocks_a_set, columns = 2 * p.channels;
-    const int column = (blockIdx.x - set * blocks_a_set) * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
-    from += (size_t)set * parts * columns;
+    const int share = threadIdx.x >> 4;
     float s = 0.0f;
     if (column < columns)
         for (int k = share; k < parts; k += 16) s += from[(size_t)k * columns + column];
     __shared__ float shared[16][16];
     shared[share][threadIdx.x & 15] = s;
     __syncthreads();
-    if (share || column >= columns) return;
-    for (int k = 1; k < 16; ++k) s += shared[k][threadIdx.x];
-    if (to) {
-        to[(size_t)set * columns + column] = s;
-        return;
-    }
+    if (!share)
+        for (int k = 1; k < 16; ++k) s += shared[k][threadIdx.x];
+    return s;
+}
+
+__device__ __forceinline__ void store_affine(const sys_group_norm_t& p, const NormArgs& a, int column, float s)
+{
     void* out = column >= p.channels ? a.dw : a.db;
     if (out) store_param(out, column >= p.channels ? column - p.channels : column, p.param_dtype, s);
 }
 
-// m1 and m2, a wavefront a group.
-__global__ __launch_bounds__(kThreads) void norm_grad_means_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
+// dw and db.
+__global__ __launch_bounds__(kThreads) void norm_grad_affine_kernel(sys_group_norm_t p, NormArgs a, int parts)
+{
+    const int columns = 2 * p.channels, column = blockIdx.x * 16 + (threadIdx.x & 15);
+    const float s = sum_parts(a.workspace, parts, columns, column);
+    if (threadIdx.x < 16 && column < columns) store_affine(p, a, column, s);
+}
+
+// The chunks of every batch entry into one.
+__global__ __launch_bounds__(kThreads) void norm_grad_chunks_kernel(sys_group_norm_t p, NormArgs a, NormShape shape, int blocks_an_entry)
+{
+    const int b = blockIdx.x / blocks_an_entry, columns = 2 * p.channels, column = (blockIdx.x - b * blocks_an_entry) * 16 + (threadIdx.x & 15);
+    const float s = sum_parts(a.workspace + (size_t)b * shape.chunks * columns, shape.chunks, columns, column);
+    if (threadIdx.x < 16 && column < columns) a.workspace[grad_space(p, shape).sums + (size_t)b * columns + column] = s;
+}
+
+// The first group_blocks workgroups: m1 and m2, a wavefront a group.  The others: dw and db.
+__global__ __launch_bounds__(kThreads) void norm_grad_means_kernel(sys_group_norm_t p, NormArgs a, NormShape shape, unsigned group_blocks)
 {
     const GradSpace g = grad_space(p, shape);
+    const float* sums = a.workspace + g.sums;
+    if (blockIdx.x >= group_blocks) {
+        const int columns = 2 * p.channels, column = (blockIdx.x - group_blocks) * 16 + (threadIdx.x & 15);
+        const float s = sum_parts(sums, p.batch, columns, column);
+        if (threadIdx.x < 16 && column < columns) store_affine(p, a, column, s);
+        return;
+    }
     const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 6;
     if (at >= (long long)p.batch * p.groups) return;
     const long long b = at / p.groups;
     const int channels = p.channels / p.groups, first = (int)(at - b * p.groups) * channels, lane = threadIdx.x & 63;
-    const float* from = a.workspace + g.sums + b * 2 * p.channels;
+    const float* from = sums + b * 2 * p.channels;
     float m1 = 0.0f, m2 = 0.0f;
     for (int k = lane; k < channels; k += 64) {
         const float w = a.w ? load_param(a.w, first + k, p.param_dtype) : 1.0f;
@@ -676,9 +761,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(sys_group_nor
         float m1[V], m2[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int group = (channel + i) / (p.channels / p.groups);
-            m1[i] = means[2 * group];
-            m2[i] = means[2 * group + 1];
+            m1[i] = means[2 * lane.group[i]];
+            m2[i] = means[2 * lane.group[i] + 1];
         }
         for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
             typename Channels<T, V>::Raw raw_x[kGradRows], raw_dy[kGradRows];
@@ -758,13 +842,16 @@ bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
     s.items = (int)items;
     s.tiles = (p.groups + (1 << s.log_tile) - 1) >> s.log_tile;
     s.threads = s.log_unit > 8 ? 1 << s.log_unit : kThreads;
-    s.slices = 1;
-    if (grad) {
-        // enough units for sixteen wavefronts a CU, but no more sums of dw and db than that
-        long long slices = (4096LL * 64 >> s.log_unit) / s.tiles;
-        slices = slices < 1 ? 1 : slices > p.batch ? p.batch : slices;
-        s.slices = (int)(slices < 1 ? 1 : slices);
-    }
+    // Entries at a time, where a lane has one row of each and wavefronts are left.
+    const long long waves = (((long long)p.batch * s.tiles) << s.log_unit) >> 6;
+    s.entries = items == 1 && waves >= 4 * 4096 ? 4 : 1;
+    const long long turns = (p.batch + s.entries - 1) / s.entries;
+    // gradients: sixteen wavefronts a CU, and no more sums of dw and db than that
+    long long slices = grad ? (4096LL * 64 >> s.log_unit) / s.tiles : turns;
+    slices = slices < 1 ? 1 : slices > turns ? turns : slices;
+    s.slices = (int)slices;
+    s.rounds = (int)((turns + slices - 1) / slices);
+    s.units = (int)(slices * s.tiles);
     *out = s;
     return true;
 }
@@ -774,9 +861,9 @@ NormShape shape_of(const sys_group_norm_t& p)
     NormShape s;
     const int v = p.channels >= most_channels(p) ? most_channels(p) : 1;
     s.columns = (p.channels + v - 1) / v;
-    // some 2048 workgroups, each of at least 16 rows a lane
-    const long long tall = s.columns < kThreads ? kThreads / s.columns : 1;
-    const long long most = (p.rows + 16 * tall - 1) / (16 * tall);
+    // some 2048 workgroups, each of at least eight rows a lane (gradients of 8 x 4096 x 320, four / eight / sixteen: 18 + 16 / 16.5 + 14.6 / 19 + 18 us)
+    const long long tall = (s.columns < kThreads ? kThreads / s.columns : 1) * 8;
+    const long long most = (p.rows + tall - 1) / tall;
     long long chunks = p.batch > 0 ? (2048LL + p.batch - 1) / p.batch : 1;
     if (chunks > most) chunks = most;
     if (chunks < 1) chunks = 1;
@@ -787,32 +874,34 @@ NormShape shape_of(const sys_group_norm_t& p)
 
 unsigned blocks_for(long long lanes) { return (unsigned)((lanes + kThreads - 1) / kThreads); }
 
-unsigned resident_blocks(const ResidentShape& s, long long units) { return (unsigned)(((units << s.log_unit) + s.threads - 1) / s.threads); }
+unsigned affine_blocks(const sys_group_norm_t& p) { return (unsigned)((2LL * p.channels + 15) / 16); }
 
-template <typename T, int V, int ITEMS>
+unsigned resident_blocks(const ResidentShape& s) { return (unsigned)((((long long)s.units << s.log_unit) + s.threads - 1) / s.threads); }
+
+template <typename T, int V, int ITEMS, int ENTRIES>
 hipError_t launch_resident(const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_resident_kernel<T, V, ITEMS>), dim3(resident_blocks(s, (long long)p.batch * s.tiles)), dim3(s.threads), 0, stream, p, a, s);
+    hipLaunchKernelGGL((norm_resident_kernel<T, V, ITEMS, ENTRIES>), dim3(resident_blocks(s)), dim3(s.threads), 0, stream, p, a, s);
     return hipGetLastError();
 }
 
-template <typename T, int V, int ITEMS>
+template <typename T, int V, int ITEMS, int ENTRIES>
 hipError_t launch_grad_resident(const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_grad_resident_kernel<T, V, ITEMS>), dim3(resident_blocks(s, (long long)s.slices * s.tiles)), dim3(s.threads), 0, stream, p, a, s);
+    hipLaunchKernelGGL((norm_grad_resident_kernel<T, V, ITEMS, ENTRIES>), dim3(resident_blocks(s)), dim3(s.threads), 0, stream, p, a, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!a.dw && !a.db)) return e;
-    const int blocks = (2 * p.channels + 15) / 16;
-    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), dim3(kThreads), 0, stream, p, a, a.workspace, nullptr, s.slices, blocks);
+    hipLaunchKernelGGL(norm_grad_affine_kernel, dim3(affine_blocks(p)), dim3(kThreads), 0, stream, p, a, s.slices);
     return hipGetLastError();
 }
 
 template <typename T, int V>
 hipError_t launch_items(bool grad, const sys_group_norm_t& p, const NormArgs& a, const ResidentShape& s, hipStream_t stream)
 {
-    if (s.items == 1) return grad ? launch_grad_resident<T, V, 1>(p, a, s, stream) : launch_resident<T, V, 1>(p, a, s, stream);
-    if (s.items <= 4) return grad ? launch_grad_resident<T, V, 4>(p, a, s, stream) : launch_resident<T, V, 4>(p, a, s, stream);
-    return grad ? launch_grad_resident<T, V, kMostItems<T, V, true>>(p, a, s, stream) : launch_resident<T, V, kMostItems<T, V, false>>(p, a, s, stream);
+    if (s.entries > 1) return grad ? launch_grad_resident<T, V, 1, 4>(p, a, s, stream) : launch_resident<T, V, 1, 4>(p, a, s, stream);
+    if (s.items == 1) return grad ? launch_grad_resident<T, V, 1, 1>(p, a, s, stream) : launch_resident<T, V, 1, 1>(p, a, s, stream);
+    if (s.items <= 4) return grad ? launch_grad_resident<T, V, 4, 1>(p, a, s, stream) : launch_resident<T, V, 4, 1>(p, a, s, stream);
+    return grad ? launch_grad_resident<T, V, kMostItems<T, V, true>, 1>(p, a, s, stream) : launch_resident<T, V, kMostItems<T, V, false>, 1>(p, a, s, stream);
 }
 
 template <typename T, int V>
@@ -825,22 +914,18 @@ hipError_t launch_chunks(bool grad, const sys_group_norm_t& p, const NormArgs& a
     if (!grad) {
         hipLaunchKernelGGL((norm_moments_kernel<T, V>), grid, block, 0, s, p, a, shape);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        hipLaunchKernelGGL((norm_statistics_kernel<T>), dim3(group_blocks), block, 0, s, p, a, shape);
+        hipLaunchKernelGGL((norm_statistics_kernel<T>), dim3((unsigned)(p.batch * p.groups)), block, 0, s, p, a, shape);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         hipLaunchKernelGGL((norm_apply_kernel<T, V>), grid, block, 0, s, p, a, shape);
         return hipGetLastError();
     }
-    const int blocks = (2 * p.channels + 15) / 16;
-    float* sums = a.workspace + grad_space(p, shape).sums;
     hipLaunchKernelGGL((norm_grad_sums_kernel<T, V>), grid, block, 0, s, p, a, shape);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3((unsigned)blocks * p.batch), block, 0, s, p, a, a.workspace, sums, shape.chunks, blocks);
+    hipLaunchKernelGGL(norm_grad_chunks_kernel, dim3(affine_blocks(p) * (unsigned)p.batch), block, 0, s, p, a, shape, (int)affine_blocks(p));
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_grad_means_kernel, dim3(group_blocks), block, 0, s, p, a, shape);
+    hipLaunchKernelGGL(norm_grad_means_kernel, dim3(group_blocks + (a.dw || a.db ? affine_blocks(p) : 0)), block, 0, s, p, a, shape, group_blocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((norm_grad_apply_kernel<T, V>), grid, block, 0, s, p, a, shape);
-    if ((e = hipGetLastError()) != hipSuccess || (!a.dw && !a.db)) return e;
-    hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), block, 0, s, p, a, sums, nullptr, p.batch, blocks);
     return hipGetLastError();
 }
 
@@ -866,14 +951,13 @@ hipError_t launch(bool grad, const sys_group_norm_t& p, const NormArgs& a, hipSt
     const long long most = 0x7fffffffLL;
     if (!p.batch) {                                        // (only the gradients come here: sums of nothing)
         if (!a.dw && !a.db) return hipSuccess;
-        const int blocks = (2 * p.channels + 15) / 16;
-        hipLaunchKernelGGL(norm_grad_parts_kernel, dim3(blocks), dim3(kThreads), 0, s, p, a, (const float*)nullptr, nullptr, 0, blocks);
+        hipLaunchKernelGGL(norm_grad_affine_kernel, dim3(affine_blocks(p)), dim3(kThreads), 0, s, p, a, 0);
         return hipGetLastError();
     }
     ResidentShape r;
     if (resident_shape(p, grad, &r) ? ((long long)p.batch * r.tiles << r.log_unit) > most * kThreads || (long long)p.batch * r.tiles > most
                                     : 64LL * p.batch * p.groups > most * kThreads || (long long)shape_of(p).chunks * p.batch > most
-                                          || (2LL * p.channels + 15) / 16 * p.batch > most)
+                                          || (long long)affine_blocks(p) * p.batch > most)
         return hipErrorInvalidConfiguration;
     switch (p.dtype) {
     case SYS_F32: return launch_type<float>(grad, p, a, s);
