@@ -65,10 +65,12 @@ struct RowBuffer {
         : at((T*)base + t0 * row_stride), left(((long long)(end - 1 - t0) * row_stride + columns) * (long long)sizeof(T)), row(row_stride)
     {
     }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile() const
+    // the rows from `down` rows below the present tile's first one on
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile(int down = 0) const
     {
-        const int high = (int)(left >> 32);
-        return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, high < 0 ? 0u : high ? 0xffffffffu : (unsigned)left, 0x00027000);
+        const long long bytes = left - down * row * (long long)sizeof(T);
+        const int high = (int)(bytes >> 32);
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(at + down * row), 0, high < 0 ? 0u : high ? 0xffffffffu : (unsigned)bytes, 0x00027000);
     }
     __device__ __forceinline__ void next() { at += kScanTile * row, left -= kScanTile * row * (long long)sizeof(T); }
     __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }

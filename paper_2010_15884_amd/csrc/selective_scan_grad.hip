@@ -62,46 +62,59 @@ __host__ __device__ Workspace workspace_of(const sys_selective_scan_t& p, const 
     return w;
 }
 
-// What a lane owns of four positions 4k + part.
-struct Own {
-    float u, s, pre, dy, z;
-};
-
-template <typename T>
-struct Columns {
-    const T *u, *delta, *z, *dy;
-    float bias;
-    __device__ __forceinline__ Columns(const sys_selective_scan_t& p, const ScanArgs& a, const ScanPlace& at)
-        : u((const T*)a.u + at.batch * p.u_batch + at.channel), delta((const T*)a.delta + at.batch * p.delta_batch + at.channel),
-          z(a.z ? (const T*)a.z + at.batch * p.z_batch + at.channel : nullptr), dy((const T*)a.dy + at.batch * p.y_batch + at.channel),
-          bias(a.delta_bias ? a.delta_bias[at.channel] : 0.0f)
-    {
-    }
-    __device__ __forceinline__ Own load(const sys_selective_scan_t& p, const ScanPlace& at, int t) const
-    {
-        Own o = {};
-        const bool on = at.there && t < at.length && t < at.end;
-        if (on) {
-            o.u = (float)u[t * p.u_row];
-            o.pre = (float)delta[t * p.delta_row] + bias;
-            o.dy = (float)dy[t * p.y_row];
-            if (z) o.z = (float)z[t * p.z_row];
-            o.s = p.softplus ? softplus(o.pre) : o.pre;
-        }
-        return o;
-    }
-};
-
-// B and C of a chunk in LDS, [position][4 NS].
+// B or C of a chunk for LDS, [position][4 NS]: all of a lane's loads are under way before the first is used.  What is not there is read from a
+// place that is, and stored as 0.
 template <typename T, int NS>
-__device__ __forceinline__ void load_states(const sys_selective_scan_t& p, const void* from, long long batch_stride, long long row, const ScanPlace& at, float* lds)
-{
-    const T* rows = (const T*)from + at.batch * batch_stride + (size_t)at.group * p.states;
-    for (int k = threadIdx.x; k < kChunk<NS> * 4 * NS; k += kScanThreads) {
-        const int t = at.begin + k / (4 * NS), n = k % (4 * NS);
-        lds[k] = t < at.length && n < p.states ? (float)rows[t * row + n] : 0.0f;
+struct ChunkStates {
+    static constexpr int kEach = kChunk<NS> * 4 * NS / kScanThreads;
+    static_assert(kEach * kScanThreads == kChunk<NS> * 4 * NS && kScanThreads % (4 * NS) == 0, "a lane keeps its state");
+    T v[kEach];
+    __device__ __forceinline__ ChunkStates(const sys_selective_scan_t& p, const void* from, long long batch_stride, long long row, const ScanPlace& at)
+    {
+        const int n = (int)threadIdx.x % (4 * NS);
+        const T* column = (const T*)from + at.batch * batch_stride + (size_t)at.group * p.states + (n < p.states ? n : p.states - 1);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int t = at.begin + (i * kScanThreads + (int)threadIdx.x) / (4 * NS);
+            v[i] = column[(t < p.length ? t : p.length - 1) * row];
+        }
     }
-}
+    __device__ __forceinline__ void store(float* lds, int states, const ScanPlace& at) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int k = i * kScanThreads + (int)threadIdx.x;
+            lds[k] = k % (4 * NS) < states && at.begin + k / (4 * NS) < at.length ? (float)v[i] : 0.0f;
+        }
+    }
+};
+
+// A lane's columns: positions 4k + part of a span or tile.
+template <typename T, int OWN>
+struct OwnColumn {
+    RowBuffer<T> rows;
+    unsigned at[OWN];
+    __device__ __forceinline__ OwnColumn(const void* base, long long batch_stride, long long row, int channels, const ScanPlace& place, int end)
+        : rows(base ? (const T*)base + place.batch * batch_stride : nullptr, row, channels, place.begin, end)
+    {
+        if (!base) rows.left = -1;
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) at[k] = rows.offset(4 * k + (int)(threadIdx.x & 3), place.channel);
+    }
+    __device__ __forceinline__ void load(int down, unsigned (&v)[OWN]) const
+    {
+        const __amdgpu_buffer_rsrc_t buffer = rows.tile(down);
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) v[k] = buffer_load<T>(buffer, at[k]);
+    }
+    // positions from place.end on are not written, nor are channels that are not there
+    __device__ __forceinline__ void store(const ScanPlace& place, int down, const float (&v)[OWN]) const
+    {
+        const __amdgpu_buffer_rsrc_t buffer = rows.tile(down);
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) buffer_store<T>(buffer, place.there ? at[k] : kNowhere, (T)v[k]);
+    }
+};
 
 template <typename F>
 __device__ __forceinline__ void four_steps(F&& f)
@@ -124,14 +137,24 @@ __device__ __forceinline__ void four_steps_back(F&& f)
 template <typename T, int NS>
 __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
 {
-    const ScanPlace at = scan_place(p, shape, a.lengths, blockIdx.x);
+    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kOwn = kS / 4;
+    const ScanPlace at = scan_place(p, shape, a.lengths, xcd_place(blockIdx.x, gridDim.x));
     const int part = threadIdx.x & 3, n0 = part * NS;
-    const Workspace w = workspace_of(p, shape, 4 * NS);
+    const Workspace w = workspace_of(p, shape, kWidth);
     float *ends = a.workspace, *back = ends + w.back, *sums = ends + w.sums;
-    __shared__ __attribute__((aligned(16))) float tile_b[kChunk<NS> * 4 * NS], tile_c[kChunk<NS> * 4 * NS];
-    load_states<T, NS>(p, a.b, p.b_batch, p.b_row, at, tile_b);
-    load_states<T, NS>(p, a.c, p.c_batch, p.c_row, at, tile_c);
-    const Columns<T> columns(p, a, at);
+    __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
+    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
+    const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
+    const OwnColumn<T, kOwn> dy(a.dy, p.y_batch, p.y_row, p.channels, at, at.length), z(a.z, p.z_batch, p.z_row, p.channels, at, at.length);
+    unsigned next_u[kOwn], next_delta[kOwn], next_dy[kOwn], next_z[kOwn];
+    auto fetch = [&](int down) {
+        u.load(down, next_u);
+        delta.load(down, next_delta);
+        dy.load(down, next_dy);
+        z.load(down, next_z);
+    };
+    fetch(0);
+    const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f;
     float decay[NS], h[NS], product[NS], own_back[NS], s_sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -139,32 +162,47 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
         h[i] = own_back[i] = 0.0f;
         product[i] = 1.0f;
     }
+    states_b.store(tile_b, p.states, at);
+    states_c.store(tile_c, p.states, at);
     __syncthreads();
-    for (int k = 0; k < kChunk<NS> / 4; ++k) {
-        const Own o = columns.load(p, at, at.begin + 4 * k + part);
-        const float e_own = a.z ? o.dy * silu(o.z) : o.dy, x_own = o.s * o.u;
-        s_sum += o.s;
-        four_steps([&](auto lane) {
-            constexpr int j = decltype(lane)::value;
-            const float s = quad_take<j>(o.s), x = quad_take<j>(x_own), e = quad_take<j>(e_own);
-            float bt[NS], ct[NS];
-            take<NS>(tile_b + (4 * k + j) * 4 * NS + n0, bt);
-            take<NS>(tile_c + (4 * k + j) * 4 * NS + n0, ct);
+#pragma unroll 1
+    for (int down = 0; down < kRows; down += kS) {
+        float own_s[kOwn], own_x[kOwn], own_e[kOwn];
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const float decayed = fast_exp2(s * decay[i]);
-                h[i] = __builtin_fmaf(decayed, h[i], x * bt[i]);
-                product[i] *= decayed;
-                own_back[i] = __builtin_fmaf(ct[i] * e, product[i], own_back[i]);
-            }
-        });
+        for (int k = 0; k < kOwn; ++k) {
+            const bool on = at.begin + down + 4 * k + part < at.length;
+            const float pre = loaded<T>(next_delta[k]) + bias;
+            own_s[k] = on ? (p.softplus ? softplus(pre) : pre) : 0.0f;
+            own_x[k] = on ? own_s[k] * loaded<T>(next_u[k]) : 0.0f;
+            own_e[k] = on ? loaded<T>(next_dy[k]) : 0.0f;
+            if (a.z) own_e[k] *= on ? silu(loaded<T>(next_z[k])) : 0.0f;
+            s_sum += own_s[k];
+        }
+        fetch(down + kS);                              // (past the end: zeros)
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            four_steps([&](auto lane) {
+                constexpr int j = decltype(lane)::value;
+                const float s = quad_take<j>(own_s[k]), x = quad_take<j>(own_x[k]), e = quad_take<j>(own_e[k]);
+                float bt[NS], ct[NS];
+                take<NS>(tile_b + (down + 4 * k + j) * kWidth + n0, bt);
+                take<NS>(tile_c + (down + 4 * k + j) * kWidth + n0, ct);
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    const float decayed = fast_exp2(s * decay[i]);
+                    h[i] = __builtin_fmaf(decayed, h[i], x * bt[i]);
+                    product[i] *= decayed;
+                    own_back[i] = __builtin_fmaf(ct[i] * e, product[i], own_back[i]);
+                }
+            });
+        }
     }
     if (!at.there) return;
     const size_t row = ((size_t)at.batch * shape.chunks + at.chunk) * p.channels + at.channel;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        ends[row * (4 * NS) + n0 + i] = h[i];
-        back[row * (4 * NS) + n0 + i] = own_back[i];
+        ends[row * kWidth + n0 + i] = h[i];
+        back[row * kWidth + n0 + i] = own_back[i];
     }
     s_sum = quad_sum(s_sum);
     if (part == 0) sums[row] = s_sum;
@@ -249,19 +287,32 @@ __device__ __forceinline__ void add_over_channels(float (&v)[16], float (&out)[2
 template <typename T, int NS, bool GATE>
 __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
 {
-    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kSpans = kRows / kS;
-    const ScanPlace at = scan_place(p, shape, a.lengths, blockIdx.x);
+    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kSpans = kRows / kS, kOwn = kS / 4;
+    const unsigned block = xcd_place(blockIdx.x, gridDim.x);
+    const ScanPlace at = scan_place(p, shape, a.lengths, block);
     const int part = threadIdx.x & 3, n0 = part * NS, wave = threadIdx.x >> 6;
     const Workspace w = workspace_of(p, shape, kWidth);
     const float *ends = a.workspace, *back = ends + w.back;
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
-    __shared__ __attribute__((aligned(16))) float kept[kSpans][NS][kScanThreads];             // the state before every span
-    __shared__ float kept_s[kRows / 4][kScanThreads], kept_x[kRows / 4][kScanThreads];        // what this lane owns
-    __shared__ __attribute__((aligned(16))) float parts[kParts][kS * 2 * kWidth];             // sums over channels: [position][dB | dC][state]
-    load_states<T, NS>(p, a.b, p.b_batch, p.b_row, at, tile_b);
-    load_states<T, NS>(p, a.c, p.c_batch, p.c_row, at, tile_c);
-    const Columns<T> columns(p, a, at);
+    __shared__ float kept[kSpans][NS][kScanThreads];                                // the state before every span
+    __shared__ float kept_s[kSpans][kOwn][kScanThreads], kept_x[kSpans][kOwn][kScanThreads];     // what this lane owns
+    __shared__ __attribute__((aligned(16))) float parts[kParts][kS * 2 * kWidth];   // sums over channels: [position][dB | dC][state]
+
+    // everything that the forward sweep needs is asked for at once
+    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
+    const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
+    const OwnColumn<T, kOwn> dy(a.dy, p.y_batch, p.y_row, p.channels, at, at.length), z(GATE ? a.z : nullptr, p.z_batch, p.z_row, p.channels, at, at.length);
+    const long long values = (long long)p.length * p.channels;
+    const OwnColumn<T, kOwn> du(a.du, values, p.channels, p.channels, at, at.end), ddelta(a.ddelta, values, p.channels, p.channels, at, at.end);
+    const OwnColumn<T, kOwn> dz(GATE ? a.dz : nullptr, values, p.channels, p.channels, at, at.end);
+    unsigned all_u[kSpans][kOwn], all_delta[kSpans][kOwn];
+#pragma unroll
+    for (int span = 0; span < kSpans; ++span) {
+        u.load(span * kS, all_u[span]);
+        delta.load(span * kS, all_delta[span]);
+    }
     const size_t row = ((size_t)at.batch * shape.chunks + at.chunk) * p.channels + at.channel;
+    const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f, skip = a.d ? a.d[at.channel] : 0.0f;
     float decay[NS], h[NS], carry[NS], d_a[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -270,7 +321,27 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
         carry[i] = at.there ? back[row * kWidth + n0 + i] : 0.0f;
         d_a[i] = 0.0f;
     }
-    const float skip = a.d ? a.d[at.channel] : 0.0f;
+    states_b.store(tile_b, p.states, at);
+    states_c.store(tile_c, p.states, at);
+#pragma unroll
+    for (int span = 0; span < kSpans; ++span) {
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const bool on = at.there && at.begin + span * kS + 4 * k + part < at.length;
+            const float pre = loaded<T>(all_delta[span][k]) + bias;
+            const float s = on ? (p.softplus ? softplus(pre) : pre) : 0.0f;
+            kept_s[span][k][threadIdx.x] = s;
+            kept_x[span][k][threadIdx.x] = on ? s * loaded<T>(all_u[span][k]) : 0.0f;
+        }
+    }
+    unsigned next_u[kOwn], next_delta[kOwn], next_dy[kOwn], next_z[kOwn];
+    auto fetch = [&](int span) {
+        u.load(span * kS, next_u);
+        delta.load(span * kS, next_delta);
+        dy.load(span * kS, next_dy);
+        z.load(span * kS, next_z);
+    };
+    fetch(kSpans - 1);
     __syncthreads();
 
     // forwards: the state before every span
@@ -278,18 +349,15 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
     for (int span = 0; span < kSpans; ++span) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) kept[span][i][threadIdx.x] = h[i];
-#pragma unroll 1
-        for (int k = span * (kS / 4); k < (span + 1) * (kS / 4); ++k) {
-            const Own o = columns.load(p, at, at.begin + 4 * k + part);
-            const float x_own = o.s * o.u;
-            kept_s[k][threadIdx.x] = o.s;
-            kept_x[k][threadIdx.x] = x_own;
-            if (span == kSpans - 1) continue;
+        if (span == kSpans - 1) break;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const float own_s = kept_s[span][k][threadIdx.x], own_x = kept_x[span][k][threadIdx.x];
             four_steps([&](auto lane) {
                 constexpr int j = decltype(lane)::value;
-                const float s = quad_take<j>(o.s), x = quad_take<j>(x_own);
+                const float s = quad_take<j>(own_s), x = quad_take<j>(own_x);
                 float bt[NS];
-                take<NS>(tile_b + (4 * k + j) * kWidth + n0, bt);
+                take<NS>(tile_b + (span * kS + 4 * k + j) * kWidth + n0, bt);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(fast_exp2(s * decay[i]), h[i], x * bt[i]);
             });
@@ -301,19 +369,28 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
     for (int span = kSpans - 1; span >= 0; --span) {
         const int t_span = at.begin + span * kS;
         float state[kS + 1][NS], decayed[kS][NS];
-        float own_s[kS / 4], own_x[kS / 4], own_e[kS / 4];
-        Own own[kS / 4];
+        float own_s[kOwn], own_x[kOwn], own_e[kOwn], own_u[kOwn], own_slope[kOwn], own_dz[kOwn];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const bool on = at.there && t_span + 4 * k + part < at.length;
+            own_s[k] = kept_s[span][k][threadIdx.x];
+            own_x[k] = kept_x[span][k][threadIdx.x];
+            own_u[k] = on ? loaded<T>(next_u[k]) : 0.0f;
+            own_slope[k] = p.softplus ? sigmoid(loaded<T>(next_delta[k]) + bias) : 1.0f;
+            own_e[k] = on ? loaded<T>(next_dy[k]) : 0.0f;
+            if (GATE) {
+                const float gate = on ? loaded<T>(next_z[k]) : 0.0f, open = sigmoid(gate);
+                own_dz[k] = own_e[k] * open * __builtin_fmaf(gate, 1.0f - open, 1.0f);
+                own_e[k] *= gate * open;
+            }
+        }
+        fetch(span ? span - 1 : 0);                    // (the first span's come once more, and are not used)
 #pragma unroll
         for (int i = 0; i < NS; ++i) state[0][i] = kept[span][i][threadIdx.x];
         // the states of this span
 #pragma unroll
-        for (int k = 0; k < kS / 4; ++k) {
-            const int t = t_span + 4 * k + part;
-            own[k] = columns.load(p, at, t);
-            own_s[k] = kept_s[span * (kS / 4) + k][threadIdx.x];
-            own_x[k] = kept_x[span * (kS / 4) + k][threadIdx.x];
-            own_e[k] = GATE ? own[k].dy * silu(own[k].z) : own[k].dy;
-            float own_y = 0.0f;
+        for (int k = 0; k < kOwn; ++k) {
+            float sums_of[4];
             four_steps([&](auto lane) {
                 constexpr int j = decltype(lane)::value;
                 const float s = quad_take<j>(own_s[k]), x = quad_take<j>(own_x[k]);
@@ -326,22 +403,21 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
                     state[4 * k + j + 1][i] = __builtin_fmaf(decayed[4 * k + j][i], state[4 * k + j][i], x * bt[i]);
                     if (GATE) sum = __builtin_fmaf(ct[i], state[4 * k + j + 1][i], sum);
                 }
-                if (GATE) {
-                    sum = quad_sum(sum);
-                    own_y = part == j ? sum : own_y;
-                }
+                sums_of[j] = sum;
             });
-            if (GATE && at.there && t < at.end) {
-                const float y = __builtin_fmaf(skip, own[k].u, own_y);
-                ((T*)a.dz)[((size_t)at.batch * p.length + t) * p.channels + at.channel] = (T)(t < at.length ? own[k].dy * y * silu_grad(own[k].z) : 0.0f);
-            }
+            if (GATE) own_dz[k] *= __builtin_fmaf(skip, own_u[k], quad_sums(sums_of));
+        }
+        if (GATE) {
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) own_dz[k] = t_span + 4 * k + part < at.length ? own_dz[k] : 0.0f;
+            dz.store(at, span * kS, own_dz);
         }
         // and the gradient, from its end
         constexpr int kBatch = NS >= 8 ? 1 : 8 / NS;         // positions whose 16 values are added up together
-        float values[NS == 16 ? 2 : 1][16];
+        float values_of[NS == 16 ? 2 : 1][16], own_du[kOwn], own_ddelta[kOwn];
 #pragma unroll
-        for (int k = kS / 4 - 1; k >= 0; --k) {
-            float own_gb = 0.0f, own_qa = 0.0f;
+        for (int k = kOwn - 1; k >= 0; --k) {
+            float gb_of[4], qa_of[4];
             four_steps_back([&](auto lane) {
                 constexpr int j = decltype(lane)::value;
                 const int t = 4 * k + j;                     // within the span
@@ -353,11 +429,11 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
                 for (int i = 0; i < NS; ++i) {
                     const float g = __builtin_fmaf(ct[i], e, carry[i]);
                     if constexpr (NS == 16) {
-                        values[0][i] = g * x;
-                        values[1][i] = state[t + 1][i] * e;
+                        values_of[0][i] = g * x;
+                        values_of[1][i] = state[t + 1][i] * e;
                     } else {
-                        values[0][(t % kBatch) * 2 * NS + i] = g * x;
-                        values[0][(t % kBatch) * 2 * NS + NS + i] = state[t + 1][i] * e;
+                        values_of[0][(t % kBatch) * 2 * NS + i] = g * x;
+                        values_of[0][(t % kBatch) * 2 * NS + NS + i] = state[t + 1][i] * e;
                     }
                     gb = __builtin_fmaf(g, bt[i], gb);
                     carry[i] = g * decayed[t][i];
@@ -365,17 +441,15 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
                     d_a[i] = __builtin_fmaf(q, s, d_a[i]);
                     qa = __builtin_fmaf(q, decay[i], qa);
                 }
-                gb = quad_sum(gb);
-                qa = quad_sum(qa);
-                own_gb = part == j ? gb : own_gb;
-                own_qa = part == j ? qa : own_qa;
+                gb_of[j] = gb;
+                qa_of[j] = qa;
                 if (t % kBatch == 0) {
                     const int high = ((threadIdx.x >> 5) & 1) * 8 + ((threadIdx.x >> 4) & 1) * 4 + ((threadIdx.x >> 3) & 1) * 2;
                     float* to = parts[wave * 2 + ((threadIdx.x >> 2) & 1)];
 #pragma unroll
                     for (int set = 0; set < (NS == 16 ? 2 : 1); ++set) {
                         float sum[2];
-                        add_over_channels(values[set], sum);
+                        add_over_channels(values_of[set], sum);
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
                             const int v = high + m;
@@ -385,21 +459,19 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
                     }
                 }
             });
-            const int t = t_span + 4 * k + part;
-            const float ds = own_gb * own[k].u + own_qa * kLn2;                  // (decay is A log2 e)
-            const float ddelta = p.softplus ? ds * sigmoid(own[k].pre) : ds;
-            const bool on = at.there && t < at.length && t < at.end;
-            d_skip += on ? own_e[k] * own[k].u : 0.0f;
-            d_bias += on ? ddelta : 0.0f;
-            if (at.there && t < at.end) {
-                const size_t to = ((size_t)at.batch * p.length + t) * p.channels + at.channel;
-                ((T*)a.du)[to] = (T)(on ? __builtin_fmaf(own_gb, own_s[k], skip * own_e[k]) : 0.0f);
-                ((T*)a.ddelta)[to] = (T)(on ? ddelta : 0.0f);
-            }
+            const bool on = at.there && t_span + 4 * k + part < at.length;
+            const float gb = quad_sums(gb_of), qa = quad_sums(qa_of);
+            const float ds = __builtin_fmaf(gb, own_u[k], qa * kLn2);            // (decay is A log2 e)
+            own_ddelta[k] = on ? ds * own_slope[k] : 0.0f;
+            own_du[k] = on ? __builtin_fmaf(gb, own_s[k], skip * own_e[k]) : 0.0f;
+            d_skip = __builtin_fmaf(own_e[k], own_u[k], d_skip);
+            d_bias += own_ddelta[k];
         }
+        du.store(at, span * kS, own_du);
+        ddelta.store(at, span * kS, own_ddelta);
         __syncthreads();
         {
-            const int channel_block = blockIdx.x % shape.channel_blocks;
+            const int channel_block = block % shape.channel_blocks;
             float* to = a.workspace + w.states + (((size_t)channel_block * p.batch + at.batch) * p.length + t_span) * (2 * kWidth);
             for (int k = threadIdx.x; k < kS * 2 * kWidth; k += kScanThreads) {
                 if (t_span + k / (2 * kWidth) >= at.end) break;
