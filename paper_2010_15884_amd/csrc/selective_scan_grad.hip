@@ -5,11 +5,12 @@
 //   dA   = sum_t q_t s_t,  dB_t = sum_d g_t x_t,  dC_t = sum_d h_t e_t,  dD = sum_t e_t u_t,  dz_t = dy_t (sum_n C_t h_t + D u_t) silu'(z_t)
 //
 // Both recurrences run along the positions, one from each end.  The positions are cut into chunks:
-//   scan_ends_kernel    every chunk from a zero start: the state at its end, sum s, and what its positions hand back to the one before
-//                       it, sum_t (a_first .. a_t) C_t e_t -- with the running product, so one sweep serves both directions;
+//   scan_ends_kernel    every chunk from a zero start: the state and sum s at its end and before each of its four spans, and what its
+//                       positions hand back to the chunk before it, sum_t (a_first .. a_t) C_t e_t -- with the running product, so that one sweep
+//                       serves both directions;
 //   scan_chain_kernel   along the chunks: the state before each, the gradient behind each;
-//   scan_grad_kernel    every chunk again, from those: the states forward, a copy every few positions; then, backwards, these few
-//                       positions' states and decays once more into registers and the recurrence of the gradient over them;
+//   scan_grad_kernel    every chunk's spans from the last to the first: the state before a span is that of the zero start plus e^(A sum s) times
+//                       the chunk's; the span's states and decays go into registers, and the recurrence of the gradient runs over them;
 //   scan_sums_kernel    adds up what the workgroups have summed over their channels (dB, dC) and their positions (dA, dD, ddelta_bias).
 // Each sum has a fixed order.
 #include "launch.h"
@@ -21,7 +22,7 @@ namespace {
 
 // Positions whose states and decays are in registers at a time: 64 of each a lane at most; and those of a chunk.
 template <int NS> constexpr int kSpan = NS <= 4 ? 16 : 64 / NS;
-template <int NS> constexpr int kChunk = 4 * kSpan<NS>;
+template <int NS> constexpr int kChunk = 4 * kSpan<NS>;       // (kSpans of them)
 constexpr int kParts = 8;            // partial sums over channels in a workgroup: two a wavefront
 
 int chunk_rows_of(int states)
@@ -44,19 +45,23 @@ ScanShape backward_shape(const sys_selective_scan_t& p)
 // The workspace: where its parts begin, in floats.
 struct Workspace {
     size_t back;                   // [batch][chunk][channel][width], behind the same for `ends` at 0
-    size_t sums;                   // [batch][chunk][channel]
+    size_t spans;                  // [batch][chunk][span 1 ..][channel][width]
+    size_t sums;                   // [batch][chunk][span][channel]: sum s up to the span's end
     size_t params;                 // [batch][chunk][channel][width + 2]: dA, dD, ddelta_bias
     size_t states;                 // [channel block][batch][position][dB | dC][width]
     size_t floats;
 };
+
+constexpr int kSpans = 4;          // a chunk
 
 __host__ __device__ Workspace workspace_of(const sys_selective_scan_t& p, const ScanShape& shape, int width)
 {
     Workspace w;
     const size_t rows = (size_t)p.batch * shape.chunks * p.channels;
     w.back = rows * width;
-    w.sums = w.back + rows * width;
-    w.params = w.sums + rows;
+    w.spans = w.back + rows * width;
+    w.sums = w.spans + rows * (kSpans - 1) * width;
+    w.params = w.sums + rows * kSpans;
     w.states = w.params + rows * (width + 2);
     w.floats = w.states + (size_t)shape.channel_blocks * p.batch * p.length * 2 * width;
     return w;
@@ -89,30 +94,34 @@ struct ChunkStates {
     }
 };
 
-// A lane's columns: positions 4k + part of a span or tile.
+// A lane's column of a tensor: positions 4k + part of a span.  One offset is kept; the others are added up where they are used, behind a wall
+// that stops the compiler from keeping all of them in registers that the states need.
 template <typename T, int OWN>
 struct OwnColumn {
     RowBuffer<T> rows;
-    unsigned at[OWN];
+    unsigned at, step;
     __device__ __forceinline__ OwnColumn(const void* base, long long batch_stride, long long row, int channels, const ScanPlace& place, int end)
-        : rows(base ? (const T*)base + place.batch * batch_stride : nullptr, row, channels, place.begin, end)
+        : rows(base ? (const T*)base + place.batch * batch_stride : nullptr, row, channels, place.begin, end), at(rows.offset((int)(threadIdx.x & 3), place.channel)),
+          step(rows.offset(4, 0))
     {
         if (!base) rows.left = -1;
-#pragma unroll
-        for (int k = 0; k < OWN; ++k) at[k] = rows.offset(4 * k + (int)(threadIdx.x & 3), place.channel);
     }
     __device__ __forceinline__ void load(int down, unsigned (&v)[OWN]) const
     {
         const __amdgpu_buffer_rsrc_t buffer = rows.tile(down);
+        unsigned first = at;
+        asm volatile("" : "+v"(first));
 #pragma unroll
-        for (int k = 0; k < OWN; ++k) v[k] = buffer_load<T>(buffer, at[k]);
+        for (int k = 0; k < OWN; ++k) v[k] = buffer_load<T>(buffer, first + k * step);
     }
     // positions from place.end on are not written, nor are channels that are not there
     __device__ __forceinline__ void store(const ScanPlace& place, int down, const float (&v)[OWN]) const
     {
         const __amdgpu_buffer_rsrc_t buffer = rows.tile(down);
+        unsigned first = at;
+        asm volatile("" : "+v"(first));
 #pragma unroll
-        for (int k = 0; k < OWN; ++k) buffer_store<T>(buffer, place.there ? at[k] : kNowhere, (T)v[k]);
+        for (int k = 0; k < OWN; ++k) buffer_store<T>(buffer, place.there ? first + k * step : kNowhere, (T)v[k]);
     }
 };
 
@@ -125,15 +134,6 @@ __device__ __forceinline__ void four_steps(F&& f)
     f(std::integral_constant<int, 3>());
 }
 
-template <typename F>
-__device__ __forceinline__ void four_steps_back(F&& f)
-{
-    f(std::integral_constant<int, 3>());
-    f(std::integral_constant<int, 2>());
-    f(std::integral_constant<int, 1>());
-    f(std::integral_constant<int, 0>());
-}
-
 template <typename T, int NS>
 __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
 {
@@ -141,7 +141,10 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
     const ScanPlace at = scan_place(p, shape, a.lengths, xcd_place(blockIdx.x, gridDim.x));
     const int part = threadIdx.x & 3, n0 = part * NS;
     const Workspace w = workspace_of(p, shape, kWidth);
-    float *ends = a.workspace, *back = ends + w.back, *sums = ends + w.sums;
+    float *ends = a.workspace, *back = ends + w.back;
+    const size_t entry = (size_t)at.batch * shape.chunks + at.chunk, row = entry * p.channels + at.channel;
+    float* spans = ends + w.spans + (entry * (kSpans - 1) * p.channels + at.channel) * kWidth + n0;
+    float* sums = ends + w.sums + entry * kSpans * p.channels + at.channel;
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
     const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
     const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
@@ -176,9 +179,18 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
             own_x[k] = on ? own_s[k] * loaded<T>(next_u[k]) : 0.0f;
             own_e[k] = on ? loaded<T>(next_dy[k]) : 0.0f;
             if (a.z) own_e[k] *= on ? silu(loaded<T>(next_z[k])) : 0.0f;
-            s_sum += own_s[k];
         }
+        float span_sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) span_sum += own_s[k];
+        s_sum += quad_sum(span_sum);
+        if (at.there && part == 0) *sums = s_sum;          // at the end of this span
+        sums += p.channels;
         fetch(down + kS);                              // (past the end: zeros)
+        if (down && at.there) {
+            Channels<float, NS>::store(spans, h);
+            spans += (size_t)p.channels * kWidth;
+        }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             four_steps([&](auto lane) {
@@ -198,14 +210,8 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
         }
     }
     if (!at.there) return;
-    const size_t row = ((size_t)at.batch * shape.chunks + at.chunk) * p.channels + at.channel;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        ends[row * kWidth + n0 + i] = h[i];
-        back[row * kWidth + n0 + i] = own_back[i];
-    }
-    s_sum = quad_sum(s_sum);
-    if (part == 0) sums[row] = s_sum;
+    Channels<float, NS>::store(ends + row * kWidth + n0, h);
+    Channels<float, NS>::store(back + row * kWidth + n0, own_back);
 }
 
 // A lane a (sequence, channel, state): the state before every chunk and the gradient behind it, in place of what the chunks left.
@@ -218,7 +224,8 @@ __global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_
     const long long b = channel_of / p.channels;
     if (b >= p.batch) return;
     const Workspace w = workspace_of(p, shape, width);
-    float *ends = a.workspace, *back = ends + w.back, *sums = ends + w.sums;
+    float *ends = a.workspace, *back = ends + w.back;
+    const float* sums = ends + w.sums;                 // of whole chunks: behind their last spans
     const bool is = n < p.states;
     const float decay = is ? a.a[(size_t)d * p.states + n] * kLog2e : 0.0f;
     const size_t state = ((size_t)b * p.channels + d) * p.states + n;
@@ -231,7 +238,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_
         for (int k = 0; k < kAhead; ++k) {
             const size_t row = first + (size_t)(k0 + k < shape.chunks ? k0 + k : k0) * p.channels;
             end[k] = ends[row * width + n];
-            factor[k] = fast_exp2(sums[row] * decay);
+            factor[k] = fast_exp2(sums[((row - d) * kSpans + (kSpans - 1) * (size_t)p.channels) + d] * decay);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_
         for (int k = 0; k < kAhead; ++k) {
             const size_t row = first + (size_t)(k0 - k >= 0 ? k0 - k : k0) * p.channels;
             own[k] = back[row * width + n];
-            factor[k] = fast_exp2(sums[row] * decay);
+            factor[k] = fast_exp2(sums[((row - d) * kSpans + (kSpans - 1) * (size_t)p.channels) + d] * decay);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -287,124 +294,100 @@ __device__ __forceinline__ void add_over_channels(float (&v)[16], float (&out)[2
 template <typename T, int NS, bool GATE>
 __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
 {
-    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kSpans = kRows / kS, kOwn = kS / 4;
+    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kOwn = kS / 4;
+    static_assert(kRows == kSpans * kS, "a chunk");
     const unsigned block = xcd_place(blockIdx.x, gridDim.x);
     const ScanPlace at = scan_place(p, shape, a.lengths, block);
-    const int part = threadIdx.x & 3, n0 = part * NS, wave = threadIdx.x >> 6;
+    const int part = threadIdx.x & 3, n0 = part * NS, wave = threadIdx.x >> 6, own_channel = threadIdx.x >> 2;
     const Workspace w = workspace_of(p, shape, kWidth);
     const float *ends = a.workspace, *back = ends + w.back;
+    const size_t entry = (size_t)at.batch * shape.chunks + at.chunk, row = entry * p.channels + at.channel;
+    const float* spans = ends + w.spans + (entry * (kSpans - 1) * p.channels + at.channel) * kWidth + n0;
+    const float* sums = ends + w.sums + entry * kSpans * p.channels + at.channel;
+    typedef float F4 __attribute__((ext_vector_type(4)));
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
-    __shared__ float kept[kSpans][NS][kScanThreads];                                // the state before every span
-    __shared__ float kept_s[kSpans][kOwn][kScanThreads], kept_x[kSpans][kOwn][kScanThreads];     // what this lane owns
+    // s, x and e of a span: written by the lane that owns a position, read by the four of its channel, which are of one wavefront (no barrier)
+    __shared__ F4 steps[kS][kScanChannels];
     __shared__ __attribute__((aligned(16))) float parts[kParts][kS * 2 * kWidth];   // sums over channels: [position][dB | dC][state]
 
-    // everything that the forward sweep needs is asked for at once
     const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
     const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
     const OwnColumn<T, kOwn> dy(a.dy, p.y_batch, p.y_row, p.channels, at, at.length), z(GATE ? a.z : nullptr, p.z_batch, p.z_row, p.channels, at, at.length);
     const long long values = (long long)p.length * p.channels;
     const OwnColumn<T, kOwn> du(a.du, values, p.channels, p.channels, at, at.end), ddelta(a.ddelta, values, p.channels, p.channels, at, at.end);
     const OwnColumn<T, kOwn> dz(GATE ? a.dz : nullptr, values, p.channels, p.channels, at, at.end);
-    unsigned all_u[kSpans][kOwn], all_delta[kSpans][kOwn];
-#pragma unroll
-    for (int span = 0; span < kSpans; ++span) {
-        u.load(span * kS, all_u[span]);
-        delta.load(span * kS, all_delta[span]);
-    }
-    const size_t row = ((size_t)at.batch * shape.chunks + at.chunk) * p.channels + at.channel;
-    const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f, skip = a.d ? a.d[at.channel] : 0.0f;
-    float decay[NS], h[NS], carry[NS], d_a[NS];
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        decay[i] = n0 + i < p.states ? a.a[(size_t)at.channel * p.states + n0 + i] * kLog2e : 0.0f;
-        h[i] = at.there ? ends[row * kWidth + n0 + i] : 0.0f;
-        carry[i] = at.there ? back[row * kWidth + n0 + i] : 0.0f;
-        d_a[i] = 0.0f;
-    }
-    states_b.store(tile_b, p.states, at);
-    states_c.store(tile_c, p.states, at);
-#pragma unroll
-    for (int span = 0; span < kSpans; ++span) {
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            const bool on = at.there && at.begin + span * kS + 4 * k + part < at.length;
-            const float pre = loaded<T>(all_delta[span][k]) + bias;
-            const float s = on ? (p.softplus ? softplus(pre) : pre) : 0.0f;
-            kept_s[span][k][threadIdx.x] = s;
-            kept_x[span][k][threadIdx.x] = on ? s * loaded<T>(all_u[span][k]) : 0.0f;
-        }
-    }
     unsigned next_u[kOwn], next_delta[kOwn], next_dy[kOwn], next_z[kOwn];
+    float next_state[NS], next_sum;
     auto fetch = [&](int span) {
         u.load(span * kS, next_u);
         delta.load(span * kS, next_delta);
         dy.load(span * kS, next_dy);
         z.load(span * kS, next_z);
+        const int before = span ? span - 1 : 0;        // (the first span begins with the chunk's state, and reads another one)
+        Channels<float, NS>::load(spans + (size_t)before * p.channels * kWidth, next_state);
+        next_sum = sums[(size_t)before * p.channels];
     };
     fetch(kSpans - 1);
-    __syncthreads();
-
-    // forwards: the state before every span
-#pragma unroll 1
-    for (int span = 0; span < kSpans; ++span) {
+    const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f, skip = a.d ? a.d[at.channel] : 0.0f;
+    float decay[NS], h0[NS], carry[NS], d_a[NS];
+    Channels<float, NS>::load(ends + row * kWidth + n0, h0);
+    Channels<float, NS>::load(back + row * kWidth + n0, carry);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) kept[span][i][threadIdx.x] = h[i];
-        if (span == kSpans - 1) break;
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            const float own_s = kept_s[span][k][threadIdx.x], own_x = kept_x[span][k][threadIdx.x];
-            four_steps([&](auto lane) {
-                constexpr int j = decltype(lane)::value;
-                const float s = quad_take<j>(own_s), x = quad_take<j>(own_x);
-                float bt[NS];
-                take<NS>(tile_b + (span * kS + 4 * k + j) * kWidth + n0, bt);
-#pragma unroll
-                for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(fast_exp2(s * decay[i]), h[i], x * bt[i]);
-            });
-        }
+    for (int i = 0; i < NS; ++i) {
+        decay[i] = n0 + i < p.states ? a.a[(size_t)at.channel * p.states + n0 + i] * kLog2e : 0.0f;
+        h0[i] = at.there ? h0[i] : 0.0f;               // (a channel that is not there adds nothing to the sums)
+        carry[i] = at.there ? carry[i] : 0.0f;
+        d_a[i] = 0.0f;
     }
+    states_b.store(tile_b, p.states, at);
+    states_c.store(tile_c, p.states, at);
+    __syncthreads();
 
     float d_skip = 0.0f, d_bias = 0.0f;
 #pragma unroll 1
     for (int span = kSpans - 1; span >= 0; --span) {
         const int t_span = at.begin + span * kS;
         float state[kS + 1][NS], decayed[kS][NS];
-        float own_s[kOwn], own_x[kOwn], own_e[kOwn], own_u[kOwn], own_slope[kOwn], own_dz[kOwn];
+        float own_s[kOwn], own_e[kOwn], own_u[kOwn], own_slope[kOwn], own_dz[kOwn];
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             const bool on = at.there && t_span + 4 * k + part < at.length;
-            own_s[k] = kept_s[span][k][threadIdx.x];
-            own_x[k] = kept_x[span][k][threadIdx.x];
+            const float pre = loaded<T>(next_delta[k]) + bias;
+            own_s[k] = on ? (p.softplus ? softplus(pre) : pre) : 0.0f;
+            own_slope[k] = p.softplus ? sigmoid(pre) : 1.0f;
             own_u[k] = on ? loaded<T>(next_u[k]) : 0.0f;
-            own_slope[k] = p.softplus ? sigmoid(loaded<T>(next_delta[k]) + bias) : 1.0f;
             own_e[k] = on ? loaded<T>(next_dy[k]) : 0.0f;
             if (GATE) {
                 const float gate = on ? loaded<T>(next_z[k]) : 0.0f, open = sigmoid(gate);
                 own_dz[k] = own_e[k] * open * __builtin_fmaf(gate, 1.0f - open, 1.0f);
                 own_e[k] *= gate * open;
             }
+            steps[4 * k + part][own_channel] = F4{own_s[k], own_s[k] * own_u[k], own_e[k], 0.0f};
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const float from_start = at.there ? next_state[i] : 0.0f;
+            state[0][i] = span ? __builtin_fmaf(fast_exp2(next_sum * decay[i]), h0[i], from_start) : h0[i];
         }
         fetch(span ? span - 1 : 0);                    // (the first span's come once more, and are not used)
-#pragma unroll
-        for (int i = 0; i < NS; ++i) state[0][i] = kept[span][i][threadIdx.x];
         // the states of this span
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             float sums_of[4];
-            four_steps([&](auto lane) {
-                constexpr int j = decltype(lane)::value;
-                const float s = quad_take<j>(own_s[k]), x = quad_take<j>(own_x[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const F4 step = steps[4 * k + j][own_channel];
                 float bt[NS], ct[NS], sum = 0.0f;
                 take<NS>(tile_b + (span * kS + 4 * k + j) * kWidth + n0, bt);
                 if (GATE) take<NS>(tile_c + (span * kS + 4 * k + j) * kWidth + n0, ct);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
-                    decayed[4 * k + j][i] = fast_exp2(s * decay[i]);
-                    state[4 * k + j + 1][i] = __builtin_fmaf(decayed[4 * k + j][i], state[4 * k + j][i], x * bt[i]);
+                    decayed[4 * k + j][i] = fast_exp2(step[0] * decay[i]);
+                    state[4 * k + j + 1][i] = __builtin_fmaf(decayed[4 * k + j][i], state[4 * k + j][i], step[1] * bt[i]);
                     if (GATE) sum = __builtin_fmaf(ct[i], state[4 * k + j + 1][i], sum);
                 }
                 sums_of[j] = sum;
-            });
+            }
             if (GATE) own_dz[k] *= __builtin_fmaf(skip, own_u[k], quad_sums(sums_of));
         }
         if (GATE) {
@@ -418,10 +401,11 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
 #pragma unroll
         for (int k = kOwn - 1; k >= 0; --k) {
             float gb_of[4], qa_of[4];
-            four_steps_back([&](auto lane) {
-                constexpr int j = decltype(lane)::value;
+#pragma unroll
+            for (int j = 3; j >= 0; --j) {
                 const int t = 4 * k + j;                     // within the span
-                const float s = quad_take<j>(own_s[k]), x = quad_take<j>(own_x[k]), e = quad_take<j>(own_e[k]);
+                const F4 step = steps[t][own_channel];
+                const float s = step[0], x = step[1], e = step[2];
                 float bt[NS], ct[NS], gb = 0.0f, qa = 0.0f;
                 take<NS>(tile_b + (span * kS + t) * kWidth + n0, bt);
                 take<NS>(tile_c + (span * kS + t) * kWidth + n0, ct);
@@ -458,7 +442,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
                         }
                     }
                 }
-            });
+            }
             const bool on = at.there && t_span + 4 * k + part < at.length;
             const float gb = quad_sums(gb_of), qa = quad_sums(qa_of);
             const float ds = __builtin_fmaf(gb, own_u[k], qa * kLn2);            // (decay is A log2 e)
