@@ -5,7 +5,7 @@
 //   dA   = sum_t q_t s_t,  dB_t = sum_d g_t x_t,  dC_t = sum_d h_t e_t,  dD = sum_t e_t u_t,  dz_t = dy_t (sum_n C_t h_t + D u_t) silu'(z_t)
 //
 // Both recurrences run along the positions, one from each end.  The positions are cut into chunks:
-//   scan_ends_kernel    every chunk from a zero start: the state and sum s at its end and before each of its four spans, and what its
+//   scan_ends_kernel    every chunk from a zero start: the state and sum s at its end and before each of its spans, and what its
 //                       positions hand back to the chunk before it, sum_t (a_first .. a_t) C_t e_t -- with the running product, so that one sweep
 //                       serves both directions;
 //   scan_chain_kernel   along the chunks: the state before each, the gradient behind each;
@@ -20,48 +20,49 @@
 namespace sysconv {
 namespace {
 
-// Positions whose states and decays are in registers at a time: 64 of each a lane at most; and those of a chunk.
+// Positions of a span, whose states and decays are in registers at a time, 64 of each a lane at most; spans of a chunk at most.
 template <int NS> constexpr int kSpan = NS <= 4 ? 16 : 64 / NS;
-template <int NS> constexpr int kChunk = 4 * kSpan<NS>;       // (kSpans of them)
+constexpr int kMostSpans = 8;
 constexpr int kParts = 8;            // partial sums over channels in a workgroup: two a wavefront
 
-int chunk_rows_of(int states)
-{
-    const int ns = scan_states_a_lane(states);
-    return 4 * (ns <= 4 ? 16 : 64 / ns);
-}
+struct GradShape : ScanShape {
+    int spans;                       // of a chunk
+};
 
-ScanShape backward_shape(const sys_selective_scan_t& p)
+GradShape backward_shape(const sys_selective_scan_t& p)
 {
-    ScanShape s;
+    GradShape s;
     s.channels_a_group = p.channels / p.groups;
     s.blocks_a_group = (s.channels_a_group + kScanChannels - 1) / kScanChannels;
     s.channel_blocks = s.blocks_a_group * p.groups;
-    s.chunk_rows = chunk_rows_of(p.states);
-    s.chunks = (p.length + s.chunk_rows - 1) / s.chunk_rows;
+    const int ns = scan_states_a_lane(p.states), span = ns <= 4 ? 16 : 64 / ns;
+    // Long chunks leave the chain along them little to read and write; short ones leave work for all CUs: as long as there are eight
+    // workgroups a CU.
+    const long long spans = ((long long)p.length + span - 1) / span, all = spans * s.channel_blocks * p.batch;
+    s.spans = all / 2048 < 1 ? 1 : all / 2048 > kMostSpans ? kMostSpans : (int)(all / 2048);
+    s.chunk_rows = s.spans * span;
+    s.chunks = (int)((spans + s.spans - 1) / s.spans);
     return s;
 }
 
 // The workspace: where its parts begin, in floats.
 struct Workspace {
     size_t back;                   // [batch][chunk][channel][width], behind the same for `ends` at 0
-    size_t spans;                  // [batch][chunk][span 1 ..][channel][width]
+    size_t spans;                  // [batch][chunk][span 1 ..][channel][width]: the state before the span
     size_t sums;                   // [batch][chunk][span][channel]: sum s up to the span's end
     size_t params;                 // [batch][chunk][channel][width + 2]: dA, dD, ddelta_bias
     size_t states;                 // [channel block][batch][position][dB | dC][width]
     size_t floats;
 };
 
-constexpr int kSpans = 4;          // a chunk
-
-__host__ __device__ Workspace workspace_of(const sys_selective_scan_t& p, const ScanShape& shape, int width)
+__host__ __device__ Workspace workspace_of(const sys_selective_scan_t& p, const GradShape& shape, int width)
 {
     Workspace w;
     const size_t rows = (size_t)p.batch * shape.chunks * p.channels;
     w.back = rows * width;
     w.spans = w.back + rows * width;
-    w.sums = w.spans + rows * (kSpans - 1) * width;
-    w.params = w.sums + rows * kSpans;
+    w.sums = w.spans + rows * (shape.spans - 1) * width;
+    w.params = w.sums + rows * shape.spans;
     w.states = w.params + rows * (width + 2);
     w.floats = w.states + (size_t)shape.channel_blocks * p.batch * p.length * 2 * width;
     return w;
@@ -71,23 +72,25 @@ __host__ __device__ Workspace workspace_of(const sys_selective_scan_t& p, const 
 // place that is, and stored as 0.
 template <typename T, int NS>
 struct ChunkStates {
-    static constexpr int kEach = kChunk<NS> * 4 * NS / kScanThreads;
-    static_assert(kEach * kScanThreads == kChunk<NS> * 4 * NS && kScanThreads % (4 * NS) == 0, "a lane keeps its state");
+    static constexpr int kEach = kMostSpans * kSpan<NS> * 4 * NS / kScanThreads;
+    static_assert(kEach * kScanThreads == kMostSpans * kSpan<NS> * 4 * NS && kScanThreads % (4 * NS) == 0, "a lane keeps its state");
     T v[kEach];
-    __device__ __forceinline__ ChunkStates(const sys_selective_scan_t& p, const void* from, long long batch_stride, long long row, const ScanPlace& at)
+    __device__ __forceinline__ ChunkStates(const sys_selective_scan_t& p, const void* from, long long batch_stride, long long row, const ScanPlace& at, int rows)
     {
         const int n = (int)threadIdx.x % (4 * NS);
         const T* column = (const T*)from + at.batch * batch_stride + (size_t)at.group * p.states + (n < p.states ? n : p.states - 1);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
+            if (i * kScanThreads >= rows * 4 * NS) break;
             const int t = at.begin + (i * kScanThreads + (int)threadIdx.x) / (4 * NS);
             v[i] = column[(t < p.length ? t : p.length - 1) * row];
         }
     }
-    __device__ __forceinline__ void store(float* lds, int states, const ScanPlace& at) const
+    __device__ __forceinline__ void store(float* lds, int states, const ScanPlace& at, int rows) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
+            if (i * kScanThreads >= rows * 4 * NS) break;
             const int k = i * kScanThreads + (int)threadIdx.x;
             lds[k] = k % (4 * NS) < states && at.begin + k / (4 * NS) < at.length ? (float)v[i] : 0.0f;
         }
@@ -135,18 +138,18 @@ __device__ __forceinline__ void four_steps(F&& f)
 }
 
 template <typename T, int NS>
-__global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
+__global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_scan_t p, ScanArgs a, GradShape shape)
 {
-    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kOwn = kS / 4;
+    constexpr int kS = kSpan<NS>, kRows = kMostSpans * kS, kWidth = 4 * NS, kOwn = kS / 4;
     const ScanPlace at = scan_place(p, shape, a.lengths, xcd_place(blockIdx.x, gridDim.x));
     const int part = threadIdx.x & 3, n0 = part * NS;
     const Workspace w = workspace_of(p, shape, kWidth);
     float *ends = a.workspace, *back = ends + w.back;
     const size_t entry = (size_t)at.batch * shape.chunks + at.chunk, row = entry * p.channels + at.channel;
-    float* spans = ends + w.spans + (entry * (kSpans - 1) * p.channels + at.channel) * kWidth + n0;
-    float* sums = ends + w.sums + entry * kSpans * p.channels + at.channel;
+    float* spans = ends + w.spans + (entry * (shape.spans - 1) * p.channels + at.channel) * kWidth + n0;
+    float* sums = ends + w.sums + entry * shape.spans * p.channels + at.channel;
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
-    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
+    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at, shape.chunk_rows), states_c(p, a.c, p.c_batch, p.c_row, at, shape.chunk_rows);
     const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
     const OwnColumn<T, kOwn> dy(a.dy, p.y_batch, p.y_row, p.channels, at, at.length), z(a.z, p.z_batch, p.z_row, p.channels, at, at.length);
     unsigned next_u[kOwn], next_delta[kOwn], next_dy[kOwn], next_z[kOwn];
@@ -165,11 +168,11 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
         h[i] = own_back[i] = 0.0f;
         product[i] = 1.0f;
     }
-    states_b.store(tile_b, p.states, at);
-    states_c.store(tile_c, p.states, at);
+    states_b.store(tile_b, p.states, at, shape.chunk_rows);
+    states_c.store(tile_c, p.states, at, shape.chunk_rows);
     __syncthreads();
 #pragma unroll 1
-    for (int down = 0; down < kRows; down += kS) {
+    for (int down = 0; down < shape.chunk_rows; down += kS) {
         float own_s[kOwn], own_x[kOwn], own_e[kOwn];
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_ends_kernel(sys_selective_s
 }
 
 // A lane a (sequence, channel, state): the state before every chunk and the gradient behind it, in place of what the chunks left.
-__global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape, int width)
+__global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_scan_t p, ScanArgs a, GradShape shape, int width)
 {
     const long long lane = (long long)blockIdx.x * kScanThreads + threadIdx.x;
     const int n = (int)(lane % width);
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_
         for (int k = 0; k < kAhead; ++k) {
             const size_t row = first + (size_t)(k0 + k < shape.chunks ? k0 + k : k0) * p.channels;
             end[k] = ends[row * width + n];
-            factor[k] = fast_exp2(sums[((row - d) * kSpans + (kSpans - 1) * (size_t)p.channels) + d] * decay);
+            factor[k] = fast_exp2(sums[((row - d) * shape.spans + (shape.spans - 1) * (size_t)p.channels) + d] * decay);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -254,7 +257,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_chain_kernel(sys_selective_
         for (int k = 0; k < kAhead; ++k) {
             const size_t row = first + (size_t)(k0 - k >= 0 ? k0 - k : k0) * p.channels;
             own[k] = back[row * width + n];
-            factor[k] = fast_exp2(sums[((row - d) * kSpans + (kSpans - 1) * (size_t)p.channels) + d] * decay);
+            factor[k] = fast_exp2(sums[((row - d) * shape.spans + (shape.spans - 1) * (size_t)p.channels) + d] * decay);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -292,25 +295,24 @@ __device__ __forceinline__ void add_over_channels(float (&v)[16], float (&out)[2
 }
 
 template <typename T, int NS, bool GATE>
-__global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape)
+__global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_scan_t p, ScanArgs a, GradShape shape)
 {
-    constexpr int kS = kSpan<NS>, kRows = kChunk<NS>, kWidth = 4 * NS, kOwn = kS / 4;
-    static_assert(kRows == kSpans * kS, "a chunk");
+    constexpr int kS = kSpan<NS>, kRows = kMostSpans * kS, kWidth = 4 * NS, kOwn = kS / 4;
     const unsigned block = xcd_place(blockIdx.x, gridDim.x);
     const ScanPlace at = scan_place(p, shape, a.lengths, block);
     const int part = threadIdx.x & 3, n0 = part * NS, wave = threadIdx.x >> 6, own_channel = threadIdx.x >> 2;
     const Workspace w = workspace_of(p, shape, kWidth);
     const float *ends = a.workspace, *back = ends + w.back;
     const size_t entry = (size_t)at.batch * shape.chunks + at.chunk, row = entry * p.channels + at.channel;
-    const float* spans = ends + w.spans + (entry * (kSpans - 1) * p.channels + at.channel) * kWidth + n0;
-    const float* sums = ends + w.sums + entry * kSpans * p.channels + at.channel;
+    const float* spans = ends + w.spans + (entry * (shape.spans - 1) * p.channels + at.channel) * kWidth + n0;
+    const float* sums = ends + w.sums + entry * shape.spans * p.channels + at.channel;
     typedef float F4 __attribute__((ext_vector_type(4)));
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
     // s, x and e of a span: written by the lane that owns a position, read by the four of its channel, which are of one wavefront (no barrier)
     __shared__ F4 steps[kS][kScanChannels];
     __shared__ __attribute__((aligned(16))) float parts[kParts][kS * 2 * kWidth];   // sums over channels: [position][dB | dC][state]
 
-    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at), states_c(p, a.c, p.c_batch, p.c_row, at);
+    const ChunkStates<T, NS> states_b(p, a.b, p.b_batch, p.b_row, at, shape.chunk_rows), states_c(p, a.c, p.c_batch, p.c_row, at, shape.chunk_rows);
     const OwnColumn<T, kOwn> u(a.u, p.u_batch, p.u_row, p.channels, at, at.length), delta(a.delta, p.delta_batch, p.delta_row, p.channels, at, at.length);
     const OwnColumn<T, kOwn> dy(a.dy, p.y_batch, p.y_row, p.channels, at, at.length), z(GATE ? a.z : nullptr, p.z_batch, p.z_row, p.channels, at, at.length);
     const long long values = (long long)p.length * p.channels;
@@ -323,11 +325,12 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
         delta.load(span * kS, next_delta);
         dy.load(span * kS, next_dy);
         z.load(span * kS, next_z);
-        const int before = span ? span - 1 : 0;        // (the first span begins with the chunk's state, and reads another one)
-        Channels<float, NS>::load(spans + (size_t)before * p.channels * kWidth, next_state);
-        next_sum = sums[(size_t)before * p.channels];
+        if (span) {                                    // (the first span begins with the chunk's state)
+            Channels<float, NS>::load(spans + (size_t)(span - 1) * p.channels * kWidth, next_state);
+            next_sum = sums[(size_t)(span - 1) * p.channels];
+        }
     };
-    fetch(kSpans - 1);
+    fetch(shape.spans - 1);
     const float bias = a.delta_bias ? a.delta_bias[at.channel] : 0.0f, skip = a.d ? a.d[at.channel] : 0.0f;
     float decay[NS], h0[NS], carry[NS], d_a[NS];
     Channels<float, NS>::load(ends + row * kWidth + n0, h0);
@@ -339,13 +342,13 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
         carry[i] = at.there ? carry[i] : 0.0f;
         d_a[i] = 0.0f;
     }
-    states_b.store(tile_b, p.states, at);
-    states_c.store(tile_c, p.states, at);
+    states_b.store(tile_b, p.states, at, shape.chunk_rows);
+    states_c.store(tile_c, p.states, at, shape.chunk_rows);
     __syncthreads();
 
     float d_skip = 0.0f, d_bias = 0.0f;
 #pragma unroll 1
-    for (int span = kSpans - 1; span >= 0; --span) {
+    for (int span = shape.spans - 1; span >= 0; --span) {
         const int t_span = at.begin + span * kS;
         float state[kS + 1][NS], decayed[kS][NS];
         float own_s[kOwn], own_e[kOwn], own_u[kOwn], own_slope[kOwn], own_dz[kOwn];
@@ -482,7 +485,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
 // The first `state_blocks` workgroups: dB and dC, a lane an element.  The others: dA, dD and ddelta_bias, 16 columns x 16 shares of the
 // sequences and chunks a workgroup.
 template <typename T>
-__global__ __launch_bounds__(kScanThreads) void scan_sums_kernel(sys_selective_scan_t p, ScanArgs a, ScanShape shape, int width, unsigned state_blocks)
+__global__ __launch_bounds__(kScanThreads) void scan_sums_kernel(sys_selective_scan_t p, ScanArgs a, GradShape shape, int width, unsigned state_blocks)
 {
     const Workspace w = workspace_of(p, shape, width);
     if (blockIdx.x < state_blocks) {
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_sums_kernel(sys_selective_s
 template <typename T, int NS>
 hipError_t launch_states(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s)
 {
-    const ScanShape shape = backward_shape(p);
+    const GradShape shape = backward_shape(p);
     const long long blocks = (long long)shape.channel_blocks * shape.chunks * p.batch;
     const long long chains = ((long long)p.batch * p.channels * (4 * NS) + kScanThreads - 1) / kScanThreads;
     const long long state_blocks = (2LL * p.batch * p.length * p.groups * p.states + kScanThreads - 1) / kScanThreads;
