@@ -105,6 +105,24 @@ def test_long_sequences_in_chunks():
     _check_all(c, lengths)
 
 
+@pytest.mark.parametrize("case", [
+    # thousands of channels in few sequences
+    (1, 83, 3300, 16, BF16, 1, True, True, True, False, None),
+    (1, 81, 3211, 5, F32, 1, False, True, False, True, None),
+    (3, 70, 1100, 16, F32, 2, True, False, True, True, [70, 0, 33]),
+    (2, 66, 1650, 33, F16, 3, True, True, True, True, [17, 65]),
+    (1, 97, 3203, 17, BF16, 1, True, True, True, True, None),
+], ids=lambda c: "-".join(str(v) for v in c[:6]).replace("torch.", ""))
+def test_many_channels(case):
+    c = _make(sum(case[:4]), *case[:10], case[10])
+    args = dict(state=c["state"], lengths=case[10])
+    want, bound = R.scan(*_inputs(c), **args), R.scan(*_inputs(c), bound=True, **args)
+    y, state = _forward(c)
+    chain = (case[1] + 2) * (12 * want["sA"] + 6) * R.U
+    R.check(state, want["state"], chain * bound["state"], "state")
+    R.check(y, want["y"], (chain + (case[3] + 24) * R.U) * bound["y"], "y")
+
+
 def test_step_sizes_of_every_size():
     """softplus far out on both sides: results keep their relative accuracy where e^delta is all that is left."""
     delta = torch.tensor([-100.0, -80.0, -40.0, -20.0, -10.0, -5.0, -1e-4, 0.0, 1e-4, 1.0, 5.0, 15.0, 30.0, 80.0], device="cuda")[None, :, None].contiguous()
@@ -180,6 +198,23 @@ def test_offsets_beyond_32_bits():
     y = B.sys_selective_scan_update(*args, cache, *rest, softplus=True, d_slots=slots)
     assert torch.equal(y, B.sys_selective_scan_update(*args, small, *rest, softplus=True))
     assert torch.equal(cache[slots.long()], small)
+
+
+def test_rows_beyond_32_bits_and_the_widest_that_are_taken():
+    far = torch.empty(75 << 25, dtype=BF16, device="cuda")
+    for channels, states in ((70, 16), (3300, 5)):
+        c = _make(8, 1, 75, channels, states, BF16)
+        u = far.as_strided((1, 75, channels), (far.numel(), 1 << 25, 1))
+        u.copy_(c["u"])
+        assert torch.equal(_forward(dict(c, u=u))[0], _forward(c)[0])
+        grads, far_grads = (B.sys_selective_scan_backward(c["dy"], v, *_inputs(c)[1:], softplus=True) for v in (c["u"], u))
+        assert all(p is q is None or torch.equal(p, q) for p, q in zip(grads, far_grads))
+    c = _make(9, 1, 2, 70, 16, BF16)
+    u = far.as_strided((1, 2, 70), (far.numel(), (1 << 26) - 1, 1))
+    u.copy_(c["u"])
+    assert torch.equal(_forward(dict(c, u=u))[0], _forward(c)[0])
+    with pytest.raises(B.SysconvError):
+        _forward(dict(c, u=far.as_strided((1, 2, 70), (far.numel(), 1 << 26, 1))))
 
 
 def test_gradients_against_differences():
