@@ -9,6 +9,8 @@
 // value is taken off every other one, some differences at a time give their own mean and sum of squared distances, and
 // (count, mean, distances) are merged pairwise, n = n1 + n2, mean = mean1 + d n2/n, M2 = M2_1 + M2_2 + d^2 n1 n2/n with
 // d = mean2 - mean1 (the first value may be far from all others).
+#include <type_traits>
+
 #include "launch.h"
 #include "sequence.h"
 
@@ -30,16 +32,20 @@ __device__ __forceinline__ Moments merged(Moments a, Moments b)
 
 __device__ __forceinline__ Moments from_lane(Moments m, int k) { return {__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.m2, k)}; }
 
-__device__ __forceinline__ float activated(float v, int activation)
+template <int V, int ACTIVATION>
+__device__ __forceinline__ void activate(float (&v)[V])
 {
-    if (activation == SYS_ACT_SILU) return silu(v);
-    return activation == SYS_ACT_RELU ? (v > 0.0f ? v : v != v ? v : 0.0f) : v;
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = ACTIVATION == SYS_ACT_SILU ? silu(v[k]) : ACTIVATION == SYS_ACT_RELU && v[k] <= 0.0f ? 0.0f : v[k];   // (a NaN stays)
 }
 
-__device__ __forceinline__ float activated_grad(float v, int activation)
+// work(integral_constant) of the activation: one branch for a lane's rows (a branch for each value had taken 2 us of 35).
+template <typename F>
+__device__ __forceinline__ void by_activation(int activation, F&& work)
 {
-    if (activation == SYS_ACT_SILU) return silu_grad(v);
-    return activation == SYS_ACT_RELU ? (v > 0.0f ? 1.0f : 0.0f) : 1.0f;
+    if (activation == SYS_ACT_SILU) work(std::integral_constant<int, SYS_ACT_SILU>());
+    else if (activation == SYS_ACT_RELU) work(std::integral_constant<int, SYS_ACT_RELU>());
+    else work(std::integral_constant<int, SYS_ACT_NONE>());
 }
 
 // What is taken off a group's values: the first one of the batch entry.
@@ -49,14 +55,14 @@ __device__ __forceinline__ float group_first(const sys_group_norm_t& p, const T*
     return (float)x[(long long)group * (p.channels / p.groups)];
 }
 
-// The groups of V neighbouring channels, one division for all of them.
-template <int V>
-__device__ __forceinline__ void groups_of(int channel, int channels_a_group, int (&group)[V])
+// The groups of V neighbouring channels, one division for all of them; counted from `from` on.
+template <int V, typename Index>
+__device__ __forceinline__ void groups_of(int channel, int channels_a_group, Index from, Index (&group)[V])
 {
     int g = channel / channels_a_group, in_group = channel - g * channels_a_group;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        group[i] = g;
+        group[i] = from + g;
         const bool next = ++in_group == channels_a_group;
         g += next;
         in_group = next ? 0 : in_group;
@@ -105,19 +111,21 @@ struct ResidentLane {
     }
 };
 
-// Rows of a lane, `tall` apart; zeros, which are not used, past the last one.
+// Rows of a lane, `tall` apart; past the last one that row again, which is not used.  No load depends on a branch, so what is made of the
+// first rows need not wait for the last ones.
 template <typename T, int V, int ITEMS>
 struct ResidentRows {
     typename Channels<T, V>::Raw raw[ITEMS];
-    __device__ __forceinline__ void load(const T* from, long long row_stride, int rows, int row, int tall, int items)
+    __device__ __forceinline__ void load(const T* from, long long row_stride, int rows, int row, int tall)
     {
-        from += row * row_stride;
+        int r = row < rows ? row : rows - 1;
+        from += r * row_stride;
         const long long step = tall * row_stride;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            raw[i] = typename Channels<T, V>::Raw{};
-            if ((ITEMS == 1 || i < items) && row + i * tall < rows) raw[i] = Channels<T, V>::raw(from);
-            from += step;
+            raw[i] = Channels<T, V>::raw(from);
+            r += tall;
+            from += r < rows ? step : 0;
         }
     }
 };
@@ -142,35 +150,73 @@ __device__ __forceinline__ void forget(Raw& raw)
     }
 }
 
-// Adds up over the lanes of a unit that share a group: merge(l, r) of two values, in an order that depends on the shape alone.
-// Units of more than a wavefront go through LDS, [wavefront][group of the tile]; every wavefront of the workgroup has to come here.
-template <int ENTRIES, typename M, typename FromLane, typename Merge>
-__device__ __forceinline__ void over_unit(const ResidentShape& s, int tile_group, M (&m)[ENTRIES], M* shared, FromLane from, Merge merge)
+// v + v of lane ^ (1 << BIT).
+template <int BIT>
+__device__ __forceinline__ float add_lane(float v)
 {
-    for (int bit = 0; bit < s.log_unit && bit < 6; ++bit) {
-        if (bit >= s.log_group && bit < s.log_group + s.log_tile) continue;
-#pragma unroll
-        for (int e = 0; e < ENTRIES; ++e) m[e] = merge(m[e], from(m[e], 1 << bit));
-    }
-    if (s.log_unit <= 6) return;
-    const int waves = 1 << (s.log_unit - 6), first = (threadIdx.x >> s.log_unit) * waves;
-    const unsigned lane = threadIdx.x & 63;
-#pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) {
-        __syncthreads();                            // (what the sum before this one left has been read)
-        if (lane < (1u << (s.log_group + s.log_tile)) && (lane & ((1u << s.log_group) - 1)) == 0)
-            shared[((threadIdx.x >> 6) << s.log_tile) + tile_group] = m[e];
-        __syncthreads();
-        m[e] = shared[(first << s.log_tile) + tile_group];
-        for (int k = 1; k < waves; ++k) m[e] = merge(m[e], shared[((first + k) << s.log_tile) + tile_group]);
+    if constexpr (BIT == 0) return v + dpp<0xB1>(v);                    // quad_perm 1 0 3 2
+    else if constexpr (BIT == 1) return v + dpp<0x4E>(v);               // quad_perm 2 3 0 1
+    else if constexpr (BIT == 2) return v + dpp<0x1B>(dpp<0x141>(v));   // the half row mirrored, and every quad of it
+    else if constexpr (BIT == 3) return v + dpp<0x128>(v);              // the row turned by 8
+    else {
+        const unsigned u = __builtin_bit_cast(unsigned, v);
+        unsigned low, high;
+        if constexpr (BIT == 4) {
+            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+            low = r[0], high = r[1];
+        } else {
+            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            low = r[0], high = r[1];
+        }
+        return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
     }
 }
 
-constexpr int kMostTile = 32;                       // groups a tile, and entries of `shared` a wavefront
+// Sums over the lanes of a wavefront that share a unit and a group; every lane gets them.
+template <int N>
+__device__ __forceinline__ void sum_lanes(const ResidentShape& s, float (&v)[N])
+{
+    const int wide = s.log_group + s.log_tile;
+    auto add = [&](auto bit) {
+        constexpr int kBit = decltype(bit)::value;
+        if (kBit >= s.log_unit || (kBit >= s.log_group && kBit < wide)) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = add_lane<kBit>(v[i]);
+    };
+    add(std::integral_constant<int, 0>()), add(std::integral_constant<int, 1>()), add(std::integral_constant<int, 2>());
+    add(std::integral_constant<int, 3>()), add(std::integral_constant<int, 4>()), add(std::integral_constant<int, 5>());
+}
 
-// Moments of a lane's rows.
+constexpr int kMostTile = 32;                       // groups a tile
+
+// Units of more than a wavefront: what the wavefronts have goes through LDS, [entry][wavefront][group of the tile].  Every wavefront of the
+// workgroup has to come here.
+template <int ENTRIES, int MOST, typename M>
+__device__ __forceinline__ void put_wavefront(const ResidentShape& s, int tile_group, const M (&m)[ENTRIES], M (&shared)[ENTRIES][MOST])
+{
+    const unsigned lane = threadIdx.x & 63;
+    __syncthreads();                                // (what was here before has been read)
+    if (lane < (1u << (s.log_group + s.log_tile)) && (lane & ((1u << s.log_group) - 1)) == 0) {
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) shared[e][((threadIdx.x >> 6) << s.log_tile) + tile_group] = m[e];
+    }
+    __syncthreads();
+}
+
+// work(e, what a wavefront put there) for the wavefronts of the unit, in their order.
+template <int ENTRIES, int MOST, typename M, typename F>
+__device__ __forceinline__ void each_wavefront(const ResidentShape& s, int tile_group, const M (&shared)[ENTRIES][MOST], F&& work)
+{
+    const int waves = 1 << (s.log_unit - 6), first = (threadIdx.x >> s.log_unit) * waves;
+    for (int k = 0; k < waves; ++k) {
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) work(e, shared[e][((first + k) << s.log_tile) + tile_group]);
+    }
+}
+
+// Moments of a lane's rows: all of `items`, or all but the last one.
 template <typename T, int V, int ITEMS>
-__device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>& rows, float first, bool there, int count, int row, int tall, int items)
+__device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>& rows, float first, bool there, bool whole, int items)
 {
     Moments m = {0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -183,10 +229,12 @@ __device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>&
         const float mean = sum * (1.0f / V);
 #pragma unroll
         for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - first) - mean, (v[k] - first) - mean, square);
-        const bool on = there && row + i * tall < count;
-        const Moments own = {on ? (float)V : 0.0f, on ? mean : 0.0f, on ? square : 0.0f};
-        m = i == 0 ? own : merged(m, own);
+        const float on = i + 1 < items || whole ? 1.0f : 0.0f, d = mean - m.mean;
+        m.mean = i == 0 ? mean : __builtin_fmaf(d, on * (1.0f / (i + 1)), m.mean);
+        m.m2 = __builtin_fmaf(on, __builtin_fmaf(d * d, (float)V * i / (i + 1), square), m.m2);
     }
+    m.n = there ? (float)(V * (items - !whole)) : 0.0f;
+    if (m.n == 0.0f) m = {0.0f, 0.0f, 0.0f};
     return m;
 }
 
@@ -194,7 +242,7 @@ __device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>&
 template <typename T, int V, int ITEMS, int ENTRIES>
 __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
 {
-    __shared__ Moments shared[16 * kMostTile];
+    __shared__ Moments shared[ENTRIES][16 * kMostTile];
     const ResidentLane at(p, s, s.units, xcd_place(blockIdx.x, gridDim.x));
     const int b0 = at.unit / s.tiles * ENTRIES;
     ResidentRows<T, V, ITEMS> rows[ENTRIES];
@@ -202,19 +250,48 @@ __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p,
 #pragma unroll
     for (int e = 0; e < ENTRIES; ++e) {
         const T* x = (const T*)a.x + (b0 + e < p.batch ? b0 + e : p.batch - 1) * p.x_batch;
-        rows[e].load(x + at.channel, p.x_row, (int)p.rows, at.row, at.tall, s.items);
+        rows[e].load(x + at.channel, p.x_row, (int)p.rows, at.row, at.tall);
         first[e] = group_first<T>(p, x, at.group);
     }
     float w[V], shift[V];
     load_affine<T, V>(p, a, at.channel, w, shift);
+    const bool whole = at.row + (s.items - 1) * at.tall < (int)p.rows;
     Moments m[ENTRIES];
 #pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) m[e] = lane_moments<T, V, ITEMS>(rows[e], first[e], at.there, (int)p.rows, at.row, at.tall, s.items);
-    over_unit<ENTRIES>(s, at.tile_group, m, shared, [](Moments v, int k) { return from_lane(v, k); }, [](Moments l, Moments r) { return merged(l, r); });
+    for (int e = 0; e < ENTRIES; ++e) m[e] = lane_moments<T, V, ITEMS>(rows[e], first[e], at.there, whole, s.items);
+    // the mean of several means and the sum of squared distances from it, first over the lanes, then over the wavefronts
+    float n[1] = {m[0].n}, mean_of[ENTRIES], m2_of[ENTRIES];
+    sum_lanes(s, n);
+    const float share = n[0] > 0.0f ? 1.0f / n[0] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < ENTRIES; ++e) mean_of[e] = m[e].n * m[e].mean;
+    sum_lanes(s, mean_of);
+#pragma unroll
+    for (int e = 0; e < ENTRIES; ++e) {
+        mean_of[e] *= share;
+        const float d = m[e].mean - mean_of[e];
+        m2_of[e] = __builtin_fmaf(m[e].n * d, d, m[e].m2);
+    }
+    sum_lanes(s, m2_of);
+#pragma unroll
+    for (int e = 0; e < ENTRIES; ++e) m[e] = {n[0], mean_of[e], m2_of[e]};
+    const float all = (float)p.rows * (float)(p.channels / p.groups);
+    if (s.log_unit > 6) {
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) mean_of[e] = m2_of[e] = 0.0f;
+        put_wavefront(s, at.tile_group, m, shared);
+        each_wavefront(s, at.tile_group, shared, [&](int e, const Moments& o) { mean_of[e] = __builtin_fmaf(o.n, o.mean, mean_of[e]); });
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) mean_of[e] *= 1.0f / all;
+        each_wavefront(s, at.tile_group, shared, [&](int e, const Moments& o) {
+            const float d = o.mean - mean_of[e];
+            m2_of[e] += __builtin_fmaf(o.n * d, d, o.m2);
+        });
+    }
 #pragma unroll
     for (int e = 0; e < ENTRIES; ++e) {
         if (!at.there || b0 + e >= p.batch) continue;
-        const float mean = m[e].mean + first[e], rstd = 1.0f / __builtin_sqrtf(m[e].m2 / m[e].n + p.eps);
+        const float mean = mean_of[e] + first[e], rstd = 1.0f / __builtin_sqrtf(m2_of[e] / all + p.eps);
         if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
             const size_t group = (size_t)(b0 + e) * p.groups + at.group;
             if (a.mean) a.mean[group] = mean;
@@ -225,21 +302,26 @@ __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p,
         float scale[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) scale[k] = w[k] * rstd;
+        by_activation(p.activation, [&](auto activation) {
+            int items = s.items;
+            T* to = y;
+            // (else the rows' addresses are made all at once, and the comparisons kept from the loop above, in registers that are not there)
+            if (ITEMS > 1) asm volatile("" : "+s"(items), "+v"(to));
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            if (ITEMS > 1 && i >= s.items) continue;
-            if (at.row + i * at.tall >= (int)p.rows) continue;
-            float v[V];
-            if (ITEMS > 1) forget(rows[e].raw[i]);
-            Channels<T, V>::values(rows[e].raw[i], v);
+            for (int i = 0; i < ITEMS; ++i) {
+                if (ITEMS > 1 && i >= items) continue;
+                if (i + 1 == items && !whole) continue;
+                float v[V];
+                if (ITEMS > 1) forget(rows[e].raw[i]);
+                Channels<T, V>::values(rows[e].raw[i], v);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf(v[k] - mean, scale[k], shift[k]);
-            if (p.activation != SYS_ACT_NONE) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = activated(v[k], p.activation);
+                for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf(v[k] - mean, scale[k], shift[k]);
+                activate<V, decltype(activation)::value>(v);
+                Channels<T, V>::store_nt(to, v);
+                to += step;
+                if (ITEMS > 1) asm volatile("" : "+v"(to));
             }
-            Channels<T, V>::store_nt(y + i * step, v);
-        }
+        });
     }
 }
 
@@ -250,19 +332,21 @@ struct Pair {
     float a, b;
 };
 
-// f and hat of V channels of a row, whose statistics are the channels' own or one group's.
-__device__ __forceinline__ float pick(const float* v, int k) { return v[k]; }
-__device__ __forceinline__ float pick(float v, int) { return v; }
+template <int ACTIVATION>
+__device__ __forceinline__ float activation_grad(float v)
+{
+    return ACTIVATION == SYS_ACT_SILU ? silu_grad(v) : ACTIVATION == SYS_ACT_RELU ? (v > 0.0f ? 1.0f : 0.0f) : 1.0f;
+}
 
-template <int V, typename Statistic>
-__device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[V], const Statistic& mean, const Statistic& rstd, const float (&w)[V], const float (&shift)[V], int activation,
-                                         float (&f)[V], float (&hat)[V])
+// f and hat of V channels of a row.
+template <int V, int ACTIVATION>
+__device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[V], float mean, float rstd, const float (&w)[V], const float (&shift)[V], float (&f)[V], float (&hat)[V])
 {
 #pragma unroll
-    for (int k = 0; k < V; ++k) hat[k] = (x[k] - pick(mean, k)) * pick(rstd, k), f[k] = dy[k];
-    if (activation == SYS_ACT_NONE) return;
-#pragma unroll
-    for (int k = 0; k < V; ++k) f[k] *= activated_grad(__builtin_fmaf(hat[k], w[k], shift[k]), activation);
+    for (int k = 0; k < V; ++k) {
+        hat[k] = (x[k] - mean) * rstd;
+        f[k] = dy[k] * activation_grad<ACTIVATION>(__builtin_fmaf(hat[k], w[k], shift[k]));
+    }
 }
 
 // A unit goes through the batch entries of its slice, ENTRIES at a time, and adds up dw and db of its channels: [slice][f | f hat][channel] in the
@@ -270,7 +354,7 @@ __device__ __forceinline__ void row_grad(const float (&x)[V], const float (&dy)[
 template <typename T, int V, int ITEMS, int ENTRIES>
 __global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
 {
-    __shared__ Pair shared[8 * kMostTile];
+    __shared__ Pair shared[ENTRIES][8 * kMostTile];
     __shared__ float sums[512];
     const ResidentLane at(p, s, s.units, xcd_place(blockIdx.x, gridDim.x));
     const int slice = at.unit / s.tiles;
@@ -280,6 +364,7 @@ __global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_
 #pragma unroll
     for (int k = 0; k < V; ++k) f_sum[k] = hat_sum[k] = 0.0f;
     const float share = 1.0f / ((float)p.rows * (float)(p.channels / p.groups));
+    const bool whole = at.row + (s.items - 1) * at.tall < (int)p.rows;
     // as many rounds for every unit, so that all wavefronts of a workgroup meet at its barriers
     for (int round = 0; round < s.rounds; ++round) {
         const int b0 = (round * s.slices + slice) * ENTRIES;
@@ -288,57 +373,69 @@ __global__ __launch_bounds__(512) void norm_grad_resident_kernel(sys_group_norm_
 #pragma unroll
         for (int e = 0; e < ENTRIES; ++e) {
             const int b = b0 + e < p.batch ? b0 + e : p.batch - 1;
-            rows_x[e].load(x + b * p.x_batch, p.x_row, (int)p.rows, at.row, at.tall, s.items);
-            rows_dy[e].load(dy + b * p.y_batch, p.y_row, (int)p.rows, at.row, at.tall, s.items);
+            rows_x[e].load(x + b * p.x_batch, p.x_row, (int)p.rows, at.row, at.tall);
+            rows_dy[e].load(dy + b * p.y_batch, p.y_row, (int)p.rows, at.row, at.tall);
             mean[e] = a.mean_in[(size_t)b * p.groups + at.group];
             rstd[e] = a.rstd_in[(size_t)b * p.groups + at.group];
         }
-        Pair m[ENTRIES];
+        float m[2 * ENTRIES];                       // sums of f w and of f w hat
 #pragma unroll
-        for (int e = 0; e < ENTRIES; ++e) {
-            m[e] = {0.0f, 0.0f};
+        for (int e = 0; e < 2 * ENTRIES; ++e) m[e] = 0.0f;
+        by_activation(p.activation, [&](auto activation) {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                if (ITEMS > 1 && i >= s.items) continue;
-                float v[V], g[V], f[V], hat[V];
-                Channels<T, V>::values(rows_x[e].raw[i], v);
-                Channels<T, V>::values(rows_dy[e].raw[i], g);
-                row_grad<V>(v, g, mean[e], rstd[e], w, shift, p.activation, f, hat);
-                if (at.there && b0 + e < p.batch && at.row + i * at.tall < (int)p.rows) {
+            for (int e = 0; e < ENTRIES; ++e) {
+                const bool there = at.there && b0 + e < p.batch;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        f_sum[k] += f[k];
-                        hat_sum[k] = __builtin_fmaf(f[k], hat[k], hat_sum[k]);
-                        m[e].a = __builtin_fmaf(f[k], w[k], m[e].a);
-                        m[e].b = __builtin_fmaf(f[k] * w[k], hat[k], m[e].b);
+                for (int i = 0; i < ITEMS; ++i) {
+                    if (ITEMS > 1 && i >= s.items) continue;
+                    float v[V], g[V], f[V], hat[V];
+                    Channels<T, V>::values(rows_x[e].raw[i], v);
+                    Channels<T, V>::values(rows_dy[e].raw[i], g);
+                    row_grad<V, decltype(activation)::value>(v, g, mean[e], rstd[e], w, shift, f, hat);
+                    if (there && (i + 1 < s.items || whole)) {
+#pragma unroll
+                        for (int k = 0; k < V; ++k) {
+                            f_sum[k] += f[k];
+                            hat_sum[k] = __builtin_fmaf(f[k], hat[k], hat_sum[k]);
+                            m[2 * e] = __builtin_fmaf(f[k], w[k], m[2 * e]);
+                            m[2 * e + 1] = __builtin_fmaf(f[k] * w[k], hat[k], m[2 * e + 1]);
+                        }
                     }
                 }
             }
+        });
+        sum_lanes(s, m);
+        if (s.log_unit > 6) {
+            Pair pair[ENTRIES];
+#pragma unroll
+            for (int e = 0; e < ENTRIES; ++e) pair[e] = {m[2 * e], m[2 * e + 1]}, m[2 * e] = m[2 * e + 1] = 0.0f;
+            put_wavefront(s, at.tile_group, pair, shared);
+            each_wavefront(s, at.tile_group, shared, [&](int e, const Pair& o) { m[2 * e] += o.a, m[2 * e + 1] += o.b; });
         }
-        over_unit<ENTRIES>(s, at.tile_group, m, shared, [](Pair v, int k) { return Pair{__shfl_xor(v.a, k), __shfl_xor(v.b, k)}; },
-                           [](Pair l, Pair r) { return Pair{l.a + r.a, l.b + r.b}; });
 #pragma unroll
         for (int e = 0; e < ENTRIES; ++e) {
             if (!at.there || b0 + e >= p.batch) continue;
-            const float m1 = m[e].a * share, m2 = m[e].b * share;
+            const float m1 = m[2 * e] * share, m2 = m[2 * e + 1] * share;
             T* dx = (T*)a.dx + ((size_t)(b0 + e) * p.rows + at.row) * p.channels + at.channel;
             const long long step = (long long)at.tall * p.channels;
+            by_activation(p.activation, [&](auto activation) {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                if (ITEMS > 1 && i >= s.items) continue;
-                if (at.row + i * at.tall >= (int)p.rows) continue;
-                float v[V], g[V], f[V], hat[V];
-                if (ITEMS * ENTRIES > 1) {
-                    forget(rows_x[e].raw[i]);
-                    forget(rows_dy[e].raw[i]);
+                for (int i = 0; i < ITEMS; ++i) {
+                    if (ITEMS > 1 && i >= s.items) continue;
+                    if (i + 1 == s.items && !whole) continue;
+                    float v[V], g[V], f[V], hat[V];
+                    if (ITEMS * ENTRIES > 1) {
+                        forget(rows_x[e].raw[i]);
+                        forget(rows_dy[e].raw[i]);
+                    }
+                    Channels<T, V>::values(rows_x[e].raw[i], v);
+                    Channels<T, V>::values(rows_dy[e].raw[i], g);
+                    row_grad<V, decltype(activation)::value>(v, g, mean[e], rstd[e], w, shift, f, hat);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) v[k] = rstd[e] * (__builtin_fmaf(f[k], w[k], -m1) - hat[k] * m2);
+                    Channels<T, V>::store_nt(dx + i * step, v);
                 }
-                Channels<T, V>::values(rows_x[e].raw[i], v);
-                Channels<T, V>::values(rows_dy[e].raw[i], g);
-                row_grad<V>(v, g, mean[e], rstd[e], w, shift, p.activation, f, hat);
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = rstd[e] * (__builtin_fmaf(f[k], w[k], -m1) - hat[k] * m2);
-                Channels<T, V>::store_nt(dx + i * step, v);
-            }
+            });
         }
     }
     if (!a.dw && !a.db) return;
@@ -406,7 +503,7 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
         const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
         float n = 0.0f, mean[V], m2[V], first[V];
         int group[V];
-        groups_of<V>(channel, channels, group);
+        groups_of<V>(channel, channels, 0, group);
 #pragma unroll
         for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f, first[i] = group_first<T>(p, x, group[i]);
         if (there) {
@@ -541,34 +638,33 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(sys_group_norm_t p
         float mean[V], scale[V], shift[V];
         load_affine<T, V>(p, a, channel, scale, shift);
         int group[V];
-        groups_of<V>(channel, channels, group);
+        groups_of<V>(channel, channels, 0, group);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             mean[i] = statistics[2 * group[i]];
             scale[i] *= statistics[2 * group[i] + 1];
         }
-        for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
-            typename Channels<T, V>::Raw raw[kNormRows];
+        by_activation(p.activation, [&](auto activation) {
+            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
+                typename Channels<T, V>::Raw raw[kNormRows];
 #pragma unroll
-            for (int k = 0; k < kNormRows; ++k) {
-                const long long row = r + (long long)k * at.tall;
-                raw[k] = Channels<T, V>::raw(x + (row < end ? row : r) * p.x_row);
-            }
-#pragma unroll
-            for (int k = 0; k < kNormRows; ++k) {
-                const long long row = r + (long long)k * at.tall;
-                if (row >= end) break;
-                float v[V];
-                Channels<T, V>::values(raw[k], v);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(v[i] - mean[i], scale[i], shift[i]);
-                if (p.activation != SYS_ACT_NONE) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] = activated(v[i], p.activation);
+                for (int k = 0; k < kNormRows; ++k) {
+                    const long long row = r + (long long)k * at.tall;
+                    raw[k] = Channels<T, V>::raw(x + (row < end ? row : r) * p.x_row);
                 }
-                Channels<T, V>::store_nt(y + row * p.y_row, v);
+#pragma unroll
+                for (int k = 0; k < kNormRows; ++k) {
+                    const long long row = r + (long long)k * at.tall;
+                    if (row >= end) continue;
+                    float v[V];
+                    Channels<T, V>::values(raw[k], v);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(v[i] - mean[i], scale[i], shift[i]);
+                    activate<V, decltype(activation)::value>(v);
+                    Channels<T, V>::store_nt(y + row * p.y_row, v);
+                }
             }
-        }
+        });
     }
 }
 
@@ -591,19 +687,46 @@ __host__ __device__ GradSpace grad_space(const sys_group_norm_t& p, const NormSh
 
 constexpr int kGradRows = 4;       // rows of x and of dy on their way together
 
-// Constants of a lane's channels in the gradients.
+// Those rows; past the end the first one again.
+template <typename T, int V>
+struct GradRows {
+    typename Channels<T, V>::Raw x[kGradRows], dy[kGradRows];
+    __device__ __forceinline__ void load(const sys_group_norm_t& p, const T* from_x, const T* from_dy, long long r, int tall, long long end)
+    {
+#pragma unroll
+        for (int k = 0; k < kGradRows; ++k) {
+            const long long row = r + (long long)k * tall < end ? r + (long long)k * tall : r;
+            x[k] = Channels<T, V>::raw(from_x + row * p.x_row);
+            dy[k] = Channels<T, V>::raw(from_dy + row * p.y_row);
+        }
+    }
+};
+
+// Constants of a lane's channels in the gradients: hat = (x - mean) rstd is not formed, the activation's argument is (x - mean) scale + shift with
+// scale = rstd w.
 template <typename T, int V>
 struct GradLane {
-    float mean[V], rstd[V], w[V], shift[V];
-    int group[V];
-    __device__ __forceinline__ GradLane(const sys_group_norm_t& p, const NormArgs& a, int b, int channel)
+    float mean[V], scale[V], shift[V];
+    __device__ __forceinline__ GradLane(const sys_group_norm_t& p, const NormArgs& a, const size_t (&group)[V], int channel)
     {
-        load_affine<T, V>(p, a, channel, w, shift);
-        groups_of<V>(channel, p.channels / p.groups, group);
+        load_affine<T, V>(p, a, channel, scale, shift);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            mean[i] = a.mean_in[(size_t)b * p.groups + group[i]];
-            rstd[i] = a.rstd_in[(size_t)b * p.groups + group[i]];
+            mean[i] = a.mean_in[group[i]];
+            scale[i] *= a.rstd_in[group[i]];
+        }
+    }
+    // f and x - mean of a row
+    template <int ACTIVATION, typename Raw>
+    __device__ __forceinline__ void row(Raw x, Raw dy, float (&f)[V], float (&away)[V]) const
+    {
+        forget(x), forget(dy);
+        Channels<T, V>::values(x, away);
+        Channels<T, V>::values(dy, f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            away[i] -= mean[i];
+            f[i] *= activation_grad<ACTIVATION>(__builtin_fmaf(away[i], scale[i], shift[i]));
         }
     }
 };
@@ -624,31 +747,30 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sums_kernel(sys_group_norm
 #pragma unroll
         for (int i = 0; i < V; ++i) f_sum[i] = hat_sum[i] = 0.0f;
         if (there) {
-            const GradLane<T, V> lane(p, a, b, channel);
+            size_t group[V];
+            groups_of<V>(channel, p.channels / p.groups, (size_t)b * p.groups, group);
             const T* x = (const T*)a.x + b * p.x_batch + channel;
             const T* dy = (const T*)a.dy + b * p.y_batch + channel;
-            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
-                typename Channels<T, V>::Raw raw_x[kGradRows], raw_dy[kGradRows];
+            GradRows<T, V> rows;
+            const GradLane<T, V> lane(p, a, group, channel);
+            by_activation(p.activation, [&](auto activation) {
+                for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
+                    rows.load(p, x, dy, r, at.tall, end);
 #pragma unroll
-                for (int k = 0; k < kGradRows; ++k) {
-                    const long long row = r + (long long)k * at.tall < end ? r + (long long)k * at.tall : r;
-                    raw_x[k] = Channels<T, V>::raw(x + row * p.x_row);
-                    raw_dy[k] = Channels<T, V>::raw(dy + row * p.y_row);
-                }
+                    for (int k = 0; k < kGradRows; ++k) {
+                        if (r + (long long)k * at.tall >= end) continue;
+                        float f[V], away[V];
+                        lane.template row<decltype(activation)::value>(rows.x[k], rows.dy[k], f, away);
 #pragma unroll
-                for (int k = 0; k < kGradRows; ++k) {
-                    if (r + (long long)k * at.tall >= end) break;
-                    float v[V], g[V], f[V], hat[V];
-                    Channels<T, V>::values(raw_x[k], v);
-                    Channels<T, V>::values(raw_dy[k], g);
-                    row_grad<V>(v, g, lane.mean, lane.rstd, lane.w, lane.shift, p.activation, f, hat);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        f_sum[i] += f[i];
-                        hat_sum[i] = __builtin_fmaf(f[i], hat[i], hat_sum[i]);
+                        for (int i = 0; i < V; ++i) {
+                            f_sum[i] += f[i];
+                            hat_sum[i] = __builtin_fmaf(f[i], away[i], hat_sum[i]);
+                        }
                     }
                 }
-            }
+            });
+#pragma unroll
+            for (int i = 0; i < V; ++i) hat_sum[i] *= a.rstd_in[group[i]];
         }
         for (int which = 0; which < 2; ++which) {
             __syncthreads();
@@ -751,40 +873,38 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(sys_group_nor
     const Lanes at(shape.columns);
     if (!at.there) return;
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
-    const float* means = a.workspace + grad_space(p, shape).means + 2 * (size_t)b * p.groups;
+    const float* means = a.workspace + grad_space(p, shape).means;
     for (int column = at.column; column < shape.columns; column += at.wide) {
         const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
         const T* x = (const T*)a.x + b * p.x_batch + channel;
         const T* dy = (const T*)a.dy + b * p.y_batch + channel;
         T* dx = (T*)a.dx + (size_t)b * p.rows * p.channels + channel;
-        const GradLane<T, V> lane(p, a, b, channel);
-        float m1[V], m2[V];
+        GradRows<T, V> rows;
+        size_t group[V];
+        groups_of<V>(channel, p.channels / p.groups, (size_t)b * p.groups, group);
+        const GradLane<T, V> lane(p, a, group, channel);
+        float rstd[V], m1[V], m2[V];                // (rstd^2 m2 may pass what fp32 holds where dx does not)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            m1[i] = means[2 * lane.group[i]];
-            m2[i] = means[2 * lane.group[i] + 1];
+            rstd[i] = a.rstd_in[group[i]];
+            m1[i] = means[2 * group[i]];
+            m2[i] = means[2 * group[i] + 1] * rstd[i];
         }
-        for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
-            typename Channels<T, V>::Raw raw_x[kGradRows], raw_dy[kGradRows];
+        by_activation(p.activation, [&](auto activation) {
+            for (long long r = begin + at.row; r < end; r += (long long)at.tall * kGradRows) {
+                rows.load(p, x, dy, r, at.tall, end);
 #pragma unroll
-            for (int k = 0; k < kGradRows; ++k) {
-                const long long row = r + (long long)k * at.tall < end ? r + (long long)k * at.tall : r;
-                raw_x[k] = Channels<T, V>::raw(x + row * p.x_row);
-                raw_dy[k] = Channels<T, V>::raw(dy + row * p.y_row);
+                for (int k = 0; k < kGradRows; ++k) {
+                    const long long row = r + (long long)k * at.tall;
+                    if (row >= end) continue;
+                    float f[V], away[V];
+                    lane.template row<decltype(activation)::value>(rows.x[k], rows.dy[k], f, away);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) f[i] = __builtin_fmaf(f[i], lane.scale[i], rstd[i] * __builtin_fmaf(away[i], -m2[i], -m1[i]));
+                    Channels<T, V>::store_nt(dx + row * p.channels, f);
+                }
             }
-#pragma unroll
-            for (int k = 0; k < kGradRows; ++k) {
-                const long long row = r + (long long)k * at.tall;
-                if (row >= end) break;
-                float v[V], g[V], f[V], hat[V];
-                Channels<T, V>::values(raw_x[k], v);
-                Channels<T, V>::values(raw_dy[k], g);
-                row_grad<V>(v, g, lane.mean, lane.rstd, lane.w, lane.shift, p.activation, f, hat);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = lane.rstd[i] * (__builtin_fmaf(f[i], lane.w[i], -m1[i]) - hat[i] * m2[i]);
-                Channels<T, V>::store_nt(dx + row * p.channels, v);
-            }
-        }
+        });
     }
 }
 
@@ -808,13 +928,7 @@ int log2_up(long long n)
 }
 
 // Rows of a lane that are held: at most 64 registers for x, 32 each for x and dy.
-template <typename T, int V, bool GRAD>
-constexpr int kMostItems = V * (int)sizeof(T) > 8 ? (GRAD ? 8 : 16) : (GRAD ? 16 : 32);
-
-int most_items(const sys_group_norm_t& p, int v, bool grad)
-{
-    return v * (p.dtype == SYS_F32 ? 4 : 2) > 8 ? (grad ? 8 : 16) : (grad ? 16 : 32);
-}
+constexpr int most_items(int bytes, bool grad) { return (bytes > 8 ? 16 : 32) >> grad; }
 
 // Whether a call's rows stay in registers, and how they lie there.
 bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
@@ -828,7 +942,7 @@ bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
     // a part of a row of at least 64 bytes, where the unit is more than a wavefront
     s.log_tile = 0;
     const long long lanes = p.rows << s.log_group;
-    const int most = most_items(p, v, grad);
+    const int most = most_items(v * element, grad);
     if (lanes > 64) {
         while (s.log_group + s.log_tile < 6 && s.log_tile < 5 && (p.channels / p.groups * element << s.log_tile) < 64 && (1 << s.log_tile) < p.groups) ++s.log_tile;
     }
@@ -901,7 +1015,10 @@ hipError_t launch_items(bool grad, const sys_group_norm_t& p, const NormArgs& a,
     if (s.entries > 1) return grad ? launch_grad_resident<T, V, 1, 4>(p, a, s, stream) : launch_resident<T, V, 1, 4>(p, a, s, stream);
     if (s.items == 1) return grad ? launch_grad_resident<T, V, 1, 1>(p, a, s, stream) : launch_resident<T, V, 1, 1>(p, a, s, stream);
     if (s.items <= 4) return grad ? launch_grad_resident<T, V, 4, 1>(p, a, s, stream) : launch_resident<T, V, 4, 1>(p, a, s, stream);
-    return grad ? launch_grad_resident<T, V, kMostItems<T, V, true>, 1>(p, a, s, stream) : launch_resident<T, V, kMostItems<T, V, false>, 1>(p, a, s, stream);
+    if (s.items <= 8) return grad ? launch_grad_resident<T, V, 8, 1>(p, a, s, stream) : launch_resident<T, V, 8, 1>(p, a, s, stream);
+    if (s.items <= 16 && !grad) return launch_resident<T, V, 16, 1>(p, a, s, stream);
+    if constexpr (most_items(V * (int)sizeof(T), false) > 16) return grad ? launch_grad_resident<T, V, 16, 1>(p, a, s, stream) : launch_resident<T, V, 32, 1>(p, a, s, stream);
+    return hipErrorInvalidValue;                           // (resident_shape has no such shape)
 }
 
 template <typename T, int V>
