@@ -5,6 +5,8 @@
 //
 // All three are bound by memory: K <= 8 multiply-adds an element beside 4 to 12 bytes.  A lane owns 16 bytes of neighbouring channels
 // and walks down the rows, so every load and store of a wavefront is a contiguous piece of a row and the taps stay in registers.
+#include <type_traits>
+
 #include "launch.h"
 #include "sequence.h"
 
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void causal_conv_kernel(sys_causal_conv1d
 
 constexpr int kRun = 32;           // rows a lane in the backward kernel
 constexpr int kRunWaves = 4;       // runs a workgroup: a wavefront each, whose sums for the taps are added in LDS
-constexpr int kAhead = 4;          // rows whose loads are in flight while as many are worked on
+constexpr int kAhead = 2;          // rows whose loads are in flight while as many are worked on (4: 55 us, its registers leave three wavefronts a SIMD)
 
 // What a lane of the backward kernel carries down the rows.  In rows e of state ++ x, e = 0 .. len+K-2: dext[e] = sum_j w[j] dpre[e-j]
 // (dpre is 0 outside 0 .. len-1), plus the gradient of the state behind the sequence in its last K-1 rows; the first K-1 rows are the
@@ -140,7 +142,6 @@ struct GradWindow {
     float tap[K][V], bias[V];
     float rows[K][V], dpre[K][V];      // rows e .. e+K-1; dpre[e-(K-1)] .. dpre[e]
     float sums[K + 1][V];              // of the taps and the bias
-    bool silu_there;
 
     // the windows move on by a row: next is row e+K-1 of state ++ x
     __device__ __forceinline__ void move(typename Channels<T, V>::Raw next)
@@ -151,10 +152,11 @@ struct GradWindow {
             for (int i = 0; i < V; ++i) rows[j][i] = rows[j + 1][i], dpre[j][i] = dpre[j + 1][i];
         Channels<T, V>::values(next, rows[K - 1]);
     }
+    template <bool SILU>
     __device__ __forceinline__ void differentiate(typename Channels<T, V>::Raw dy)
     {
         Channels<T, V>::values(dy, dpre[K - 1]);
-        if (!silu_there) return;
+        if (!SILU) return;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float pre = bias[i];
@@ -190,7 +192,7 @@ struct GradWindow {
 
 // Rows begin .. end-1 of dext.  WHOLE: every row of x and dy that they need exists, and none is a state's; else each is asked for (the
 // same for all lanes of a wavefront).  Either way kAhead rows are in flight while as many are worked on.
-template <typename T, int K, int V, bool WHOLE>
+template <typename T, int K, int V, bool WHOLE, bool SILU>
 __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const CausalConvArgs& a, GradWindow<T, K, V>& w, const T* x, const T* dy, const T* state,
                                          int b, int c0, int len, int begin, int end)
 {
@@ -216,7 +218,7 @@ __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const Cau
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
         w.move(more[j]);
-        if (WHOLE || begin - (K - 1) + j >= 0) w.differentiate(more_dy[j]);      // (zeros where there is no dy)
+        if (WHOLE || begin - (K - 1) + j >= 0) w.template differentiate<SILU>(more_dy[j]);      // (zeros where there is no dy)
         else w.nothing();
     }
     for (int e0 = begin; e0 < end; e0 += kAhead) {
@@ -232,7 +234,7 @@ __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const Cau
             w.move(now[k]);
             float out[V];
             if (WHOLE || (e >= 0 && e < len)) {
-                w.differentiate(now_dy[k]);
+                w.template differentiate<SILU>(now_dy[k]);
                 w.add();               // (0 * a row that holds a NaN would be one)
             } else {
                 w.nothing();
@@ -281,15 +283,19 @@ __global__ __launch_bounds__(kRunWaves * 64) void causal_conv_grad_kernel(sys_ca
     if (there) {
         load_taps<T, K, V>(p, a.w, c0, w.tap);
         load_bias<T, V>(p, a.bias, c0, w.bias);
-        w.silu_there = p.activation == SYS_ACT_SILU;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) w.dpre[j][i] = w.rows[j][i] = 0.0f;
         // the last run goes on through the K-1 rows behind the sequence
         const int begin = run * kRun;
-        if (begin >= 2 * (K - 1) && begin + kRun <= len && run != runs - 1) grad_run<T, K, V, true>(p, a, w, x, dy, state, b, c0, len, begin, begin + kRun);
-        else grad_run<T, K, V, false>(p, a, w, x, dy, state, b, c0, len, begin, run == runs - 1 ? p.length + K - 1 : begin + kRun);
+        auto go = [&](auto silu_there) {
+            constexpr bool kSilu = decltype(silu_there)::value;
+            if (begin >= 2 * (K - 1) && begin + kRun <= len && run != runs - 1) grad_run<T, K, V, true, kSilu>(p, a, w, x, dy, state, b, c0, len, begin, begin + kRun);
+            else grad_run<T, K, V, false, kSilu>(p, a, w, x, dy, state, b, c0, len, begin, run == runs - 1 ? p.length + K - 1 : begin + kRun);
+        };
+        if (p.activation == SYS_ACT_SILU) go(std::true_type());
+        else go(std::false_type());
     }
 
     // the workgroup's sums, [K+1][channels] a workgroup
