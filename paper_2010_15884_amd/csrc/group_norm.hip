@@ -939,12 +939,16 @@ bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
     s.log_group = log2_up(s.columns_a_group);
     const int most_log = grad ? 9 : 10;                    // 512 lanes leave 256 registers, 1024 leave 128
     if (s.log_group > most_log) return false;
-    // a part of a row of at least 64 bytes, where the unit is more than a wavefront
+    // Where the unit is more than a wavefront, a part of a row of at least 64 bytes (16 x 4096 x 512 in 32 groups, bf16, 32 / 64 / 128 bytes: 59 / 31 /
+    // 47 us) -- but not at the price of more than 16 rows a lane while there are few units (4 and 8 x 1024 x 320 in 32 groups: 12.5 and 12.7 us
+    // with 80 bytes, 9.2 and 9.7 with 40; 16 x 1024 x 320: 13.7 and 15.2).
     s.log_tile = 0;
     const long long lanes = p.rows << s.log_group;
     const int most = most_items(v * element, grad);
     if (lanes > 64) {
-        while (s.log_group + s.log_tile < 6 && s.log_tile < 5 && (p.channels / p.groups * element << s.log_tile) < 64 && (1 << s.log_tile) < p.groups) ++s.log_tile;
+        while (s.log_group + s.log_tile < 6 && s.log_tile < 5 && (p.channels / p.groups * element << s.log_tile) < 64 && (1 << s.log_tile) < p.groups
+               && (p.rows <= 16LL << (most_log - s.log_group - s.log_tile - 1) || (long long)p.batch * p.groups >> (s.log_tile + 1) >= 128))
+            ++s.log_tile;
     }
     const int wide = s.log_group + s.log_tile;
     // up to four rows a lane, then the whole workgroup, then as many rows as there are registers for
@@ -952,7 +956,8 @@ bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
     if (s.log_unit > most_log) s.log_unit = most_log;
     const long long tall = 1LL << (s.log_unit - wide);
     const long long items = (p.rows + tall - 1) / tall;
-    if (items > most) return false;
+    const bool thin = lanes > 64 && (1 << s.log_tile) < p.groups && (p.channels / p.groups * element << s.log_tile) < 64;
+    if (items > (thin && most > 16 ? 16 : most)) return false;     // (4 x 4096 x 320 in 32 groups, 32 rows a lane: 29 us, in chunks 17)
     s.items = (int)items;
     s.tiles = (p.groups + (1 << s.log_tile) - 1) >> s.log_tile;
     s.threads = s.log_unit > 8 ? 1 << s.log_unit : kThreads;

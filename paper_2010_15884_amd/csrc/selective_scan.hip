@@ -223,8 +223,9 @@ ScanShape forward_shape(const sys_selective_scan_t& p, bool ragged)
     const long long workgroups = (long long)s.channel_blocks * p.batch;
     const int tiles = (p.length + kScanTile - 1) / kScanTile;
     // Chunks cost 1.65 times the work, so they begin where a wavefront a SIMD is not there; then sixteen wavefronts a CU, in chunks of at
-    // least two tiles (one sequence of 4096 positions and channels, eight / sixteen / thirty-two a CU: 161 / 149 / 153 us).  With lengths some
-    // chunks will be empty (seven sequences of 0 .. 517 positions: 49 / 37 / 31).
+    // least two tiles (one sequence of 4096 positions and channels, eight / sixteen / thirty-two a CU: 161 / 149 / 153 us; with / without chunks
+    // 2 x 2048 x 4096 130 / 232, 4 x 2048 x 4096 237 / 257, 4 x 1024 x 4096 130 / 120, 6 x 1024 x 4096 189 / 169).  With lengths some chunks will be
+    // empty (seven sequences of 0 .. 517 positions, eight / sixteen / thirty-two a CU: 49 / 37 / 31).
     long long chunks = workgroups >= 256 ? 1 : (ragged ? 2048 : 1024) / (workgroups ? workgroups : 1);
     if (chunks > tiles / 2) chunks = tiles / 2;
     if (chunks > 64) chunks = 64;

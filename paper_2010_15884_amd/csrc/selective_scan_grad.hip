@@ -36,10 +36,11 @@ GradShape backward_shape(const sys_selective_scan_t& p)
     s.blocks_a_group = (s.channels_a_group + kScanChannels - 1) / kScanChannels;
     s.channel_blocks = s.blocks_a_group * p.groups;
     const int ns = scan_states_a_lane(p.states), span = ns <= 4 ? 16 : 64 / ns;
-    // Long chunks leave the chain along them little to read and write; short ones leave work for all CUs: as long as there are eight
-    // workgroups a CU.
+    // Long chunks leave the chain along them little to read and write; short ones leave work for all CUs: as long as there are two
+    // workgroups a CU (16 states in bf16, eight / four / two a CU: 1 x 1024 positions x 2048 channels 81 / 69 / 64 us, 1 x 4096 x 2048 174 / 166 / 166,
+    // 2 x 2048 x 4096 301 / 301 / 301).
     const long long spans = ((long long)p.length + span - 1) / span, all = spans * s.channel_blocks * p.batch;
-    s.spans = all / 2048 < 1 ? 1 : all / 2048 > kMostSpans ? kMostSpans : (int)(all / 2048);
+    s.spans = all / 512 < 1 ? 1 : all / 512 > kMostSpans ? kMostSpans : (int)(all / 512);
     s.chunk_rows = s.spans * span;
     s.chunks = (int)((spans + s.spans - 1) / s.spans);
     return s;

@@ -174,10 +174,6 @@ def _allocated(t, stream, make):
         return make(_calls.empty, t.device)
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
 def _run(name, packed, stream, *pointers):
     status = getattr(_calls, name)(packed, *pointers, _b._stream_handle(stream))
     if status:
