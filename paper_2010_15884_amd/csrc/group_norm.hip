@@ -965,8 +965,11 @@ bool resident_shape(const sys_group_norm_t& p, bool grad, ResidentShape* out)
     const long long waves = (((long long)p.batch * s.tiles) << s.log_unit) >> 6;
     s.entries = items == 1 && waves >= 4 * 4096 ? 4 : 1;
     const long long turns = (p.batch + s.entries - 1) / s.entries;
-    // gradients: sixteen wavefronts a CU, and no more sums of dw and db than that
-    long long slices = grad ? (4096LL * 64 >> s.log_unit) / s.tiles : turns;
+    // Gradients: eight wavefronts a CU where lanes hold 16 bytes of several rows, or one row (whose sums of dw and db are soon more than it), else
+    // sixteen, and no more sums of dw and db than that (eight / sixteen / twenty-four a CU: 8192 x 64 x 64 channels 50 / 63 / 67 us, 8192 x 32 x 10
+    // 21 / 28 / 37, 256 x 256 x 256 in 32 groups 31 / 39 / 44; 4096 x 16 x 320 in 32 groups 80 / 61 / 58, 512 x 64 x 320 39 / 27 / 28).
+    const long long grad_waves = items == 1 || v * element == 16 ? 2048 : 4096;
+    long long slices = grad ? (grad_waves * 64 >> s.log_unit) / s.tiles : turns;
     slices = slices < 1 ? 1 : slices > turns ? turns : slices;
     s.slices = (int)slices;
     s.rounds = (int)((turns + slices - 1) / slices);
