@@ -282,8 +282,9 @@ int sys_conv2d_has(int projection, int kh, int kw);
  * As everywhere in this library a call validates its arguments before the first HIP call, only
  * enqueues kernels on `stream`, allocates nothing and keeps nothing.  Some of these operators
  * combine parts of a long axis in device memory of the caller's: *_workspace gives the bytes for
- * a call (0: none needed, pass NULL), 4-byte aligned, contents of no matter before or after, not
- * to be used by calls that may run at the same time.  Optional pointers may be NULL.  Outputs must
+ * a call (0: none needed, pass NULL; one that is given all the same is checked like one of 4
+ * bytes), 4-byte aligned, contents of no matter before or after, not to be used by calls that may
+ * run at the same time.  Optional pointers may be NULL.  Outputs and workspace must
  * not overlap inputs or each other (SYS_ERR_ALIAS; whole ranges from the first to the last element
  * are compared), except where a state is updated in place.
  *
@@ -369,6 +370,9 @@ typedef struct {
  *   d_D, d_delta_bias (optional)  [channels] fp32
  *   d_state  [batch, channels, states] fp32 (optional): h before the first position; zeros without it
  *   d_state_out  like d_state (optional, written): h behind the last one
+ *   SYS_ERR_UNSUPPORTED  more than SYS_MAX_STATES states, rows further apart than SYS_MAX_SCAN_ROW elements,
+ *            pointers off their element's alignment
+ *   SYS_ERR_SIZE  negative sizes, no channels, groups that do not divide the channels, strides of y that make rows overlap
  */
 int sys_selective_scan(const sys_selective_scan_t *p, const void *d_u, const void *d_delta, const float *d_A,
                        const void *d_B, const void *d_C, const float *d_D, const void *d_z, const float *d_delta_bias,

@@ -6,6 +6,11 @@
 // are the bound.  The recurrence runs down the positions, so what can run side by side is batch x channels x states; where that
 // leaves SIMDs idle the positions are cut into chunks: one launch finds each chunk's end state from a zero start, the next one starts
 // every chunk from the states of those before it, combined in its prologue with e^(A sum s), and computes the outputs.
+//
+// Measured, bf16, 16 states, gated: one sequence of 4096 positions and channels (2^28 elements) 145 us = 59 for the end states + 88 for the outputs,
+// 5.1 and 7.9 vector instructions an element, VALUs 86 and 84 % busy, LDS 14 and 19; one sweep alone could take no less than 47.
+// Not faster: 8 or 32 positions a tile (151, 151), sixteen lanes a channel in one sweep without chunks (240 to 258: one wavefront a SIMD waits
+// for every step), the scheduler set on instruction-level parallelism.
 #include "launch.h"
 #include "sequence.h"
 #include "scan_tile.h"
@@ -166,7 +171,8 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(sys_selective_scan_t
 
 // ---------------------------------------------------------------- single tokens
 
-// V neighbouring states a lane, `lanes` lanes (a power of two) a channel; the states are read and written once: bound by memory.
+// V neighbouring states a lane, `lanes` lanes (a power of two) a channel; the states are read and written once: bound by memory
+// (64 tokens of 4096 channels with 16 states, 34 MB of states and 1 MB else: 11.2 us, 3.1 TB/s; a call from the host takes 13).
 template <typename T, int V>
 __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(sys_selective_scan_t p, ScanArgs a, int log_lanes)
 {

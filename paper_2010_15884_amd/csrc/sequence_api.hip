@@ -40,6 +40,8 @@ struct Ranges {
     }
     void in(const void* p, Wide elements, size_t element) { add(p, elements, element, false); }
     void out(const void* p, Wide elements, size_t element) { add(p, elements, element, true); }
+    // One that is given though none is needed is held apart as well: whether a misplaced one is refused does not depend on the sizes.
+    void workspace(const void* p, size_t bytes) { add(p, bytes ? bytes / sizeof(float) : 1, sizeof(float), true); }
 
     bool overlap() const
     {
@@ -170,7 +172,7 @@ int sys_causal_conv1d_backward(const sys_causal_conv1d_t* p, const void* d_dy, c
     r.out(d_dw, (Wide)p->channels * p->width, pe);
     r.out(d_dbias, p->channels, pe);
     r.out(d_dstate, state, e);
-    r.out(d_workspace, need / sizeof(float), sizeof(float));
+    r.workspace(d_workspace, need);
     if ((st = check(r)) != SYS_OK) return st;
     sysconv::CausalConvArgs a = {};
     a.dy = d_dy, a.x = d_x, a.w = d_w, a.bias = d_bias, a.state = d_state, a.lengths = d_lengths, a.dstate_out = d_dstate_out;
@@ -233,7 +235,7 @@ int sys_selective_scan(const sys_selective_scan_t* p, const void* d_u, const voi
     r.in(d_lengths, p->batch, sizeof(int));
     r.out(d_y, extent(p->batch, p->length, p->channels, p->y_batch, p->y_row), e);
     r.out(d_state_out, state, sizeof(float));
-    r.out(d_workspace, need / sizeof(float), sizeof(float));
+    r.workspace(d_workspace, need);
     if ((st = check(r)) != SYS_OK || !p->batch) return st;
     sysconv::ScanArgs a = {};
     a.u = d_u, a.delta = d_delta, a.a = d_A, a.b = d_B, a.c = d_C, a.d = d_D, a.z = d_z, a.delta_bias = d_delta_bias, a.state = d_state;
@@ -283,7 +285,7 @@ int sys_selective_scan_backward(const sys_selective_scan_t* p, const void* d_dy,
     r.out(d_dz, values, e);
     r.out(d_ddelta_bias, p->channels, sizeof(float));
     r.out(d_dstate, state, sizeof(float));
-    r.out(d_workspace, need / sizeof(float), sizeof(float));
+    r.workspace(d_workspace, need);
     if ((st = check(r)) != SYS_OK) return st;
     sysconv::ScanArgs a = {};
     a.dy = d_dy, a.u = d_u, a.delta = d_delta, a.a = d_A, a.b = d_B, a.c = d_C, a.d = d_D, a.z = d_z, a.delta_bias = d_delta_bias, a.state = d_state;
@@ -346,7 +348,7 @@ int sys_group_norm(const sys_group_norm_t* p, const void* d_x, const void* d_w, 
     r.out(d_y, extent(p->batch, p->rows, p->channels, p->y_batch, p->y_row), e);
     r.out(d_mean, groups, sizeof(float));
     r.out(d_rstd, groups, sizeof(float));
-    r.out(d_workspace, need / sizeof(float), sizeof(float));
+    r.workspace(d_workspace, need);
     if ((st = check(r)) != SYS_OK || !p->batch) return st;
     sysconv::NormArgs a = {};
     a.x = d_x, a.w = d_w, a.b = d_b, a.y = d_y, a.mean = d_mean, a.rstd = d_rstd, a.workspace = (float*)d_workspace;
@@ -378,7 +380,7 @@ int sys_group_norm_backward(const sys_group_norm_t* p, const void* d_dy, const v
     r.out(d_dx, (Wide)p->batch * (Wide)p->rows * p->channels, e);
     r.out(d_dw, p->channels, pe);
     r.out(d_db, p->channels, pe);
-    r.out(d_workspace, need / sizeof(float), sizeof(float));
+    r.workspace(d_workspace, need);
     if ((st = check(r)) != SYS_OK) return st;
     sysconv::NormArgs a = {};
     a.dy = d_dy, a.x = d_x, a.w = d_w, a.b = d_b, a.mean_in = d_mean, a.rstd_in = d_rstd, a.dx = d_dx, a.dw = d_dw, a.db = d_db;
