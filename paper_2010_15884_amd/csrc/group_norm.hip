@@ -11,8 +11,8 @@
 // far from all others), or for many at once as mean = sum n_i mean_i / n, M2 = sum M2_i + n_i (mean_i - mean)^2.
 //
 // Measured, bf16: 16 x 4096 x 512 in 32 groups with SiLU 32.2 us, 4.2 TB/s of x and y (a copy of as many bytes: 22; every CU holds one unit,
-// so all load, then all store, in pieces of 64 bytes); 8192 rows of 64 x 64 channels 28.4, 4.7 TB/s, their gradients 50, 4.0 TB/s of x, dy
-// and dx; gradients of 8 x 4096 x 320 in 32 groups, f16, in chunks 34.1 = 14.7 sums + 7.2 combining + 13.7 dx, less overlap.
+// so all load, then all store, in pieces of 64 bytes); 8192 rows of 64 x 64 channels 27.4, 4.9 TB/s, their gradients 50, 4.0 TB/s of x, dy
+// and dx; gradients of 8 x 4096 x 320 in 32 groups, f16, in chunks 33.6 = 14.7 sums + 7.2 combining + 13.4 dx, less what overlaps.
 #include <type_traits>
 
 #include "launch.h"
@@ -50,6 +50,14 @@ __device__ __forceinline__ void by_activation(int activation, F&& work)
     if (activation == SYS_ACT_SILU) work(std::integral_constant<int, SYS_ACT_SILU>());
     else if (activation == SYS_ACT_RELU) work(std::integral_constant<int, SYS_ACT_RELU>());
     else work(std::integral_constant<int, SYS_ACT_NONE>());
+}
+
+// 1 / sqrt(v) to an ulp or so; the instruction takes no v below the smallest normal number.  (A quotient, a root and a quotient rounded by the book had
+// been a fifth of the instructions for rows of 64 x 64 channels.)
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool tiny = v < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.0f);
 }
 
 // What is taken off a group's values: the first one of the batch entry.
@@ -233,8 +241,13 @@ __device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>&
         const float mean = sum * (1.0f / V);
 #pragma unroll
         for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - first) - mean, (v[k] - first) - mean, square);
+        if (i == 0) {                               // (a lane without any row is put right below)
+            m.mean = mean;
+            m.m2 = square;
+            continue;
+        }
         const float on = i + 1 < items || whole ? 1.0f : 0.0f, d = mean - m.mean;
-        m.mean = i == 0 ? mean : __builtin_fmaf(d, on * (1.0f / (i + 1)), m.mean);
+        m.mean = __builtin_fmaf(d, on * (1.0f / (i + 1)), m.mean);
         m.m2 = __builtin_fmaf(on, __builtin_fmaf(d * d, (float)V * i / (i + 1), square), m.m2);
     }
     m.n = there ? (float)(V * (items - !whole)) : 0.0f;
@@ -295,7 +308,7 @@ __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p,
 #pragma unroll
     for (int e = 0; e < ENTRIES; ++e) {
         if (!at.there || b0 + e >= p.batch) continue;
-        const float mean = mean_of[e] + first[e], rstd = 1.0f / __builtin_sqrtf(m2_of[e] / all + p.eps);
+        const float mean = mean_of[e] + first[e], rstd = inverse_root(__builtin_fmaf(m2_of[e], 1.0f / all, p.eps));
         if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
             const size_t group = (size_t)(b0 + e) * p.groups + at.group;
             if (a.mean) a.mean[group] = mean;
@@ -617,7 +630,7 @@ __global__ __launch_bounds__(kThreads) void norm_statistics_kernel(sys_group_nor
     __syncthreads();
     if (threadIdx.x) return;
     for (int k = 1; k < kThreads / 64; ++k) m = merged(m, shared[k]);
-    const float rstd = 1.0f / __builtin_sqrtf(m.m2 / m.n + p.eps);
+    const float rstd = inverse_root(m.m2 / m.n + p.eps);
     const float mean = m.mean + group_first<T>(p, (const T*)a.x + b * p.x_batch, group);
     float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * (size_t)blockIdx.x;
     to[0] = mean;
