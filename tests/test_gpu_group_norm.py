@@ -101,6 +101,33 @@ def test_forward_and_gradients(case):
     _check_all(_make(sum(case[:4]), batch, rows, channels, dtype, affine, params, offset=offset), groups, activation)
 
 
+LAYOUTS = [
+    # groups of every width a lane may hold (1, 2, 4, 8 channels), few and many units, whole and ragged last rows, from 1 to 32 rows a lane
+    (2, 1024, 70, 10, F16, "SILU"), (1, 1023, 70, 10, BF16, "NONE"), (3, 31, 70, 10, F32, "RELU"),
+    (4, 1024, 320, 32, F16, "SILU"), (1, 700, 320, 32, BF16, "RELU"), (9, 1023, 160, 16, F16, "NONE"), (2, 4096, 60, 6, F32, "SILU"),
+    (3, 2047, 24, 2, BF16, "SILU"), (40, 130, 60, 5, F16, "NONE"), (130, 97, 20, 5, F32, "SILU"), (64, 513, 12, 1, F16, "SILU"),
+    (2, 4096, 64, 2, BF16, "SILU"), (1, 4097, 64, 2, BF16, "NONE"), (70, 255, 128, 4, F16, "RELU"), (5, 1000, 40, 5, BF16, "SILU"),
+    # rows of many lanes
+    (3, 1, 8192, 1, BF16, "SILU"), (2, 5, 4096, 1, F16, "NONE"), (1, 3, 6000, 2, F32, "SILU"), (1, 4, 8000, 1, F32, "NONE"),
+    # tokens, several entries a unit: units in a wavefront, of one, of several
+    (20000, 1, 256, 64, BF16, "SILU"), (2101, 1, 4096, 1, F16, "NONE"), (16387, 1, 500, 1, BF16, "RELU"),
+]
+
+
+@pytest.mark.parametrize("case", LAYOUTS, ids=lambda c: "-".join(str(v) for v in c).replace("torch.", ""))
+def test_layouts(case):
+    batch, rows, channels, groups, dtype, activation = case
+    _check_all(_make(sum(case[:4]), batch, rows, channels, dtype), groups, activation)
+
+
+def test_variances_of_every_size():
+    """Without eps the results are the same at every power of two; the square of the smallest is 2^-120."""
+    for rows, channels, groups in ((50, 24, 3), (1, 256, 4), (6000, 40, 4)):
+        c = _make(rows, 2, rows, channels, F32)
+        for exponent in (-60, -30, 40):
+            _check_all(dict(c, x=c["x"] * 2.0 ** exponent), groups, "SILU", eps=0.0)
+
+
 def test_means_far_from_zero():
     """Squares summed as they come would lose the variance: 4096^2 2^-24 = 1."""
     for rows, channels, groups in ((500, 24, 3), (1, 256, 4), (64, 16, 2)):
