@@ -399,10 +399,10 @@ hipError_t launch_rows(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hi
 template <typename T, int K, int V>
 hipError_t launch_forward(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s)
 {
-    // Rows a lane: 16 read the K-1 rows above a chunk the least often, 4 leave the most wavefronts (K = 4 in bf16, 4 / 8 / 16 rows: 1 x 2048 x 1024
+    // Rows a lane: 16 read the K-1 rows above a chunk the least often, where they leave three wavefronts a SIMD, 4 leave the most (K = 4 in bf16, 4 / 8 / 16 rows: 1 x 2048 x 1024
     // 3.8 / 4.8 / 6.8 us, 4 x 1024 x 2048 8.0 / 8.8 / 9.1, 8 x 2048 x 1024 14.2 / 14.1 / 14.6, 4 x 4096 x 2048 26.6 / 25.3 / 24.3).
     const double waves = (double)p.batch * p.length * ((p.channels + V - 1) / V) / (16 * 64);
-    return waves >= 3072 ? launch_rows<T, K, V, 16>(p, a, s) : launch_rows<T, K, V, 4>(p, a, s);
+    return waves >= 3 * 1024 ? launch_rows<T, K, V, 16>(p, a, s) : launch_rows<T, K, V, 4>(p, a, s);
 }
 
 template <typename T, int K, int V>
