@@ -15,7 +15,18 @@ namespace sysconv {
 constexpr int kScanThreads = 256;
 constexpr int kScanChannels = kScanThreads / 4;     // a workgroup
 constexpr int kScanTile = 16;                       // positions a tile
-static_assert(15 * SYS_MAX_SCAN_ROW + (1LL << 24) < (1LL << 30), "a tile's offsets in bytes fit 32 bits (up to 2^24 channels)");
+
+// An offset within a tile that is never read or written: no tile's buffer reaches it, and every element of a tile lies below it.
+constexpr unsigned kNowhere = 0xfffffff0u;
+static_assert(4 * ((kScanTile - 1) * SYS_MAX_SCAN_ROW + (1LL << 24)) <= kNowhere, "a tile's rows lie below kNowhere (up to 2^24 channels)");
+
+// The size of a tile's buffer: the bytes from its first element to the end of the last row that exists, where they are that many.
+__host__ __device__ __forceinline__ unsigned buffer_size(long long bytes)
+{
+    const int high = (int)(bytes >> 32);
+    const unsigned low = (unsigned)bytes;
+    return high < 0 ? 0u : high || low > kNowhere ? kNowhere : low;
+}
 
 struct ScanShape {
     int channels_a_group, blocks_a_group, channel_blocks;   // of 64 channels
@@ -69,8 +80,7 @@ struct RowBuffer {
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile(int down = 0) const
     {
         const long long bytes = left - down * row * (long long)sizeof(T);
-        const int high = (int)(bytes >> 32);
-        return __builtin_amdgcn_make_buffer_rsrc((void*)(at + down * row), 0, high < 0 ? 0u : high ? 0xffffffffu : (unsigned)bytes, 0x00027000);
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(at + down * row), 0, buffer_size(bytes), 0x00027000);
     }
     __device__ __forceinline__ void next() { at += kScanTile * row, left -= kScanTile * row * (long long)sizeof(T); }
     __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }
@@ -97,8 +107,6 @@ __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rsrc_t b, unsigned 
     if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), b, offset, 0, 0);
     else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), b, offset, 0, 0);
 }
-
-constexpr unsigned kNowhere = 0xfffffff0u;          // an offset that is never written
 
 // B or C of kScanTile positions for LDS, [position][4 * NS], zeros past the last state and the sequence's end: first into registers ...
 template <typename T, int NS>
