@@ -20,6 +20,13 @@ constexpr int kScanTile = 16;                       // positions a tile
 constexpr unsigned kNowhere = 0xfffffff0u;
 static_assert(4 * ((kScanTile - 1) * SYS_MAX_SCAN_ROW + (1LL << 24)) <= kNowhere, "a tile's rows lie below kNowhere (up to 2^24 channels)");
 
+// Bytes from row t0 to the end of the last row that exists, row end - 1; none or less where no row does, whatever the stride (rows that are
+// used again, or of an empty sequence, which has no memory at all).
+__host__ __device__ __forceinline__ long long bytes_left(int t0, int end, long long row, int columns, size_t element)
+{
+    return ((long long)(end - 1 - t0) * row + (t0 < end ? columns : 0)) * (long long)element;
+}
+
 // The size of a tile's buffer: the bytes from its first element to the end of the last row that exists, where they are that many.
 __host__ __device__ __forceinline__ unsigned buffer_size(long long bytes)
 {
@@ -73,7 +80,7 @@ struct RowBuffer {
     long long left;                    // bytes from there to the end of the last row that exists; none left: every load gives 0
     long long row;
     __device__ __forceinline__ RowBuffer(const void* base, long long row_stride, int columns, int t0, int end)
-        : at((T*)base + t0 * row_stride), left(((long long)(end - 1 - t0) * row_stride + columns) * (long long)sizeof(T)), row(row_stride)
+        : at((T*)base + t0 * row_stride), left(bytes_left(t0, end, row_stride, columns, sizeof(T))), row(row_stride)
     {
     }
     // the rows from `down` rows below the present tile's first one on
