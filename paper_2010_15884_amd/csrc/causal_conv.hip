@@ -209,6 +209,7 @@ __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const Cau
     const T* whole_dy = dy + begin * p.y_row;
     auto load_x = [&](int e) { return WHOLE ? C::raw(whole_x + (e - begin) * p.x_row) : raw_row<T, K, V>(x, state, p.x_row, p.channels, e, len, c0); };
     auto load_dy = [&](int e) { return WHOLE || (e >= 0 && e < len) ? C::raw(WHOLE ? whole_dy + (e - begin) * p.y_row : dy + e * p.y_row) : typename C::Raw{}; };
+    const int zero_from = len ? len + K - 1 : 0;                       // rows that no dpre reaches (0 times an infinite tap would be a NaN)
     typename C::Raw first[K - 1], more[K - 1], more_dy[K - 1], ahead[kAhead], ahead_dy[kAhead];
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
@@ -223,8 +224,9 @@ __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const Cau
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
         w.move(more[j]);
-        if (WHOLE || begin - (K - 1) + j >= 0) w.template differentiate<SILU>(more_dy[j]);      // (zeros where there is no dy)
-        else w.nothing();
+        const int e = begin - (K - 1) + j;
+        if (WHOLE || (e >= 0 && e < len)) w.template differentiate<SILU>(more_dy[j]);
+        else w.nothing();              // (the derivative times a dy of 0 may be a NaN)
     }
     for (int e0 = begin; e0 < end; e0 += kAhead) {
         typename C::Raw now[kAhead], now_dy[kAhead];
@@ -250,6 +252,10 @@ __device__ __forceinline__ void grad_run(const sys_causal_conv1d_t& p, const Cau
                 continue;
             }
             if (e >= end) break;
+            if (e >= zero_from) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) out[i] = 0.0f;
+            }
             if (dstate_out && e >= len && e < len + K - 1) {
                 float tail[V];
                 C::load(dstate_out + (size_t)(e - len) * p.channels, tail);
