@@ -34,8 +34,6 @@ __device__ __forceinline__ Moments merged(Moments a, Moments b)
     return {n, b.n > 0.0f ? __builtin_fmaf(d, share, a.mean) : a.mean, b.n > 0.0f ? a.m2 + b.m2 + d * d * a.n * share : a.m2};
 }
 
-__device__ __forceinline__ Moments from_lane(Moments m, int k) { return {__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.m2, k)}; }
-
 template <int V, int ACTIVATION>
 __device__ __forceinline__ void activate(float (&v)[V])
 {
@@ -597,41 +595,59 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
     }
 }
 
-// A group's entries in [chunk][channel], dealt out to the lanes of a workgroup: f(chunk, channel of the group).
-template <typename F>
-__device__ __forceinline__ void each_entry(int chunks, int channels, F&& f)
+// Sum over the lanes of a workgroup; every lane gets it.
+__device__ __forceinline__ double workgroup_sum(double v, double (&shared)[kThreads / 64])
 {
-    if (channels >= kThreads) {
-        for (int chunk = 0; chunk < chunks; ++chunk)
-            for (int c = threadIdx.x; c < channels; c += kThreads) f(chunk, c);
-    } else {
-        const int tall = kThreads / channels, row = (int)threadIdx.x / channels, c = (int)threadIdx.x - row * channels;
-        if (row < tall)
-            for (int chunk = row; chunk < chunks; chunk += tall) f(chunk, c);
-    }
+    for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k);
+    __syncthreads();                                // (what was here before has been read)
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = shared[0];
+    for (int k = 1; k < kThreads / 64; ++k) v += shared[k];
+    return v;
 }
 
-// mean and rstd of every group, a workgroup each: [batch][group] pairs behind the chunks' sums, and the caller's arrays.
+// mean and rstd of every group, a workgroup each: [batch][group] pairs behind the chunks' sums, and the caller's arrays.  The entries are thousands to
+// a lane for few wide groups, so their sums are in 64 bits: in 32 they had cost rstd 22 units of 2^-24 (1 x 16384 x 2048 in one group).  Taking
+// one entry's mean off the others leaves the squares 2^-53 of their own size, which is at most the number of values times that of the variance.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_statistics_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
+    constexpr int kEntries = 8;                     // of a lane on their way together
     const int b = blockIdx.x / p.groups, group = blockIdx.x - b * p.groups;
     const int channels = p.channels / p.groups;
     const float* from = a.workspace + (size_t)b * shape.chunks * 2 * p.channels + (size_t)group * channels;
-    const float last_rows = (float)(p.rows - (shape.chunks - 1) * shape.chunk_rows);
-    Moments m = {0.0f, 0.0f, 0.0f};
-    each_entry(shape.chunks, channels, [&](int chunk, int c) {
-        const float* entry = from + (size_t)chunk * 2 * p.channels + c;
-        m = merged(m, Moments{chunk + 1 < shape.chunks ? (float)shape.chunk_rows : last_rows, entry[0], entry[p.channels]});
-    });
-    for (int k = 1; k < 64; k <<= 1) m = merged(m, from_lane(m, k));
-    __shared__ Moments shared[kThreads / 64];
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
-    __syncthreads();
+    const double all = (double)p.rows * channels, chunk_rows = (double)shape.chunk_rows, last_rows = (double)(p.rows - (shape.chunks - 1) * shape.chunk_rows);
+    const double origin = *from;
+    // a group's entries in [chunk][channel], dealt out to the lanes: 256 channels side by side, or those of several chunks
+    const int wide = channels < kThreads ? channels : kThreads, tall = kThreads / wide, row = (int)threadIdx.x / wide, first = (int)threadIdx.x - row * wide;
+    double sum = 0.0, squares = 0.0;
+    for (int chunk = row < tall ? row : shape.chunks, c = first; chunk < shape.chunks;) {
+        float mean[kEntries], m2[kEntries];
+        double rows[kEntries];
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k) {
+            const bool there = chunk < shape.chunks;
+            const float* entry = there ? from + (size_t)chunk * 2 * p.channels + c : from;
+            mean[k] = entry[0];
+            m2[k] = entry[p.channels];
+            rows[k] = !there ? 0.0 : chunk + 1 < shape.chunks ? chunk_rows : last_rows;
+            c += wide;
+            if (c >= channels) c = first, chunk += tall;
+        }
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k) {
+            const double d = mean[k] - origin;
+            sum += rows[k] * d;
+            squares += rows[k] > 0.0 ? rows[k] * d * d + m2[k] : 0.0;
+        }
+    }
+    __shared__ double shared[kThreads / 64];
+    sum = workgroup_sum(sum, shared);
+    squares = workgroup_sum(squares, shared);
     if (threadIdx.x) return;
-    for (int k = 1; k < kThreads / 64; ++k) m = merged(m, shared[k]);
-    const float rstd = inverse_root(m.m2 / m.n + p.eps);
-    const float mean = m.mean + group_first<T>(p, (const T*)a.x + b * p.x_batch, group);
+    const float rstd = inverse_root((float)((squares - sum * (sum / all)) / all + p.eps));
+    const float mean = (float)(origin + sum / all + group_first<T>(p, (const T*)a.x + b * p.x_batch, group));
     float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * (size_t)blockIdx.x;
     to[0] = mean;
     to[1] = rstd;
