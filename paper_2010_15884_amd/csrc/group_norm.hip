@@ -5,10 +5,11 @@
 // read once, wait there for the group's sums, and are written once (norm_resident_kernel, norm_grad_resident_kernel).  Else a first
 // launch sums up chunks of rows channel by channel, one or two small ones combine them, and a last one reads the rows again.
 //
-// Values and squares are never summed as they come, so a mean far from zero costs no digits of the variance: the group's first
-// value is taken off every other one, some differences at a time give their own mean and sum of squared distances, and these are
-// put together as n = n1 + n2, mean = mean1 + d n2/n, M2 = M2_1 + M2_2 + d^2 n1 n2/n with d = mean2 - mean1 (the first value may be
-// far from all others), or for many at once as mean = sum n_i mean_i / n, M2 = sum M2_i + n_i (mean_i - mean)^2.
+// Squares are never summed as they come, so a mean far from zero costs no digits of the variance: what a lane has seen of the group's mean is taken
+// off its values, some differences at a time give their own mean and sum of squared distances, and these are put together as n = n1 + n2,
+// mean = mean1 + d n2/n, M2 = M2_1 + M2_2 + d^2 n1 n2/n with d = mean2 - mean1, or for many at once as mean = sum n_i mean_i / n,
+// M2 = sum M2_i + n_i (mean_i - mean)^2.  Means stay in two parts until they have been subtracted: rounded to 32 bits they would bring their own size
+// into d.  No one value is taken off all the others, for it may be far from them, and its size would stay in the mean's last digit.
 //
 // Measured, bf16: 16 x 4096 x 512 in 32 groups with SiLU 32.2 us, 4.2 TB/s of x and y (a copy of as many bytes: 22; every CU holds one unit,
 // so all load, then all store, in pieces of 64 bytes); 8192 rows of 64 x 64 channels 27.4, 4.9 TB/s, their gradients 50, 4.0 TB/s of x, dy
@@ -56,13 +57,6 @@ __device__ __forceinline__ float inverse_root(float v)
 {
     const bool tiny = v < 0x1p-100f;
     return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.0f);
-}
-
-// What is taken off a group's values: the first one of the batch entry.
-template <typename T>
-__device__ __forceinline__ float group_first(const sys_group_norm_t& p, const T* x, int group)
-{
-    return (float)x[(long long)group * (p.channels / p.groups)];
 }
 
 // The groups of V neighbouring channels, one division for all of them; counted from `from` on.
@@ -224,21 +218,30 @@ __device__ __forceinline__ void each_wavefront(const ResidentShape& s, int tile_
     }
 }
 
+// n values, their mean (origin + mean: the mean of some of them, and where the mean of all lies from there), and the sum of squared distances from it.
+struct PartMoments {
+    float n, origin, mean, m2;
+};
+
 // Moments of a lane's rows: all of `items`, or all but the last one.
 template <typename T, int V, int ITEMS>
-__device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>& rows, float first, bool there, bool whole, int items)
+__device__ __forceinline__ PartMoments lane_moments(const ResidentRows<T, V, ITEMS>& rows, bool there, bool whole, int items)
 {
-    Moments m = {0.0f, 0.0f, 0.0f};
+    PartMoments m = {0.0f, 0.0f, 0.0f, 0.0f};
+    float head[V];
+    Channels<T, V>::values(rows.raw[0], head);
+#pragma unroll
+    for (int k = 0; k < V; ++k) m.origin = __builtin_fmaf(head[k], 1.0f / V, m.origin);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         if (ITEMS > 1 && i >= items) continue;
         float v[V], sum = 0.0f, square = 0.0f;
         Channels<T, V>::values(rows.raw[i], v);
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum += v[k] - first;
+        for (int k = 0; k < V; ++k) sum += v[k] - m.origin;
         const float mean = sum * (1.0f / V);
 #pragma unroll
-        for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - first) - mean, (v[k] - first) - mean, square);
+        for (int k = 0; k < V; ++k) square = __builtin_fmaf((v[k] - m.origin) - mean, (v[k] - m.origin) - mean, square);
         if (i == 0) {                               // (a lane without any row is put right below)
             m.mean = mean;
             m.m2 = square;
@@ -249,7 +252,7 @@ __device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>&
         m.m2 = __builtin_fmaf(on, __builtin_fmaf(d * d, (float)V * i / (i + 1), square), m.m2);
     }
     m.n = there ? (float)(V * (items - !whole)) : 0.0f;
-    if (m.n == 0.0f) m = {0.0f, 0.0f, 0.0f};
+    if (m.n == 0.0f) m = {0.0f, 0.0f, 0.0f, 0.0f};
     return m;
 }
 
@@ -257,56 +260,55 @@ __device__ __forceinline__ Moments lane_moments(const ResidentRows<T, V, ITEMS>&
 template <typename T, int V, int ITEMS, int ENTRIES>
 __global__ __launch_bounds__(1024) void norm_resident_kernel(sys_group_norm_t p, NormArgs a, ResidentShape s)
 {
-    __shared__ Moments shared[ENTRIES][16 * kMostTile];
+    __shared__ PartMoments shared[ENTRIES][ITEMS == 1 ? 16 : 16 * kMostTile];         // (one row a lane is a row in all, whose units of several wavefronts are one group)
     const ResidentLane at(p, s, s.units, xcd_place(blockIdx.x, gridDim.x));
     const int b0 = at.unit / s.tiles * ENTRIES;
     ResidentRows<T, V, ITEMS> rows[ENTRIES];
-    float first[ENTRIES];
 #pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) {
-        const T* x = (const T*)a.x + (b0 + e < p.batch ? b0 + e : p.batch - 1) * p.x_batch;
-        rows[e].load(x + at.channel, p.x_row, (int)p.rows, at.row, at.tall);
-        first[e] = group_first<T>(p, x, at.group);
-    }
+    for (int e = 0; e < ENTRIES; ++e) rows[e].load((const T*)a.x + (b0 + e < p.batch ? b0 + e : p.batch - 1) * p.x_batch + at.channel, p.x_row, (int)p.rows, at.row, at.tall);
     float w[V], shift[V];
     load_affine<T, V>(p, a, at.channel, w, shift);
     const bool whole = at.row + (s.items - 1) * at.tall < (int)p.rows;
-    Moments m[ENTRIES];
+    PartMoments m[ENTRIES];
 #pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) m[e] = lane_moments<T, V, ITEMS>(rows[e], first[e], at.there, whole, s.items);
-    // the mean of several means and the sum of squared distances from it, first over the lanes, then over the wavefronts
-    float n[1] = {m[0].n}, mean_of[ENTRIES], m2_of[ENTRIES];
+    for (int e = 0; e < ENTRIES; ++e) m[e] = lane_moments<T, V, ITEMS>(rows[e], at.there, whole, s.items);
+    // the mean of several means, then the sum of squared distances from it and where the mean lies from there (in 32 bits it was rounded on the way),
+    // over the lanes; and the same of the wavefronts
+    float n[1] = {m[0].n}, mean_of[ENTRIES], sums[2 * ENTRIES];
     sum_lanes(s, n);
     const float share = n[0] > 0.0f ? 1.0f / n[0] : 0.0f;
 #pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) mean_of[e] = m[e].n * m[e].mean;
+    for (int e = 0; e < ENTRIES; ++e) mean_of[e] = m[e].n * share * (m[e].origin + m[e].mean);
     sum_lanes(s, mean_of);
 #pragma unroll
     for (int e = 0; e < ENTRIES; ++e) {
-        mean_of[e] *= share;
-        const float d = m[e].mean - mean_of[e];
-        m2_of[e] = __builtin_fmaf(m[e].n * d, d, m[e].m2);
+        const float d = (m[e].origin - mean_of[e]) + m[e].mean;
+        sums[2 * e] = m[e].n * d;
+        sums[2 * e + 1] = __builtin_fmaf(m[e].n * d, d, m[e].m2);
     }
-    sum_lanes(s, m2_of);
+    sum_lanes(s, sums);
 #pragma unroll
-    for (int e = 0; e < ENTRIES; ++e) m[e] = {n[0], mean_of[e], m2_of[e]};
+    for (int e = 0; e < ENTRIES; ++e) m[e] = {n[0], mean_of[e], sums[2 * e] * share, __builtin_fmaf(sums[2 * e] * share, -sums[2 * e], sums[2 * e + 1])};
     const float all = (float)p.rows * (float)(p.channels / p.groups);
     if (s.log_unit > 6) {
-#pragma unroll
-        for (int e = 0; e < ENTRIES; ++e) mean_of[e] = m2_of[e] = 0.0f;
         put_wavefront(s, at.tile_group, m, shared);
-        each_wavefront(s, at.tile_group, shared, [&](int e, const Moments& o) { mean_of[e] = __builtin_fmaf(o.n, o.mean, mean_of[e]); });
+        // (distances from the first wavefront's mean: their squares are at most 16, the wavefronts, times the sum that is left of them)
+        const int first_wave = (threadIdx.x >> s.log_unit) << (s.log_unit - 6);
 #pragma unroll
-        for (int e = 0; e < ENTRIES; ++e) mean_of[e] *= 1.0f / all;
-        each_wavefront(s, at.tile_group, shared, [&](int e, const Moments& o) {
-            const float d = o.mean - mean_of[e];
-            m2_of[e] += __builtin_fmaf(o.n * d, d, o.m2);
+        for (int e = 0; e < ENTRIES; ++e) mean_of[e] = shared[e][(first_wave << s.log_tile) + at.tile_group].origin, sums[2 * e] = sums[2 * e + 1] = 0.0f;
+        each_wavefront(s, at.tile_group, shared, [&](int e, const PartMoments& o) {
+            const float d = (o.origin - mean_of[e]) + o.mean;
+            sums[2 * e] = __builtin_fmaf(o.n, d, sums[2 * e]);
+            sums[2 * e + 1] += __builtin_fmaf(o.n * d, d, o.m2);
         });
+#pragma unroll
+        for (int e = 0; e < ENTRIES; ++e) m[e] = {all, mean_of[e], sums[2 * e] * (1.0f / all), __builtin_fmaf(sums[2 * e] * (1.0f / all), -sums[2 * e], sums[2 * e + 1])};
     }
 #pragma unroll
     for (int e = 0; e < ENTRIES; ++e) {
         if (!at.there || b0 + e >= p.batch) continue;
-        const float mean = mean_of[e] + first[e], rstd = inverse_root(__builtin_fmaf(m2_of[e], 1.0f / all, p.eps));
+        const float m2 = m[e].m2 < 0.0f ? 0.0f : m[e].m2;                   // (of equal values it may be, by roundings; a NaN stays)
+        const float mean = m[e].origin + m[e].mean, rstd = inverse_root(__builtin_fmaf(m2, 1.0f / all, p.eps));
         if (at.row == 0 && at.channel == at.group * (p.channels / p.groups)) {
             const size_t group = (size_t)(b0 + e) * p.groups + at.group;
             if (a.mean) a.mean[group] = mean;
@@ -501,13 +503,12 @@ struct Lanes {
 // Rows of a lane that are on their way together.
 constexpr int kNormRows = 8;
 
-// Mean (less the group's first value) and sum of squared distances of every channel in a chunk of rows: [batch][chunk][mean | m2][channel].
+// Mean and sum of squared distances of every channel in a chunk of rows: [batch][chunk][mean | m2][channel].
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t p, NormArgs a, NormShape shape)
 {
     const int b = blockIdx.x / shape.chunks, chunk = blockIdx.x - b * shape.chunks;
     const Lanes at(shape.columns);
-    const int channels = p.channels / p.groups;
     const long long begin = chunk * shape.chunk_rows, end = begin + shape.chunk_rows < p.rows ? begin + shape.chunk_rows : p.rows;
     const T* x = (const T*)a.x + b * p.x_batch;
     float* to = a.workspace + ((size_t)b * shape.chunks + chunk) * 2 * p.channels;
@@ -516,11 +517,9 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
         const bool there = at.there && c0 + at.column < shape.columns;
         const int column = c0 + at.column < shape.columns ? c0 + at.column : shape.columns - 1;
         const int channel = column * V + V <= p.channels ? column * V : p.channels - V;
-        float n = 0.0f, mean[V], m2[V], first[V];
-        int group[V];
-        groups_of<V>(channel, channels, 0, group);
+        float n = 0.0f, mean[V], rest[V], m2[V];    // the mean: mean + rest
 #pragma unroll
-        for (int i = 0; i < V; ++i) mean[i] = m2[i] = 0.0f, first[i] = group_first<T>(p, x, group[i]);
+        for (int i = 0; i < V; ++i) mean[i] = rest[i] = m2[i] = 0.0f;
         if (there) {
             const T* from = x + channel;
             for (long long r = begin + at.row; r < end; r += (long long)at.tall * kNormRows) {
@@ -530,6 +529,7 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
                     const long long row = r + (long long)k * at.tall;
                     raw[k] = Channels<T, V>::raw(from + (row < end ? row : r) * p.x_row);
                 }
+                if (n == 0.0f) Channels<T, V>::values(raw[0], mean);      // (of no rows: taken off the first ones, it moves to their mean with them)
                 float count = 0.0f, sum[V], square[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[i] = square[i] = 0.0f;
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
                     Channels<T, V>::values(raw[k], v);
                     count += on;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(on, v[i] - first[i], sum[i]);      // (the row that stands in for one that is not there is in the sum)
+                    for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(on, v[i] - mean[i], sum[i]);       // (the row that stands in for one that is not there is in the sum)
                 }
                 const float inverse = fast_rcp(count);
 #pragma unroll
@@ -552,20 +552,24 @@ __global__ __launch_bounds__(kThreads) void norm_moments_kernel(sys_group_norm_t
                     Channels<T, V>::values(raw[k], v);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float d = (v[i] - first[i]) - sum[i];
+                        const float d = (v[i] - mean[i]) - sum[i];
                         square[i] = __builtin_fmaf(on * d, d, square[i]);
                     }
                 }
                 const float all = n + count, share = count * fast_rcp(all);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float d = sum[i] - mean[i];
-                    mean[i] = __builtin_fmaf(d, share, mean[i]);
+                    const float d = sum[i] - rest[i];
                     m2[i] += square[i] + d * d * n * share;
+                    const float step = __builtin_fmaf(d, share, rest[i]), now = mean[i] + step;
+                    rest[i] = (mean[i] - now) + step;
+                    mean[i] = now;
                 }
                 n = all;
             }
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) mean[i] += rest[i];
         // the rows of the workgroup, by halves
         for (int tall = at.tall; tall > 1;) {
             const int half = (tall + 1) / 2;
@@ -646,8 +650,9 @@ __global__ __launch_bounds__(kThreads) void norm_statistics_kernel(sys_group_nor
     sum = workgroup_sum(sum, shared);
     squares = workgroup_sum(squares, shared);
     if (threadIdx.x) return;
-    const float rstd = inverse_root((float)((squares - sum * (sum / all)) / all + p.eps));
-    const float mean = (float)(origin + sum / all + group_first<T>(p, (const T*)a.x + b * p.x_batch, group));
+    const double m2 = squares - sum * (sum / all);
+    const float rstd = inverse_root((float)((m2 < 0.0 ? 0.0 : m2 / all) + p.eps));       // (of equal values it may be, by roundings; a NaN stays)
+    const float mean = (float)(origin + sum / all);
     float* to = a.workspace + (size_t)p.batch * shape.chunks * 2 * p.channels + 2 * (size_t)blockIdx.x;
     to[0] = mean;
     to[1] = rstd;
