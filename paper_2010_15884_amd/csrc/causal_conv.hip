@@ -388,6 +388,13 @@ __global__ __launch_bounds__(kThreads) void causal_conv_step_kernel(sys_causal_c
 
 // ---------------------------------------------------------------- launches
 
+// Channels a lane of the forward kernel.
+int lane_channels(const sys_causal_conv1d_t& p)
+{
+    const int v = p.dtype == SYS_F32 ? kLaneChannels<float> : kLaneChannels<f16_t>;
+    return p.channels >= v ? v : 1;
+}
+
 int runs_of(const sys_causal_conv1d_t& p) { return p.length ? (p.length + kRun - 1) / kRun : 1; }
 int run_groups_of(const sys_causal_conv1d_t& p) { return (runs_of(p) + kRunWaves - 1) / kRunWaves; }
 
@@ -405,10 +412,7 @@ hipError_t launch_rows(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hi
 template <typename T, int K, int V>
 hipError_t launch_forward(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s)
 {
-    // Rows a lane: 16 read the K-1 rows above a chunk the least often, where they leave three wavefronts a SIMD, 4 leave the most (K = 4 in bf16, 4 / 8 / 16 rows: 1 x 2048 x 1024
-    // 3.8 / 4.8 / 6.8 us, 4 x 1024 x 2048 8.0 / 8.8 / 9.1, 8 x 2048 x 1024 14.2 / 14.1 / 14.6, 4 x 4096 x 2048 26.6 / 25.3 / 24.3).
-    const double waves = (double)p.batch * p.length * ((p.channels + V - 1) / V) / (16 * 64);
-    return waves >= 3 * 1024 ? launch_rows<T, K, V, 16>(p, a, s) : launch_rows<T, K, V, 4>(p, a, s);
+    return causal_conv_rows_a_lane(p) == 16 ? launch_rows<T, K, V, 16>(p, a, s) : launch_rows<T, K, V, 4>(p, a, s);
 }
 
 template <typename T, int K, int V>
@@ -444,7 +448,7 @@ hipError_t launch_width(Form form, const sys_causal_conv1d_t& p, const CausalCon
 {
     constexpr int V = kLaneChannels<T>;
     switch (form) {
-    case kForward: return p.channels >= V ? launch_forward<T, K, V>(p, a, s) : launch_forward<T, K, 1>(p, a, s);
+    case kForward: return lane_channels(p) == V ? launch_forward<T, K, V>(p, a, s) : launch_forward<T, K, 1>(p, a, s);
     // half as wide: the windows, taps and sums of 16 bytes take 230 registers (4 taps; level in time) or more than there are (8)
     case kBackward: return p.channels >= V / 2 ? launch_backward<T, K, V / 2>(p, a, s) : launch_backward<T, K, 1>(p, a, s);
     // lanes that share channels would read states that others have moved on
@@ -477,6 +481,15 @@ hipError_t launch(Form form, const sys_causal_conv1d_t& p, const CausalConvArgs&
 }
 
 }  // namespace
+
+// 16 rows read the K-1 rows above a chunk the least often, where they leave three wavefronts a SIMD, 4 leave the most (K = 4 in bf16, 4 / 8 / 16 rows:
+// 1 x 2048 x 1024 3.8 / 4.8 / 6.8 us, 4 x 1024 x 2048 8.0 / 8.8 / 9.1, 8 x 2048 x 1024 14.2 / 14.1 / 14.6, 4 x 4096 x 2048 26.6 / 25.3 / 24.3).
+int causal_conv_rows_a_lane(const sys_causal_conv1d_t& p)
+{
+    const int v = lane_channels(p);
+    const double waves = (double)p.batch * p.length * ((p.channels + v - 1) / v) / (16 * 64);
+    return waves >= 3 * 1024 ? 16 : 4;
+}
 
 hipError_t launch_causal_conv(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s) { return launch(kForward, p, a, s); }
 hipError_t launch_causal_conv_grad(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s) { return launch(kBackward, p, a, s); }

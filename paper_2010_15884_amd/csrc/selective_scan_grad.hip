@@ -574,6 +574,8 @@ hipError_t launch_type(const sys_selective_scan_t& p, const ScanArgs& a, hipStre
 
 }  // namespace
 
+int scan_grad_spans(const sys_selective_scan_t& p) { return backward_shape(p).spans; }
+
 hipError_t launch_scan_grad(const sys_selective_scan_t& p, const ScanArgs& a, hipStream_t s)
 {
     switch (p.dtype) {

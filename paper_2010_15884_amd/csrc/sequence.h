@@ -188,6 +188,10 @@ struct NormArgs {
     float* workspace;
 };
 
+// The kernels that a call takes: rows a lane of the causal convolution, spans a chunk of the scan's gradients.
+int causal_conv_rows_a_lane(const sys_causal_conv1d_t& p);
+int scan_grad_spans(const sys_selective_scan_t& p);
+
 hipError_t launch_causal_conv(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s);
 hipError_t launch_causal_conv_grad(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s);
 hipError_t launch_causal_conv_step(const sys_causal_conv1d_t& p, const CausalConvArgs& a, hipStream_t s);
