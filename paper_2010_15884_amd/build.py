@@ -70,7 +70,7 @@ def build_c_demo(verbose: bool = True) -> str:
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
 # argument checks, the design planner, the tap scaling, the shapes of launches and workspaces
-HOST_LOGIC = ["api.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip", "group_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
+HOST_LOGIC = ["api.hip", "causal_conv.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip", "group_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
 
 
 def build_host_sanitized(verbose: bool = True, driver: str = "abi_san_driver") -> str:
