@@ -135,6 +135,15 @@ struct OwnColumn {
     }
 };
 
+// What the lanes of a wavefront have written to LDS can be read by its others from here on.  Its accesses are carried out in order, so this only keeps the compiler
+// from moving them; no instruction comes of it.
+__device__ __forceinline__ void wavefront_sees_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <typename F>
 __device__ __forceinline__ void four_steps(F&& f)
 {
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
     const float* sums = ends + w.sums + entry * shape.spans * p.channels + at.channel;
     typedef float F4 __attribute__((ext_vector_type(4)));
     __shared__ __attribute__((aligned(16))) float tile_b[kRows * kWidth], tile_c[kRows * kWidth];
-    // s, x and e of a span: written by the lane that owns a position, read by the four of its channel, which are of one wavefront (no barrier)
+    // s, x and e of a span: written by the lane that owns a position, read by the four of its channel, which are of one wavefront (no barrier of the workgroup)
     __shared__ F4 steps[kS][kScanChannels];
     __shared__ __attribute__((aligned(16))) float parts[kParts][kS * 2 * kWidth];   // sums over channels: [position][dB | dC][state]
 
@@ -374,6 +383,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_grad_kernel(sys_selective_s
             }
             steps[4 * k + part][own_channel] = F4{own_s[k], own_s[k] * own_u[k], own_e[k], 0.0f};
         }
+        wavefront_sees_lds();
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             const float from_start = at.there ? next_state[i] : 0.0f;
