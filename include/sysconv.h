@@ -276,8 +276,15 @@ int sys_conv2d_has(int projection, int kh, int kw);
  * that a tensor may be a part of the columns of a wider projection.  Inputs may have any strides
  * (0 for a row or batch that is used again); rows and batches of an output must not overlap.
  * Elements are fp32, fp16 or bf16 (sys_dtype_t); sums, statistics, exponentials and states are
- * fp32, and each result is rounded once, where it is stored.  Results do not depend on the run:
- * there are no atomic sums.
+ * fp32 (64 bits where a group norm combines its chunks), and each result is rounded once, where it
+ * is stored.  Results do not depend on the run: there are no atomic sums.
+ *
+ * e^x is the base-2 exponential instruction of a product, off by some (|x| + 3) 2^-24 of itself where
+ * a library's is off by one or two units: sigmoid(x) and the SiLU by (|x| + 6) 2^-24, a decay
+ * e^(s A) by |s A| as much.  softplus keeps its relative accuracy (8 units) down to e^x of the smallest
+ * normal number.  A NaN or infinity goes where the formula takes it, but where the formula has an
+ * infinity the scan may give a NaN (states are worked on in fours, sixteens and so on, and infinity times
+ * the 0 of one that is not there is a NaN).
  *
  * As everywhere in this library a call validates its arguments before the first HIP call, only
  * enqueues kernels on `stream`, allocates nothing and keeps nothing.  Some of these operators

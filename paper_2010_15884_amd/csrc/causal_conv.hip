@@ -6,9 +6,9 @@
 // All three are bound by memory: K <= 8 multiply-adds an element beside 4 to 12 bytes.  A lane owns 16 bytes of neighbouring channels
 // and walks down the rows, so every load and store of a wavefront is a contiguous piece of a row and the taps stay in registers.
 //
-// Measured, bf16, 4 taps, SiLU: 2 x 4096 positions x 4096 channels 26.5 us, 5.1 TB/s of the bytes of x and y (a copy of as many: 22 us);
-// gradients of 4 x 2048 x 4096 52.8 us, 3.8 TB/s of x, dy and dx (47.4 the kernel, 4.7 the sums of the taps' parts);
-// 8 tokens of 2048 channels 3.3 us, a launch.
+// Measured, bf16, 4 taps, SiLU: 2 x 4096 positions x 4096 channels 24.7 us, 5.4 TB/s of the bytes of x and y (a copy of as many: 22 us);
+// gradients of 4 x 2048 x 4096 50.5 us, 4.0 TB/s of x, dy and dx (by the profiler about 48 the kernel, 5 the sums of the taps' parts);
+// 8 tokens of 2048 channels some 3.5 us, a launch.
 #include <type_traits>
 
 #include "launch.h"

@@ -11,9 +11,11 @@
 // M2 = sum M2_i + n_i (mean_i - mean)^2.  Means stay in two parts until they have been subtracted: rounded to 32 bits they would bring their own size
 // into d.  No one value is taken off all the others, for it may be far from them, and its size would stay in the mean's last digit.
 //
-// Measured, bf16: 16 x 4096 x 512 in 32 groups with SiLU 32.2 us, 4.2 TB/s of x and y (a copy of as many bytes: 22; every CU holds one unit,
-// so all load, then all store, in pieces of 64 bytes); 8192 rows of 64 x 64 channels 27.4, 4.9 TB/s, their gradients 50, 4.0 TB/s of x, dy
-// and dx; gradients of 8 x 4096 x 320 in 32 groups, f16, in chunks 33.6 = 14.7 sums + 7.2 combining + 13.4 dx, less what overlaps.
+// Measured, bf16: 16 x 4096 x 512 in 32 groups with SiLU 31.8 us, 4.2 TB/s of x and y (a copy of as many bytes: 22; every CU holds one unit,
+// so all load, then all store, in pieces of 64 bytes); 8192 rows of 64 x 64 channels 26.6, 5.0 TB/s, their gradients 50, 4.0 TB/s of x, dy
+// and dx; gradients of 8 x 4096 x 320 in 32 groups, f16, in chunks 33.0, by the profiler about 15 sums, 7 combining and 14 dx.  Chunks of few wide groups
+// are far from their bytes: 1 x 16384 x 2048 in one group 1780 us, nearly all of it one workgroup that adds up [chunk][channel] (4 x 4096 x 320 in 32
+// groups: 17.4).
 #include <type_traits>
 
 #include "launch.h"

@@ -7,10 +7,11 @@
 // leaves SIMDs idle the positions are cut into chunks: one launch finds each chunk's end state from a zero start, the next one starts
 // every chunk from the states of those before it, combined in its prologue with e^(A sum s), and computes the outputs.
 //
-// Measured, bf16, 16 states, gated: one sequence of 4096 positions and channels (2^28 elements) 145 us = 59 for the end states + 88 for the outputs,
-// 5.1 and 7.9 vector instructions an element, VALUs 86 and 84 % busy, LDS 14 and 19; one sweep alone could take no less than 47.
-// Not faster: 8 or 32 positions a tile (151, 151), sixteen lanes a channel in one sweep without chunks (240 to 258: one wavefront a SIMD waits
-// for every step), the scheduler set on instruction-level parallelism.
+// Measured, bf16, 16 states, gated: one sequence of 4096 positions and channels (2^28 elements) 130 us; by the profiler 58 for the end states and 86 for
+// the outputs, 5.2 and 7.9 vector instructions an element, VALUs 85 % busy, LDS 14 and 19; one sweep alone could take no less than 47.
+// (The end state of the last chunk is worked out too, and not used.)
+// Not faster, when it took 145: 8 or 32 positions a tile (151, 151), sixteen lanes a channel in one sweep without chunks (240 to 258: one wavefront a
+// SIMD waits for every step), the scheduler set on instruction-level parallelism.
 #include "launch.h"
 #include "sequence.h"
 #include "scan_tile.h"
@@ -171,8 +172,8 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(sys_selective_scan_t
 
 // ---------------------------------------------------------------- single tokens
 
-// V neighbouring states a lane, `lanes` lanes (a power of two) a channel; the states are read and written once: bound by memory
-// (64 tokens of 4096 channels with 16 states, 34 MB of states and 1 MB else: 11.2 us, 3.1 TB/s; a call from the host takes 13).
+// V neighbouring states a lane, `lanes` lanes (a power of two) a channel; the states are read and written once.  64 tokens of 4096 channels with 16
+// states, 34 MB of states and 1 MB else: 11 us, 3.2 TB/s, with the VALUs three quarters busy, most of that with the indices' divisions; a call from the host 11.4.
 template <typename T, int V>
 __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(sys_selective_scan_t p, ScanArgs a, int log_lanes)
 {
@@ -229,9 +230,9 @@ ScanShape forward_shape(const sys_selective_scan_t& p, bool ragged)
     const long long workgroups = (long long)s.channel_blocks * p.batch;
     const int tiles = (p.length + kScanTile - 1) / kScanTile;
     // Chunks cost 1.65 times the work, so they begin where a wavefront a SIMD is not there; then sixteen wavefronts a CU, in chunks of at
-    // least two tiles (one sequence of 4096 positions and channels, eight / sixteen / thirty-two a CU: 161 / 149 / 153 us; with / without chunks
-    // 2 x 2048 x 4096 130 / 232, 4 x 2048 x 4096 237 / 257, 4 x 1024 x 4096 130 / 120, 6 x 1024 x 4096 189 / 169).  With lengths some chunks will be
-    // empty (seven sequences of 0 .. 517 positions, eight / sixteen / thirty-two a CU: 49 / 37 / 31).
+    // least two tiles (one sequence of 4096 positions and channels, eight / sixteen / thirty-two a CU: 148 / 131 / 131 us; with / without chunks
+    // 2 x 2048 x 4096 130 / 247, 4 x 2048 x 4096 246 / 248, 4 x 1024 x 4096 129 / 127, 6 x 1024 x 4096 197 / 171).  With lengths some chunks will be
+    // empty (seven sequences of 0 .. 517 positions, eight / sixteen / thirty-two a CU: 48 / 36 / 30).
     long long chunks = workgroups >= 256 ? 1 : (ragged ? 2048 : 1024) / (workgroups ? workgroups : 1);
     if (chunks > tiles / 2) chunks = tiles / 2;
     if (chunks > 64) chunks = 64;

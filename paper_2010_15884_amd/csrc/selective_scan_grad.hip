@@ -14,9 +14,9 @@
 //   scan_sums_kernel    adds up what the workgroups have summed over their channels (dB, dC) and their positions (dA, dD, ddelta_bias).
 // Each sum has a fixed order.
 //
-// Bound by the vector ALUs.  4 x 2048 positions x 2048 channels, 16 states, gated, bf16 (2^28 elements): 350 us = 94 ends (10.9 vector instructions
-// an element) + 11 chain + 254 grad (24.5; the VALUs 88 % busy) + 16 sums, less what the launches overlap; an exponential and fourteen
-// multiply-adds an element are 110 us.
+// Bound by the vector ALUs.  4 x 2048 positions x 2048 channels, 16 states, gated, bf16 (2^28 elements): 337 us; by the profiler about 95 ends (10.8 vector
+// instructions an element), 11 chain, 250 grad (24.6; the VALUs 88 % busy, 21 % of the LDS cycles bank conflicts that nothing here accounts for)
+// and 17 sums; an exponential and fourteen multiply-adds an element are 110 us.
 #include "launch.h"
 #include "sequence.h"
 #include "scan_tile.h"

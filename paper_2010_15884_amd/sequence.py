@@ -7,7 +7,10 @@ torch.  With ``stream`` (a hipStream_t) outputs and workspaces are allocated on 
 is done with them.
 
 Types, shapes and strides are checked and packed once for every combination that a program calls with (a "plan": what the C entry point is
-told, and the workspace's size); a later call with the same ones finds it by them, which leaves a third of the host time of a small call.
+told, and the workspace's size); a later call with the same ones finds it by them, which takes a third off the host time of a small call.
+
+Outputs carry no autograd graph, also where inputs require gradients: a model that trains calls the ``_backward`` functions, as the
+``torch.autograd.Function`` classes of examples/state_space_layer.py do.
 
 The functions are reached through ``binding`` (``binding.sys_causal_conv1d`` and so on).
 """
