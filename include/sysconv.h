@@ -441,6 +441,111 @@ int sys_group_norm_backward(const sys_group_norm_t *p, const void *d_dy, const v
 size_t sys_group_norm_backward_workspace(const sys_group_norm_t *p);
 
 /*
+ * ---- Operators of a gated delta rule layer -------------------------------------------------
+ *
+ * The scan's sibling whose state is a matrix a head, and the norm that its queries and keys (and those of other mixers) go through.
+ * Tensors are [batch, length, heads, dim]; the heads of a row lie next to each other, batch and row strides are the caller's, so that
+ * queries, keys and values may be columns of one projection.  Types, strides, lengths, slots, workspaces, errors: as above.
+ */
+typedef enum { SYS_NORM_RMS = 0, SYS_NORM_L2 = 1 } sys_head_norm_kind_t;
+
+#define SYS_MAX_HEAD_DIM 512     /* entries of a head that is normalised: 1 .. 512 */
+#define SYS_MAX_KEY_DIM 128      /* of a key of the delta rule: 1 .. 128 */
+#define SYS_MAX_VALUE_DIM 1024   /* of a value: 1 .. 1024 */
+
+typedef struct {
+    int dtype;                   /* of q, k, their results and gradients */
+    int param_dtype;             /* of the weights and their gradients: dtype or SYS_F32 */
+    int norm;                    /* a sys_head_norm_kind_t */
+    int rotary;                  /* entries of a head that are turned: even, 0 .. dim */
+    int interleaved;             /* 1: entries 2i and 2i+1 are a pair; 0: i and rotary/2 + i */
+    int batch, length;           /* >= 0 */
+    int q_heads, k_heads, dim;   /* k_heads 0: queries alone */
+    int positions;               /* rows of the tables */
+    float eps;                   /* >= 0 */
+    long long q_batch, q_row, k_batch, k_row;       /* strides of q and k */
+    long long yq_batch, yq_row, yk_batch, yk_row;   /* of the results (backward: of dyq and dyk) */
+} sys_head_norm_t;
+
+/*
+ * Norm of every head of q and k, and the rotation of its position in the same pass:
+ *   z = x w / sqrt(E[x^2] + eps)  (SYS_NORM_RMS),  x w / sqrt(sum x^2 + eps)  (SYS_NORM_L2),
+ *   y = z, with each pair (a, b) of the first `rotary` entries replaced by (a cos - b sin, b cos + a sin)
+ *   d_q, d_yq  [batch, length, q_heads, dim];  d_k, d_yk  [batch, length, k_heads, dim] (none with k_heads 0)
+ *   d_wq, d_wk (optional)  [dim]
+ *   d_cos, d_sin  [positions, rotary/2] fp32 (where rotary > 0): pair i at position p turns by the angle of row p, column i
+ *   d_positions (optional)  [batch, length]: the table's row of each token; one outside 0 .. positions-1 marks a token that is not
+ *            there: its rows are 0, and so are its gradients.  Without it position t is row t (length <= positions: SYS_ERR_SIZE).
+ *   Rows behind a sequence's length are 0.
+ */
+int sys_head_norm(const sys_head_norm_t *p, const void *d_q, const void *d_k, const void *d_wq, const void *d_wk,
+                  const float *d_cos, const float *d_sin, const int *d_positions, const int *d_lengths,
+                  void *d_yq, void *d_yk, hipStream_t stream);
+
+/*
+ * Its gradients: d_dq, d_dk like q and k, contiguous; d_dwq, d_dwk like the weights (optional; each needs its weights).  The
+ * sizes of the heads are worked out again from q and k.
+ */
+int sys_head_norm_backward(const sys_head_norm_t *p, const void *d_dyq, const void *d_dyk, const void *d_q, const void *d_k,
+                           const void *d_wq, const void *d_wk, const float *d_cos, const float *d_sin, const int *d_positions,
+                           const int *d_lengths, void *d_dq, void *d_dk, void *d_dwq, void *d_dwk, void *d_workspace,
+                           hipStream_t stream);
+size_t sys_head_norm_backward_workspace(const sys_head_norm_t *p);
+
+typedef struct {
+    int dtype;                              /* of q, k, v, delta, beta, y and their gradients */
+    int softplus;                           /* 1: step sizes are softplus(delta + bias); 0: delta + bias */
+    int sigmoid;                            /* 1: strengths are 1 / (1 + e^-beta); 0: beta */
+    int batch, length;                      /* >= 0 */
+    int key_heads, value_heads;             /* value head h uses key head h / (value_heads / key_heads) */
+    int key_dim, value_dim;
+    int slots;                              /* sys_gated_delta_rule_update: states in d_state; else ignored */
+    float scale;                            /* of the queries */
+    int reserved;                           /* 0 */
+    long long q_batch, q_row, k_batch, k_row, v_batch, v_row;
+    long long delta_batch, delta_row, beta_batch, beta_row;
+    long long y_batch, y_row;               /* strides of y (backward: of dy) */
+} sys_gated_delta_t;
+
+/*
+ * Gated delta rule: for every sequence and value head, a state S of key_dim x value_dim (column S[., c] belongs to entry c of the values)
+ *   s_t = softplus(delta_t + delta_bias),  a_t = e^(s_t A),  b_t = 1 / (1 + e^-beta_t),
+ *   u_t = b_t (v_t - a_t S_{t-1}^T k_t),   S_t = a_t S_{t-1} + k_t u_t^T,   y_t = scale * S_t^T q_t
+ *   d_q, d_k  [batch, length, key_heads, key_dim];  d_v, d_y  [batch, length, value_heads, value_dim]
+ *   d_delta, d_beta  [batch, length, value_heads];  d_A  [value_heads] fp32;  d_delta_bias (optional)  [value_heads] fp32
+ *   d_state  [batch, value_heads, key_dim, value_dim] fp32 (optional): S before the first position; zeros without it
+ *   d_state_out  like d_state (optional, written): S behind the last one
+ *   SYS_ERR_UNSUPPORTED  dimensions beyond the limits above, rows further apart than SYS_MAX_SCAN_ROW elements, pointers off their element's alignment
+ *   SYS_ERR_SIZE  negative sizes, no heads, key heads that do not divide the value heads, strides of y that make rows overlap
+ * Keys are meant to have a length of about one (sys_head_norm, SYS_NORM_L2): with b_t |k_t|^2 > 2 the recurrence itself grows.
+ */
+int sys_gated_delta_rule(const sys_gated_delta_t *p, const void *d_q, const void *d_k, const void *d_v, const void *d_delta,
+                         const float *d_A, const void *d_beta, const float *d_delta_bias, const float *d_state, const int *d_lengths,
+                         void *d_y, float *d_state_out, void *d_workspace, hipStream_t stream);
+size_t sys_gated_delta_rule_workspace(const sys_gated_delta_t *p);
+
+/*
+ * Its gradients.  d_dy [batch, length, value_heads, value_dim]; d_dstate_out (optional): gradient of state_out.
+ * Written, all contiguous: d_dq, d_dk (summed over the value heads of a key head), d_dv, d_ddelta, d_dbeta like their inputs; d_dA, d_ddelta_bias (optional;
+ * it needs d_delta_bias) [value_heads] fp32; d_dstate like d_state (optional; it needs d_state).
+ */
+int sys_gated_delta_rule_backward(const sys_gated_delta_t *p, const void *d_dy, const void *d_q, const void *d_k, const void *d_v,
+                                  const void *d_delta, const float *d_A, const void *d_beta, const float *d_delta_bias,
+                                  const float *d_state, const int *d_lengths, const float *d_dstate_out, void *d_dq, void *d_dk,
+                                  void *d_dv, void *d_ddelta, float *d_dA, void *d_dbeta, float *d_ddelta_bias, float *d_dstate,
+                                  void *d_workspace, hipStream_t stream);
+size_t sys_gated_delta_rule_backward_workspace(const sys_gated_delta_t *p);
+
+/*
+ * One token for each of `batch` requests (length and the row strides are ignored): q, k [batch, key_heads, key_dim], v, y [batch,
+ * value_heads, value_dim], delta, beta [batch, value_heads], d_state [slots, value_heads, key_dim, value_dim] fp32; slots as
+ * sys_causal_conv1d_update.
+ */
+int sys_gated_delta_rule_update(const sys_gated_delta_t *p, const void *d_q, const void *d_k, const void *d_v, const void *d_delta,
+                                const float *d_A, const void *d_beta, const float *d_delta_bias, const float *d_state,
+                                const int *d_slots, void *d_y, float *d_state_out, hipStream_t stream);
+
+/*
  * Plain device-to-device copy of n floats with 16-byte accesses.  It is the
  * yard-stick the benchmark prints beside every convolution ("what the memory
  * system gives a streaming kernel of this footprint") and the kernel of known

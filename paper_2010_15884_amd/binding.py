@@ -359,9 +359,11 @@ def sys_version() -> int:
 
 
 # the operators on channels-last sequences
-from .sequence import (ACTIVATIONS, SYS_ACT_NONE, SYS_ACT_RELU, SYS_ACT_SILU, SYS_BF16, SYS_F16, SYS_F32,  # noqa: E402, F401
-                       SYS_MAX_CAUSAL_WIDTH, SYS_MAX_STATES, ScanGradients, sys_causal_conv1d, sys_causal_conv1d_backward,
-                       sys_causal_conv1d_update, sys_group_norm, sys_group_norm_backward, sys_selective_scan,
+from .sequence import (ACTIVATIONS, NORMS, SYS_ACT_NONE, SYS_ACT_RELU, SYS_ACT_SILU, SYS_BF16, SYS_F16, SYS_F32,  # noqa: E402, F401
+                       SYS_MAX_CAUSAL_WIDTH, SYS_MAX_HEAD_DIM, SYS_MAX_KEY_DIM, SYS_MAX_STATES, SYS_MAX_VALUE_DIM, SYS_NORM_L2,
+                       SYS_NORM_RMS, DeltaGradients, ScanGradients, sys_causal_conv1d, sys_causal_conv1d_backward,
+                       sys_causal_conv1d_update, sys_gated_delta_rule, sys_gated_delta_rule_backward, sys_gated_delta_rule_update,
+                       sys_group_norm, sys_group_norm_backward, sys_head_norm, sys_head_norm_backward, sys_selective_scan,
                        sys_selective_scan_backward, sys_selective_scan_update)
 from .sequence import EXPORTS as _SEQUENCE_EXPORTS  # noqa: E402
 

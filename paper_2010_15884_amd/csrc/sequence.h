@@ -188,6 +188,23 @@ struct NormArgs {
     float* workspace;
 };
 
+struct HeadNormArgs {
+    const void *q, *k, *wq, *wk, *dyq, *dyk;
+    const float *cosine, *sine;
+    const int *positions, *lengths;
+    void *yq, *yk, *dwq, *dwk;         // backward: yq, yk are dq, dk
+    float* workspace;
+};
+
+struct DeltaArgs {
+    const void *q, *k, *v, *delta, *beta, *dy;
+    const float *a, *delta_bias, *state, *dstate_out;
+    const int *lengths, *slots;
+    void *y, *dq, *dk, *dv, *ddelta, *dbeta;
+    float *state_out, *da, *ddelta_bias, *dstate;
+    void* workspace;
+};
+
 // The kernels that a call takes: rows a lane of the causal convolution, spans a chunk of the scan's gradients.
 int causal_conv_rows_a_lane(const sys_causal_conv1d_t& p);
 int scan_grad_spans(const sys_selective_scan_t& p);
@@ -207,5 +224,15 @@ hipError_t launch_group_norm(const sys_group_norm_t& p, const NormArgs& a, hipSt
 hipError_t launch_group_norm_grad(const sys_group_norm_t& p, const NormArgs& a, hipStream_t s);
 size_t group_norm_workspace(const sys_group_norm_t& p);
 size_t group_norm_grad_workspace(const sys_group_norm_t& p);
+
+hipError_t launch_head_norm(const sys_head_norm_t& p, const HeadNormArgs& a, hipStream_t s);
+hipError_t launch_head_norm_grad(const sys_head_norm_t& p, const HeadNormArgs& a, hipStream_t s);
+size_t head_norm_grad_workspace(const sys_head_norm_t& p);
+
+hipError_t launch_delta(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_grad(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_step(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s);
+size_t delta_workspace(const sys_gated_delta_t& p);
+size_t delta_grad_workspace(const sys_gated_delta_t& p);
 
 }  // namespace sysconv

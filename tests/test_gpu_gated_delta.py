@@ -1,0 +1,178 @@
+"""The gated delta rule against its recurrence in 64 bits (tests/delta_reference.py has the tolerances' derivation)."""
+import pytest
+import torch
+
+import delta_reference as D
+import sequence_reference as R
+from paper_2010_15884_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+INPUTS = ("q", "k", "v", "delta", "A", "beta", "delta_bias")
+
+
+def _make(seed, batch, length, key_heads, heads, key_dim, value_dim, dtype, bias=True, state=False, lengths=None, odd=3):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    unit = lambda t: 0.99 * t / t.norm(dim=-1, keepdim=True)  # noqa: E731
+    row = rand(batch, length, odd + 2 * key_heads * key_dim + heads * value_dim)
+    qk = row[..., odd:odd + 2 * key_heads * key_dim].unflatten(-1, (2 * key_heads, key_dim))
+    # keys that lie close to each other, as they do behind an activation
+    qk.copy_(unit(qk + 0.7))
+    row = row.to(dtype)
+    at = lambda a, h, d: row[..., odd + a:odd + a + h * d].unflatten(-1, (h, d))  # noqa: E731
+    c = {"q": at(0, key_heads, key_dim), "k": at(key_heads * key_dim, key_heads, key_dim), "v": at(2 * key_heads * key_dim, heads, value_dim)}
+    gates = rand(batch, length, 2 * heads).to(dtype)
+    c["delta"], c["beta"] = gates.split(heads, dim=-1)
+    c["A"] = -torch.rand(heads, generator=g, device="cuda") * 1.5
+    c["A"][:1] = 0.0                               # a head that forgets nothing by itself
+    c["delta_bias"] = 0.5 * rand(heads) - 2.0 if bias else None
+    c["state"] = rand(batch, heads, key_dim, value_dim) if state else None
+    c["dy"] = rand(batch, length, heads * value_dim + 1).to(dtype)[..., 1:].unflatten(-1, (heads, value_dim))
+    c["dstate_out"] = rand(batch, heads, key_dim, value_dim) if state else None
+    if lengths is not None:
+        for b, n in enumerate(lengths):
+            for name, bad in (("q", "nan"), ("k", "inf"), ("v", "nan"), ("delta", "inf"), ("beta", "nan"), ("dy", "-inf")):
+                c[name][b, max(n, 0):] = float(bad)
+    c["lengths"] = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    return c
+
+
+def _forward(c, **more):
+    out = torch.full((c["v"].shape[0], c["v"].shape[2], c["q"].shape[3], c["v"].shape[3]), float("nan"), device="cuda")
+    how = dict(dict(softplus=True, sigmoid=True), **more)
+    y = B.sys_gated_delta_rule(*[c[n] for n in INPUTS], d_state=c["state"], d_state_out=out, d_lengths=c["lengths"], **how)
+    return y, out
+
+
+def _reference(c, grad=False, softplus=True, sigmoid=True, scale=None):
+    return D.gated_delta(*[c[n] for n in INPUTS], scale=scale, softplus=softplus, sigmoid_beta=sigmoid, state=c["state"],
+                         lengths=None if c["lengths"] is None else c["lengths"].tolist(), dy=c["dy"] if grad else None,
+                         dstate_out=c["dstate_out"] if grad else None)
+
+
+def _steps(c):
+    return min(c["q"].shape[1], 32) + c["q"].shape[1] // 64 + 1          # positions of a short sequence, else blocks: no more than this
+
+
+def _check_forward(c, **how):
+    want = _reference(c, **how)
+    allowed = D.delta_allowed(dict(c, dy=None, scale=how.get("scale")), want, _steps(c), c["q"].dtype)
+    y, state = _forward(c, **how)
+    R.check(state, want["state"], allowed["state"], "state")
+    R.check(y, want["y"], allowed["y"], "y")
+
+
+CASES = [
+    # batch, length, key heads, heads, key dim, value dim, dtype, bias, state, lengths
+    (1, 1, 1, 1, 1, 1, F32, True, True, None),
+    (2, 1, 2, 4, 128, 128, BF16, True, True, None),
+    (1, 5, 1, 2, 64, 64, F16, False, False, None),
+    (2, 33, 2, 2, 16, 8, F32, True, True, None),
+    (1, 64, 1, 1, 32, 33, F32, True, False, None),
+    (2, 65, 1, 3, 128, 64, BF16, True, True, None),
+    (1, 63, 2, 2, 40, 72, F16, True, True, None),
+    (2, 130, 1, 2, 127, 130, F32, True, True, None),
+    (1, 200, 3, 3, 65, 100, BF16, False, True, None),
+    (3, 129, 1, 1, 128, 16, F16, True, False, None),
+    (1, 128, 1, 4, 24, 256, F32, True, True, None),
+    (4, 150, 2, 4, 64, 48, F32, True, True, [150, 0, 1, 64]),
+    (3, 100, 1, 2, 128, 40, BF16, True, False, [65, -5, 999]),
+    (3, 20, 1, 2, 20, 12, F16, True, True, [3, 20, 0]),
+    (1, 16, 1, 1, 128, 1024, BF16, True, True, None),
+]
+ids = lambda c: "-".join(str(v) for v in c[:7]).replace("torch.", "")  # noqa: E731
+
+
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_forward(case):
+    _check_forward(_make(sum(case[:6]), *case))
+
+
+def test_step_sizes_and_strengths_as_they_come():
+    c = _make(31, 2, 90, 2, 2, 64, 64, F32, bias=False, state=True)
+    c["delta"], c["beta"] = c["delta"].abs() * 0.1, torch.rand_like(c["beta"])
+    _check_forward(c, softplus=False, sigmoid=False, scale=-0.7)
+
+
+def test_chunks_of_a_long_sequence():
+    _check_forward(_make(32, 1, 1111, 1, 2, 48, 24, F32, state=True))
+    _check_forward(_make(33, 2, 600, 1, 1, 128, 32, BF16, lengths=[600, 431]))
+
+
+def test_decays_that_leave_nothing():
+    """Steps so large that a ratio of decays underflows, followed by small ones."""
+    c = _make(34, 1, 200, 1, 2, 32, 32, F32, bias=False, state=True)
+    c["A"] = torch.tensor([-1.0, -3.0], device="cuda")
+    c["delta"] = torch.full((1, 200, 2), 0.01, device="cuda")
+    c["delta"][0, 70:75] = 60.0
+    c["delta"][0, 130] = 1e30
+    want = _reference(c, softplus=False)
+    assert torch.isfinite(want["y"]).all()
+    allowed = D.delta_allowed(dict(c, dy=None), want, _steps(c) + 64, F32)
+    y, state = _forward(c, softplus=False)
+    R.check(state, want["state"], allowed["state"], "state")
+    R.check(y, want["y"], allowed["y"], "y")
+
+
+def _step(c, state, **more):
+    first = {n: c[n] if n in ("A", "delta_bias") else c[n][:, 0] for n in INPUTS}
+    how = dict(dict(softplus=True, sigmoid=True), **more)
+    return B.sys_gated_delta_rule_update(*[first[n] for n in INPUTS[:6]], state, first["delta_bias"], **how)
+
+
+@pytest.mark.parametrize("dtype,key_dim,value_dim", [(F32, 64, 64), (BF16, 128, 128), (F16, 50, 30), (F32, 1, 1), (BF16, 100, 65), (F16, 128, 200)])
+def test_single_tokens(dtype, key_dim, value_dim):
+    c = _make(41, 5, 1, 2, 4, key_dim, value_dim, dtype, state=True)
+    want = _reference(c)
+    allowed = D.delta_allowed(dict(c, dy=None), want, 1, dtype)
+    cache = torch.randn((9, 4, key_dim, value_dim), device="cuda")
+    order = [7, 0, 3, 8, 1]
+    slots = torch.tensor(order, dtype=torch.int32, device="cuda")
+    cache[order] = c["state"]
+    before, other = cache.clone(), torch.full_like(cache, 5.0)
+    y = _step(c, cache, d_slots=slots, d_state_out=other)
+    assert torch.equal(cache, before)
+    R.check(y, want["y"][:, 0], allowed["y"][:, 0], "y")
+    R.check(other[order], want["state"], allowed["state"], "state")
+    rest = [i for i in range(9) if i not in order]
+    assert (other[rest] == 5.0).all()
+    again = _step(c, cache, d_slots=slots)                              # in place
+    assert torch.equal(again, y) and torch.equal(cache[order], other[order]) and torch.equal(cache[rest], before[rest])
+    plain = c["state"].clone()
+    assert torch.equal(_step(c, plain), y) and torch.equal(plain, other[order])
+
+
+def test_requests_that_are_not_there():
+    c = _make(42, 4, 1, 1, 2, 64, 68, BF16, state=True)
+    cache = torch.randn((3, 2, 64, 68), device="cuda")
+    before = cache.clone()
+    y = _step(c, cache, d_slots=torch.tensor([2, -1, 3, 2 ** 31 - 1], dtype=torch.int32, device="cuda"))
+    assert (y[1:] == 0).all() and not (y[0] == 0).all()
+    assert torch.equal(cache[:2], before[:2]) and not torch.equal(cache[2], before[2])
+
+
+def test_prompts_continue_token_by_token():
+    c = _make(43, 2, 150, 2, 4, 64, 64, F32, state=True)
+    y, state = _forward(c)
+    part = {n: c[n] if n in ("A", "delta_bias", "state") else (None if c[n] is None else c[n][:, :147]) for n in (*INPUTS, "state", "lengths")}
+    head, cache = _forward(part)
+    scale = float(y.abs().max())
+    assert float((head - y[:, :147]).abs().max()) < 1e-5 * scale
+    for t in range(147, 150):
+        one = {n: c[n] if n in ("A", "delta_bias") else c[n][:, t:t + 1] for n in INPUTS}
+        got = _step(one, cache)
+        assert float((got - y[:, t]).abs().max()) < 1e-5 * scale
+    assert float((cache - state).abs().max()) < 1e-5 * float(state.abs().max())
+
+
+def test_empty():
+    c = _make(44, 2, 3, 1, 2, 16, 8, F32, state=True)
+    cut = {n: c[n] if n in ("A", "delta_bias", "state", "lengths") else c[n][:, :0] for n in (*INPUTS, "state", "lengths")}
+    y, state = _forward(cut)
+    assert y.shape[1] == 0 and torch.equal(state, c["state"])
+    y, state = _forward(dict(cut, state=None))
+    assert (state == 0).all()
+    none = {n: c[n] if n in ("A", "delta_bias") or c[n] is None else c[n][:0] for n in (*INPUTS, "state", "lengths")}
+    assert _forward(none)[0].shape[0] == 0
