@@ -452,6 +452,7 @@ typedef enum { SYS_NORM_RMS = 0, SYS_NORM_L2 = 1 } sys_head_norm_kind_t;
 #define SYS_MAX_HEAD_DIM 512     /* entries of a head that is normalised: 1 .. 512 */
 #define SYS_MAX_KEY_DIM 128      /* of a key of the delta rule: 1 .. 128 */
 #define SYS_MAX_VALUE_DIM 1024   /* of a value: 1 .. 1024 */
+#define SYS_MAX_DELTA_ROW ((1LL << 24) - 1)  /* elements from row to row of the delta rule's tensors */
 
 typedef struct {
     int dtype;                   /* of q, k, their results and gradients */
@@ -515,7 +516,7 @@ typedef struct {
  *   d_delta, d_beta  [batch, length, value_heads];  d_A  [value_heads] fp32;  d_delta_bias (optional)  [value_heads] fp32
  *   d_state  [batch, value_heads, key_dim, value_dim] fp32 (optional): S before the first position; zeros without it
  *   d_state_out  like d_state (optional, written): S behind the last one
- *   SYS_ERR_UNSUPPORTED  dimensions beyond the limits above, rows further apart than SYS_MAX_SCAN_ROW elements, pointers off their element's alignment
+ *   SYS_ERR_UNSUPPORTED  dimensions beyond the limits above, rows further apart than SYS_MAX_DELTA_ROW elements, pointers off their element's alignment
  *   SYS_ERR_SIZE  negative sizes, no heads, key heads that do not divide the value heads, strides of y that make rows overlap
  * Keys are meant to have a length of about one (sys_head_norm, SYS_NORM_L2): with b_t |k_t|^2 > 2 the recurrence itself grows.
  */

@@ -1,0 +1,606 @@
+// Gated delta rule in chunks of 64 positions on the matrix cores (delta_tile.h has the formulas, the precision and the layout).
+//
+// Two launches.  The first makes X, P and K^T of all chunks side by side, a workgroup a chunk of a value head.  The second goes through the chunks: a workgroup
+// of four wavefronts a tile of value columns, the state in registers (wavefront w the rows of step w of the keys), S, R and U handed round as bf16
+// parts through LDS with three barriers a chunk; operands that do not depend on the state are loaded a chunk ahead.
+#include "delta_tile.h"
+#include "launch.h"
+
+namespace sysconv {
+namespace {
+
+// ---------------------------------------------------------------- the chunks' matrices
+
+template <typename T, int KD, bool GRAD>
+__global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+{
+    constexpr int NX = kInputParts<T>, KS = KD / 32, RP = kResultParts<T>, kPitch = KD + 8, kSide = kChunk + 4;
+    const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, head = rest % p.value_heads, b = rest / p.value_heads;
+    const int shared = p.value_heads / p.key_heads, key_head = head / shared;
+    const bool first = head % shared == 0;         // of the value heads of a key head: it writes what they have in common
+    const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
+    if (rows <= 0) return;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
+
+    __shared__ __attribute__((aligned(16))) bf16_t keys[NX][kChunk][kPitch];
+    __shared__ __attribute__((aligned(16))) float am[kChunk][kSide], xm[kChunk][kSide];
+    __shared__ double sums[kChunk];                // of the logarithms of the decays, to base 2
+    __shared__ float strengths[kChunk];
+
+    // K into LDS
+    const T* k = (const T*)a.k + b * p.k_batch + t0 * p.k_row + key_head * p.key_dim;
+    const T* q = (const T*)a.q + b * p.q_batch + t0 * p.q_row + key_head * p.key_dim;
+    for (int i = tid; i < kChunk * KD / 8; i += kDeltaThreads) {
+        const int row = i / (KD / 8), at = i % (KD / 8) * 8;
+        float v[8];
+        b8 parts[NX];
+        load_eight(k + row * p.k_row, at, p.key_dim, row < rows, v);
+        split8(v, parts);
+#pragma unroll
+        for (int n = 0; n < NX; ++n) {
+            *(b8*)&keys[n][row][at] = parts[n];
+            if (first) *(b8*)(w.k + (kc * NX + n) * kChunk * KD + row * KD + at) = parts[n];
+        }
+    }
+    // the rows of Q that this wavefront works on
+    b8 qa[KS][NX];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const int row = 16 * wave + r, at = 32 * s + 8 * g;
+        float v[8];
+        load_eight(q + row * p.q_row, at, p.key_dim, row < rows, v);
+        split8(v, qa[s]);
+        if (first && !GRAD) {
+#pragma unroll
+            for (int n = 0; n < NX; ++n) *(b8*)(w.q + (kc * NX + n) * kChunk * KD + row * KD + at) = qa[s][n];
+        }
+    }
+    if (wave == 0) {
+        float step = 0.0f, strength = 0.0f;
+        if (lane < rows) {
+            step = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? a.delta_bias[head] : 0.0f);
+            strength = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
+            if (p.softplus) step = softplus(step);
+            if (p.sigmoid) strength = sigmoid(strength);
+        }
+        // in 64 bits: a ratio of decays is the exponential of a small difference of what may be large sums.  A decay of 2^-10000 is 0 as any smaller one, and
+        // leaves the differences behind it their digits (NaN passes)
+        double sum = (double)step * (double)a.a[head] * 1.4426950408889634;
+        sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const double other = __shfl_up(sum, m);
+            if (lane >= m) sum += other;
+        }
+        const double end = __shfl(sum, 63);
+        sums[lane] = sum;
+        strengths[lane] = strength;
+        float* out = w.scalars + vc * kScalars * kChunk;
+        out[kGamma * kChunk + lane] = fast_exp2((float)sum);
+        out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
+        out[kStrength * kChunk + lane] = strength;
+    }
+    __syncthreads();
+
+    // K K^T and Q K^T, rows of this wavefront (as they lie), columns up to its own; scaled and cut to triangles
+    b8 ka[KS][NX];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int n = 0; n < NX; ++n) ka[s][n] = *(const b8*)&keys[n][16 * wave + r][32 * s + 8 * g];
+    double row_sum[4];
+    float row_strength[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) row_sum[e] = sums[16 * wave + 4 * g + e], row_strength[e] = strengths[16 * wave + 4 * g + e];
+    constexpr int kKeptParts = GRAD ? 3 : RP;
+    bf16_t* const kept = GRAD ? w.pt : w.p;
+    for (int n = 0; n <= (GRAD ? 3 : wave | 1); ++n) {
+        f4 kk = {}, qk = {};
+        if (n <= wave) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                b8 kb[NX];
+#pragma unroll
+                for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][16 * n + r][32 * s + 8 * g];
+                kk = multiply<2>(ka[s], kb, kk);
+                qk = multiply<2>(qa[s], kb, qk);
+            }
+        }
+        const int column = 16 * n + r;
+        const double column_sum = sums[column];
+        f4 mixed;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = 16 * wave + 4 * g + e;
+            const float ratio = fast_exp2((float)(row_sum[e] - column_sum));
+            if (n <= wave) am[row][column] = column < row ? row_strength[e] * (ratio * kk[e]) : 0.0f;
+            mixed[e] = column <= row ? p.scale * (ratio * qk[e]) : 0.0f;
+        }
+        u2 parts[kKeptParts];
+        split4(mixed, parts);
+#pragma unroll
+        for (int m = 0; m < kKeptParts; ++m) {
+            bf16_t* plane = kept + (vc * kKeptParts + m) * kSquare;
+            if (GRAD) {
+                *(u2*)(plane + column * kChunk + 16 * wave + 4 * g) = parts[m];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) plane[(16 * wave + 4 * g + e) * kChunk + column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+            }
+        }
+    }
+    // K^T, eight positions at a time
+    if (first) {
+        for (int i = tid; i < KD * kChunk / 8; i += kDeltaThreads) {
+            const int d = i % KD, at = i / KD * 8;
+#pragma unroll
+            for (int n = 0; n < NX; ++n) {
+                b8 v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = keys[n][at + j][d];
+                *(b8*)(w.kt + (kc * NX + n) * kChunk * KD + d * kChunk + at) = v;
+            }
+        }
+    }
+    __syncthreads();
+    if (GRAD && first) {
+        // Q^T the same way, through the place of K
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int n = 0; n < NX; ++n) *(b8*)&keys[n][16 * wave + r][32 * s + 8 * g] = qa[s][n];
+    }
+
+    // X: the 16 x 16 blocks on the diagonal by substitution, a column a lane (four times over) ...
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        x[i] = i == r ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) x[i] = __builtin_fmaf(-am[16 * wave + i][16 * wave + j], x[j], x[i]);
+    }
+    if (g == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) xm[16 * wave + i][16 * wave + r] = x[i];
+    }
+    __syncthreads();
+    if (GRAD && first) {
+        for (int i = tid; i < KD * kChunk / 8; i += kDeltaThreads) {
+            const int d = i % KD, at = i / KD * 8;
+#pragma unroll
+            for (int n = 0; n < NX; ++n) {
+                b8 v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = keys[n][at + j][d];
+                *(b8*)(w.qt + (kc * NX + n) * kChunk * KD + d * kChunk + at) = v;
+            }
+        }
+    }
+    // ... and those below, X_ij = -X_ii (sum_k A_ik X_kj), a column of blocks a wavefront, in fp32
+    f4 column[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) column[0][e] = xm[16 * wave + 4 * g + e][16 * wave + r];
+#pragma unroll
+    for (int d = 1; d < 4; ++d) {
+        const int i = wave + d;
+        if (i < 4) {
+            f4 sum = {}, block = {};
+#pragma unroll
+            for (int m = 0; m < d; ++m) {
+                const f4 v = *(const f4*)&am[16 * i + r][16 * (wave + m) + 4 * g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], column[m][e], sum, 0, 0, 0);
+            }
+            const f4 v = *(const f4*)&xm[16 * i + r][16 * i + 4 * g];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) block = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], sum[e], block, 0, 0, 0);
+            column[d] = -block;
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 4; ++d)
+        if (wave + d < 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) xm[16 * (wave + d) + 4 * g + e][16 * wave + r] = column[d][e];
+        }
+    for (int i = 0; i < wave; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) xm[16 * i + 4 * g + e][16 * wave + r] = 0.0f;
+    __syncthreads();
+    for (int turn = 0; turn < (GRAD ? 2 : 1); ++turn) {
+        const int row = tid >> 2, at = (tid & 3) * 16;
+        bf16_t* out = (turn ? w.xt : w.x) + vc * 3 * kSquare + row * kChunk + at;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[8];
+            b8 parts[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = turn ? xm[at + 8 * h + j][row] : xm[row][at + 8 * h + j];
+            split8(v, parts);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) *(b8*)(out + n * kSquare + 8 * h) = parts[n];
+        }
+    }
+}
+
+// ---------------------------------------------------------------- the sweep
+
+// Where a workgroup keeps B operands: [step][part][column tile], 1 KB each, 16 bytes a lane.
+template <int STEPS, int PARTS, int NT>
+struct Operands {
+    b8 v[STEPS][PARTS][NT][64];
+    // all of step `step` from two tiles of D that lie above each other, or half of it from one
+    __device__ __forceinline__ void put(int step, int n, int lane, f4 upper, f4 lower)
+    {
+        float both[8];
+        b8 parts[PARTS];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) both[e] = upper[e], both[4 + e] = lower[e];
+        split8(both, parts);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) v[step][m][n][lane] = parts[m];
+    }
+    __device__ __forceinline__ void put_half(int tile, int n, int lane, f4 d)
+    {
+        u2 parts[PARTS];
+        split4(d, parts);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) ((u2*)&v[tile >> 1][m][n][lane])[tile & 1] = parts[m];
+    }
+    __device__ __forceinline__ void take(int step, int n, int lane, b8 (&out)[PARTS]) const
+    {
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) out[m] = v[step][m][n][lane];
+    }
+};
+
+template <typename T, int KD, int NT, bool GRAD>
+__global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+{
+    constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64, RP = kResultParts<T>;
+    const unsigned place = xcd_place(blockIdx.x, gridDim.x);
+    const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
+    const int key_head = head / (p.value_heads / p.key_heads);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk;
+    const int steps = (wave >> 1) + 1;             // of X and P: what lies above their diagonals is zero
+    const int my_row = tile_row(wave, 4 * g);      // the first of this lane's four positions
+    int column[NT];
+    bool there[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) column[n] = (tile * NT + n) * 16 + r, there[n] = column[n] < p.value_dim;
+
+    __shared__ Operands<KS, 3, NT> states;
+    __shared__ Operands<2, 3, NT> misses, writes;
+    __shared__ Operands<2, RP, NT> values;
+
+    // the state
+    const size_t state_base = ((size_t)b * p.value_heads + head) * p.key_dim * p.value_dim;
+    const unsigned state_bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
+    f4 s[TW][NT];
+    {
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state + state_base), 0, a.state ? state_bytes : 0u, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                    s[i][n][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0));
+                }
+    }
+    auto put_state = [&] {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if constexpr (TW == 2) states.put(wave, n, lane, s[0][n], s[1][n]);
+            else states.put_half(wave, n, lane, s[0][n]);
+        }
+    };
+
+    ChunkRows<T> v((const T*)a.v + b * p.v_batch + head * p.value_dim, p.v_row, p.value_dim, 0, last);
+    ChunkRows<T> y(GRAD ? nullptr : (const T*)a.y + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, 0, p.length);
+    unsigned v_at[NT][4], y_at[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v_at[n][e] = there[n] ? v.offset(my_row + e, column[n]) : kNowhere;
+            y_at[n][e] = there[n] ? y.offset(my_row + e, column[n]) : kNowhere;
+        }
+    const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks;
+
+    b8 ka[KS][NX], qa[GRAD ? 1 : KS][NX], kta[TW][2][NX], xa[2][3], pa[2][RP];
+    unsigned next_v[NT][4];
+    f4 gamma, left, strength;
+    float end;
+    auto fetch_keys = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int n = 0; n < NX; ++n) {
+                ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KD, wave, i, lane);
+                if (!GRAD) qa[i][n] = operand(w.q + ((kc + c) * NX + n) * kChunk * KD, KD, wave, i, lane);
+            }
+    };
+    auto fetch_values = [&] {
+        const __amdgpu_buffer_rsrc_t rows = v.buffer();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) next_v[n][e] = buffer_load<T>(rows, v_at[n][e]);
+        v.move(1);
+    };
+    auto fetch_inverse = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (i < steps) {
+#pragma unroll
+                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.x + ((vc + c) * 3 + n) * kSquare, kChunk, wave, i, lane);
+            }
+    };
+    auto fetch_mixed = [&](int c) {
+        if (!GRAD) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i < steps) {
+#pragma unroll
+                    for (int n = 0; n < RP; ++n) pa[i][n] = operand(w.p + ((vc + c) * RP + n) * kSquare, kChunk, wave, i, lane);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, kChunk, TW * wave + i, m, lane);
+    };
+    auto fetch_scalars = [&](int c) {
+        const float* from = w.scalars + (vc + c) * kScalars * kChunk;
+        gamma = *(const f4*)(from + kGamma * kChunk + my_row);
+        left = *(const f4*)(from + kLeft * kChunk + my_row);
+        strength = *(const f4*)(from + kStrength * kChunk + my_row);
+        end = from[kGamma * kChunk + kChunk - 1];
+    };
+    if (chunks > 0) {
+        fetch_keys(0), fetch_values(), fetch_inverse(0), fetch_mixed(0), fetch_scalars(0);
+        put_state();
+    }
+    for (int c = 0; c < chunks; ++c) {
+        const int next = c + 1 < chunks ? c + 1 : c;
+        lds_barrier();
+        if (GRAD) {
+            // S before the chunk
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    u2 parts[RP];
+                    split4(s[i][n], parts);
+#pragma unroll
+                    for (int m = 0; m < RP; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (column[n] < shape.columns)
+                                w.s[(((vc + c) * RP + m) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column[n]] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+                }
+        }
+        // K S and Q S
+        f4 ks[NT] = {}, out[NT] = {};
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                b8 parts[3];
+                states.take(i, n, lane, parts);
+                ks[n] = multiply<2>(ka[i], parts, ks[n]);
+                if (!GRAD) out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
+            }
+        fetch_keys(next);
+        // b (V - e^G (K S))
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f4 miss;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) miss[e] = strength[e] * __builtin_fmaf(-gamma[e], ks[n][e], loaded<T>(next_v[n][e]));
+            misses.put_half(wave, n, lane, miss);
+        }
+        if (c + 1 < chunks) fetch_values();
+        lds_barrier();
+        // U
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f4 u = {};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i < steps) {
+                    b8 parts[3];
+                    misses.take(i, n, lane, parts);
+                    u = multiply<2>(xa[i], parts, u);
+                }
+            writes.put_half(wave, n, lane, left * u);
+            if (!GRAD) {
+                values.put_half(wave, n, lane, u);
+            } else {
+                u2 parts[RP];
+                split4(u, parts);
+#pragma unroll
+                for (int m = 0; m < RP; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (column[n] < shape.columns)
+                            w.u[(((vc + c) * RP + m) * kChunk + my_row + e) * shape.columns + column[n]] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+            }
+        }
+        fetch_inverse(next);
+        lds_barrier();
+        // the state behind the chunk, and its outputs
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i) s[i][n] *= end;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                b8 parts[3];
+                writes.take(m, n, lane, parts);
+#pragma unroll
+                for (int i = 0; i < TW; ++i) s[i][n] = multiply<2>(kta[i][m], parts, s[i][n]);
+            }
+        }
+        put_state();
+        if (!GRAD) {
+            const __amdgpu_buffer_rsrc_t rows = y.buffer();
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f4 o = out[n] * (gamma * p.scale);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i < steps) {
+                        b8 parts[RP];
+                        values.take(i, n, lane, parts);
+                        o = multiply<RP - 1>(pa[i], parts, o);
+                    }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)o[e]);
+            }
+            y.move(1);
+        }
+        fetch_mixed(next), fetch_scalars(next);
+    }
+    if (!GRAD) {
+        T* behind = (T*)a.y + b * p.y_batch + head * p.value_dim;
+        for (int t = chunks * kChunk + (threadIdx.x >> 4); t < p.length; t += kDeltaThreads / 16)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                if (there[n]) behind[t * p.y_row + column[n]] = (T)0.0f;
+        if (a.state_out) {
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state_out + state_base), 0, state_bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                        const float value = s[i][n][e];        // (an element of a vector is not a place that bits can be taken from)
+                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), to, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0);
+                    }
+        }
+    }
+}
+
+template <typename T, int KD, bool GRAD>
+hipError_t matrices(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, hipStream_t s)
+{
+    const long long blocks = (long long)shape.chunks * p.value_heads * p.batch;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (blocks) hipLaunchKernelGGL((delta_matrices_kernel<T, KD, GRAD>), dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, shape, w);
+    return hipGetLastError();
+}
+
+template <typename T, int KD, bool GRAD>
+hipError_t sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, hipStream_t s)
+{
+    DeltaShape of = shape;
+    of.tiles = (shape.columns + 15) / 16;
+    const long long blocks = (long long)of.tiles * p.value_heads * p.batch;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((delta_sweep_kernel<T, KD, 1, GRAD>), dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, of, w);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(bool is_sweep, const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s)
+{
+    auto run = [&](auto kd, auto g) {
+        constexpr int KD = decltype(kd)::value;
+        constexpr bool GRAD = decltype(g)::value;
+        return is_sweep ? sweep<T, KD, GRAD>(p, a, shape, w, s) : matrices<T, KD, GRAD>(p, a, shape, w, s);
+    };
+    auto wide = [&](auto g) { return shape.padded == 64 ? run(std::integral_constant<int, 64>(), g) : run(std::integral_constant<int, 128>(), g); };
+    return grad ? wide(std::true_type()) : wide(std::false_type());
+}
+
+hipError_t launch(bool is_sweep, const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s)
+{
+    switch (p.dtype) {
+    case SYS_F32: return launch_type<float>(is_sweep, p, a, shape, w, grad, s);
+    case SYS_F16: return launch_type<f16_t>(is_sweep, p, a, shape, w, grad, s);
+    default: return launch_type<bf16_t>(is_sweep, p, a, shape, w, grad, s);
+    }
+}
+
+// Sequences of up to this many positions go a position at a time.
+constexpr int kShort = 16;
+
+}  // namespace
+
+hipError_t launch_delta_matrices(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s)
+{
+    return launch(false, p, a, shape, w, grad, s);
+}
+hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s)
+{
+    return launch(true, p, a, shape, w, grad, s);
+}
+
+DeltaShape delta_shape(const sys_gated_delta_t& p)
+{
+    DeltaShape s = {};
+    s.chunks = delta_chunks(p);
+    s.padded = delta_padded(p);
+    s.columns = (p.value_dim + 31) / 32 * 32;
+    return s;
+}
+
+size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool grad, void* base, DeltaPlanes* w)
+{
+    const size_t value_chunks = (size_t)p.batch * p.value_heads * shape.chunks, key_chunks = (size_t)p.batch * p.key_heads * shape.chunks;
+    const size_t input = p.dtype == SYS_F32 ? 3 : p.dtype == SYS_F16 ? 2 : 1, result = p.dtype == SYS_F32 ? 3 : 2;
+    const size_t keys = key_chunks * input * kChunk * shape.padded * sizeof(bf16_t), square = value_chunks * kSquare * sizeof(bf16_t);
+    const size_t begin = ((uintptr_t)base + 255) / 256 * 256;
+    size_t at = begin;
+    auto take = [&](auto*& to, size_t bytes) {
+        to = (std::remove_reference_t<decltype(to)>)at;
+        at += (bytes + 255) / 256 * 256;
+    };
+    DeltaPlanes of = {};
+    take(of.x, 3 * square);
+    take(of.k, keys);
+    take(of.kt, keys);
+    take(of.scalars, value_chunks * kScalars * kChunk * sizeof(float));
+    if (!grad) {
+        take(of.p, result * square);
+        take(of.q, keys);
+    } else {
+        take(of.xt, 3 * square);
+        take(of.pt, 3 * square);
+        take(of.qt, keys);
+        const size_t state = value_chunks * result * shape.padded * shape.columns * sizeof(bf16_t), rows = value_chunks * result * kChunk * shape.columns * sizeof(bf16_t);
+        take(of.s, state);
+        take(of.ds, state);
+        take(of.u, rows);
+        take(of.z, rows);
+        take(of.dg, 2 * value_chunks * kChunk * sizeof(float));
+    }
+    if (w) *w = of;
+    return at - begin + 256;                       // (the base may lie anywhere)
+}
+
+size_t delta_workspace(const sys_gated_delta_t& p)
+{
+    return p.length > kShort && p.batch ? delta_planes(p, delta_shape(p), false, nullptr, nullptr) : 0;
+}
+
+hipError_t launch_delta(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s)
+{
+    if (p.length <= kShort) return launch_delta_positions(p, a, s);
+    const DeltaShape shape = delta_shape(p);
+    DeltaPlanes w;
+    delta_planes(p, shape, false, a.workspace, &w);
+    const hipError_t e = launch_delta_matrices(p, a, shape, w, false, s);
+    return e != hipSuccess ? e : launch_delta_sweep(p, a, shape, w, false, s);
+}
+
+}  // namespace sysconv

@@ -5,8 +5,8 @@
 // dealt to the groups of lanes in turn.  Both products with the state are taken of S_{t-1} in one sweep, S_t^T q = a S_{t-1}^T q + (k . q) u, so a
 // position costs one sum over the rows (in the lane, over the wavefront's groups, over the wavefronts through LDS: one barrier).
 // A position is four multiply-adds an element of the state against, for single tokens, 8 bytes of it: those are bound by memory.
+#include "delta_tile.h"
 #include "launch.h"
-#include "sequence.h"
 
 namespace sysconv {
 namespace {
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(sys_gated_delta_t 
     constexpr int kLanes = kColumns / V, kGroups = kThreads / kLanes, kRows = (KD + kGroups - 1) / kGroups;
     const int block = blockIdx.x % blocks, head = blockIdx.x / blocks % p.value_heads, b = blockIdx.x / blocks / p.value_heads;
     const int column = block * kColumns + (threadIdx.x % kLanes) * V, group = threadIdx.x / kLanes, wave = threadIdx.x >> 6;
-    const bool there = column < p.value_dim;                           // (V divides the dimension)
+    const bool there = column < p.value_dim;                           // (V divides it)
     const int key_head = head / (p.value_heads / p.key_heads);
     long long place = b;
     if (slotted && a.slots) place = a.slots[b];
@@ -31,15 +31,24 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(sys_gated_delta_t 
         if (group == 0 && there) Channels<T, V>::store(y, zero);
         return;
     }
-    const size_t base = ((size_t)place * p.value_heads + head) * p.key_dim * p.value_dim + column;
-
+    // a head's state as a buffer: rows and columns that are not there lie past its end, are zeros and not written
+    const size_t base = ((size_t)place * p.value_heads + head) * p.key_dim * p.value_dim;
+    const unsigned bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
+    const unsigned offset = there ? (unsigned)(group * p.value_dim + column) * 4u : kNowhere, row_bytes = (unsigned)(kGroups * p.value_dim) * 4u;
     float s[kRows][V];
+    {
+        const __amdgpu_buffer_rsrc_t state = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state + base), 0, a.state ? bytes : 0u, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+        for (int i = 0; i < kRows; ++i) {
+            const unsigned at = there ? offset + i * row_bytes : kNowhere;
+            if constexpr (V == 4) {
+                const f4 v = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(state, at, 0, 0));
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[i][j] = 0.0f;
-        const int row = group + i * kGroups;
-        if (a.state && there && row < p.key_dim) Channels<float, V>::load(a.state + base + (size_t)row * p.value_dim, s[i]);
+                for (int j = 0; j < V; ++j) s[i][j] = v[j];
+            } else {
+                s[i][0] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(state, at, 0, 0));
+            }
+        }
     }
     const T* q = (const T*)a.q + b * p.q_batch + key_head * p.key_dim;
     const T* k = (const T*)a.k + b * p.k_batch + key_head * p.key_dim;
@@ -127,11 +136,17 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(sys_gated_delta_t 
         for (int t = last + group; t < length; t += kGroups)
             if (there) Channels<T, V>::store(y + t * p.y_row, zero);
     }
-    if (a.state_out && there) {
+    if (a.state_out) {
+        const __amdgpu_buffer_rsrc_t state = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state_out + base), 0, bytes, 0x00027000);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int row = group + i * kGroups;
-            if (row < p.key_dim) Channels<float, V>::store(a.state_out + base + (size_t)row * p.value_dim, s[i]);
+            const unsigned at = there ? offset + i * row_bytes : kNowhere;
+            if constexpr (V == 4) {
+                const f4 v = {s[i][0], s[i][1], s[i][2], s[i][3]};
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), state, at, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, s[i][0]), state, at, 0, 0);
+            }
         }
     }
 }
@@ -165,13 +180,7 @@ hipError_t launch(bool step, const sys_gated_delta_t& p, const DeltaArgs& a, hip
 }  // namespace
 
 hipError_t launch_delta_step(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s) { return launch(true, p, a, s); }
-
-hipError_t launch_delta(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s)
-{
-    return launch(false, p, a, s);
-}
-
-size_t delta_workspace(const sys_gated_delta_t&) { return 0; }
+hipError_t launch_delta_positions(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s) { return launch(false, p, a, s); }
 
 hipError_t launch_delta_grad(const sys_gated_delta_t&, const DeltaArgs&, hipStream_t) { return hipErrorNotSupported; }
 size_t delta_grad_workspace(const sys_gated_delta_t&) { return 0; }

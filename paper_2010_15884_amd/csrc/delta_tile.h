@@ -1,0 +1,177 @@
+// How the gated delta rule in chunks is laid on the matrix cores (delta_chunk.hip, delta_grad.hip).
+//
+// Over a chunk of 64 positions with the state S before it, G_i the sum of the logarithms of the decays up to position i,
+//   X = (I + A)^-1,  A_ij = b_i e^(G_i - G_j) k_i . k_j (j < i)
+//   U = X (b (V - e^G (K S))),  Y = scale e^G (Q S) + P U,  P_ij = scale e^(G_i - G_j) q_i . k_j (j <= i)
+//   S' = e^(G_end) S + K^T (e^(G_end - G) U)
+// A, X and P belong to the keys and queries alone and are made for all chunks side by side; what is left to do one chunk after
+// the other are products with S, U and the like, whose columns (of the values) do not meet.
+//
+// Precision: v_mfma_f32_16x16x32_bf16 on numbers that are split into bf16 parts, accumulated in fp32.  Inputs in bf16 are one part, in fp16
+// two, in fp32 three, exactly; states, U and what leads to them are three (24 bits), and products of parts i and j are taken up to
+// i + j = 2, so that what is left out is below 2^-24 of the term, as in split_bf16.h.  Where a product only leads to results in 16 bits, two parts (16 bits) are
+// enough.  The split keeps fp32's range; infinities in it become NaN, and a NaN reaches all positions of its chunk (0 times NaN).
+//
+// Layout: D of an instruction holds rows 4 (lane / 16) + i of column lane % 16, B takes rows 8 (lane / 16) + j of column lane % 16.
+// With the rows of A permuted (row m of tile 2s + h is row 32 s + 8 (m / 4) + 4 h + m % 4 of the matrix) two tiles of D are a B operand as they
+// lie: products follow each other without an exchange between lanes, and every A operand is 16 bytes of a row of a matrix.
+#pragma once
+
+#include "scan_tile.h"
+#include "sequence.h"
+#include "split_bf16.h"
+
+#include <type_traits>
+
+namespace sysconv {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+constexpr int kChunk = 64;
+constexpr int kDeltaThreads = 256;
+constexpr int kSquare = kChunk * kChunk;           // elements of X, P
+
+// Parts of an input.
+template <typename T> constexpr int kInputParts = sizeof(T) == 4 ? 3 : std::is_same<T, f16_t>::value ? 2 : 1;
+// Parts of what leads to results of this type alone.
+template <typename T> constexpr int kResultParts = sizeof(T) == 4 ? 3 : 2;
+
+__device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// c += a b, parts whose order is at most MOST, the small ones first.
+template <int MOST, int NA, int NB>
+__device__ __forceinline__ f4 multiply(const b8 (&a)[NA], const b8 (&b)[NB], f4 c)
+{
+#pragma unroll
+    for (int order = MOST; order >= 0; --order)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (order - i >= 0 && order - i < NB) c = mfma(a[i], b[order - i], c);
+    return c;
+}
+
+// Eight numbers as N parts each.
+template <int N>
+__device__ __forceinline__ void split8(const float (&v)[8], b8 (&out)[N])
+{
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = v[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        u4 packed;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            packed[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(f2{rest[2 * i], rest[2 * i + 1]}, b2));
+            if (n + 1 < N) {
+                rest[2 * i] -= __builtin_bit_cast(float, packed[i] << 16);
+                rest[2 * i + 1] -= __builtin_bit_cast(float, packed[i] & 0xffff0000u);
+            }
+        }
+        out[n] = __builtin_bit_cast(b8, packed);
+    }
+}
+
+// Four numbers as N parts each, 8 bytes a part.
+template <int N>
+__device__ __forceinline__ void split4(f4 rest, u2 (&out)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned packed = __builtin_bit_cast(unsigned, __builtin_convertvector(f2{rest[2 * i], rest[2 * i + 1]}, b2));
+            out[n][i] = packed;
+            if (n + 1 < N) {
+                rest[2 * i] -= __builtin_bit_cast(float, packed << 16);
+                rest[2 * i + 1] -= __builtin_bit_cast(float, packed & 0xffff0000u);
+            }
+        }
+}
+
+// The row of a matrix that is row m of tile `tile` of an A operand, and of D.
+__device__ __forceinline__ constexpr int tile_row(int tile, int m) { return 32 * (tile >> 1) + 8 * (m >> 2) + 4 * (tile & 1) + (m & 3); }
+
+// A operand: rows of `tile`, columns 32 step .. 32 step + 31 of a row-major matrix.
+__device__ __forceinline__ b8 operand(const bf16_t* matrix, int columns, int tile, int step, int lane)
+{
+    return *(const b8*)(matrix + tile_row(tile, lane & 15) * columns + 32 * step + 8 * (lane >> 4));
+}
+
+// The barrier of a workgroup whose wavefronts exchange through LDS alone: loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, row-major.  Per value head and
+// chunk X [64][64] (three parts), P (kResultParts; gradients: transposes of both, three parts), and for every position the Scalars; per key head and chunk
+// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, kResultParts each.
+struct DeltaPlanes {
+    bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
+    bf16_t *s, *ds, *u, *z;            // [padded][columns], [64][columns]
+    float* scalars;                    // [kScalars][64]
+    float* dg;                         // gradients of the logarithms of decays and of strengths, [2][batch][value_heads][64 chunks]
+};
+
+struct DeltaShape {
+    int chunks;                        // of a sequence
+    int padded;                        // the key dimension as the kernels have it, 64 or 128
+    int columns;                       // the value dimension rounded up to 32
+    int tiles;                         // of columns
+};
+
+enum Scalars { kGamma, kLeft, kStrength, kScalars };   // e^G, e^(G_end - G), b
+
+inline int delta_padded(const sys_gated_delta_t& p) { return p.key_dim <= 64 ? 64 : 128; }
+inline int delta_chunks(const sys_gated_delta_t& p) { return (p.length + kChunk - 1) / kChunk; }
+
+__device__ __forceinline__ bf16_t as_bf16(unsigned bits) { return __builtin_bit_cast(bf16_t, (unsigned short)bits); }
+
+// Eight neighbouring entries of a row as fp32; zeros past its end and where the row is not there.
+template <typename T>
+__device__ __forceinline__ void load_eight(const T* row, int at, int columns, bool there, float (&out)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = 0.0f;
+    if (!there || at >= columns) return;
+    if (at + 8 <= columns) {
+        if constexpr (sizeof(T) == 2) {
+            Channels<T, 8>::load(row + at, out);
+        } else {
+            Channels<T, 4>::load(row + at, *(float(*)[4])out);
+            Channels<T, 4>::load(row + at + 4, *(float(*)[4])(out + 4));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at + i < columns) out[i] = (float)row[at + i];
+    }
+}
+
+// Entries of neighbouring positions of a chunk, one column a lane, addressed as a buffer that ends with the last row that exists (zeros behind it).
+template <typename T>
+struct ChunkRows {
+    T* at;                             // row 0 of the present chunk
+    long long left, row;               // bytes to the end of the last row
+    __device__ __forceinline__ ChunkRows(const void* base, long long row_stride, int columns, int chunk, int end)
+        : at((T*)base + chunk * kChunk * row_stride), left(bytes_left(chunk * kChunk, end, row_stride, columns, sizeof(T))), row(row_stride)
+    {
+    }
+    __device__ __forceinline__ void move(int chunks) { at += chunks * kChunk * row, left -= chunks * kChunk * row * (long long)sizeof(T); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, buffer_size(left), 0x00027000); }
+    __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }
+};
+
+// The two kernels in front of all others (delta_chunk.hip): the chunks' matrices, and the sweep forwards, which gives the outputs or, for gradients, S and U.
+hipError_t launch_delta_matrices(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
+hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
+DeltaShape delta_shape(const sys_gated_delta_t& p);
+// The planes of a call, from `base` on (a null pointer: for their size), and the bytes that they take.
+size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool grad, void* base, DeltaPlanes* w);
+// A position at a time (delta_rule.hip).
+hipError_t launch_delta_positions(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s);
+
+}  // namespace sysconv

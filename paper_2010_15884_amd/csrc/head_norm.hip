@@ -44,32 +44,27 @@ __device__ __forceinline__ float lanes_sum(float v, int log)
 template <int V, int S>
 struct Slots {
     int first[S], second[S], angle[2][S];
-    bool is[S], has_second[S], turns[S];
-    __device__ __forceinline__ Slots(const sys_head_norm_t& p, const NormPlan& n, int part)
+    unsigned there, pairs, turned;     // a bit a slot: it exists, with a second piece, and is turned
+    __device__ __forceinline__ Slots(const sys_head_norm_t& p, const NormPlan& n, int part) : there(0), pairs(0), turned(0)
     {
         const int tail = p.dim - p.rotary, half = (tail + 1) / 2;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             const int s = part + (i << n.parts_log);
-            is[i] = s < n.slots;
-            turns[i] = s < n.turned;
-            if (turns[i]) {
-                const bool pair = V == 1 && p.interleaved;
-                first[i] = pair ? 2 * s : s * V;
-                second[i] = pair ? 2 * s + 1 : p.rotary / 2 + s * V;
-                has_second[i] = true;
-                angle[0][i] = p.interleaved && V > 1 ? first[i] / 2 : s * V;
-                angle[1][i] = second[i] / 2;       // (interleaved pieces alone)
-            } else {
-                first[i] = p.rotary + (s - n.turned) * V;
-                second[i] = first[i] + half;
-                has_second[i] = is[i] && second[i] < p.dim;
-                angle[0][i] = angle[1][i] = 0;
-            }
-            if (!is[i]) first[i] = second[i] = 0;
-            if (!has_second[i]) second[i] = first[i];
+            const bool turn = s < n.turned, both = V == 1 && p.interleaved;
+            const int f = turn ? (both ? 2 * s : s * V) : p.rotary + (s - n.turned) * V;
+            const int g = turn ? (both ? 2 * s + 1 : p.rotary / 2 + s * V) : f + half;
+            const bool is = s < n.slots, second_is = is && (turn || g < p.dim);
+            first[i] = is ? f : 0;
+            second[i] = second_is ? g : first[i];
+            angle[0][i] = turn ? (p.interleaved && V > 1 ? f / 2 : s * V) : 0;
+            angle[1][i] = turn ? g / 2 : 0;        // (interleaved pieces alone)
+            there |= (unsigned)is << i, pairs |= (unsigned)second_is << i, turned |= (unsigned)turn << i;
         }
     }
+    __device__ __forceinline__ bool is(int i) const { return there >> i & 1; }
+    __device__ __forceinline__ bool has_second(int i) const { return pairs >> i & 1; }
+    __device__ __forceinline__ bool turns(int i) const { return turned >> i & 1; }
 };
 
 // Cosines and sines of a lane's pairs at a row of the tables: [piece][pair] for interleaved pieces, else [0][entry].
@@ -82,7 +77,7 @@ struct Angles {
         const float* sine = a.sine + row * (p.rotary / 2);
 #pragma unroll
         for (int i = 0; i < S; ++i)
-            if (at.turns[i]) {
+            if (at.turns(i)) {
                 if (V > 1 && p.interleaved) {
                     constexpr int H = V > 1 ? V / 2 : 1;
                     Channels<float, H>::load(cosine + at.angle[0][i], *(float(*)[H])c[i]);
@@ -191,13 +186,13 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(sys_head_norm_t p, 
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     if (S > 1 || V == 1) {
-                        x[0][i][j] = slots.is[i] ? x[0][i][j] : 0.0f;
-                        x[1][i][j] = slots.has_second[i] ? x[1][i][j] : 0.0f;
+                        x[0][i][j] = slots.is(i) ? x[0][i][j] : 0.0f;
+                        x[1][i][j] = slots.has_second(i) ? x[1][i][j] : 0.0f;
                     }
                     sum = __builtin_fmaf(x[0][i][j], x[0][i][j], sum);
                     sum = __builtin_fmaf(x[1][i][j], x[1][i][j], sum);
                 }
-                if (S == 1 && V > 1 && !slots.is[i]) sum = 0.0f;
+                if (S == 1 && V > 1 && !slots.is(i)) sum = 0.0f;
             }
         }
         fetch(head + at.step);
@@ -224,10 +219,10 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(sys_head_norm_t p, 
             float f[V], g[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) f[j] = at.there ? x[0][i][j] * r * w[0][i][j] : 0.0f, g[j] = at.there ? x[1][i][j] * r * w[1][i][j] : 0.0f;
-            if (at.there && slots.turns[i]) angles.turn(p.interleaved, i, 1.0f, f, g);
-            if (slots.is[i]) {
+            if (at.there && slots.turns(i)) angles.turn(p.interleaved, i, 1.0f, f, g);
+            if (slots.is(i)) {
                 Channels<T, V>::store(y + slots.first[i], f);
-                if (slots.has_second[i]) Channels<T, V>::store(y + slots.second[i], g);
+                if (slots.has_second(i)) Channels<T, V>::store(y + slots.second[i], g);
             }
         }
     }
@@ -295,13 +290,13 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
                             Channels<T, V>::values(next[h][i], x[h][i]);
                             Channels<T, V>::values(next[2 + h][i], z[h][i]);
                         }
-                        if (slots.turns[i]) angles.turn(p.interleaved, i, -1.0f, z[0][i], z[1][i]);
+                        if (slots.turns(i)) angles.turn(p.interleaved, i, -1.0f, z[0][i], z[1][i]);
 #pragma unroll
                         for (int j = 0; j < V; ++j) {
-                            x[0][i][j] = slots.is[i] ? x[0][i][j] : 0.0f;
-                            x[1][i][j] = slots.has_second[i] ? x[1][i][j] : 0.0f;
-                            z[0][i][j] = slots.is[i] ? z[0][i][j] : 0.0f;
-                            z[1][i][j] = slots.has_second[i] ? z[1][i][j] : 0.0f;
+                            x[0][i][j] = slots.is(i) ? x[0][i][j] : 0.0f;
+                            x[1][i][j] = slots.has_second(i) ? x[1][i][j] : 0.0f;
+                            z[0][i][j] = slots.is(i) ? z[0][i][j] : 0.0f;
+                            z[1][i][j] = slots.has_second(i) ? z[1][i][j] : 0.0f;
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 sum = __builtin_fmaf(x[h][i][j], x[h][i][j], sum);
@@ -328,9 +323,9 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
                                 f[h][j] = r * __builtin_fmaf(-x[h][i][j], along, z[h][i][j] * w[h][i][j]);
                             }
                     }
-                    if (slots.is[i]) {
+                    if (slots.is(i)) {
                         Channels<T, V>::store(dx + slots.first[i], f[0]);
-                        if (slots.has_second[i]) Channels<T, V>::store(dx + slots.second[i], f[1]);
+                        if (slots.has_second(i)) Channels<T, V>::store(dx + slots.second[i], f[1]);
                     }
                 }
             }
@@ -352,7 +347,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
                 for (int j = 0; j < V; ++j) {
                     float v = dw[k][h][i][j];
                     for (int m = 1 << n.parts_log; m < 64; m <<= 1) v += __shfl_xor(v, m);
-                    if ((threadIdx.x & 63) >> n.parts_log == 0 && (h ? slots.has_second[i] : slots.is[i]))
+                    if ((threadIdx.x & 63) >> n.parts_log == 0 && (h ? slots.has_second(i) : slots.is(i)))
                         joined[threadIdx.x >> 6][(h ? slots.second[i] : slots.first[i]) + j] = v;
                 }
         __syncthreads();

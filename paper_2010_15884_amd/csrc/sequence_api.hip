@@ -153,7 +153,7 @@ int check(const sys_gated_delta_t& p, bool step, bool writes_y)
     if (p.length > kMostRows) return SYS_ERR_UNSUPPORTED;
     if (!step && p.length > 1)
         for (long long s : {p.q_row, p.k_row, p.v_row, p.delta_row, p.beta_row, p.y_row})
-            if (s > SYS_MAX_SCAN_ROW) return SYS_ERR_UNSUPPORTED;
+            if (s > SYS_MAX_DELTA_ROW) return SYS_ERR_UNSUPPORTED;
     return SYS_OK;
 }
 
