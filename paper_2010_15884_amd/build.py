@@ -17,7 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsysconv.so")
-SOURCES = ["api.hip", "causal_conv.hip", "conv1d.hip", "conv1d_arrays.hip", "conv1d_split.hip", "conv1d_stride2.hip", "conv1d_stt.hip", "conv2d.hip", "conv2d_mfma.hip", "conv2d_split.hip", "conv2d_stride2.hip", "copy.hip", "delta_chunk.hip", "delta_rule.hip",
+SOURCES = ["api.hip", "causal_conv.hip", "conv1d.hip", "conv1d_arrays.hip", "conv1d_split.hip", "conv1d_stride2.hip", "conv1d_stt.hip", "conv2d.hip", "conv2d_mfma.hip", "conv2d_split.hip", "conv2d_stride2.hip", "copy.hip", "delta_chunk.hip", "delta_grad.hip", "delta_rule.hip",
            "group_norm.hip", "head_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -25,7 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextr
 # Per-file additions.  The matrix-core kernels keep their accumulators in ordinary vector registers
 # (the results go straight to the vector ALUs; from accumulation registers every value would
 # first need a v_accvgpr_read).
-FILE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("conv1d_split.hip", "conv2d_mfma.hip", "conv2d_split.hip", "delta_chunk.hip")}
+FILE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("conv1d_split.hip", "conv2d_mfma.hip", "conv2d_split.hip", "delta_chunk.hip", "delta_grad.hip")}
 
 
 def _compile(src: str) -> str:
@@ -70,7 +70,7 @@ def build_c_demo(verbose: bool = True) -> str:
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
 # argument checks, the design planner, the tap scaling, the shapes of launches and workspaces
-HOST_LOGIC = ["api.hip", "causal_conv.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip", "delta_chunk.hip", "delta_rule.hip", "group_norm.hip", "head_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
+HOST_LOGIC = ["api.hip", "causal_conv.hip", "conv1d_split.hip", "conv1d_stt.hip", "conv2d_mfma.hip", "conv2d_split.hip", "delta_chunk.hip", "delta_grad.hip", "delta_rule.hip", "group_norm.hip", "head_norm.hip", "selective_scan.hip", "selective_scan_grad.hip", "sequence_api.hip"]
 
 
 def build_host_sanitized(verbose: bool = True, driver: str = "abi_san_driver") -> str:

@@ -80,6 +80,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         out[kGamma * kChunk + lane] = fast_exp2((float)sum);
         out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
         out[kStrength * kChunk + lane] = strength;
+        if (GRAD) ((double*)(out + kSums * kChunk))[lane] = sum;
     }
     __syncthreads();
 
@@ -225,35 +226,6 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 }
 
 // ---------------------------------------------------------------- the sweep
-
-// Where a workgroup keeps B operands: [step][part][column tile], 1 KB each, 16 bytes a lane.
-template <int STEPS, int PARTS, int NT>
-struct Operands {
-    b8 v[STEPS][PARTS][NT][64];
-    // all of step `step` from two tiles of D that lie above each other, or half of it from one
-    __device__ __forceinline__ void put(int step, int n, int lane, f4 upper, f4 lower)
-    {
-        float both[8];
-        b8 parts[PARTS];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) both[e] = upper[e], both[4 + e] = lower[e];
-        split8(both, parts);
-#pragma unroll
-        for (int m = 0; m < PARTS; ++m) v[step][m][n][lane] = parts[m];
-    }
-    __device__ __forceinline__ void put_half(int tile, int n, int lane, f4 d)
-    {
-        u2 parts[PARTS];
-        split4(d, parts);
-#pragma unroll
-        for (int m = 0; m < PARTS; ++m) ((u2*)&v[tile >> 1][m][n][lane])[tile & 1] = parts[m];
-    }
-    __device__ __forceinline__ void take(int step, int n, int lane, b8 (&out)[PARTS]) const
-    {
-#pragma unroll
-        for (int m = 0; m < PARTS; ++m) out[m] = v[step][m][n][lane];
-    }
-};
 
 template <typename T, int KD, int NT, bool GRAD>
 __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
@@ -582,7 +554,7 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
         take(of.ds, state);
         take(of.u, rows);
         take(of.z, rows);
-        take(of.dg, 2 * value_chunks * kChunk * sizeof(float));
+        take(of.dg, 2 * value_chunks * sizeof(float));
     }
     if (w) *w = of;
     return at - begin + 256;                       // (the base may lie anywhere)

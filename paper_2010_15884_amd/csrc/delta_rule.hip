@@ -182,7 +182,4 @@ hipError_t launch(bool step, const sys_gated_delta_t& p, const DeltaArgs& a, hip
 hipError_t launch_delta_step(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s) { return launch(true, p, a, s); }
 hipError_t launch_delta_positions(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s) { return launch(false, p, a, s); }
 
-hipError_t launch_delta_grad(const sys_gated_delta_t&, const DeltaArgs&, hipStream_t) { return hipErrorNotSupported; }
-size_t delta_grad_workspace(const sys_gated_delta_t&) { return 0; }
-
 }  // namespace sysconv

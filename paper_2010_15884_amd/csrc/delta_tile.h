@@ -106,6 +106,35 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Where a workgroup keeps B operands: [step][part][column tile], 1 KB each, 16 bytes a lane.
+template <int STEPS, int PARTS, int NT>
+struct Operands {
+    b8 v[STEPS][PARTS][NT][64];
+    // all of step `step` from two tiles of D that lie above each other, or half of it from one
+    __device__ __forceinline__ void put(int step, int n, int lane, f4 upper, f4 lower)
+    {
+        float both[8];
+        b8 parts[PARTS];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) both[e] = upper[e], both[4 + e] = lower[e];
+        split8(both, parts);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) v[step][m][n][lane] = parts[m];
+    }
+    __device__ __forceinline__ void put_half(int tile, int n, int lane, f4 d)
+    {
+        u2 parts[PARTS];
+        split4(d, parts);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) ((u2*)&v[tile >> 1][m][n][lane])[tile & 1] = parts[m];
+    }
+    __device__ __forceinline__ void take(int step, int n, int lane, b8 (&out)[PARTS]) const
+    {
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) out[m] = v[step][m][n][lane];
+    }
+};
+
 // What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, row-major.  Per value head and
 // chunk X [64][64] (three parts), P (kResultParts; gradients: transposes of both, three parts), and for every position the Scalars; per key head and chunk
 // K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, kResultParts each.
@@ -113,7 +142,7 @@ struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
     bf16_t *s, *ds, *u, *z;            // [padded][columns], [64][columns]
     float* scalars;                    // [kScalars][64]
-    float* dg;                         // gradients of the logarithms of decays and of strengths, [2][batch][value_heads][64 chunks]
+    float* dg;                         // every chunk's share of the gradients of A and the bias
 };
 
 struct DeltaShape {
@@ -123,7 +152,7 @@ struct DeltaShape {
     int tiles;                         // of columns
 };
 
-enum Scalars { kGamma, kLeft, kStrength, kScalars };   // e^G, e^(G_end - G), b
+enum Scalars { kGamma, kLeft, kStrength, kSums = 4, kScalars = 6 };    // e^G, e^(G_end - G), b; G in 64 bits, to base 2 (for gradients)
 
 inline int delta_padded(const sys_gated_delta_t& p) { return p.key_dim <= 64 ? 64 : 128; }
 inline int delta_chunks(const sys_gated_delta_t& p) { return (p.length + kChunk - 1) / kChunk; }

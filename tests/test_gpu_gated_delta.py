@@ -176,3 +176,139 @@ def test_empty():
     assert (state == 0).all()
     none = {n: c[n] if n in ("A", "delta_bias") or c[n] is None else c[n][:0] for n in (*INPUTS, "state", "lengths")}
     assert _forward(none)[0].shape[0] == 0
+
+
+# ---------------------------------------------------------------- gradients
+
+def _backward(c, **more):
+    how = dict(dict(softplus=True, sigmoid=True), **more)
+    return B.sys_gated_delta_rule_backward(c["dy"], *[c[n] for n in INPUTS], d_state=c["state"], d_lengths=c["lengths"], d_dstate_out=c["dstate_out"], **how)
+
+
+def _check_gradients(c, **how):
+    want = _reference(c, grad=True, **how)
+    allowed = D.delta_allowed(dict(c, scale=how.get("scale")), want, c["q"].shape[1] // 64 + 1, c["q"].dtype)
+    got = _backward(c, **how)
+    for name in ("dv", "dstate", "dq", "dk", "dbeta", "ddelta", "dA", "ddelta_bias"):
+        have = getattr(got, name)
+        needs = {"ddelta_bias": "delta_bias", "dstate": "state"}.get(name)
+        if needs and c[needs] is None:
+            assert have is None
+        else:
+            R.check(have, want[name], allowed[name], name)
+
+
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_gradients(case):
+    _check_gradients(_make(sum(case[:6]) + 1, *case))
+
+
+def test_gradients_of_step_sizes_and_strengths_as_they_come():
+    c = _make(51, 2, 90, 2, 2, 64, 64, F32, bias=False, state=True)
+    c["delta"], c["beta"] = c["delta"].abs() * 0.1, torch.rand_like(c["beta"])
+    c["beta"][0, 10:20] = 0.0
+    _check_gradients(c, softplus=False, sigmoid=False, scale=-0.7)
+
+
+def test_gradients_of_a_long_sequence():
+    _check_gradients(_make(52, 1, 700, 1, 2, 48, 24, F32, state=True))
+    _check_gradients(_make(53, 2, 400, 1, 1, 128, 32, BF16, lengths=[400, 131]))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_gradients_are_close_in_norm(dtype):
+    """Sums over many terms are nearer than their worst case: what the matrix cores are given is worth 24 bits, and 16 where only 16-bit results come of it."""
+    c = _make(54, 2, 330, 2, 4, 128, 128, dtype, state=True)
+    want, got = _reference(c, grad=True), _backward(c)
+    y, state = _forward(c)
+    far = lambda a, b: float((R.wide(a) - b).norm() / b.norm())  # noqa: E731
+    rounding = {F32: 0.0, F16: 2.0 ** -11, BF16: 2.0 ** -8}[dtype]
+    assert far(y, want["y"]) < 2e-6 + rounding and far(state, want["state"]) < 2e-6
+    assert far(got.dstate, want["dstate"]) < 2e-6
+    for name in ("dq", "dk", "dv", "dbeta", "ddelta"):
+        assert far(getattr(got, name), want[name]) < (4e-6 if dtype == F32 else 2.0 ** -14) + rounding, name
+    for name in ("dA", "ddelta_bias"):
+        assert far(getattr(got, name), want[name]) < 1e-5, name
+
+
+def test_gradients_of_empty_calls():
+    c = _make(55, 2, 3, 1, 2, 16, 8, F32, state=True)
+    cut = {n: c[n] if n in ("A", "delta_bias", "state", "lengths", "dstate_out") else c[n][:, :0] for n in (*INPUTS, "state", "lengths", "dy", "dstate_out")}
+    g = _backward(cut)
+    assert torch.equal(g.dstate, c["dstate_out"]) and (g.dA == 0).all() and (g.ddelta_bias == 0).all()
+    none = {n: c[n] if n in ("A", "delta_bias") or c[n] is None else c[n][:0] for n in (*INPUTS, "state", "lengths", "dy", "dstate_out")}
+    g = _backward(none)
+    assert (g.dA == 0).all() and g.dq.shape[0] == 0
+
+
+# ---------------------------------------------------------------- as programs call them
+
+def test_outputs_given_and_strided():
+    c = _make(61, 2, 100, 1, 2, 64, 32, BF16)
+    room = torch.full((3, 100, 3, 32), 7.0, device="cuda", dtype=BF16)
+    B.sys_gated_delta_rule(*[c[n] for n in INPUTS], softplus=True, sigmoid=True, d_y=room[:2, :, :2])
+    assert torch.equal(room[:2, :, :2], _forward(c)[0])
+    assert (room[2] == 7).all() and (room[:, :, 2] == 7).all()
+
+
+def test_repeated_rows():
+    """Inputs whose batch stride is 0: one sequence for all."""
+    c = _make(62, 1, 130, 2, 2, 64, 64, F32)
+    same = {n: c[n] if c[n] is None or n in ("A", "delta_bias") else c[n].expand(3, *c[n].shape[1:]) for n in (*INPUTS, "state", "lengths")}
+    y, state = _forward(same)
+    one, one_state = _forward(c)
+    for b in range(3):
+        assert torch.equal(y[b], one[0]) and torch.equal(state[b], one_state[0])
+
+
+def test_other_stream():
+    c = _make(63, 2, 200, 2, 4, 128, 64, BF16, state=True)
+    want, grads = _forward(c), _backward(c)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    y, state = _forward(c, stream=side.cuda_stream)
+    got = _backward(c, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(state, want[1])
+    assert all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+def test_captured_prompts_tokens_and_gradients():
+    c = _make(64, 2, 150, 2, 4, 64, 64, BF16, state=True)
+    cache = c["state"].clone()
+
+    def call():
+        y, state = _forward(c)
+        step = _step(c, cache)
+        return (y, state, step, *_backward(c))
+    start = cache.clone()
+    call()
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    with torch.cuda.graph(other):
+        again = call()
+    for turn in range(3):
+        c["v"].mul_(-0.5)
+        c["dy"].mul_(1.5)
+        cache.copy_(start)
+        want = call()
+        moved = cache.clone()
+        for g, o in ((graph, out), (other, again)):
+            cache.copy_(start)
+            for t in o:
+                t.fill_(3.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(o, want)) and torch.equal(cache, moved)
+
+
+def test_nan_stays_in_its_head_and_before_its_chunk():
+    c = _make(65, 2, 200, 2, 2, 64, 64, BF16, state=True)
+    clean, _ = _forward(c)
+    c["v"][0, 140, 1, 3] = float("nan")
+    y, state = _forward(c)
+    assert torch.equal(y[1], clean[1]) and torch.equal(y[0, :, 0], clean[0, :, 0]) and torch.equal(y[0, :128, 1], clean[0, :128, 1])
+    others = torch.arange(64, device="cuda") != 3
+    assert torch.equal(y[0, :, 1][:, others], clean[0, :, 1][:, others]) and torch.isnan(y[0, 140:, 1, 3]).all() and torch.isnan(state[0, 1, :, 3]).all()
