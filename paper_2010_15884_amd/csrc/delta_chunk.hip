@@ -6,6 +6,8 @@
 #include "delta_tile.h"
 #include "launch.h"
 
+#include <initializer_list>
+
 namespace sysconv {
 namespace {
 
@@ -28,32 +30,44 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     __shared__ double sums[kChunk];                // of the logarithms of the decays, to base 2
     __shared__ float strengths[kChunk];
 
-    // K into LDS
+    // K into LDS, and the rows of Q that this wavefront works on
     const T* k = (const T*)a.k + b * p.k_batch + t0 * p.k_row + key_head * p.key_dim;
     const T* q = (const T*)a.q + b * p.q_batch + t0 * p.q_row + key_head * p.key_dim;
-    for (int i = tid; i < kChunk * KD / 8; i += kDeltaThreads) {
-        const int row = i / (KD / 8), at = i % (KD / 8) * 8;
-        float v[8];
-        b8 parts[NX];
-        load_eight(k + row * p.k_row, at, p.key_dim, row < rows, v);
-        split8(v, parts);
-#pragma unroll
-        for (int n = 0; n < NX; ++n) {
-            *(b8*)&keys[n][row][at] = parts[n];
-            if (first) *(b8*)(w.k + (kc * NX + n) * kChunk * KD + row * KD + at) = parts[n];
-        }
-    }
-    // the rows of Q that this wavefront works on
+    constexpr int kPieces = kChunk * KD / 8 / kDeltaThreads;
     b8 qa[KS][NX];
+    {
+        Eight<T> from_k[kPieces], from_q[KS];
+        const ChunkRows<T> k_rows(k - t0 * p.k_row, p.k_row, p.key_dim, chunk, last), q_rows(q - t0 * p.q_row, p.q_row, p.key_dim, chunk, last);
+        const __amdgpu_buffer_rsrc_t k_buffer = k_rows.buffer(), q_buffer = q_rows.buffer();
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const int row = 16 * wave + r, at = 32 * s + 8 * g;
-        float v[8];
-        load_eight(q + row * p.q_row, at, p.key_dim, row < rows, v);
-        split8(v, qa[s]);
-        if (first && !GRAD) {
+        for (int i = 0; i < kPieces; ++i) {
+            const int row = (tid + i * kDeltaThreads) / (KD / 8), at = (tid + i * kDeltaThreads) % (KD / 8) * 8;
+            if (shape.whole) from_k[i].load(k_buffer, at < p.key_dim ? k_rows.offset(row, at) : kNowhere);
+            else from_k[i].load(k + row * p.k_row, at, p.key_dim, row < rows);
+        }
 #pragma unroll
-            for (int n = 0; n < NX; ++n) *(b8*)(w.q + (kc * NX + n) * kChunk * KD + row * KD + at) = qa[s][n];
+        for (int s = 0; s < KS; ++s) {
+            const int row = 16 * wave + r, at = 32 * s + 8 * g;
+            if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.offset(row, at) : kNowhere);
+            else from_q[s].load(q + row * p.q_row, at, p.key_dim, row < rows);
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int row = (tid + i * kDeltaThreads) / (KD / 8), at = (tid + i * kDeltaThreads) % (KD / 8) * 8;
+            b8 parts[NX];
+            from_k[i].split(parts);
+#pragma unroll
+            for (int n = 0; n < NX; ++n) *(b8*)&keys[n][row][at] = parts[n];
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            from_q[s].split(qa[s]);
+            if (first) {
+                const int row = 16 * wave + r;
+#pragma unroll
+                for (int n = 0; n < NX; ++n)
+                    *(b8*)(w.q + (kc * NX + n) * kChunk * KD + ((tile_of(row) * KS + s) * 64 + g * 16 + row_in_tile(row)) * 8) = qa[s][n];
+            }
         }
     }
     if (wave == 0) {
@@ -84,6 +98,35 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     }
     __syncthreads();
 
+    // A plane's pieces from LDS: K^T (Q^T), eight positions of a column; a square, or its transpose, without the quarter above (below) the diagonal
+    auto transposed = [&](bf16_t* to) {
+        for (int i = wave; i < KD / 16 * 2; i += kDeltaThreads / 64) {
+            const int d = tile_row(i / 2, r), at = 32 * (i % 2) + 8 * g;
+#pragma unroll
+            for (int n = 0; n < NX; ++n) {
+                b8 v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = keys[n][at + j][d];
+                *(b8*)(to + (kc * NX + n) * kChunk * KD + (i * 64 + lane) * 8) = v;
+            }
+        }
+    };
+    auto square = [&](auto of, bf16_t* to, bool turned) {
+        constexpr int N = decltype(of)::value;
+        for (int i = wave; i < 8; i += kDeltaThreads / 64) {
+            const int tile = i / 2, step = i % 2;
+            if (turned ? step < tile / 2 : step > tile / 2) continue;
+            const int row = tile_row(tile, r), at = 32 * step + 8 * g;
+            float v[8];
+            b8 parts[N];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = turned ? xm[at + j][row] : xm[row][at + j];
+            split8(v, parts);
+#pragma unroll
+            for (int n = 0; n < N; ++n) *(b8*)(to + n * kSquare + (i * 64 + lane) * 8) = parts[n];
+        }
+    };
+
     // K K^T and Q K^T, rows of this wavefront (as they lie), columns up to its own; scaled and cut to triangles
     b8 ka[KS][NX];
 #pragma unroll
@@ -94,9 +137,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     float row_strength[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) row_sum[e] = sums[16 * wave + 4 * g + e], row_strength[e] = strengths[16 * wave + 4 * g + e];
-    constexpr int kKeptParts = GRAD ? 3 : RP;
-    bf16_t* const kept = GRAD ? w.pt : w.p;
-    for (int n = 0; n <= (GRAD ? 3 : wave | 1); ++n) {
+    for (int n = 0; n <= (wave | 1); ++n) {
         f4 kk = {}, qk = {};
         if (n <= wave) {
 #pragma unroll
@@ -110,48 +151,37 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         }
         const int column = 16 * n + r;
         const double column_sum = sums[column];
-        f4 mixed;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = 16 * wave + 4 * g + e;
             const float ratio = fast_exp2((float)(row_sum[e] - column_sum));
             if (n <= wave) am[row][column] = column < row ? row_strength[e] * (ratio * kk[e]) : 0.0f;
-            mixed[e] = column <= row ? p.scale * (ratio * qk[e]) : 0.0f;
-        }
-        u2 parts[kKeptParts];
-        split4(mixed, parts);
-#pragma unroll
-        for (int m = 0; m < kKeptParts; ++m) {
-            bf16_t* plane = kept + (vc * kKeptParts + m) * kSquare;
-            if (GRAD) {
-                *(u2*)(plane + column * kChunk + 16 * wave + 4 * g) = parts[m];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) plane[(16 * wave + 4 * g + e) * kChunk + column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
-            }
+            xm[row][column] = column <= row ? p.scale * (ratio * qk[e]) : 0.0f;
         }
     }
-    // K^T, eight positions at a time
     if (first) {
-        for (int i = tid; i < KD * kChunk / 8; i += kDeltaThreads) {
-            const int d = i % KD, at = i / KD * 8;
+        // K as it is and transposed, 1 KB a wavefront
+        for (int i = wave; i < 4 * KS; i += kDeltaThreads / 64)
 #pragma unroll
-            for (int n = 0; n < NX; ++n) {
-                b8 v;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = keys[n][at + j][d];
-                *(b8*)(w.kt + (kc * NX + n) * kChunk * KD + d * kChunk + at) = v;
-            }
-        }
+            for (int n = 0; n < NX; ++n)
+                *(b8*)(w.k + (kc * NX + n) * kChunk * KD + (i * 64 + lane) * 8) = *(const b8*)&keys[n][tile_row(i / KS, r)][32 * (i % KS) + 8 * g];
+        transposed(w.kt);
     }
     __syncthreads();
+    // P (its transpose for gradients) from xm
+    {
+        constexpr int N = GRAD ? 3 : RP;
+        square(std::integral_constant<int, N>(), (GRAD ? w.pt : w.p) + vc * N * kSquare, GRAD);
+    }
     if (GRAD && first) {
-        // Q^T the same way, through the place of K
+        // Q^T the same way as K^T, through its place
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int n = 0; n < NX; ++n) *(b8*)&keys[n][16 * wave + r][32 * s + 8 * g] = qa[s][n];
     }
+    __syncthreads();
+    if (GRAD && first) transposed(w.qt);
 
     // X: the 16 x 16 blocks on the diagonal by substitution, a column a lane (four times over) ...
     float x[16];
@@ -166,18 +196,6 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         for (int i = 0; i < 16; ++i) xm[16 * wave + i][16 * wave + r] = x[i];
     }
     __syncthreads();
-    if (GRAD && first) {
-        for (int i = tid; i < KD * kChunk / 8; i += kDeltaThreads) {
-            const int d = i % KD, at = i / KD * 8;
-#pragma unroll
-            for (int n = 0; n < NX; ++n) {
-                b8 v;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = keys[n][at + j][d];
-                *(b8*)(w.qt + (kc * NX + n) * kChunk * KD + d * kChunk + at) = v;
-            }
-        }
-    }
     // ... and those below, X_ij = -X_ii (sum_k A_ik X_kj), a column of blocks a wavefront, in fp32
     f4 column[4];
 #pragma unroll
@@ -209,20 +227,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 #pragma unroll
         for (int e = 0; e < 4; ++e) xm[16 * i + 4 * g + e][16 * wave + r] = 0.0f;
     __syncthreads();
-    for (int turn = 0; turn < (GRAD ? 2 : 1); ++turn) {
-        const int row = tid >> 2, at = (tid & 3) * 16;
-        bf16_t* out = (turn ? w.xt : w.x) + vc * 3 * kSquare + row * kChunk + at;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[8];
-            b8 parts[3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = turn ? xm[at + 8 * h + j][row] : xm[row][at + 8 * h + j];
-            split8(v, parts);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) *(b8*)(out + n * kSquare + 8 * h) = parts[n];
-        }
-    }
+    square(std::integral_constant<int, 3>(), w.x + vc * 3 * kSquare, false);
+    if (GRAD) square(std::integral_constant<int, 3>(), w.xt + vc * 3 * kSquare, true);
 }
 
 // ---------------------------------------------------------------- the sweep
@@ -285,15 +291,15 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
 
     b8 ka[KS][NX], qa[GRAD ? 1 : KS][NX], kta[TW][2][NX], xa[2][3], pa[2][RP];
     unsigned next_v[NT][4];
-    f4 gamma, left, strength;
-    float end;
+    f4 gamma, left, strength, next_gamma, next_left, next_strength;
+    float end, next_end;
     auto fetch_keys = [&](int c) {
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
             for (int n = 0; n < NX; ++n) {
-                ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KD, wave, i, lane);
-                if (!GRAD) qa[i][n] = operand(w.q + ((kc + c) * NX + n) * kChunk * KD, KD, wave, i, lane);
+                ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
+                if (!GRAD) qa[i][n] = operand(w.q + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
             }
     };
     auto fetch_values = [&] {
@@ -309,7 +315,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
         for (int i = 0; i < 2; ++i)
             if (i < steps) {
 #pragma unroll
-                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.x + ((vc + c) * 3 + n) * kSquare, kChunk, wave, i, lane);
+                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.x + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
             }
     };
     auto fetch_mixed = [&](int c) {
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
             for (int i = 0; i < 2; ++i)
                 if (i < steps) {
 #pragma unroll
-                    for (int n = 0; n < RP; ++n) pa[i][n] = operand(w.p + ((vc + c) * RP + n) * kSquare, kChunk, wave, i, lane);
+                    for (int n = 0; n < RP; ++n) pa[i][n] = operand(w.p + ((vc + c) * RP + n) * kSquare, 2, wave, i, lane);
                 }
         }
 #pragma unroll
@@ -326,17 +332,18 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, kChunk, TW * wave + i, m, lane);
+                for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
     };
     auto fetch_scalars = [&](int c) {
         const float* from = w.scalars + (vc + c) * kScalars * kChunk;
-        gamma = *(const f4*)(from + kGamma * kChunk + my_row);
-        left = *(const f4*)(from + kLeft * kChunk + my_row);
-        strength = *(const f4*)(from + kStrength * kChunk + my_row);
-        end = from[kGamma * kChunk + kChunk - 1];
+        next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
+        next_left = *(const f4*)(from + kLeft * kChunk + my_row);
+        next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
+        next_end = from[kGamma * kChunk + kChunk - 1];
     };
+    // (loads come back in their order: they are made in the order of their use, each kind when the one before it has been used up)
     if (chunks > 0) {
-        fetch_keys(0), fetch_values(), fetch_inverse(0), fetch_mixed(0), fetch_scalars(0);
+        fetch_keys(0), fetch_values(), fetch_scalars(0), fetch_inverse(0), fetch_mixed(0);
         put_state();
     }
     for (int c = 0; c < chunks; ++c) {
@@ -370,6 +377,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
                 if (!GRAD) out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
             }
         fetch_keys(next);
+        gamma = next_gamma, left = next_left, strength = next_strength, end = next_end;
         // b (V - e^G (K S))
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -379,6 +387,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
             misses.put_half(wave, n, lane, miss);
         }
         if (c + 1 < chunks) fetch_values();
+        fetch_scalars(next);
         lds_barrier();
         // U
 #pragma unroll
@@ -438,7 +447,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
             }
             y.move(1);
         }
-        fetch_mixed(next), fetch_scalars(next);
+        fetch_mixed(next);
     }
     if (!GRAD) {
         T* behind = (T*)a.y + b * p.y_batch + head * p.value_dim;
@@ -517,9 +526,14 @@ hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, co
     return launch(true, p, a, shape, w, grad, s);
 }
 
-DeltaShape delta_shape(const sys_gated_delta_t& p)
+DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a)
 {
     DeltaShape s = {};
+    // whole pieces of eight entries, at addresses that are multiples of four
+    const size_t element = p.dtype == SYS_F32 ? 4 : 2;
+    s.whole = a && p.key_dim % 8 == 0 && (uintptr_t)a->q % 4 == 0 && (uintptr_t)a->k % 4 == 0;
+    for (long long stride : {p.q_batch, p.q_row, p.k_batch, p.k_row})
+        if (stride * element % 4) s.whole = 0;
     s.chunks = delta_chunks(p);
     s.padded = delta_padded(p);
     s.columns = (p.value_dim + 31) / 32 * 32;
@@ -540,11 +554,11 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
     DeltaPlanes of = {};
     take(of.x, 3 * square);
     take(of.k, keys);
+    take(of.q, keys);
     take(of.kt, keys);
     take(of.scalars, value_chunks * kScalars * kChunk * sizeof(float));
     if (!grad) {
         take(of.p, result * square);
-        take(of.q, keys);
     } else {
         take(of.xt, 3 * square);
         take(of.pt, 3 * square);
@@ -568,7 +582,7 @@ size_t delta_workspace(const sys_gated_delta_t& p)
 hipError_t launch_delta(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s)
 {
     if (p.length <= kShort) return launch_delta_positions(p, a, s);
-    const DeltaShape shape = delta_shape(p);
+    const DeltaShape shape = delta_shape(p, &a);
     DeltaPlanes w;
     delta_planes(p, shape, false, a.workspace, &w);
     const hipError_t e = launch_delta_matrices(p, a, shape, w, false, s);

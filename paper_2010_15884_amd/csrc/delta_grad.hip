@@ -6,9 +6,11 @@
 // and U.  Then all chunks side by side: with the ratios of decays r_ij = e^(G_i - G_j) and
 //   B_ij = r_ij dO_i . U_j  (j <= i),   C_ij = -r_ij Z_i . U_j  (j < i),
 //   dQ = e^G (dO S^T) + B K,   Kr = -e^G (Z S^T) + C K,   Kc = E (U dS'^T) + B^T Q + (b C)^T K,   dK = b Kr + Kc,
-//   db_i = Z_i . V_i + k_i . Kr_i,   dG_i = q_i . dQ_i + b_i k_i . Kr_i - k_i . Kc_i,
-//   dG_end += e^(G_end) <S, dS'> + sum_i E_i k_i . (dS' U_i),   and the logarithm of a decay gets the sum of dG from its position on.
-// (Each of these sums is taken of products that are there already: a row of K or Q times what has been found for it.)
+//   db_i = Z_i . V_i + k_i . Kr_i,   and the logarithm of a decay gets the sum of the gradients dG of the sums G from its position on.
+// The shares of B and C in dG_i cancel between a row and a column of the two positions' entry: with
+//   H_ij = B_ij q_i . k_j + b_i C_ij k_i . k_j  (j < i)  they are the row's sum less the column's, of the same numbers,
+// and what else there is comes from the products with the states: q_i . (e^G S dO)_i + b_i k_i . (-e^G S Z)_i from the position on, E_i k_i . (dS' U_i) up
+// to it, e^(G_end) <S, dS'> for all; sums over the positions of a chunk are in 64 bits.
 #include "delta_tile.h"
 #include "launch.h"
 
@@ -70,12 +72,12 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_del
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int n = 0; n < NX; ++n) ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KD, wave, i, lane);
+            for (int n = 0; n < NX; ++n) ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (i >= first_step) {
 #pragma unroll
-                for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.pt + ((vc + c) * 3 + n) * kSquare, kChunk, wave, i, lane);
+                for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.pt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
             }
     };
     auto fetch_outs = [&] {
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_del
         for (int i = 0; i < 2; ++i)
             if (i >= first_step) {
 #pragma unroll
-                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.xt + ((vc + c) * 3 + n) * kSquare, kChunk, wave, i, lane);
+                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.xt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
             }
     };
     auto fetch_rest = [&](int c) {
@@ -104,8 +106,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_del
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
-                    kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, kChunk, TW * wave + i, m, lane);
-                    qta[i][m][n] = operand(w.qt + ((kc + c) * NX + n) * kChunk * KD, kChunk, TW * wave + i, m, lane);
+                    kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
+                    qta[i][m][n] = operand(w.qt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
                 }
         const float* from = w.scalars + (vc + c) * kScalars * kChunk;
         gamma = *(const f4*)(from + kGamma * kChunk + my_row);
@@ -232,12 +234,12 @@ __device__ __forceinline__ float together(const b8 (&parts)[N], int i)
     return v;
 }
 
-// A workgroup a chunk of a key head, through the value heads that share it; wavefront w the positions 16 w .. 16 w + 15.  S, dS' and U of 32 value columns at a time
+// A workgroup a chunk of a key head, through the value heads that share it; wavefront w the positions of tile w.  S, dS' and U of 32 value columns at a time
 // go through LDS, as the operands that all four wavefronts need.
 template <typename T, int KD>
 __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KT = KD / 16, TW = KD / 64, kPitch = kChunk + 8;
+    constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KS = KD / 32, KT = KD / 16, TW = KD / 64, kPitch = kChunk + 8;
     const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, key_head = rest % p.key_heads, b = rest / p.key_heads;
     const int shared = p.value_heads / p.key_heads;
     const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
         Squares squares;
         __device__ Pool() {}
     } pool;
-    __shared__ float rows_dg[kChunk], rows_db[kChunk], rows_end[kChunk], waves_end[4];
+    __shared__ float rows_dg[kChunk], rows_db[kChunk], rows_end[kChunk], columns_dg[4][kChunk], waves_end[4];
 
     f4 dq_all[KT] = {}, dk_all[KT] = {};
     for (int h = 0; h < shared; ++h) {
@@ -296,9 +298,9 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
                     next_ds[i * RP + m] = *(const b8*)(from_ds + ((size_t)m * KD + 64 * i + row) * shape.columns + at);
                 }
                 next_u[m] = *(const b8*)(from_u + ((size_t)m * kChunk + row) * shape.columns + at);
-                next_z[m] = *(const b8*)(from_z + ((size_t)m * kChunk + 16 * wave + r) * shape.columns + 32 * step + 8 * g);
+                next_z[m] = *(const b8*)(from_z + ((size_t)m * kChunk + tile_row(wave, r)) * shape.columns + 32 * step + 8 * g);
             }
-            const int mine = 16 * wave + r;
+            const int mine = tile_row(wave, r);
             load_eight(dy + mine * p.y_row, 32 * step + 8 * g, p.value_dim, mine < rows, next_dy);
             load_eight(v + mine * p.v_row, 32 * step + 8 * g, p.value_dim, mine < rows, next_v);
         };
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
         for (int step = 0; step < steps; ++step) {
             lds_barrier();
             {
-                const int tile = tid >> 6, to = (tid & 3) * 16 + (tid >> 2 & 15);
+                const int tile = tile_of(tid >> 2), to = (tid & 3) * 16 + row_in_tile(tid >> 2);
 #pragma unroll
                 for (int m = 0; m < RP; ++m) {
 #pragma unroll
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
             zv = multiply<RP - 1>(za, va, zv);
 #pragma unroll
             for (int n = 0; n < 4; ++n)
-                if (n <= wave) {
+                if (n / 2 <= wave / 2) {
                     b8 ub[RP];
 #pragma unroll
                     for (int m = 0; m < RP; ++m) ub[m] = pool.columns.u[n][m][lane];
@@ -358,24 +360,49 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
         // the squares B and C, as they are and transposed
         const float* scalars = w.scalars + vc * kScalars * kChunk;
         const double* sums = (const double*)(scalars + kSums * kChunk);
-        const int mine = 16 * wave + 4 * g;
+        const int mine = tile_row(wave, 4 * g), middle = wave >> 1;
         const f4 gamma = *(const f4*)(scalars + kGamma * kChunk + mine), left = *(const f4*)(scalars + kLeft * kChunk + mine);
         const f4 strength = *(const f4*)(scalars + kStrength * kChunk + mine);
         double mine_sum[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) mine_sum[e] = sums[mine + e];
+        // (new addresses for every head, as far as the compiler knows: loaded ahead of the loop these operands would take all registers)
+        const bf16_t *kt = w.kt + kc * NX * kChunk * KD, *qt = w.qt + kc * NX * kChunk * KD, *kp = w.k + kc * NX * kChunk * KD, *qp = w.q + kc * NX * kChunk * KD;
+        asm volatile("" : "+s"(kt), "+s"(qt), "+s"(kp), "+s"(qp));
+        f4 of_g = {}, of_b = {}, of_end = {};
 #pragma unroll
         for (int n = 0; n < 4; ++n)
-            if (n <= (wave | 1)) {
-                const int column = 16 * n + r;
+            if (n / 2 <= middle) {
+                f4 kk = {}, qk = {};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    b8 ka[NX], qa[NX], kb[NX];
+#pragma unroll
+                    for (int m = 0; m < NX; ++m) {
+                        ka[m] = operand(kp + m * kChunk * KD, KS, wave, s, lane);
+                        qa[m] = operand(qp + m * kChunk * KD, KS, wave, s, lane);
+                        kb[m] = operand(kp + m * kChunk * KD, KS, n, s, lane);
+                    }
+                    kk = multiply<2>(ka, kb, kk);
+                    qk = multiply<2>(qa, kb, qk);
+                }
+                const int column = tile_row(n, r);
                 const double column_sum = sums[column];
                 f4 fb, fc;
+                float of_column = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float ratio = fast_exp2((float)(mine_sum[e] - column_sum));
                     fb[e] = column <= mine + e ? p.scale * (ratio * dp[n][e]) : 0.0f;
                     fc[e] = column < mine + e ? -(ratio * da[n][e]) : 0.0f;
+                    const float both_of = column < mine + e ? __builtin_fmaf(fb[e], qk[e], strength[e] * (fc[e] * kk[e])) : 0.0f;
+                    of_g[e] += both_of;
+                    of_column += both_of;
+                    of_b[e] = __builtin_fmaf(fc[e], kk[e], of_b[e]);
                 }
+                of_column += __shfl_xor(of_column, 16);
+                of_column += __shfl_xor(of_column, 32);
+                if (g == 0) columns_dg[wave][column] = of_column;
                 u2 pb[RP], pc[RP], pct[RP];
                 split4(fb, pb);
                 split4(fc, pc);
@@ -390,43 +417,37 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
                         pool.squares.c[m][mine + e][column] = as_bf16(pc[m][e / 2] >> 16 * (e & 1));
                     }
                 }
+            } else if (g == 0) {
+                columns_dg[wave][tile_row(n, r)] = 0.0f;
             }
         lds_barrier();
-        f4 of_g = {}, of_b = {}, of_end = {};
-        // (a new address for every head, as far as the compiler knows: loaded ahead of the loop these operands would take all registers)
-        const bf16_t *kt = w.kt + kc * NX * kChunk * KD, *qt = w.qt + kc * NX * kChunk * KD;
-        asm volatile("" : "+s"(kt), "+s"(qt));
-        const int middle = wave >> 1;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
             __builtin_amdgcn_sched_barrier(0);
             f4 kr = -(gamma * zs[t]), kcol = left * us[t], qrow = gamma * p.scale * dq[t];
-            // q and k of these positions
-            f4 q = {}, k = {};
-#pragma unroll
-            for (int n = 0; n < NX; ++n) {
-                const u2 qv = *(const u2*)(qt + n * kChunk * KD + (16 * t + r) * kChunk + mine);
-                const u2 kv = *(const u2*)(kt + n * kChunk * KD + (16 * t + r) * kChunk + mine);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    q[e] += (float)as_bf16(qv[e / 2] >> 16 * (e & 1));
-                    k[e] += (float)as_bf16(kv[e / 2] >> 16 * (e & 1));
-                }
-            }
-            of_end += k * kcol;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 b8 kb[NX], qb[NX], m1[RP], m2[RP];
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
-                    kb[n] = *(const b8*)(kt + n * kChunk * KD + (16 * t + r) * kChunk + 32 * s + 8 * g);
-                    qb[n] = *(const b8*)(qt + n * kChunk * KD + (16 * t + r) * kChunk + 32 * s + 8 * g);
+                    kb[n] = operand(kt + n * kChunk * KD, 2, t, s, lane);
+                    qb[n] = operand(qt + n * kChunk * KD, 2, t, s, lane);
+                }
+                if (s == middle) {
+                    // the entries of these positions' own keys and queries are a half of this operand
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float k = wave & 1 ? together(kb, 4 + e) : together(kb, e), q = wave & 1 ? together(qb, 4 + e) : together(qb, e);
+                        of_g[e] += __builtin_fmaf(q, gamma[e] * p.scale * dq[t][e], -(strength[e] * gamma[e]) * (k * zs[t][e]));
+                        of_b[e] = __builtin_fmaf(-k, gamma[e] * zs[t][e], of_b[e]);
+                        of_end[e] = __builtin_fmaf(k, left[e] * us[t][e], of_end[e]);
+                    }
                 }
                 if (s <= middle) {
 #pragma unroll
                     for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.b[m][16 * wave + r][32 * s + 8 * g];
-                        m2[m] = *(const b8*)&pool.squares.c[m][16 * wave + r][32 * s + 8 * g];
+                        m1[m] = *(const b8*)&pool.squares.b[m][tile_row(wave, r)][32 * s + 8 * g];
+                        m2[m] = *(const b8*)&pool.squares.c[m][tile_row(wave, r)][32 * s + 8 * g];
                     }
                     qrow = multiply<RP - 1>(m1, kb, qrow);
                     kr = multiply<RP - 1>(m2, kb, kr);
@@ -434,8 +455,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
                 if (s >= middle) {
 #pragma unroll
                     for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.bt[m][16 * wave + r][32 * s + 8 * g];
-                        m2[m] = *(const b8*)&pool.squares.ct[m][16 * wave + r][32 * s + 8 * g];
+                        m1[m] = *(const b8*)&pool.squares.bt[m][tile_row(wave, r)][32 * s + 8 * g];
+                        m2[m] = *(const b8*)&pool.squares.ct[m][tile_row(wave, r)][32 * s + 8 * g];
                     }
                     kcol = multiply<RP - 1>(m1, qb, kcol);
                     kcol = multiply<RP - 1>(m2, kb, kcol);
@@ -443,8 +464,6 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
             }
             dq_all[t] += qrow;
             dk_all[t] += strength * kr + kcol;
-            of_b += k * kr;
-            of_g += q * qrow + k * (strength * kr - kcol);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -464,17 +483,18 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
         if (lane == 0) waves_end[wave] = both;
         lds_barrier();
         if (wave == 0) {
-            double dg = (double)rows_dg[lane], de = (double)rows_end[lane];
-#pragma unroll
-            for (int m = 32; m; m >>= 1) de += __shfl_xor(de, m);
-            const double end = (double)scalars[kGamma * kChunk + kChunk - 1];
-            de += end * ((double)waves_end[0] + (double)waves_end[1] + (double)waves_end[2] + (double)waves_end[3]);
+            // gradients of the sums G that end in a position and behind it, and of what is left behind the positions before it
+            const double own = (double)rows_end[lane];
+            double dg = (double)rows_dg[lane] - ((double)columns_dg[0][lane] + (double)columns_dg[1][lane] + (double)columns_dg[2][lane] + (double)columns_dg[3][lane]), de = own;
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1) {
-                const double other = __shfl_down(dg, m);
-                if (lane + m < 64) dg += other;
+                const double behind = __shfl_down(dg, m), before = __shfl_up(de, m);
+                if (lane + m < 64) dg += behind;
+                if (lane >= m) de += before;
             }
-            const float log_decay = (float)(dg + de);
+            const double end = (double)scalars[kGamma * kChunk + kChunk - 1];
+            const float log_decay =
+                (float)(dg + (de - own) + end * ((double)waves_end[0] + (double)waves_end[1] + (double)waves_end[2] + (double)waves_end[3]));
             float of_a = 0.0f, of_bias = 0.0f, db = 0.0f;
             if (lane < rows) {
                 const float pre = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? a.delta_bias[head] : 0.0f);
@@ -505,7 +525,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
     for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int row = 16 * wave + 4 * g + e, column = 16 * t + r;
+            const int row = tile_row(wave, 4 * g) + e, column = tile_row(t, r);
             if (row < here && column < p.key_dim) {
                 const long long at = ((at0 + row) * p.key_heads + key_head) * p.key_dim + column;
                 ((T*)a.dq)[at] = (T)dq_all[t][e];
@@ -559,7 +579,7 @@ size_t delta_grad_workspace(const sys_gated_delta_t& p) { return p.length && p.b
 
 hipError_t launch_delta_grad(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s)
 {
-    const DeltaShape shape = delta_shape(p);
+    const DeltaShape shape = delta_shape(p, &a);
     DeltaPlanes w = {};
     if (p.batch) {
         if (p.length) delta_planes(p, shape, true, a.workspace, &w);

@@ -89,13 +89,17 @@ __device__ __forceinline__ void split4(f4 rest, u2 (&out)[N])
         }
 }
 
-// The row of a matrix that is row m of tile `tile` of an A operand, and of D.
+// The row of a matrix that is row m of tile `tile` of an A operand, and of D; and the other way round.
 __device__ __forceinline__ constexpr int tile_row(int tile, int m) { return 32 * (tile >> 1) + 8 * (m >> 2) + 4 * (tile & 1) + (m & 3); }
+__device__ __forceinline__ constexpr int tile_of(int row) { return 2 * (row >> 5) + (row >> 2 & 1); }
+__device__ __forceinline__ constexpr int row_in_tile(int row) { return 4 * (row >> 3 & 3) + (row & 3); }
 
-// A operand: rows of `tile`, columns 32 step .. 32 step + 31 of a row-major matrix.
-__device__ __forceinline__ b8 operand(const bf16_t* matrix, int columns, int tile, int step, int lane)
+// Matrices lie in the workspace as the operands that are taken of them: 1 KB a tile of rows and step of 32 columns, where lane l has the eight entries from
+// column 8 (l / 16) on of row l % 16 of the tile.  (Row-major, a load's neighbouring lanes would be in rows of their own: 45 cache accesses an
+// instruction instead of 16, and the addresses' unit was what the sweep waited for: 163 us against 110 for 4096 positions of 32 heads of 128 x 128.)
+__device__ __forceinline__ b8 operand(const bf16_t* matrix, int steps, int tile, int step, int lane)
 {
-    return *(const b8*)(matrix + tile_row(tile, lane & 15) * columns + 32 * step + 8 * (lane >> 4));
+    return *(const b8*)(matrix + ((tile * steps + step) * 64 + lane) * 8);
 }
 
 // The barrier of a workgroup whose wavefronts exchange through LDS alone: loads from memory stay in flight.
@@ -135,9 +139,10 @@ struct Operands {
     }
 };
 
-// What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, row-major.  Per value head and
+// What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, as operands.  Per value head and
 // chunk X [64][64] (three parts), P (kResultParts; gradients: transposes of both, three parts), and for every position the Scalars; per key head and chunk
-// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, kResultParts each.
+// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, kResultParts each,
+// row-major.
 struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
     bf16_t *s, *ds, *u, *z;            // [padded][columns], [64][columns]
@@ -150,6 +155,7 @@ struct DeltaShape {
     int padded;                        // the key dimension as the kernels have it, 64 or 128
     int columns;                       // the value dimension rounded up to 32
     int tiles;                         // of columns
+    int whole;                         // rows of q and k may be loaded 16 bytes at a time
 };
 
 enum Scalars { kGamma, kLeft, kStrength, kSums = 4, kScalars = 6 };    // e^G, e^(G_end - G), b; G in 64 bits, to base 2 (for gradients)
@@ -194,10 +200,50 @@ struct ChunkRows {
     __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }
 };
 
+// Eight neighbouring entries of a row on their way into parts.
+template <typename T>
+struct Eight {
+    u4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rows, unsigned offset)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 16 * i, 0));
+    }
+    __device__ __forceinline__ void load(const T* row, int at, int columns, bool there)
+    {
+        float f[8];
+        load_eight(row, at, columns, there, f);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            T t[16 / sizeof(T)];
+#pragma unroll
+            for (int j = 0; j < 16 / (int)sizeof(T); ++j) t[j] = (T)f[16 / sizeof(T) * i + j];
+            v[i] = __builtin_bit_cast(u4, t);
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ void split(b8 (&out)[N]) const
+    {
+        if constexpr (N == 1) {
+            out[0] = __builtin_bit_cast(b8, v[0]);
+        } else {
+            typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const Piece piece = __builtin_bit_cast(Piece, v[i]);
+#pragma unroll
+                for (int j = 0; j < 16 / (int)sizeof(T); ++j) f[16 / sizeof(T) * i + j] = (float)piece[j];
+            }
+            split8(f, out);
+        }
+    }
+};
+
 // The two kernels in front of all others (delta_chunk.hip): the chunks' matrices, and the sweep forwards, which gives the outputs or, for gradients, S and U.
 hipError_t launch_delta_matrices(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
 hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
-DeltaShape delta_shape(const sys_gated_delta_t& p);
+DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a = nullptr);
 // The planes of a call, from `base` on (a null pointer: for their size), and the bytes that they take.
 size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool grad, void* base, DeltaPlanes* w);
 // A position at a time (delta_rule.hip).
