@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     const bool first = head % shared == 0;         // of the value heads of a key head: it writes what they have in common
     const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
     if (rows <= 0) return;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
     const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
 
     __shared__ __attribute__((aligned(16))) bf16_t keys[NX][kChunk][kPitch];
@@ -31,25 +31,24 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     __shared__ float strengths[kChunk];
 
     // K into LDS, and the rows of Q that this wavefront works on
-    const T* k = (const T*)a.k + b * p.k_batch + t0 * p.k_row + key_head * p.key_dim;
-    const T* q = (const T*)a.q + b * p.q_batch + t0 * p.q_row + key_head * p.key_dim;
     constexpr int kPieces = kChunk * KD / 8 / kDeltaThreads;
     b8 qa[KS][NX];
     {
         Eight<T> from_k[kPieces], from_q[KS];
-        const ChunkRows<T> k_rows(k - t0 * p.k_row, p.k_row, p.key_dim, chunk, last), q_rows(q - t0 * p.q_row, p.q_row, p.key_dim, chunk, last);
+        const ChunkRows<T> k_rows((const T*)a.k + b * p.k_batch + key_head * p.key_dim, p.k_row, p.key_dim, chunk, last);
+        const ChunkRows<T> q_rows((const T*)a.q + b * p.q_batch + key_head * p.key_dim, p.q_row, p.key_dim, chunk, last);
         const __amdgpu_buffer_rsrc_t k_buffer = k_rows.buffer(), q_buffer = q_rows.buffer();
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int row = (tid + i * kDeltaThreads) / (KD / 8), at = (tid + i * kDeltaThreads) % (KD / 8) * 8;
             if (shape.whole) from_k[i].load(k_buffer, at < p.key_dim ? k_rows.offset(row, at) : kNowhere);
-            else from_k[i].load(k + row * p.k_row, at, p.key_dim, row < rows);
+            else from_k[i].load_each(k_buffer, k_rows.offset(row, at), p.key_dim - at);
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const int row = 16 * wave + r, at = 32 * s + 8 * g;
             if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.offset(row, at) : kNowhere);
-            else from_q[s].load(q + row * p.q_row, at, p.key_dim, row < rows);
+            else from_q[s].load_each(q_buffer, q_rows.offset(row, at), p.key_dim - at);
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -71,16 +70,23 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         }
     }
     if (wave == 0) {
-        float step = 0.0f, strength = 0.0f;
+        // in 64 bits: what a step size is off by adds up over all positions that a state lives through, and a ratio of decays is the exponential of a small
+        // difference of what may be large sums (with the step sizes of sequence.h, off by up to 8 2^-24, the gradients of A were off by 2e-6 of themselves
+        // after 2048 positions, now 5e-7)
+        double step = 0.0, strength = 0.0, slope = 0.0;
         if (lane < rows) {
-            step = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? a.delta_bias[head] : 0.0f);
-            strength = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
-            if (p.softplus) step = softplus(step);
-            if (p.sigmoid) strength = sigmoid(strength);
+            step = (double)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? (double)a.delta_bias[head] : 0.0);
+            strength = (double)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
+            slope = 1.0;
+            if (p.softplus) {
+                const double small = exp(-fabs(step)), large = step < 0.0 ? small : 1.0;
+                slope = large / (1.0 + small);
+                step = (step < 0.0 ? 0.0 : step) + log1p(small);       // (a NaN comes back with `small`)
+            }
+            if (p.sigmoid) strength = 1.0 / (1.0 + exp(-strength));
         }
-        // in 64 bits: a ratio of decays is the exponential of a small difference of what may be large sums.  A decay of 2^-10000 is 0 as any smaller one, and
-        // leaves the differences behind it their digits (NaN passes)
-        double sum = (double)step * (double)a.a[head] * 1.4426950408889634;
+        // a decay of 2^-10000 is 0 as any smaller one, and leaves the differences behind it their digits (NaN passes)
+        double sum = step * (double)a.a[head] * 1.4426950408889634;
         sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -89,12 +95,16 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         }
         const double end = __shfl(sum, 63);
         sums[lane] = sum;
-        strengths[lane] = strength;
+        strengths[lane] = (float)strength;
         float* out = w.scalars + vc * kScalars * kChunk;
         out[kGamma * kChunk + lane] = fast_exp2((float)sum);
         out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
-        out[kStrength * kChunk + lane] = strength;
-        if (GRAD) ((double*)(out + kSums * kChunk))[lane] = sum;
+        out[kStrength * kChunk + lane] = (float)strength;
+        if (GRAD) {
+            out[kStep * kChunk + lane] = (float)step;
+            out[kSlope * kChunk + lane] = (float)slope;
+            ((double*)(out + kSums * kChunk))[lane] = sum;
+        }
     }
     __syncthreads();
 
@@ -240,7 +250,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
     const unsigned place = xcd_place(blockIdx.x, gridDim.x);
     const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
     const int key_head = head / (p.value_heads / p.key_heads);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk;
     const int steps = (wave >> 1) + 1;             // of X and P: what lies above their diagonals is zero
     const int my_row = tile_row(wave, 4 * g);      // the first of this lane's four positions
@@ -354,16 +364,10 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
 #pragma unroll
             for (int i = 0; i < TW; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    u2 parts[RP];
-                    split4(s[i][n], parts);
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int m = 0; m < RP; ++m)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (column[n] < shape.columns)
-                                w.s[(((vc + c) * RP + m) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column[n]] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
-                }
+                    for (int e = 0; e < 4; ++e)
+                        if (column[n] < shape.columns) w.s[((vc + c) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column[n]] = s[i][n][e];
         }
         // K S and Q S
         f4 ks[NT] = {}, out[NT] = {};
@@ -403,15 +407,9 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
             writes.put_half(wave, n, lane, left * u);
             if (!GRAD) {
                 values.put_half(wave, n, lane, u);
-            } else {
-                u2 parts[RP];
-                split4(u, parts);
+            } else if (column[n] < shape.columns) {
 #pragma unroll
-                for (int m = 0; m < RP; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (column[n] < shape.columns)
-                            w.u[(((vc + c) * RP + m) * kChunk + my_row + e) * shape.columns + column[n]] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+                for (int e = 0; e < 4; ++e) w.u[((vc + c) * kChunk + my_row + e) * shape.columns + column[n]] = u[e];
             }
         }
         fetch_inverse(next);
@@ -534,6 +532,9 @@ DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a)
     s.whole = a && p.key_dim % 8 == 0 && (uintptr_t)a->q % 4 == 0 && (uintptr_t)a->k % 4 == 0;
     for (long long stride : {p.q_batch, p.q_row, p.k_batch, p.k_row})
         if (stride * element % 4) s.whole = 0;
+    s.whole_values = a && p.value_dim % 8 == 0 && (uintptr_t)a->v % 4 == 0 && (uintptr_t)a->dy % 4 == 0;
+    for (long long stride : {p.v_batch, p.v_row, p.y_batch, p.y_row})
+        if (stride * element % 4) s.whole_values = 0;
     s.chunks = delta_chunks(p);
     s.padded = delta_padded(p);
     s.columns = (p.value_dim + 31) / 32 * 32;
@@ -563,7 +564,7 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
         take(of.xt, 3 * square);
         take(of.pt, 3 * square);
         take(of.qt, keys);
-        const size_t state = value_chunks * result * shape.padded * shape.columns * sizeof(bf16_t), rows = value_chunks * result * kChunk * shape.columns * sizeof(bf16_t);
+        const size_t state = value_chunks * shape.padded * shape.columns * sizeof(float), rows = value_chunks * kChunk * shape.columns * sizeof(float);
         take(of.s, state);
         take(of.ds, state);
         take(of.u, rows);

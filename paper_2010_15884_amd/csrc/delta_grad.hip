@@ -8,7 +8,8 @@
 //   dQ = e^G (dO S^T) + B K,   Kr = -e^G (Z S^T) + C K,   Kc = E (U dS'^T) + B^T Q + (b C)^T K,   dK = b Kr + Kc,
 //   db_i = Z_i . V_i + k_i . Kr_i,   and the logarithm of a decay gets the sum of the gradients dG of the sums G from its position on.
 // The shares of B and C in dG_i cancel between a row and a column of the two positions' entry: with
-//   H_ij = B_ij q_i . k_j + b_i C_ij k_i . k_j  (j < i)  they are the row's sum less the column's, of the same numbers,
+//   H_ij = B_ij q_i . k_j + b_i C_ij k_i . k_j  (j < i)  they are the row's sum less the column's, of the same numbers and in 64 bits (what a row's sum is
+// rounded by would reach all positions before it: dA off by 2e-6 of itself),
 // and what else there is comes from the products with the states: q_i . (e^G S dO)_i + b_i k_i . (-e^G S Z)_i from the position on, E_i k_i . (dS' U_i) up
 // to it, e^(G_end) <S, dS'> for all; sums over the positions of a chunk are in 64 bits.
 #include "delta_tile.h"
@@ -20,11 +21,11 @@ namespace {
 template <typename T, int KD>
 __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64, RP = kResultParts<T>;
+    constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64;
     const unsigned place = xcd_place(blockIdx.x, gridDim.x);
     const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
     const int key_head = head / (p.value_heads / p.key_heads);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk;
     const int first_step = wave >> 1;              // of X^T and P^T: what lies below their diagonals is zero
     const int my_row = tile_row(wave, 4 * g);
@@ -127,15 +128,9 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_del
         {
             // dS behind the chunk
 #pragma unroll
-            for (int i = 0; i < TW; ++i) {
-                u2 parts[RP];
-                split4(s[i], parts);
+            for (int i = 0; i < TW; ++i)
 #pragma unroll
-                for (int m = 0; m < RP; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w.ds[(((vc + c) * RP + m) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
-            }
+                for (int e = 0; e < 4; ++e) w.ds[((vc + c) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column] = s[i][e];
         }
         // dU
         f4 ks = {}, u = {};
@@ -169,14 +164,10 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_del
         weighted.put_half(wave, 0, lane, gamma * p.scale * own_dy);
         {
             const __amdgpu_buffer_rsrc_t rows = dv.buffer();
-            u2 parts[RP];
-            split4(z, parts);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 buffer_store<T>(rows, dv_at[e], (T)values[e]);
-#pragma unroll
-                for (int m = 0; m < RP; ++m)
-                    w.z[(((vc + c) * RP + m) * kChunk + my_row + e) * shape.columns + column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+                w.z[((vc + c) * kChunk + my_row + e) * shape.columns + column] = z[e];
             }
             dv.move(-1);
         }
@@ -234,287 +225,341 @@ __device__ __forceinline__ float together(const b8 (&parts)[N], int i)
     return v;
 }
 
-// A workgroup a chunk of a key head, through the value heads that share it; wavefront w the positions of tile w.  S, dS' and U of 32 value columns at a time
-// go through LDS, as the operands that all four wavefronts need.
-template <typename T, int KD>
-__global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+// Eight neighbouring fp32 numbers.
+struct EightFloats {
+    float v[8];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t plane, unsigned offset, int step)
+    {
+        const f4 a = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset, 128 * step, 0));
+        const f4 b = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset + 16, 128 * step, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+};
+
+// The parts of eight numbers, or of their negatives in every other tile.  The matrix cores cut the sums of an instruction off towards minus infinity; with operands whose entries
+// are mostly of one sign, as keys behind an activation are, that adds up over a row and over the positions, and the gradients of A were off by 2e-6 of
+// themselves.  With every other tile of columns negated (and its sums taken back where they are used) it cancels.
+__device__ __forceinline__ void split_signed(const float (&v)[8], int tile, b8 (&out)[3])
 {
-    constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KS = KD / 32, KT = KD / 16, TW = KD / 64, kPitch = kChunk + 8;
+    float with_sign[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) with_sign[i] = tile & 1 ? -v[i] : v[i];
+    split8(with_sign, out);
+}
+
+// A workgroup a chunk of a key head, through the value heads that share it.  Eight wavefronts: wavefront w the positions of tile w % 4 and half w / 4 of the keys' entries; of the
+// squares the first half has B and the second C.  S, dS' and U of 32 value columns at a time are split on their way into LDS, as the operands
+// that all wavefronts need, and <S, dS'> is taken there.
+constexpr int kGradThreads = 512;
+
+template <typename T, int KD>
+__global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+{
+    constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KS = KD / 32, KT = KD / 16, KH = KT / 2, kPitch = kChunk + 8;
     const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, key_head = rest % p.key_heads, b = rest / p.key_heads;
     const int shared = p.value_heads / p.key_heads;
     const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, half = __builtin_amdgcn_readfirstlane(tid >> 8), lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int here = p.length - t0 < kChunk ? p.length - t0 : kChunk;  // rows of the results
     const long long at0 = (long long)b * p.length + t0;
     T* ddelta = (T*)a.ddelta + at0 * p.value_heads;
     T* dbeta = (T*)a.dbeta + at0 * p.value_heads;
     if (rows <= 0) {
-        for (int i = tid; i < here * p.key_dim; i += kDeltaThreads) {
+        for (int i = tid; i < here * p.key_dim; i += kGradThreads) {
             const long long at = ((at0 + i / p.key_dim) * p.key_heads + key_head) * p.key_dim + i % p.key_dim;
             ((T*)a.dq)[at] = (T)0.0f;
             ((T*)a.dk)[at] = (T)0.0f;
         }
-        for (int i = tid; i < here * shared; i += kDeltaThreads) {
+        for (int i = tid; i < here * shared; i += kGradThreads) {
             const int at = i / shared * p.value_heads + key_head * shared + i % shared;
             ddelta[at] = (T)0.0f;
             dbeta[at] = (T)0.0f;
         }
-        for (int i = tid; i < 2 * shared; i += kDeltaThreads)
+        for (int i = tid; i < 2 * shared; i += kGradThreads)
             w.dg[(((size_t)b * p.value_heads + key_head * shared + i / 2) * shape.chunks + chunk) * 2 + i % 2] = 0.0f;
         return;
     }
     const size_t kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
+    const int middle = wave >> 1;
 
-    struct Columns { b8 s[KT][RP][64], ds[KT][RP][64], u[4][RP][64]; };
-    struct Squares { bf16_t b[RP][kChunk][kPitch], c[RP][kChunk][kPitch], bt[RP][kChunk][kPitch], ct[RP][kChunk][kPitch]; };
+    struct Columns { b8 s[KT][3][64], ds[KT][3][64], u[4][3][64]; };
+    struct Squares { bf16_t b[2][RP][kChunk][kPitch], bt[2][RP][kChunk][kPitch]; };            // B and b C, as they are and transposed
     __shared__ union Pool {
         Columns columns;
         Squares squares;
         __device__ Pool() {}
     } pool;
-    __shared__ float rows_dg[kChunk], rows_db[kChunk], rows_end[kChunk], columns_dg[4][kChunk], waves_end[4];
+    __shared__ float rows_db[2][kChunk], rows_end[2][kChunk], rows_zv[kChunk];
+    __shared__ double rows_dg[2][kChunk], columns_dg[8][kChunk], waves_end[8];
 
-    f4 dq_all[KT] = {}, dk_all[KT] = {};
+    f4 dq_all[KH] = {}, dk_all[KH] = {};
     for (int h = 0; h < shared; ++h) {
         const int head = key_head * shared + h;
         const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk;
-        const T* dy = (const T*)a.dy + b * p.y_batch + t0 * p.y_row + head * p.value_dim;
-        const T* v = (const T*)a.v + b * p.v_batch + t0 * p.v_row + head * p.value_dim;
-        const bf16_t* from_s = w.s + vc * RP * KD * shape.columns;
-        const bf16_t* from_ds = w.ds + vc * RP * KD * shape.columns;
-        const bf16_t* from_u = w.u + vc * RP * kChunk * shape.columns;
-        const bf16_t* from_z = w.z + vc * RP * kChunk * shape.columns;
-
-        // pieces of 16 bytes: a row's four, then the rows
-        b8 next_s[TW * RP], next_ds[TW * RP], next_u[RP], next_z[RP];
-        float next_dy[8], next_v[8];
-        auto fetch = [&](int step) {
-            const int at = 32 * step + 8 * (tid & 3), row = tid >> 2;
-#pragma unroll
-            for (int m = 0; m < RP; ++m) {
-#pragma unroll
-                for (int i = 0; i < TW; ++i) {
-                    next_s[i * RP + m] = *(const b8*)(from_s + ((size_t)m * KD + 64 * i + row) * shape.columns + at);
-                    next_ds[i * RP + m] = *(const b8*)(from_ds + ((size_t)m * KD + 64 * i + row) * shape.columns + at);
-                }
-                next_u[m] = *(const b8*)(from_u + ((size_t)m * kChunk + row) * shape.columns + at);
-                next_z[m] = *(const b8*)(from_z + ((size_t)m * kChunk + tile_row(wave, r)) * shape.columns + 32 * step + 8 * g);
-            }
-            const int mine = tile_row(wave, r);
-            load_eight(dy + mine * p.y_row, 32 * step + 8 * g, p.value_dim, mine < rows, next_dy);
-            load_eight(v + mine * p.v_row, 32 * step + 8 * g, p.value_dim, mine < rows, next_v);
+        const ChunkRows<T> dy_rows((const T*)a.dy + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, chunk, last);
+        const ChunkRows<T> v_rows((const T*)a.v + b * p.v_batch + head * p.value_dim, p.v_row, p.value_dim, chunk, last);
+        const __amdgpu_buffer_rsrc_t dy_buffer = dy_rows.buffer(), v_buffer = v_rows.buffer();
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));              // (see below)
+        const int lane = tid & 63, r = lane & 15, g = lane >> 4, operand_row = tile_row(wave, r);
+        const unsigned dy_at = dy_rows.offset(operand_row, 8 * g), v_at = v_rows.offset(operand_row, 8 * g);
+        const int piece = (tid & 255) >> 2, piece_at = 8 * (tid & 3);
+        auto plane = [&](float* of, int rows) {
+            return __builtin_amdgcn_make_buffer_rsrc((void*)(of + vc * rows * shape.columns), 0, (unsigned)(rows * shape.columns) * 4u, 0x00027000);
         };
-        f4 dq[KT] = {}, zs[KT] = {}, us[KT] = {}, dp[4] = {}, da[4] = {}, zv = {};
-        float both = 0.0f;
-        fetch(0);
+        const __amdgpu_buffer_rsrc_t from_s = plane(w.s, KD), from_ds = plane(w.ds, KD), from_u = plane(w.u, kChunk), from_z = plane(w.z, kChunk);
+        const unsigned state_at = ((tid >> 2) * shape.columns + piece_at) * 4u, u_at = (piece * shape.columns + piece_at) * 4u;
+        const unsigned z_at = (operand_row * shape.columns + 8 * g) * 4u;
+        EightFloats next_s, next_ds, next_u, next_z;
+        Eight<T> next_dy, next_v;
+        auto fetch = [&](int step) {
+            if (tid < KD * 4) next_s.load(from_s, state_at, step);
+            next_z.load(from_z, z_at, step);
+            if (shape.whole_values) next_dy.load(dy_buffer, 32 * step + 8 * g < p.value_dim ? dy_at + 32 * step * (unsigned)sizeof(T) : kNowhere);
+            else next_dy.load_each(dy_buffer, dy_at + 32 * step * (unsigned)sizeof(T), p.value_dim - 32 * step - 8 * g);
+        };
+        auto fetch_rest = [&](int step) {
+            if (tid < KD * 4) next_ds.load(from_ds, state_at, step);
+            if (half) {
+                next_u.load(from_u, u_at, step);
+            } else {
+                if (shape.whole_values) next_v.load(v_buffer, 32 * step + 8 * g < p.value_dim ? v_at + 32 * step * (unsigned)sizeof(T) : kNowhere);
+                else next_v.load_each(v_buffer, v_at + 32 * step * (unsigned)sizeof(T), p.value_dim - 32 * step - 8 * g);
+            }
+        };
+        f4 dq[KH] = {}, zs[KH] = {}, us[KH] = {}, square[4] = {};
+        double both = 0.0;                         // (<S, dS'> is the sum of key_dim x value_dim terms of either sign, and all positions of the chunk get it)
+        float zv = 0.0f;
+        fetch(0), fetch_rest(0);
         const int steps = shape.columns / 32;
         for (int step = 0; step < steps; ++step) {
             lds_barrier();
             {
-                const int tile = tile_of(tid >> 2), to = (tid & 3) * 16 + row_in_tile(tid >> 2);
+                b8 parts[3];
+                const int to = (tid & 3) * 16 + row_in_tile(tid >> 2);
+                if (tid < KD * 4) {
 #pragma unroll
-                for (int m = 0; m < RP; ++m) {
+                    for (int i = 0; i < 8; ++i) both = __builtin_fma((double)next_s.v[i], (double)next_ds.v[i], both);
+                    split_signed(next_s.v, tile_of(tid >> 2), parts);
 #pragma unroll
-                    for (int i = 0; i < TW; ++i) {
-                        pool.columns.s[4 * i + tile][m][to] = next_s[i * RP + m];
-                        pool.columns.ds[4 * i + tile][m][to] = next_ds[i * RP + m];
-                    }
-                    pool.columns.u[tile][m][to] = next_u[m];
+                    for (int m = 0; m < 3; ++m) pool.columns.s[tile_of(tid >> 2)][m][to] = parts[m];
+                    split_signed(next_ds.v, tile_of(tid >> 2), parts);
+#pragma unroll
+                    for (int m = 0; m < 3; ++m) pool.columns.ds[tile_of(tid >> 2)][m][to] = parts[m];
+                }
+                if (half) {
+                    split_signed(next_u.v, tile_of(piece), parts);
+#pragma unroll
+                    for (int m = 0; m < 3; ++m) pool.columns.u[tile_of(piece)][m][(tid & 3) * 16 + row_in_tile(piece)] = parts[m];
                 }
             }
-            b8 oa[NX], va[NX], za[RP], ua[RP];
-            split8(next_dy, oa);
-            split8(next_v, va);
+            b8 oa[NX], za[3], ua[3];
+            next_dy.split(oa);
+            split8(next_z.v, za);
+            if (!half) {
+                float values[8];
+                next_v.values(values);
 #pragma unroll
-            for (int m = 0; m < RP; ++m) za[m] = next_z[m];
+                for (int i = 0; i < 8; ++i) zv = __builtin_fmaf(next_z.v[i], values[i], zv);
+            }
             lds_barrier();
+            // (fp32 has the registers for a part of them behind the products only)
             if (step + 1 < steps) fetch(step + 1);
-#pragma unroll
-            for (int m = 0; m < RP; ++m) ua[m] = pool.columns.u[wave][m][lane];
-            zv = multiply<RP - 1>(za, va, zv);
+            if (NX < 3 && step + 1 < steps) fetch_rest(step + 1);
 #pragma unroll
             for (int n = 0; n < 4; ++n)
-                if (n / 2 <= wave / 2) {
-                    b8 ub[RP];
+                if (n / 2 <= middle) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    b8 ub[3];
 #pragma unroll
-                    for (int m = 0; m < RP; ++m) ub[m] = pool.columns.u[n][m][lane];
-                    dp[n] = multiply<RP - 1>(oa, ub, dp[n]);
-                    da[n] = multiply<RP - 1>(za, ub, da[n]);
+                    for (int m = 0; m < 3; ++m) ub[m] = pool.columns.u[n][m][lane];
+                    square[n] = half ? multiply<2>(za, ub, square[n]) : multiply<2>(oa, ub, square[n]);
                 }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                __builtin_amdgcn_sched_barrier(0);                     // (operands of one tile at a time, or the registers do not do)
-                b8 sb[RP], db[RP];
+            for (int m = 0; m < 3; ++m) ua[m] = pool.columns.u[wave][m][lane];
 #pragma unroll
-                for (int m = 0; m < RP; ++m) sb[m] = pool.columns.s[t][m][lane], db[m] = pool.columns.ds[t][m][lane];
-                dq[t] = multiply<RP - 1>(oa, sb, dq[t]);
-                zs[t] = multiply<RP - 1>(za, sb, zs[t]);
-                us[t] = multiply<RP - 1>(ua, db, us[t]);
-                if (t / TW == wave) {
+            for (int i = 0; i < KH; ++i) {
+                __builtin_amdgcn_sched_barrier(0);                     // (operands of one tile at a time: 256 registers do)
+                const int t = half * KH + i;
+                b8 part[3];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) both = __builtin_fmaf(together(sb, i), together(db, i), both);
-                }
+                for (int m = 0; m < 3; ++m) part[m] = pool.columns.s[t][m][lane];
+                dq[i] = multiply<2>(oa, part, dq[i]);
+                zs[i] = multiply<2>(za, part, zs[i]);
+                if (NX > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) part[m] = pool.columns.ds[t][m][lane];
+                us[i] = multiply<2>(ua, part, us[i]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (NX == 3 && step + 1 < steps) fetch_rest(step + 1);
         }
         lds_barrier();
-        // the squares B and C, as they are and transposed
+        int again = lane;
+        asm volatile("" : "+v"(again));
+        const int row = tile_row(wave, again & 15), mine = tile_row(wave, 4 * (again >> 4));       // of A operands; the first of four of D
+        // the squares, as they are and transposed
         const float* scalars = w.scalars + vc * kScalars * kChunk;
         const double* sums = (const double*)(scalars + kSums * kChunk);
-        const int mine = tile_row(wave, 4 * g), middle = wave >> 1;
         const f4 gamma = *(const f4*)(scalars + kGamma * kChunk + mine), left = *(const f4*)(scalars + kLeft * kChunk + mine);
         const f4 strength = *(const f4*)(scalars + kStrength * kChunk + mine);
         double mine_sum[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) mine_sum[e] = sums[mine + e];
-        // (new addresses for every head, as far as the compiler knows: loaded ahead of the loop these operands would take all registers)
+        // (new addresses for every head, as far as the compiler knows: worked out or loaded ahead of the loop they would take all registers)
         const bf16_t *kt = w.kt + kc * NX * kChunk * KD, *qt = w.qt + kc * NX * kChunk * KD, *kp = w.k + kc * NX * kChunk * KD, *qp = w.q + kc * NX * kChunk * KD;
         asm volatile("" : "+s"(kt), "+s"(qt), "+s"(kp), "+s"(qp));
+        const bf16_t* own = half ? kp : qp;        // rows of C belong to keys, those of B to queries
         f4 of_g = {}, of_b = {}, of_end = {};
+        double of_h[4] = {};
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int n = 0; n < 4; ++n) {
+            const int column = tile_row(n, again & 15);
             if (n / 2 <= middle) {
-                f4 kk = {}, qk = {};
+                f4 inner = {};
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    b8 ka[NX], qa[NX], kb[NX];
+                    b8 xa[NX], kb[NX];
 #pragma unroll
                     for (int m = 0; m < NX; ++m) {
-                        ka[m] = operand(kp + m * kChunk * KD, KS, wave, s, lane);
-                        qa[m] = operand(qp + m * kChunk * KD, KS, wave, s, lane);
-                        kb[m] = operand(kp + m * kChunk * KD, KS, n, s, lane);
+                        xa[m] = operand(own + m * kChunk * KD, KS, wave, s, again);
+                        kb[m] = operand(kp + m * kChunk * KD, KS, n, s, again);
                     }
-                    kk = multiply<2>(ka, kb, kk);
-                    qk = multiply<2>(qa, kb, qk);
+                    inner = multiply<2>(xa, kb, inner);
                 }
-                const int column = tile_row(n, r);
                 const double column_sum = sums[column];
-                f4 fb, fc;
-                float of_column = 0.0f;
+                const f4 own_square = n & 1 ? -square[n] : square[n];
+                f4 f;
+                double of_column = 0.0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float ratio = fast_exp2((float)(mine_sum[e] - column_sum));
-                    fb[e] = column <= mine + e ? p.scale * (ratio * dp[n][e]) : 0.0f;
-                    fc[e] = column < mine + e ? -(ratio * da[n][e]) : 0.0f;
-                    const float both_of = column < mine + e ? __builtin_fmaf(fb[e], qk[e], strength[e] * (fc[e] * kk[e])) : 0.0f;
-                    of_g[e] += both_of;
-                    of_column += both_of;
-                    of_b[e] = __builtin_fmaf(fc[e], kk[e], of_b[e]);
+                    const bool below = column < mine + e;
+                    if (half) {
+                        const float c = below ? -(ratio * own_square[e]) : 0.0f;
+                        of_b[e] = below ? __builtin_fmaf(c, inner[e], of_b[e]) : of_b[e];
+                        f[e] = strength[e] * c;
+                    } else {
+                        f[e] = column <= mine + e ? p.scale * (ratio * own_square[e]) : 0.0f;
+                    }
+                    const double product = below ? (double)(f[e] * inner[e]) : 0.0;
+                    of_h[e] += product;
+                    of_column += product;
                 }
                 of_column += __shfl_xor(of_column, 16);
                 of_column += __shfl_xor(of_column, 32);
-                if (g == 0) columns_dg[wave][column] = of_column;
-                u2 pb[RP], pc[RP], pct[RP];
-                split4(fb, pb);
-                split4(fc, pc);
-                split4(strength * fc, pct);
+                if (again < 16) columns_dg[4 * half + wave][column] = of_column;
+                u2 parts[RP];
+                split4(f, parts);
 #pragma unroll
                 for (int m = 0; m < RP; ++m) {
-                    *(u2*)&pool.squares.bt[m][column][mine] = pb[m];
-                    *(u2*)&pool.squares.ct[m][column][mine] = pct[m];
+                    *(u2*)&pool.squares.bt[half][m][column][mine] = parts[m];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        pool.squares.b[m][mine + e][column] = as_bf16(pb[m][e / 2] >> 16 * (e & 1));
-                        pool.squares.c[m][mine + e][column] = as_bf16(pc[m][e / 2] >> 16 * (e & 1));
-                    }
+                    for (int e = 0; e < 4; ++e) pool.squares.b[half][m][mine + e][column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
                 }
-            } else if (g == 0) {
-                columns_dg[wave][tile_row(n, r)] = 0.0f;
+            } else if (again < 16) {
+                columns_dg[4 * half + wave][column] = 0.0;
             }
+        }
         lds_barrier();
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
+        for (int i = 0; i < KH; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            f4 kr = -(gamma * zs[t]), kcol = left * us[t], qrow = gamma * p.scale * dq[t];
+            const int t = half * KH + i;
+            // (U's tile of these positions is a negative where the wavefront's number is odd)
+            const f4 of_dy = gamma * p.scale * (i & 1 ? -dq[i] : dq[i]), of_z = gamma * (i & 1 ? -zs[i] : zs[i]);
+            const f4 of_u = left * ((i ^ wave) & 1 ? -us[i] : us[i]);
+            dq_all[i] += of_dy;
+            dk_all[i] += of_u - strength * of_z;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 b8 kb[NX], qb[NX], m1[RP], m2[RP];
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
-                    kb[n] = operand(kt + n * kChunk * KD, 2, t, s, lane);
-                    qb[n] = operand(qt + n * kChunk * KD, 2, t, s, lane);
+                    kb[n] = operand(kt + n * kChunk * KD, 2, t, s, again);
+                    qb[n] = operand(qt + n * kChunk * KD, 2, t, s, again);
                 }
                 if (s == middle) {
                     // the entries of these positions' own keys and queries are a half of this operand
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float k = wave & 1 ? together(kb, 4 + e) : together(kb, e), q = wave & 1 ? together(qb, 4 + e) : together(qb, e);
-                        of_g[e] += __builtin_fmaf(q, gamma[e] * p.scale * dq[t][e], -(strength[e] * gamma[e]) * (k * zs[t][e]));
-                        of_b[e] = __builtin_fmaf(-k, gamma[e] * zs[t][e], of_b[e]);
-                        of_end[e] = __builtin_fmaf(k, left[e] * us[t][e], of_end[e]);
+                        of_g[e] += __builtin_fmaf(q, of_dy[e], -strength[e] * (k * of_z[e]));
+                        of_b[e] = __builtin_fmaf(-k, of_z[e], of_b[e]);
+                        of_end[e] = __builtin_fmaf(k, of_u[e], of_end[e]);
                     }
                 }
                 if (s <= middle) {
 #pragma unroll
                     for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.b[m][tile_row(wave, r)][32 * s + 8 * g];
-                        m2[m] = *(const b8*)&pool.squares.c[m][tile_row(wave, r)][32 * s + 8 * g];
+                        m1[m] = *(const b8*)&pool.squares.b[0][m][row][32 * s + 8 * (again >> 4)];
+                        m2[m] = *(const b8*)&pool.squares.b[1][m][row][32 * s + 8 * (again >> 4)];
                     }
-                    qrow = multiply<RP - 1>(m1, kb, qrow);
-                    kr = multiply<RP - 1>(m2, kb, kr);
+                    dq_all[i] = multiply<RP - 1>(m1, kb, dq_all[i]);
+                    dk_all[i] = multiply<RP - 1>(m2, kb, dk_all[i]);
                 }
                 if (s >= middle) {
 #pragma unroll
                     for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.bt[m][tile_row(wave, r)][32 * s + 8 * g];
-                        m2[m] = *(const b8*)&pool.squares.ct[m][tile_row(wave, r)][32 * s + 8 * g];
+                        m1[m] = *(const b8*)&pool.squares.bt[0][m][row][32 * s + 8 * (again >> 4)];
+                        m2[m] = *(const b8*)&pool.squares.bt[1][m][row][32 * s + 8 * (again >> 4)];
                     }
-                    kcol = multiply<RP - 1>(m1, qb, kcol);
-                    kcol = multiply<RP - 1>(m2, kb, kcol);
+                    dk_all[i] = multiply<RP - 1>(m1, qb, dk_all[i]);
+                    dk_all[i] = multiply<RP - 1>(m2, kb, dk_all[i]);
                 }
             }
-            dq_all[t] += qrow;
-            dk_all[t] += strength * kr + kcol;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float dg = row_sum(of_g[e]), db = row_sum(of_b[e]), de = row_sum(of_end[e]);
-            if (r == 0) {
-                rows_dg[mine + e] = dg;
-                rows_db[mine + e] = db;
-                rows_end[mine + e] = de;
+            double dg = of_h[e] + (double)of_g[e];
+#pragma unroll
+            for (int m = 1; m < 16; m <<= 1) dg += __shfl_xor(dg, m);
+            const float db = row_sum(of_b[e]), de = row_sum(of_end[e]);
+            if ((again & 15) == 0) {
+                rows_dg[half][mine + e] = dg;
+                rows_db[half][mine + e] = db;
+                rows_end[half][mine + e] = de;
             }
         }
-        // Z_i . V_i lies on the diagonal of this wavefront's tile
-        lds_barrier();
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (r == 4 * g + e) rows_db[mine + e] += zv[e];
+        zv += __shfl_xor(zv, 16);
+        zv += __shfl_xor(zv, 32);
+        if (!half && again < 16) rows_zv[row] = zv;
         for (int m = 32; m; m >>= 1) both += __shfl_xor(both, m);
-        if (lane == 0) waves_end[wave] = both;
+        if (lane == 0) waves_end[4 * half + wave] = both;
         lds_barrier();
-        if (wave == 0) {
+        if (!half && wave == 0) {
             // gradients of the sums G that end in a position and behind it, and of what is left behind the positions before it
-            const double own = (double)rows_end[lane];
-            double dg = (double)rows_dg[lane] - ((double)columns_dg[0][lane] + (double)columns_dg[1][lane] + (double)columns_dg[2][lane] + (double)columns_dg[3][lane]), de = own;
+            const double own_end = (double)rows_end[0][again] + (double)rows_end[1][again];
+            double dg = rows_dg[0][again] + rows_dg[1][again], de = own_end, end = 0.0;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) dg -= columns_dg[m][again], end += waves_end[m];
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1) {
                 const double behind = __shfl_down(dg, m), before = __shfl_up(de, m);
-                if (lane + m < 64) dg += behind;
-                if (lane >= m) de += before;
+                if (again + m < 64) dg += behind;
+                if (again >= m) de += before;
             }
-            const double end = (double)scalars[kGamma * kChunk + kChunk - 1];
-            const float log_decay =
-                (float)(dg + (de - own) + end * ((double)waves_end[0] + (double)waves_end[1] + (double)waves_end[2] + (double)waves_end[3]));
+            const float log_decay = (float)(dg + (de - own_end) + (double)scalars[kGamma * kChunk + kChunk - 1] * end);
             float of_a = 0.0f, of_bias = 0.0f, db = 0.0f;
-            if (lane < rows) {
-                const float pre = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? a.delta_bias[head] : 0.0f);
-                const float step = p.softplus ? softplus(pre) : pre;
-                const float raw = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
-                of_a = step * log_decay;
-                of_bias = a.a[head] * log_decay * (p.softplus ? sigmoid(pre) : 1.0f);
-                db = rows_db[lane];
+            if (again < rows) {
+                of_a = scalars[kStep * kChunk + again] * log_decay;
+                of_bias = a.a[head] * log_decay * scalars[kSlope * kChunk + again];
+                db = rows_zv[again] + (rows_db[0][again] + rows_db[1][again]);
                 if (p.sigmoid) {
-                    const float x = sigmoid(raw);
-                    db *= x * (1.0f - x);
+                    // (1 - b is the sigmoid of -beta, and keeps its digits there)
+                    const float raw = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + again) * p.beta_row + head];
+                    db *= sigmoid(raw) * sigmoid(-raw);
                 }
             }
-            if (lane < here) {
-                ddelta[lane * p.value_heads + head] = (T)of_bias;
-                dbeta[lane * p.value_heads + head] = (T)db;
+            if (again < here) {
+                ddelta[again * p.value_heads + head] = (T)of_bias;
+                dbeta[again * p.value_heads + head] = (T)db;
             }
 #pragma unroll
             for (int m = 32; m; m >>= 1) of_a += __shfl_xor(of_a, m), of_bias += __shfl_xor(of_bias, m);
-            if (lane == 0) {
+            if (again == 0) {
                 w.dg[vc * 2] = of_a;
                 w.dg[vc * 2 + 1] = of_bias;
             }
@@ -522,14 +567,14 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_grad_kernel(sys_gated_del
         // (the next head's operands are put where the squares lie behind a barrier of its own)
     }
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int i = 0; i < KH; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int row = tile_row(wave, 4 * g) + e, column = tile_row(t, r);
-            if (row < here && column < p.key_dim) {
-                const long long at = ((at0 + row) * p.key_heads + key_head) * p.key_dim + column;
-                ((T*)a.dq)[at] = (T)dq_all[t][e];
-                ((T*)a.dk)[at] = (T)dk_all[t][e];
+            const int column = tile_row(half * KH + i, r), mine = tile_row(wave, 4 * g);
+            if (mine + e < here && column < p.key_dim) {
+                const long long at = ((at0 + mine + e) * p.key_heads + key_head) * p.key_dim + column;
+                ((T*)a.dq)[at] = (T)dq_all[i][e];
+                ((T*)a.dk)[at] = (T)dk_all[i][e];
             }
         }
 }
@@ -563,7 +608,7 @@ hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape&
     hipLaunchKernelGGL((delta_back_kernel<T, KD>), dim3((unsigned)sweeps), dim3(kDeltaThreads), 0, s, p, a, of, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !chunks) return e;
-    hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kDeltaThreads), 0, s, p, a, shape, w);
+    hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kGradThreads), 0, s, p, a, shape, w);
     return hipGetLastError();
 }
 

@@ -141,11 +141,10 @@ struct Operands {
 
 // What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, as operands.  Per value head and
 // chunk X [64][64] (three parts), P (kResultParts; gradients: transposes of both, three parts), and for every position the Scalars; per key head and chunk
-// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, kResultParts each,
-// row-major.
+// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, row-major in fp32.
 struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
-    bf16_t *s, *ds, *u, *z;            // [padded][columns], [64][columns]
+    float *s, *ds, *u, *z;             // [padded][columns], [64][columns]
     float* scalars;                    // [kScalars][64]
     float* dg;                         // every chunk's share of the gradients of A and the bias
 };
@@ -155,36 +154,16 @@ struct DeltaShape {
     int padded;                        // the key dimension as the kernels have it, 64 or 128
     int columns;                       // the value dimension rounded up to 32
     int tiles;                         // of columns
-    int whole;                         // rows of q and k may be loaded 16 bytes at a time
+    int whole, whole_values;           // rows of q and k, of v and dy may be loaded 16 bytes at a time
 };
 
-enum Scalars { kGamma, kLeft, kStrength, kSums = 4, kScalars = 6 };    // e^G, e^(G_end - G), b; G in 64 bits, to base 2 (for gradients)
+// e^G, e^(G_end - G), b; for gradients the step size and its derivative by delta, and G in 64 bits, to base 2
+enum Scalars { kGamma, kLeft, kStrength, kStep, kSums, kSlope = 6, kScalars };
 
 inline int delta_padded(const sys_gated_delta_t& p) { return p.key_dim <= 64 ? 64 : 128; }
 inline int delta_chunks(const sys_gated_delta_t& p) { return (p.length + kChunk - 1) / kChunk; }
 
 __device__ __forceinline__ bf16_t as_bf16(unsigned bits) { return __builtin_bit_cast(bf16_t, (unsigned short)bits); }
-
-// Eight neighbouring entries of a row as fp32; zeros past its end and where the row is not there.
-template <typename T>
-__device__ __forceinline__ void load_eight(const T* row, int at, int columns, bool there, float (&out)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = 0.0f;
-    if (!there || at >= columns) return;
-    if (at + 8 <= columns) {
-        if constexpr (sizeof(T) == 2) {
-            Channels<T, 8>::load(row + at, out);
-        } else {
-            Channels<T, 4>::load(row + at, *(float(*)[4])out);
-            Channels<T, 4>::load(row + at + 4, *(float(*)[4])(out + 4));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (at + i < columns) out[i] = (float)row[at + i];
-    }
-}
 
 // Entries of neighbouring positions of a chunk, one column a lane, addressed as a buffer that ends with the last row that exists (zeros behind it).
 template <typename T>
@@ -209,16 +188,34 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 16 * i, 0));
     }
-    __device__ __forceinline__ void load(const T* row, int at, int columns, bool there)
+    // one by one; those behind the `left` that belong to the row are dropped when they are there (they lie in the buffer or past its end)
+    __device__ __forceinline__ void load_each(__amdgpu_buffer_rsrc_t rows, unsigned offset, int left)
     {
-        float f[8];
-        load_eight(row, at, columns, there, f);
+        constexpr int kEach = 4 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                unsigned word = 0;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const int at = (4 * i + j) * kEach + e;
+                    unsigned got;
+                    if constexpr (sizeof(T) == 4) got = __builtin_amdgcn_raw_buffer_load_b32(rows, offset + at * 4, 0, 0);
+                    else got = __builtin_amdgcn_raw_buffer_load_b16(rows, offset + at * 2, 0, 0);
+                    word |= (at < left ? got : 0u) << 16 * e;
+                }
+                v[i][j] = word;
+            }
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const
+    {
+        typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            T t[16 / sizeof(T)];
+            const Piece piece = __builtin_bit_cast(Piece, v[i]);
 #pragma unroll
-            for (int j = 0; j < 16 / (int)sizeof(T); ++j) t[j] = (T)f[16 / sizeof(T) * i + j];
-            v[i] = __builtin_bit_cast(u4, t);
+            for (int j = 0; j < 16 / (int)sizeof(T); ++j) f[16 / sizeof(T) * i + j] = (float)piece[j];
         }
     }
     template <int N>
@@ -227,14 +224,8 @@ struct Eight {
         if constexpr (N == 1) {
             out[0] = __builtin_bit_cast(b8, v[0]);
         } else {
-            typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
             float f[8];
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const Piece piece = __builtin_bit_cast(Piece, v[i]);
-#pragma unroll
-                for (int j = 0; j < 16 / (int)sizeof(T); ++j) f[16 / sizeof(T) * i + j] = (float)piece[j];
-            }
+            values(f);
             split8(f, out);
         }
     }
