@@ -283,7 +283,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     const size_t kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
     const int middle = wave >> 1;
 
-    struct Columns { b8 s[KT][3][64], ds[KT][3][64], u[4][3][64]; };
+    constexpr int kBlock = 64 + 4;                 // an operand's pieces, 17 for 16: lanes that write the four pieces of a row meet other banks
+    struct Columns { b8 s[KT][3][kBlock], ds[KT][3][kBlock], u[4][3][kBlock], z[4][3][kBlock], dy[4][NX][kBlock]; };
     struct Squares { bf16_t b[2][RP][kChunk][kPitch], bt[2][RP][kChunk][kPitch]; };            // B and b C, as they are and transposed
     __shared__ union Pool {
         Columns columns;
@@ -293,6 +294,20 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     __shared__ float rows_db[2][kChunk], rows_end[2][kChunk], rows_zv[kChunk];
     __shared__ double rows_dg[2][kChunk], columns_dg[8][kChunk], waves_end[8];
 
+    // K and Q, which all value heads use, as operands and transposed: as many as LDS has room for
+    constexpr bool kKeep = NX < 3, kKeepTransposed = NX == 1;
+    __shared__ b8 kept[2][kKeep ? NX : 1][kKeep ? 4 * KS : 1][64], kept_transposed[2][kKeepTransposed ? 4 * KS : 1][64];
+    if (kKeep) {
+        for (int i = tid; i < NX * 4 * KS * 64; i += kGradThreads) {
+            const int n = i / (4 * KS * 64), at = i % (4 * KS * 64);
+            (&kept[0][n][0][0])[at] = *(const b8*)(w.k + (kc * NX + n) * kChunk * KD + at * 8);
+            (&kept[1][n][0][0])[at] = *(const b8*)(w.q + (kc * NX + n) * kChunk * KD + at * 8);
+            if (kKeepTransposed) {
+                (&kept_transposed[0][0][0])[at] = *(const b8*)(w.kt + kc * kChunk * KD + at * 8);
+                (&kept_transposed[1][0][0])[at] = *(const b8*)(w.qt + kc * kChunk * KD + at * 8);
+            }
+        }
+    }
     f4 dq_all[KH] = {}, dk_all[KH] = {};
     for (int h = 0; h < shared; ++h) {
         const int head = key_head * shared + h;
@@ -302,99 +317,101 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         const __amdgpu_buffer_rsrc_t dy_buffer = dy_rows.buffer(), v_buffer = v_rows.buffer();
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));              // (see below)
-        const int lane = tid & 63, r = lane & 15, g = lane >> 4, operand_row = tile_row(wave, r);
-        const unsigned dy_at = dy_rows.offset(operand_row, 8 * g), v_at = v_rows.offset(operand_row, 8 * g);
-        const int piece = (tid & 255) >> 2, piece_at = 8 * (tid & 3);
+        const int lane = tid & 63, place = lane + (lane >> 4);
+        // pieces of eight: four a row and step; S and dS' by all lanes, Z and V by the first half of them, U and dO by the second
+        const int piece_row = (tid & 255) >> 2, piece_at = 8 * (tid & 3), piece = 17 * (tid & 3) + row_in_tile(piece_row);
+        const unsigned dy_at = dy_rows.offset(piece_row, piece_at), v_at = v_rows.offset(piece_row, piece_at);
         auto plane = [&](float* of, int rows) {
             return __builtin_amdgcn_make_buffer_rsrc((void*)(of + vc * rows * shape.columns), 0, (unsigned)(rows * shape.columns) * 4u, 0x00027000);
         };
-        const __amdgpu_buffer_rsrc_t from_s = plane(w.s, KD), from_ds = plane(w.ds, KD), from_u = plane(w.u, kChunk), from_z = plane(w.z, kChunk);
-        const unsigned state_at = ((tid >> 2) * shape.columns + piece_at) * 4u, u_at = (piece * shape.columns + piece_at) * 4u;
-        const unsigned z_at = (operand_row * shape.columns + 8 * g) * 4u;
-        EightFloats next_s, next_ds, next_u, next_z;
-        Eight<T> next_dy, next_v;
+        const __amdgpu_buffer_rsrc_t from_s = plane(w.s, KD), from_ds = plane(w.ds, KD), from_rows = plane(half ? w.u : w.z, kChunk);
+        const unsigned state_at = ((tid >> 2) * shape.columns + piece_at) * 4u, rows_at = (piece_row * shape.columns + piece_at) * 4u;
+
+        EightFloats next_s, next_ds, next_rows;
+        Eight<T> next_values;                      // V or dO
         auto fetch = [&](int step) {
-            if (tid < KD * 4) next_s.load(from_s, state_at, step);
-            next_z.load(from_z, z_at, step);
-            if (shape.whole_values) next_dy.load(dy_buffer, 32 * step + 8 * g < p.value_dim ? dy_at + 32 * step * (unsigned)sizeof(T) : kNowhere);
-            else next_dy.load_each(dy_buffer, dy_at + 32 * step * (unsigned)sizeof(T), p.value_dim - 32 * step - 8 * g);
-        };
-        auto fetch_rest = [&](int step) {
-            if (tid < KD * 4) next_ds.load(from_ds, state_at, step);
-            if (half) {
-                next_u.load(from_u, u_at, step);
-            } else {
-                if (shape.whole_values) next_v.load(v_buffer, 32 * step + 8 * g < p.value_dim ? v_at + 32 * step * (unsigned)sizeof(T) : kNowhere);
-                else next_v.load_each(v_buffer, v_at + 32 * step * (unsigned)sizeof(T), p.value_dim - 32 * step - 8 * g);
+            if (tid < KD * 4) {
+                next_s.load(from_s, state_at, step);
+                next_ds.load(from_ds, state_at, step);
             }
+            next_rows.load(from_rows, rows_at, step);
+            const __amdgpu_buffer_rsrc_t buffer = half ? dy_buffer : v_buffer;
+            const unsigned at = (half ? dy_at : v_at) + 32 * step * (unsigned)sizeof(T);
+            if (shape.whole_values) next_values.load(buffer, 32 * step + piece_at < p.value_dim ? at : kNowhere);
+            else next_values.load_each(buffer, at, p.value_dim - 32 * step - piece_at);
         };
         f4 dq[KH] = {}, zs[KH] = {}, us[KH] = {}, square[4] = {};
         double both = 0.0;                         // (<S, dS'> is the sum of key_dim x value_dim terms of either sign, and all positions of the chunk get it)
         float zv = 0.0f;
-        fetch(0), fetch_rest(0);
+        fetch(0);
         const int steps = shape.columns / 32;
         for (int step = 0; step < steps; ++step) {
             lds_barrier();
             {
                 b8 parts[3];
-                const int to = (tid & 3) * 16 + row_in_tile(tid >> 2);
                 if (tid < KD * 4) {
+                    const int tile = tile_of(tid >> 2), to = 17 * (tid & 3) + row_in_tile(tid >> 2);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) both = __builtin_fma((double)next_s.v[i], (double)next_ds.v[i], both);
-                    split_signed(next_s.v, tile_of(tid >> 2), parts);
+                    split_signed(next_s.v, tile, parts);
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.s[tile_of(tid >> 2)][m][to] = parts[m];
-                    split_signed(next_ds.v, tile_of(tid >> 2), parts);
+                    for (int m = 0; m < 3; ++m) pool.columns.s[tile][m][to] = parts[m];
+                    split_signed(next_ds.v, tile, parts);
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.ds[tile_of(tid >> 2)][m][to] = parts[m];
+                    for (int m = 0; m < 3; ++m) pool.columns.ds[tile][m][to] = parts[m];
                 }
+                const int tile = tile_of(piece_row);
                 if (half) {
-                    split_signed(next_u.v, tile_of(piece), parts);
+                    b8 values[NX];
+                    next_values.split(values);
+                    split_signed(next_rows.v, tile, parts);
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.u[tile_of(piece)][m][(tid & 3) * 16 + row_in_tile(piece)] = parts[m];
+                    for (int m = 0; m < 3; ++m) pool.columns.u[tile][m][piece] = parts[m];
+#pragma unroll
+                    for (int m = 0; m < NX; ++m) pool.columns.dy[tile][m][piece] = values[m];
+                } else {
+                    float values[8];
+                    next_values.values(values);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) zv = __builtin_fmaf(next_rows.v[i], values[i], zv);
+                    split8(next_rows.v, parts);
+#pragma unroll
+                    for (int m = 0; m < 3; ++m) pool.columns.z[tile][m][piece] = parts[m];
                 }
-            }
-            b8 oa[NX], za[3], ua[3];
-            next_dy.split(oa);
-            split8(next_z.v, za);
-            if (!half) {
-                float values[8];
-                next_v.values(values);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) zv = __builtin_fmaf(next_z.v[i], values[i], zv);
             }
             lds_barrier();
-            // (fp32 has the registers for a part of them behind the products only)
             if (step + 1 < steps) fetch(step + 1);
-            if (NX < 3 && step + 1 < steps) fetch_rest(step + 1);
+            b8 oa[NX], za[3], ua[3];
+#pragma unroll
+            for (int m = 0; m < NX; ++m) oa[m] = pool.columns.dy[wave][m][place];
+#pragma unroll
+            for (int m = 0; m < 3; ++m) za[m] = pool.columns.z[wave][m][place];
 #pragma unroll
             for (int n = 0; n < 4; ++n)
                 if (n / 2 <= middle) {
                     __builtin_amdgcn_sched_barrier(0);
                     b8 ub[3];
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) ub[m] = pool.columns.u[n][m][lane];
+                    for (int m = 0; m < 3; ++m) ub[m] = pool.columns.u[n][m][place];
                     square[n] = half ? multiply<2>(za, ub, square[n]) : multiply<2>(oa, ub, square[n]);
                 }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int m = 0; m < 3; ++m) ua[m] = pool.columns.u[wave][m][lane];
+            for (int m = 0; m < 3; ++m) ua[m] = pool.columns.u[wave][m][place];
 #pragma unroll
             for (int i = 0; i < KH; ++i) {
                 __builtin_amdgcn_sched_barrier(0);                     // (operands of one tile at a time: 256 registers do)
                 const int t = half * KH + i;
                 b8 part[3];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) part[m] = pool.columns.s[t][m][lane];
+                for (int m = 0; m < 3; ++m) part[m] = pool.columns.s[t][m][place];
                 dq[i] = multiply<2>(oa, part, dq[i]);
                 zs[i] = multiply<2>(za, part, zs[i]);
                 if (NX > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int m = 0; m < 3; ++m) part[m] = pool.columns.ds[t][m][lane];
+                for (int m = 0; m < 3; ++m) part[m] = pool.columns.ds[t][m][place];
                 us[i] = multiply<2>(ua, part, us[i]);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if (NX == 3 && step + 1 < steps) fetch_rest(step + 1);
         }
         lds_barrier();
         int again = lane;
@@ -424,8 +441,13 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                     b8 xa[NX], kb[NX];
 #pragma unroll
                     for (int m = 0; m < NX; ++m) {
-                        xa[m] = operand(own + m * kChunk * KD, KS, wave, s, again);
-                        kb[m] = operand(kp + m * kChunk * KD, KS, n, s, again);
+                        if constexpr (kKeep) {
+                            xa[m] = kept[half ? 0 : 1][m][wave * KS + s][again];
+                            kb[m] = kept[0][m][n * KS + s][again];
+                        } else {
+                            xa[m] = operand(own + m * kChunk * KD, KS, wave, s, again);
+                            kb[m] = operand(kp + m * kChunk * KD, KS, n, s, again);
+                        }
                     }
                     inner = multiply<2>(xa, kb, inner);
                 }
@@ -478,8 +500,13 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                 b8 kb[NX], qb[NX], m1[RP], m2[RP];
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
-                    kb[n] = operand(kt + n * kChunk * KD, 2, t, s, again);
-                    qb[n] = operand(qt + n * kChunk * KD, 2, t, s, again);
+                    if constexpr (kKeepTransposed) {
+                        kb[n] = kept_transposed[0][2 * t + s][again];
+                        qb[n] = kept_transposed[1][2 * t + s][again];
+                    } else {
+                        kb[n] = operand(kt + n * kChunk * KD, 2, t, s, again);
+                        qb[n] = operand(qt + n * kChunk * KD, 2, t, s, again);
+                    }
                 }
                 if (s == middle) {
                     // the entries of these positions' own keys and queries are a half of this operand
@@ -523,9 +550,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                 rows_end[half][mine + e] = de;
             }
         }
-        zv += __shfl_xor(zv, 16);
-        zv += __shfl_xor(zv, 32);
-        if (!half && again < 16) rows_zv[row] = zv;
+        zv = quad_sum(zv);
+        if (!half && (again & 3) == 0) rows_zv[16 * wave + (again >> 2)] = zv;
         for (int m = 32; m; m >>= 1) both += __shfl_xor(both, m);
         if (lane == 0) waves_end[4 * half + wave] = both;
         lds_barrier();
