@@ -1,8 +1,9 @@
 // Gated delta rule in chunks of 64 positions on the matrix cores (delta_tile.h has the formulas, the precision and the layout).
 //
 // Two launches.  The first makes X, P and K^T of all chunks side by side, a workgroup a chunk of a value head.  The second goes through the chunks: a workgroup
-// of four wavefronts a tile of value columns, the state in registers (wavefront w the rows of step w of the keys), S, R and U handed round as bf16
-// parts through LDS with three barriers a chunk; operands that do not depend on the state are loaded a chunk ahead.
+// a tile of value columns, the state in the registers of four wavefronts (wavefront w the rows of step w of the keys), S, R and U handed round as bf16
+// parts through LDS with three barriers a chunk; operands that do not depend on the state are loaded a chunk ahead.  Four more wavefronts take S and U from LDS
+// and make the outputs of them.
 #include "delta_tile.h"
 #include "launch.h"
 
@@ -244,13 +245,15 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 // ---------------------------------------------------------------- the sweep
 
 template <typename T, int KD, int NT, bool GRAD>
-__global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+__global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void delta_sweep_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
     constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64, RP = kResultParts<T>;
+    constexpr bool kAtOnce = NX * NT <= 2;         // there are registers for all operands of a product
     const unsigned place = xcd_place(blockIdx.x, gridDim.x);
     const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
     const int key_head = head / (p.value_heads / p.key_heads);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const bool chain = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0;
     const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk;
     const int steps = (wave >> 1) + 1;             // of X and P: what lies above their diagonals is zero
     const int my_row = tile_row(wave, 4 * g);      // the first of this lane's four positions
@@ -261,178 +264,238 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
 
     __shared__ Operands<KS, 3, NT> states;
     __shared__ Operands<2, 3, NT> misses, writes;
-    __shared__ Operands<2, RP, NT> values;
+    __shared__ Operands<2, GRAD ? 3 : RP, NT> values;
 
-    // the state
-    const size_t state_base = ((size_t)b * p.value_heads + head) * p.key_dim * p.value_dim;
-    const unsigned state_bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
-    f4 s[TW][NT];
-    {
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state + state_base), 0, a.state ? state_bytes : 0u, 0x00027000);
-#pragma unroll
-        for (int i = 0; i < TW; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
-                    s[i][n][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0));
-                }
-    }
-    auto put_state = [&] {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if constexpr (TW == 2) states.put(wave, n, lane, s[0][n], s[1][n]);
-            else states.put_half(wave, n, lane, s[0][n]);
-        }
-    };
-
-    ChunkRows<T> v((const T*)a.v + b * p.v_batch + head * p.value_dim, p.v_row, p.value_dim, 0, last);
-    ChunkRows<T> y(GRAD ? nullptr : (const T*)a.y + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, 0, p.length);
-    unsigned v_at[NT][4], y_at[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v_at[n][e] = there[n] ? v.offset(my_row + e, column[n]) : kNowhere;
-            y_at[n][e] = there[n] ? y.offset(my_row + e, column[n]) : kNowhere;
-        }
     const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks;
-
-    b8 ka[KS][NX], qa[GRAD ? 1 : KS][NX], kta[TW][2][NX], xa[2][3], pa[2][RP];
-    unsigned next_v[NT][4];
-    f4 gamma, left, strength, next_gamma, next_left, next_strength;
-    float end, next_end;
-    auto fetch_keys = [&](int c) {
+    // (loads come back in their order: they are made in the order of their use, a chunk ahead, each kind when the one before it has been used up)
+    if (chain) {
+        const size_t state_base = ((size_t)b * p.value_heads + head) * p.key_dim * p.value_dim;
+        const unsigned state_bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
+        f4 s[TW][NT];
+        {
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state + state_base), 0, a.state ? state_bytes : 0u, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < KS; ++i)
+            for (int i = 0; i < TW; ++i)
 #pragma unroll
-            for (int n = 0; n < NX; ++n) {
-                ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
-                if (!GRAD) qa[i][n] = operand(w.q + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                        s[i][n][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0));
+                    }
+        }
+        auto put_state = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (TW == 2) states.put(wave, n, lane, s[0][n], s[1][n]);
+                else states.put_half(wave, n, lane, s[0][n]);
             }
-    };
-    auto fetch_values = [&] {
-        const __amdgpu_buffer_rsrc_t rows = v.buffer();
+        };
+        ChunkRows<T> v((const T*)a.v + b * p.v_batch + head * p.value_dim, p.v_row, p.value_dim, 0, last);
+        unsigned v_at[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) next_v[n][e] = buffer_load<T>(rows, v_at[n][e]);
-        v.move(1);
-    };
-    auto fetch_inverse = [&](int c) {
+            for (int e = 0; e < 4; ++e) v_at[n][e] = there[n] ? v.offset(my_row + e, column[n]) : kNowhere;
+        b8 ka[KS][NX], kta[TW][2][NX], xa[2][3];
+        unsigned next_v[NT][4];
+        f4 next_gamma, next_left, next_strength;
+        float next_end;
+        auto fetch_keys = [&](int c) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i < steps) {
+            for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.x + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
+                for (int n = 0; n < NX; ++n) ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
+        };
+        auto fetch_values = [&](int c) {
+            const __amdgpu_buffer_rsrc_t rows = v.buffer();
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) next_v[n][e] = buffer_load<T>(rows, v_at[n][e]);
+            v.move(1);
+            const float* from = w.scalars + (vc + c) * kScalars * kChunk;
+            next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
+            next_left = *(const f4*)(from + kLeft * kChunk + my_row);
+            next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
+            next_end = from[kGamma * kChunk + kChunk - 1];
+        };
+        auto fetch_inverse = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i < steps) {
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.x + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
+                }
+        };
+        auto fetch_transposed = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
+        };
+        if (chunks > 0) {
+            fetch_keys(0), fetch_values(0), fetch_inverse(0), fetch_transposed(0);
+            put_state();
+        }
+        for (int c = 0; c < chunks; ++c) {
+            const int next = c + 1 < chunks ? c + 1 : c;
+            lds_barrier();
+            // K S, and of it b (V - e^G (K S))
+            f4 ks[NT][3] = {};
+            {
+                b8 parts[KS][NT][3];
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) states.take(i, n, lane, parts[i][n]);
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);        // (or they are read one by one, and each is waited for)
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) multiply_apart<2>(ka[i], parts[i][n], ks[n]);
             }
-    };
-    auto fetch_mixed = [&](int c) {
-        if (!GRAD) {
+            fetch_keys(next);
+            const f4 gamma = next_gamma, left = next_left, strength = next_strength;
+            const float end = next_end;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f4 sum = joined(ks[n]);
+                f4 miss;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) miss[e] = strength[e] * __builtin_fmaf(-gamma[e], sum[e], loaded<T>(next_v[n][e]));
+                misses.put_half(wave, n, lane, miss);
+            }
+            fetch_values(next);                    // (past the last chunk: zeros that nobody takes)
+            lds_barrier();
+            // U
+            f4 u[NT][3] = {};
+            {
+                b8 parts[2][NT][3];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) misses.take(i, n, lane, parts[i][n]);
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i < steps) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) multiply_apart<2>(xa[i], parts[i][n], u[n]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f4 sum = joined(u[n]);
+                writes.put_half(wave, n, lane, left * sum);
+                values.put_half(wave, n, lane, sum);
+            }
+            fetch_inverse(next);
+            lds_barrier();
+            // the state behind the chunk
+            {
+                b8 parts[2][NT][3];
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) writes.take(m, n, lane, parts[m][n]);
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    f4 more[TW][3] = {};
+#pragma unroll
+                    for (int i = 0; i < TW; ++i) more[i][0] = s[i][n] * end;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int i = 0; i < TW; ++i) multiply_apart<2>(kta[i][m], parts[m][n], more[i]);
+#pragma unroll
+                    for (int i = 0; i < TW; ++i) s[i][n] = joined(more[i]);
+                }
+            }
+            put_state();
+            fetch_transposed(next);
+        }
+        if (!GRAD && a.state_out) {
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state_out + state_base), 0, state_bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                        const float value = s[i][n][e];    // (an element of a vector is not a place that bits can be taken from)
+                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), to, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0);
+                    }
+        }
+    } else if (GRAD) {
+        // what the gradients need of it: S before the chunk, and U.  (From wavefronts of their own: loads that were made behind stores wait for them.)
+        for (int c = 0; c < chunks; ++c) {
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const f4 of_s = turn_quad(states.numbers(TW * wave + i, n, lane));
+                    *(f4*)(w.s + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = of_s;
+                }
+            lds_barrier();
+            lds_barrier();
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f4 u = turn_quad(values.numbers(wave, n, lane));
+                *(f4*)(w.u + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = u;
+            }
+        }
+    } else {
+        // the outputs
+        ChunkRows<T> y((const T*)a.y + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, 0, p.length);
+        unsigned y_at[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y_at[n][e] = there[n] ? y.offset(my_row + e, column[n]) : kNowhere;
+        b8 qa[KS][NX], pa[2][RP];
+        f4 next_gamma;
+        auto fetch_queries = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int n = 0; n < NX; ++n) qa[i][n] = operand(w.q + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
+            next_gamma = *(const f4*)(w.scalars + (vc + c) * kScalars * kChunk + kGamma * kChunk + my_row);
+        };
+        auto fetch_mixed = [&](int c) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (i < steps) {
 #pragma unroll
                     for (int n = 0; n < RP; ++n) pa[i][n] = operand(w.p + ((vc + c) * RP + n) * kSquare, 2, wave, i, lane);
                 }
-        }
+        };
+        if (chunks > 0) fetch_queries(0), fetch_mixed(0);
+        for (int c = 0; c < chunks; ++c) {
+            const int next = c + 1 < chunks ? c + 1 : c;
+            lds_barrier();
+            f4 out[NT] = {};
 #pragma unroll
-        for (int i = 0; i < TW; ++i)
+            for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
-    };
-    auto fetch_scalars = [&](int c) {
-        const float* from = w.scalars + (vc + c) * kScalars * kChunk;
-        next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
-        next_left = *(const f4*)(from + kLeft * kChunk + my_row);
-        next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
-        next_end = from[kGamma * kChunk + kChunk - 1];
-    };
-    // (loads come back in their order: they are made in the order of their use, each kind when the one before it has been used up)
-    if (chunks > 0) {
-        fetch_keys(0), fetch_values(), fetch_scalars(0), fetch_inverse(0), fetch_mixed(0);
-        put_state();
-    }
-    for (int c = 0; c < chunks; ++c) {
-        const int next = c + 1 < chunks ? c + 1 : c;
-        lds_barrier();
-        if (GRAD) {
-            // S before the chunk
-#pragma unroll
-            for (int i = 0; i < TW; ++i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (column[n] < shape.columns) w.s[((vc + c) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column[n]] = s[i][n][e];
-        }
-        // K S and Q S
-        f4 ks[NT] = {}, out[NT] = {};
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                b8 parts[3];
-                states.take(i, n, lane, parts);
-                ks[n] = multiply<2>(ka[i], parts, ks[n]);
-                if (!GRAD) out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
-            }
-        fetch_keys(next);
-        gamma = next_gamma, left = next_left, strength = next_strength, end = next_end;
-        // b (V - e^G (K S))
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            f4 miss;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) miss[e] = strength[e] * __builtin_fmaf(-gamma[e], ks[n][e], loaded<T>(next_v[n][e]));
-            misses.put_half(wave, n, lane, miss);
-        }
-        if (c + 1 < chunks) fetch_values();
-        fetch_scalars(next);
-        lds_barrier();
-        // U
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            f4 u = {};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i < steps) {
-                    b8 parts[3];
-                    misses.take(i, n, lane, parts);
-                    u = multiply<2>(xa[i], parts, u);
+                for (int n = 0; n < NT; ++n) {
+                    b8 parts[RP];
+                    states.take(i, n, lane, parts);
+                    out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
                 }
-            writes.put_half(wave, n, lane, left * u);
-            if (!GRAD) {
-                values.put_half(wave, n, lane, u);
-            } else if (column[n] < shape.columns) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w.u[((vc + c) * kChunk + my_row + e) * shape.columns + column[n]] = u[e];
-            }
-        }
-        fetch_inverse(next);
-        lds_barrier();
-        // the state behind the chunk, and its outputs
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int i = 0; i < TW; ++i) s[i][n] *= end;
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                b8 parts[3];
-                writes.take(m, n, lane, parts);
-#pragma unroll
-                for (int i = 0; i < TW; ++i) s[i][n] = multiply<2>(kta[i][m], parts, s[i][n]);
-            }
-        }
-        put_state();
-        if (!GRAD) {
+            const f4 gamma = next_gamma * p.scale;
+            fetch_queries(next);
+            lds_barrier();
+            lds_barrier();
             const __amdgpu_buffer_rsrc_t rows = y.buffer();
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                f4 o = out[n] * (gamma * p.scale);
+                f4 o = out[n] * gamma;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (i < steps) {
@@ -444,28 +507,13 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_sweep_kernel(sys_gated_de
                 for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)o[e]);
             }
             y.move(1);
+            fetch_mixed(next);
         }
-        fetch_mixed(next);
-    }
-    if (!GRAD) {
         T* behind = (T*)a.y + b * p.y_batch + head * p.value_dim;
-        for (int t = chunks * kChunk + (threadIdx.x >> 4); t < p.length; t += kDeltaThreads / 16)
+        for (int t = chunks * kChunk + (int)((threadIdx.x & 255) >> 4); t < p.length; t += kSweepThreads / 32)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
                 if (there[n]) behind[t * p.y_row + column[n]] = (T)0.0f;
-        if (a.state_out) {
-            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.state_out + state_base), 0, state_bytes, 0x00027000);
-#pragma unroll
-            for (int i = 0; i < TW; ++i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
-                        const float value = s[i][n][e];        // (an element of a vector is not a place that bits can be taken from)
-                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), to, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0);
-                    }
-        }
     }
 }
 
@@ -482,10 +530,13 @@ template <typename T, int KD, bool GRAD>
 hipError_t sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, hipStream_t s)
 {
     DeltaShape of = shape;
-    of.tiles = (shape.columns + 15) / 16;
+    const bool wide = delta_wide(p);
+    of.tiles = wide ? shape.columns / 32 : GRAD ? shape.columns / 16 : (p.value_dim + 15) / 16;
     const long long blocks = (long long)of.tiles * p.value_heads * p.batch;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((delta_sweep_kernel<T, KD, 1, GRAD>), dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, of, w);
+    constexpr int kMost = sizeof(T) == 4 && KD > 64 ? 1 : 2;
+    if (wide) hipLaunchKernelGGL((delta_sweep_kernel<T, KD, kMost, GRAD>), dim3((unsigned)blocks), dim3(kSweepThreads), 0, s, p, a, of, w);
+    else hipLaunchKernelGGL((delta_sweep_kernel<T, KD, 1, GRAD>), dim3((unsigned)blocks), dim3(kSweepThreads), 0, s, p, a, of, w);
     return hipGetLastError();
 }
 
@@ -522,6 +573,12 @@ hipError_t launch_delta_matrices(const sys_gated_delta_t& p, const DeltaArgs& a,
 hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s)
 {
     return launch(true, p, a, shape, w, grad, s);
+}
+
+bool delta_wide(const sys_gated_delta_t& p)
+{
+    // (keys of more than 64 entries in fp32, three parts each, take all registers with 16 columns)
+    return !(p.dtype == SYS_F32 && p.key_dim > 64) && (long long)((p.value_dim + 15) / 16) * p.value_heads * p.batch > kCus;
 }
 
 DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a)

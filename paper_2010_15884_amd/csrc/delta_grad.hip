@@ -18,191 +18,293 @@
 namespace sysconv {
 namespace {
 
-template <typename T, int KD>
-__global__ __launch_bounds__(kDeltaThreads) void delta_back_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+template <typename T, int KD, int NT>
+__global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void delta_back_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape,
+                                                                                                             DeltaPlanes w)
 {
     constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64;
+    constexpr bool kAtOnce = NX * NT <= 2;         // there are registers for all operands of a product
     const unsigned place = xcd_place(blockIdx.x, gridDim.x);
     const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
     const int key_head = head / (p.value_heads / p.key_heads);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const bool chain = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0;
+    const int last = sequence_length(a.lengths, b, p.length), chunks = (last + kChunk - 1) / kChunk, top = chunks > 0 ? chunks - 1 : 0;
     const int first_step = wave >> 1;              // of X^T and P^T: what lies below their diagonals is zero
     const int my_row = tile_row(wave, 4 * g);
-    const int column = tile * 16 + r;
-    const bool there = column < p.value_dim;
+    int column[NT];
+    bool there[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) column[n] = (tile * NT + n) * 16 + r, there[n] = column[n] < p.value_dim;
 
-    __shared__ Operands<KS, 3, 1> states;
-    __shared__ Operands<2, 3, 1> misses, writes, weighted;
-    __shared__ Operands<2, NX, 1> outs;
+    __shared__ Operands<KS, 3, NT> states;
+    __shared__ Operands<2, 3, NT> misses, writes, weighted;
+    __shared__ Operands<2, NX, NT> outs;
+    // P^T dO and Q^T (e^G dO) of the next chunk, Z of this one
+    __shared__ f4 of_outs[4][NT][64], of_queries[4 * TW][NT][64], zs[4][NT][64];
 
-    const size_t state_base = ((size_t)b * p.value_heads + head) * p.key_dim * p.value_dim;
-    const unsigned state_bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
-    f4 s[TW];
-    {
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.dstate_out + state_base), 0, a.dstate_out ? state_bytes : 0u, 0x00027000);
-#pragma unroll
-        for (int i = 0; i < TW; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
-                s[i][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, there ? (row * p.value_dim + column) * 4u : kNowhere, 0, 0));
-            }
-    }
-    auto put_state = [&] {
-        if constexpr (TW == 2) states.put(wave, 0, lane, s[0], s[1]);
-        else states.put_half(wave, 0, lane, s[0]);
-    };
-    const int top = chunks > 0 ? chunks - 1 : 0;
-    const long long dv_row = (long long)p.value_heads * p.value_dim;
-    ChunkRows<T> dy((const T*)a.dy + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, top, last);
-    ChunkRows<T> dv((const T*)a.dv + (long long)b * p.length * dv_row + head * p.value_dim, dv_row, p.value_dim, top, p.length);
-    unsigned dy_at[4], dv_at[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        dy_at[e] = there ? dy.offset(my_row + e, column) : kNowhere;
-        dv_at[e] = there ? dv.offset(my_row + e, column) : kNowhere;
-    }
     const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks;
-
-    b8 ka[KS][NX], kta[TW][2][NX], qta[TW][2][NX], xa[2][3], pa[2][3];
-    unsigned next_dy[4];
-    f4 gamma, left, strength, own_dy;
-    float end;
-    auto fetch_keys = [&](int c) {
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-            for (int n = 0; n < NX; ++n) ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i >= first_step) {
-#pragma unroll
-                for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.pt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
-            }
-    };
-    auto fetch_outs = [&] {
-        const __amdgpu_buffer_rsrc_t rows = dy.buffer();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) next_dy[e] = buffer_load<T>(rows, dy_at[e]);
-        dy.move(-1);
-    };
-    auto put_outs = [&] {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) own_dy[e] = loaded<T>(next_dy[e]);
-        outs.put_half(wave, 0, lane, own_dy);
-    };
-    auto fetch_inverse = [&](int c) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i >= first_step) {
-#pragma unroll
-                for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.xt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
-            }
-    };
-    auto fetch_rest = [&](int c) {
-#pragma unroll
-        for (int i = 0; i < TW; ++i)
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int n = 0; n < NX; ++n) {
-                    kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
-                    qta[i][m][n] = operand(w.qt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
-                }
-        const float* from = w.scalars + (vc + c) * kScalars * kChunk;
-        gamma = *(const f4*)(from + kGamma * kChunk + my_row);
-        left = *(const f4*)(from + kLeft * kChunk + my_row);
-        strength = *(const f4*)(from + kStrength * kChunk + my_row);
-        end = from[kGamma * kChunk + kChunk - 1];
-    };
-    if (chunks > 0) {
-        fetch_outs(), fetch_keys(top), fetch_inverse(top), fetch_rest(top);
-        put_state();
-        put_outs();
-    }
-    for (int c = top; c >= 0 && chunks > 0; --c) {
-        const int next = c > 0 ? c - 1 : 0;
-        lds_barrier();
-        if (c > 0) fetch_outs();
+    const long long dv_row = (long long)p.value_heads * p.value_dim;
+    if (chain) {
+        const size_t state_base = ((size_t)b * p.value_heads + head) * p.key_dim * p.value_dim;
+        const unsigned state_bytes = (unsigned)(p.key_dim * p.value_dim) * 4u;
+        f4 s[TW][NT];
         {
-            // dS behind the chunk
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.dstate_out + state_base), 0, a.dstate_out ? state_bytes : 0u, 0x00027000);
 #pragma unroll
             for (int i = 0; i < TW; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w.ds[((vc + c) * KD + tile_row(TW * wave + i, 4 * g) + e) * shape.columns + column] = s[i][e];
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                        s[i][n][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0));
+                    }
         }
-        // dU
-        f4 ks = {}, u = {};
+        auto put_state = [&] {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            b8 parts[3];
-            states.take(i, 0, lane, parts);
-            ks = multiply<2>(ka[i], parts, ks);
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (TW == 2) states.put(wave, n, lane, s[0][n], s[1][n]);
+                else states.put_half(wave, n, lane, s[0][n]);
+            }
+        };
+        b8 ka[KS][NX], kta[TW][2][NX], xa[2][3];
+        f4 next_gamma, next_left, next_strength;
+        float next_end;
+        auto fetch_keys = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int n = 0; n < NX; ++n) ka[i][n] = operand(w.k + ((kc + c) * NX + n) * kChunk * KD, KS, wave, i, lane);
+            const float* from = w.scalars + (vc + c) * kScalars * kChunk;
+            next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
+            next_left = *(const f4*)(from + kLeft * kChunk + my_row);
+            next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
+            next_end = from[kGamma * kChunk + kChunk - 1];
+        };
+        auto fetch_inverse = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i >= first_step) {
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) xa[i][n] = operand(w.xt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
+                }
+        };
+        auto fetch_transposed = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < NX; ++n) kta[i][m][n] = operand(w.kt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
+        };
+        if (chunks > 0) {
+            fetch_keys(top), fetch_inverse(top), fetch_transposed(top);
+            put_state();
+            lds_barrier();
         }
+        for (int c = top; c >= 0 && chunks > 0; --c) {
+            const int next = c > 0 ? c - 1 : 0;
+            lds_barrier();
+            // dU
+            f4 ks[NT][3] = {};
+            {
+                b8 parts[KS][NT][3];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i >= first_step) {
-                b8 parts[NX];
-                outs.take(i, 0, lane, parts);
-                u = multiply<2>(pa[i], parts, u);
-            }
-        fetch_keys(next);
-        misses.put_half(wave, 0, lane, u + left * ks);
-        lds_barrier();
-        // Z
-        f4 z = {};
+                for (int i = 0; i < KS; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i >= first_step) {
-                b8 parts[3];
-                misses.take(i, 0, lane, parts);
-                z = multiply<2>(xa[i], parts, z);
+                    for (int n = 0; n < NT; ++n) states.take(i, n, lane, parts[i][n]);
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) multiply_apart<2>(ka[i], parts[i][n], ks[n]);
             }
-        const f4 values = strength * z;
-        writes.put_half(wave, 0, lane, -(gamma * values));
-        weighted.put_half(wave, 0, lane, gamma * p.scale * own_dy);
-        {
-            const __amdgpu_buffer_rsrc_t rows = dv.buffer();
+            const f4 gamma = next_gamma, left = next_left, strength = next_strength;
+            const float end = next_end;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) misses.put_half(wave, n, lane, of_outs[wave][n][lane] + left * joined(ks[n]));
+            fetch_keys(next);
+            lds_barrier();
+            // Z
+            f4 z[NT][3] = {};
+            {
+                b8 parts[2][NT][3];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) misses.take(i, n, lane, parts[i][n]);
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i >= first_step) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) multiply_apart<2>(xa[i], parts[i][n], z[n]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f4 sum = joined(z[n]);
+                writes.put_half(wave, n, lane, -(gamma * strength * sum));
+                zs[wave][n][lane] = sum;
+            }
+            fetch_inverse(next);
+            lds_barrier();
+            // dS before the chunk
+            {
+                b8 parts[2][NT][3];
+                f4 more[TW][NT][3] = {};
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) writes.take(m, n, lane, parts[m][n]);
+#pragma unroll
+                for (int i = 0; i < TW; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) more[i][n][1] = of_queries[TW * wave + i][n][lane];
+                if (kAtOnce) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int i = 0; i < TW; ++i) more[i][n][0] = s[i][n] * end;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int i = 0; i < TW; ++i) multiply_apart<2>(kta[i][m], parts[m][n], more[i][n]);
+#pragma unroll
+                    for (int i = 0; i < TW; ++i) s[i][n] = joined(more[i][n]);
+                }
+            }
+            put_state();
+            fetch_transposed(next);
+        }
+        if (a.dstate) {
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.dstate + state_base), 0, state_bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
+                        const float value = s[i][n][e];
+                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), to, there[n] ? (row * p.value_dim + column[n]) * 4u : kNowhere, 0, 0);
+                    }
+        }
+    } else {
+        // a chunk ahead what depends on dO alone, and behind it what the gradients need: dS behind the chunk, Z, and dV
+        ChunkRows<T> dy((const T*)a.dy + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, top, last);
+        ChunkRows<T> dv((const T*)a.dv + (long long)b * p.length * dv_row + head * p.value_dim, dv_row, p.value_dim, top, p.length);
+        unsigned dy_at[NT][4], dv_at[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                buffer_store<T>(rows, dv_at[e], (T)values[e]);
-                w.z[((vc + c) * kChunk + my_row + e) * shape.columns + column] = z[e];
+                dy_at[n][e] = there[n] ? dy.offset(my_row + e, column[n]) : kNowhere;
+                dv_at[n][e] = there[n] ? dv.offset(my_row + e, column[n]) : kNowhere;
             }
-            dv.move(-1);
+        b8 qta[TW][2][NX], pa[2][3];
+        unsigned next_dy[NT][4];
+        f4 next_gamma, next_strength, queries[TW][NT];
+        auto fetch_outs = [&](int c) {
+            const __amdgpu_buffer_rsrc_t rows = dy.buffer();
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) next_dy[n][e] = buffer_load<T>(rows, dy_at[n][e]);
+            dy.move(-1);
+            const float* from = w.scalars + (vc + c) * kScalars * kChunk;
+            next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
+            next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
+        };
+        auto fetch_mixed = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i >= first_step) {
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.pt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
+                }
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < NX; ++n) qta[i][m][n] = operand(w.qt + ((kc + c) * NX + n) * kChunk * KD, 2, TW * wave + i, m, lane);
+        };
+        auto put_outs = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f4 own;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[e] = loaded<T>(next_dy[n][e]);
+                outs.put_half(wave, n, lane, own);
+                weighted.put_half(wave, n, lane, next_gamma * p.scale * own);
+            }
+        };
+        auto products = [&] {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f4 u[3] = {};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i >= first_step) {
+                        b8 parts[NX];
+                        outs.take(i, n, lane, parts);
+                        multiply_apart<2>(pa[i], parts, u);
+                    }
+                of_outs[wave][n][lane] = joined(u);
+                f4 more[TW][3] = {};
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    b8 parts[3];
+                    weighted.take(m, n, lane, parts);
+#pragma unroll
+                    for (int i = 0; i < TW; ++i) multiply_apart<2>(qta[i][m], parts, more[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < TW; ++i) queries[i][n] = joined(more[i]);
+            }
+        };
+        if (chunks > 0) {
+            fetch_outs(top), fetch_mixed(top);
+            f4 strength = next_strength;
+            put_outs();
+            lds_barrier();
+            products();
+            for (int c = top; c >= 0; --c) {
+                const int next = c > 0 ? c - 1 : 0;
+                if (c > 0) fetch_outs(next), fetch_mixed(next);        // (a buffer has no lower end: rows before the first chunk must not be asked for)
+                lds_barrier();
+#pragma unroll
+                for (int i = 0; i < TW; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        of_queries[TW * wave + i][n][lane] = queries[i][n];
+                        *(f4*)(w.ds + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) =
+                            turn_quad(states.numbers(TW * wave + i, n, lane));
+                    }
+                lds_barrier();
+                const f4 after = next_strength;
+                if (c > 0) put_outs();
+                lds_barrier();
+                const __amdgpu_buffer_rsrc_t rows = dv.buffer();
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const f4 z = zs[wave][n][lane], values = strength * z;
+                    *(f4*)(w.z + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = turn_quad(z);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) buffer_store<T>(rows, dv_at[n][e], (T)values[e]);
+                }
+                dv.move(-1);
+                strength = after;
+                if (c > 0) products();
+            }
         }
-        fetch_inverse(next);
-        lds_barrier();
+        T* behind = (T*)a.dv + (long long)b * p.length * dv_row + head * p.value_dim;
+        for (int t = chunks * kChunk + (int)((threadIdx.x & 255) >> 4); t < p.length; t += kSweepThreads / 32)
 #pragma unroll
-        for (int i = 0; i < TW; ++i) s[i] *= end;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            b8 of_z[3], of_dy[3];
-            writes.take(m, 0, lane, of_z);
-            weighted.take(m, 0, lane, of_dy);
-#pragma unroll
-            for (int i = 0; i < TW; ++i) {
-                s[i] = multiply<2>(kta[i][m], of_z, s[i]);
-                s[i] = multiply<2>(qta[i][m], of_dy, s[i]);
-            }
-        }
-        put_state();
-        if (c > 0) put_outs();
-        fetch_rest(next);
-    }
-    T* behind = (T*)a.dv + (long long)b * p.length * dv_row + head * p.value_dim;
-    for (int t = chunks * kChunk + (threadIdx.x >> 4); t < p.length; t += kDeltaThreads / 16)
-        if (there) behind[t * dv_row + column] = (T)0.0f;
-    if (a.dstate) {
-        const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc((void*)(a.dstate + state_base), 0, state_bytes, 0x00027000);
-#pragma unroll
-        for (int i = 0; i < TW; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const unsigned row = tile_row(TW * wave + i, 4 * g) + e;
-                const float value = s[i][e];
-                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, value), to, there ? (row * p.value_dim + column) * 4u : kNowhere, 0, 0);
-            }
+            for (int n = 0; n < NT; ++n)
+                if (there[n]) behind[t * dv_row + column[n]] = (T)0.0f;
     }
 }
 
@@ -228,10 +330,10 @@ __device__ __forceinline__ float together(const b8 (&parts)[N], int i)
 // Eight neighbouring fp32 numbers.
 struct EightFloats {
     float v[8];
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t plane, unsigned offset, int step)
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t plane, unsigned offset, int block)
     {
-        const f4 a = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset, 128 * step, 0));
-        const f4 b = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset + 16, 128 * step, 0));
+        const f4 a = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset, block, 0));
+        const f4 b = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(plane, offset + 16, block, 0));
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
     }
@@ -325,16 +427,16 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             return __builtin_amdgcn_make_buffer_rsrc((void*)(of + vc * rows * shape.columns), 0, (unsigned)(rows * shape.columns) * 4u, 0x00027000);
         };
         const __amdgpu_buffer_rsrc_t from_s = plane(w.s, KD), from_ds = plane(w.ds, KD), from_rows = plane(half ? w.u : w.z, kChunk);
-        const unsigned state_at = ((tid >> 2) * shape.columns + piece_at) * 4u, rows_at = (piece_row * shape.columns + piece_at) * 4u;
+        const unsigned state_at = ((tid >> 2) * 32 + piece_at) * 4u, rows_at = (piece_row * 32 + piece_at) * 4u;
 
         EightFloats next_s, next_ds, next_rows;
         Eight<T> next_values;                      // V or dO
         auto fetch = [&](int step) {
             if (tid < KD * 4) {
-                next_s.load(from_s, state_at, step);
-                next_ds.load(from_ds, state_at, step);
+                next_s.load(from_s, state_at, step * KD * 128);
+                next_ds.load(from_ds, state_at, step * KD * 128);
             }
-            next_rows.load(from_rows, rows_at, step);
+            next_rows.load(from_rows, rows_at, step * kChunk * 128);
             const __amdgpu_buffer_rsrc_t buffer = half ? dy_buffer : v_buffer;
             const unsigned at = (half ? dy_at : v_at) + 32 * step * (unsigned)sizeof(T);
             if (shape.whole_values) next_values.load(buffer, 32 * step + piece_at < p.value_dim ? at : kNowhere);
@@ -628,10 +730,13 @@ template <typename T, int KD>
 hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, hipStream_t s)
 {
     DeltaShape of = shape;
-    of.tiles = shape.columns / 16;
+    const bool wide = delta_wide(p);
+    of.tiles = shape.columns / (wide ? 32 : 16);
     const long long sweeps = (long long)of.tiles * p.value_heads * p.batch, chunks = (long long)shape.chunks * p.key_heads * p.batch;
     if (sweeps > 0x7fffffffLL || chunks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((delta_back_kernel<T, KD>), dim3((unsigned)sweeps), dim3(kDeltaThreads), 0, s, p, a, of, w);
+    constexpr int kMost = sizeof(T) == 4 && KD > 64 ? 1 : 2;
+    if (wide) hipLaunchKernelGGL((delta_back_kernel<T, KD, kMost>), dim3((unsigned)sweeps), dim3(kSweepThreads), 0, s, p, a, of, w);
+    else hipLaunchKernelGGL((delta_back_kernel<T, KD, 1>), dim3((unsigned)sweeps), dim3(kSweepThreads), 0, s, p, a, of, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !chunks) return e;
     hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kGradThreads), 0, s, p, a, shape, w);

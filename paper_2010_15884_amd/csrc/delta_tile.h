@@ -29,6 +29,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
 constexpr int kDeltaThreads = 256;
+constexpr int kSweepThreads = 512;                 // four wavefronts that go through the state, four that do the rest
 constexpr int kSquare = kChunk * kChunk;           // elements of X, P
 
 // Parts of an input.
@@ -48,6 +49,25 @@ __device__ __forceinline__ f4 multiply(const b8 (&a)[NA], const b8 (&b)[NB], f4 
         for (int i = 0; i < NA; ++i)
             if (order - i >= 0 && order - i < NB) c = mfma(a[i], b[order - i], c);
     return c;
+}
+
+// The same with a sum of its own for each order, so that instructions do not wait for each other; and the sum of these.
+template <int MOST, int NA, int NB>
+__device__ __forceinline__ void multiply_apart(const b8 (&a)[NA], const b8 (&b)[NB], f4 (&c)[MOST + 1])
+{
+#pragma unroll
+    for (int order = MOST; order >= 0; --order)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (order - i >= 0 && order - i < NB) c[order] = mfma(a[i], b[order - i], c[order]);
+}
+template <int N>
+__device__ __forceinline__ f4 joined(const f4 (&c)[N])
+{
+    f4 sum = c[N - 1];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) sum += c[i];
+    return sum;
 }
 
 // Eight numbers as N parts each.
@@ -102,6 +122,22 @@ __device__ __forceinline__ b8 operand(const bf16_t* matrix, int steps, int tile,
     return *(const b8*)(matrix + ((tile * steps + step) * 64 + lane) * 8);
 }
 
+// Four rows of a column a lane, as D has them, to four columns of a row: lane q of a quad gets row q of the quad's columns.
+__device__ __forceinline__ f4 turn_quad(f4 v)
+{
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    const float a = dpp<0xB1>(odd ? v[0] : v[1]), b = dpp<0xB1>(odd ? v[2] : v[3]);
+    const float p0 = odd ? a : v[0], p1 = odd ? v[1] : a, p2 = odd ? b : v[2], p3 = odd ? v[3] : b;
+    const float c = dpp<0x4E>(high ? p0 : p2), d = dpp<0x4E>(high ? p1 : p3);
+    return high ? f4{c, d, p2, p3} : f4{p0, p1, c, d};
+}
+
+// Where an element of S, dS, U or Z lies: blocks of 32 columns, row-major.
+__device__ __forceinline__ size_t block_place(size_t chunk, int rows, int columns, int row, int column)
+{
+    return (chunk * columns + (column & ~31)) * rows + row * 32 + (column & 31);
+}
+
 // The barrier of a workgroup whose wavefronts exchange through LDS alone: loads from memory stay in flight.
 __device__ __forceinline__ void lds_barrier()
 {
@@ -132,19 +168,33 @@ struct Operands {
 #pragma unroll
         for (int m = 0; m < PARTS; ++m) ((u2*)&v[tile >> 1][m][n][lane])[tile & 1] = parts[m];
     }
-    __device__ __forceinline__ void take(int step, int n, int lane, b8 (&out)[PARTS]) const
+    // as many parts of it as are wanted
+    template <int N>
+    __device__ __forceinline__ void take(int step, int n, int lane, b8 (&out)[N]) const
     {
 #pragma unroll
-        for (int m = 0; m < PARTS; ++m) out[m] = v[step][m][n][lane];
+        for (int m = 0; m < N; ++m) out[m] = v[step][m][n][lane];
+    }
+    // the numbers that put_half was given
+    __device__ __forceinline__ f4 numbers(int tile, int n, int lane) const
+    {
+        f4 sum = {};
+#pragma unroll
+        for (int m = PARTS - 1; m >= 0; --m) {
+            const u2 part = ((const u2*)&v[tile >> 1][m][n][lane])[tile & 1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __builtin_bit_cast(float, e & 1 ? part[e / 2] & 0xffff0000u : part[e / 2] << 16);
+        }
+        return sum;
     }
 };
 
 // What the kernel that makes the chunks' matrices leaves in the workspace for those that go through them: planes of parts, as operands.  Per value head and
 // chunk X [64][64] (three parts), P (kResultParts; gradients: transposes of both, three parts), and for every position the Scalars; per key head and chunk
-// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, row-major in fp32.
+// K, Q [64][padded] and their transposes (parts of inputs).  Gradients: S, U of the sweep forwards and dS, Z of the one backwards as well, in fp32.
 struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
-    float *s, *ds, *u, *z;             // [padded][columns], [64][columns]
+    float *s, *ds, *u, *z;             // [columns / 32][padded][32], [columns / 32][64][32]
     float* scalars;                    // [kScalars][64]
     float* dg;                         // every chunk's share of the gradients of A and the bias
 };
@@ -235,6 +285,9 @@ struct Eight {
 hipError_t launch_delta_matrices(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
 hipError_t launch_delta_sweep(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, bool grad, hipStream_t s);
 DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a = nullptr);
+// Whether the sweeps take 32 columns a workgroup, not 16: where there are more workgroups of 16 than CUs, of which each holds one.
+constexpr int kCus = 256;
+bool delta_wide(const sys_gated_delta_t& p);
 // The planes of a call, from `base` on (a null pointer: for their size), and the bytes that they take.
 size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool grad, void* base, DeltaPlanes* w);
 // A position at a time (delta_rule.hip).
