@@ -626,7 +626,8 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
         take(of.ds, state);
         take(of.u, rows);
         take(of.z, rows);
-        take(of.dg, 2 * value_chunks * sizeof(float));
+        take(of.gates, value_chunks * kGates * kChunk * sizeof(double));
+        take(of.shares, 2 * value_chunks * sizeof(double));
     }
     if (w) *w = of;
     return at - begin + 256;                       // (the base may lie anywhere)

@@ -318,13 +318,18 @@ __device__ __forceinline__ float row_sum(float v)
     return v;
 }
 
+// The first or the last four numbers of an operand.
 template <int N>
-__device__ __forceinline__ float together(const b8 (&parts)[N], int i)
+__device__ __forceinline__ f4 four_of(const b8 (&parts)[N], bool last)
 {
-    float v = (float)parts[N - 1][i];
+    f4 sum = {};
 #pragma unroll
-    for (int n = N - 2; n >= 0; --n) v += (float)parts[n][i];
-    return v;
+    for (int n = N - 1; n >= 0; --n) {
+        const u4 all = __builtin_bit_cast(u4, parts[n]);
+        const unsigned a = last ? all[2] : all[0], b = last ? all[3] : all[1];
+        sum += f4{__builtin_bit_cast(float, a << 16), __builtin_bit_cast(float, a & 0xffff0000u), __builtin_bit_cast(float, b << 16), __builtin_bit_cast(float, b & 0xffff0000u)};
+    }
+    return sum;
 }
 
 // Eight neighbouring fp32 numbers.
@@ -362,24 +367,17 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, key_head = rest % p.key_heads, b = rest / p.key_heads;
     const int shared = p.value_heads / p.key_heads;
     const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, half = __builtin_amdgcn_readfirstlane(tid >> 8), lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, half = __builtin_amdgcn_readfirstlane(tid >> 8);
+    // (the tiles of the second half the other way round: those of later positions have more below the diagonal, and wavefronts four apart share a SIMD)
+    const int quarter = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, wave = half ? 3 - quarter : quarter;
     const int here = p.length - t0 < kChunk ? p.length - t0 : kChunk;  // rows of the results
     const long long at0 = (long long)b * p.length + t0;
-    T* ddelta = (T*)a.ddelta + at0 * p.value_heads;
-    T* dbeta = (T*)a.dbeta + at0 * p.value_heads;
     if (rows <= 0) {
         for (int i = tid; i < here * p.key_dim; i += kGradThreads) {
             const long long at = ((at0 + i / p.key_dim) * p.key_heads + key_head) * p.key_dim + i % p.key_dim;
             ((T*)a.dq)[at] = (T)0.0f;
             ((T*)a.dk)[at] = (T)0.0f;
         }
-        for (int i = tid; i < here * shared; i += kGradThreads) {
-            const int at = i / shared * p.value_heads + key_head * shared + i % shared;
-            ddelta[at] = (T)0.0f;
-            dbeta[at] = (T)0.0f;
-        }
-        for (int i = tid; i < 2 * shared; i += kGradThreads)
-            w.dg[(((size_t)b * p.value_heads + key_head * shared + i / 2) * shape.chunks + chunk) * 2 + i % 2] = 0.0f;
         return;
     }
     const size_t kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
@@ -395,6 +393,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     } pool;
     __shared__ float rows_db[2][kChunk], rows_end[2][kChunk], rows_zv[kChunk];
     __shared__ double rows_dg[2][kChunk], columns_dg[8][kChunk], waves_end[8];
+    __shared__ __attribute__((aligned(16))) float scalars[kScalars * kChunk];
 
     // K and Q, which all value heads use, as operands and transposed: as many as LDS has room for
     constexpr bool kKeep = NX < 3, kKeepTransposed = NX == 1;
@@ -411,92 +410,108 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         }
     }
     f4 dq_all[KH] = {}, dk_all[KH] = {};
-    for (int h = 0; h < shared; ++h) {
-        const int head = key_head * shared + h;
-        const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk;
-        const ChunkRows<T> dy_rows((const T*)a.dy + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, chunk, last);
-        const ChunkRows<T> v_rows((const T*)a.v + b * p.v_batch + head * p.value_dim, p.v_row, p.value_dim, chunk, last);
-        const __amdgpu_buffer_rsrc_t dy_buffer = dy_rows.buffer(), v_buffer = v_rows.buffer();
-        int tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));              // (see below)
-        const int lane = tid & 63, place = lane + (lane >> 4);
+    const int steps = shape.columns / 32, items = steps * shared;      // of 32 columns, of one head after the other
+    // What is on its way from memory, an item ahead; beyond the end of a head too where there are registers for it
+    constexpr bool kBeyond = NX == 1;
+    struct Ahead {
+        EightFloats s, ds, rows;
+        Eight<T> values;                           // V or dO
+    } ahead;
+    int fetch_head = key_head * shared, fetch_step = 0;
+    auto fetch = [&](Ahead& to, int tid) {
         // pieces of eight: four a row and step; S and dS' by all lanes, Z and V by the first half of them, U and dO by the second
-        const int piece_row = (tid & 255) >> 2, piece_at = 8 * (tid & 3), piece = 17 * (tid & 3) + row_in_tile(piece_row);
-        const unsigned dy_at = dy_rows.offset(piece_row, piece_at), v_at = v_rows.offset(piece_row, piece_at);
+        const size_t vc = ((size_t)b * p.value_heads + fetch_head) * shape.chunks + chunk;
         auto plane = [&](float* of, int rows) {
             return __builtin_amdgcn_make_buffer_rsrc((void*)(of + vc * rows * shape.columns), 0, (unsigned)(rows * shape.columns) * 4u, 0x00027000);
         };
-        const __amdgpu_buffer_rsrc_t from_s = plane(w.s, KD), from_ds = plane(w.ds, KD), from_rows = plane(half ? w.u : w.z, kChunk);
-        const unsigned state_at = ((tid >> 2) * 32 + piece_at) * 4u, rows_at = (piece_row * 32 + piece_at) * 4u;
-
-        EightFloats next_s, next_ds, next_rows;
-        Eight<T> next_values;                      // V or dO
-        auto fetch = [&](int step) {
-            if (tid < KD * 4) {
-                next_s.load(from_s, state_at, step * KD * 128);
-                next_ds.load(from_ds, state_at, step * KD * 128);
-            }
-            next_rows.load(from_rows, rows_at, step * kChunk * 128);
-            const __amdgpu_buffer_rsrc_t buffer = half ? dy_buffer : v_buffer;
-            const unsigned at = (half ? dy_at : v_at) + 32 * step * (unsigned)sizeof(T);
-            if (shape.whole_values) next_values.load(buffer, 32 * step + piece_at < p.value_dim ? at : kNowhere);
-            else next_values.load_each(buffer, at, p.value_dim - 32 * step - piece_at);
-        };
+        const int row = (tid & 255) >> 2, at = 8 * (tid & 3);
+        if (tid < KD * 4) {
+            const unsigned state_at = ((tid >> 2) * 32 + at) * 4u;
+            to.s.load(plane(w.s, KD), state_at, fetch_step * KD * 128);
+            to.ds.load(plane(w.ds, KD), state_at, fetch_step * KD * 128);
+        }
+        to.rows.load(plane(half ? w.u : w.z, kChunk), (row * 32 + at) * 4u, fetch_step * kChunk * 128);
+        const T* base = half ? (const T*)a.dy + b * p.y_batch : (const T*)a.v + b * p.v_batch;
+        const ChunkRows<T> values(base + fetch_head * p.value_dim, half ? p.y_row : p.v_row, p.value_dim, chunk, last);
+        const int left = p.value_dim - 32 * fetch_step - at;
+        const unsigned offset = values.offset(row, 32 * fetch_step + at);
+        if (shape.whole_values) to.values.load(values.buffer(), left > 0 ? offset : kNowhere);
+        else to.values.load_each(values.buffer(), offset, left);
+        if (++fetch_step == steps) fetch_step = 0, ++fetch_head;
+    };
+    if (kBeyond) fetch(ahead, threadIdx.x);
+    for (int h = 0, item = 0; h < shared; ++h) {
+        const int head = key_head * shared + h;
+        const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk;
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));              // (see below)
+        const int lane = tid & 63, place = lane + (lane >> 4);
+        const int piece_row = (tid & 255) >> 2, piece = 17 * (tid & 3) + row_in_tile(piece_row);
+        auto scalar = [&] { return tid < kScalars * kChunk ? w.scalars[vc * kScalars * kChunk + tid] : 0.0f; };
+        const float early_scalar = NX < 3 ? scalar() : 0.0f;
         f4 dq[KH] = {}, zs[KH] = {}, us[KH] = {}, square[4] = {};
         double both = 0.0;                         // (<S, dS'> is the sum of key_dim x value_dim terms of either sign, and all positions of the chunk get it)
         float zv = 0.0f;
-        fetch(0);
-        const int steps = shape.columns / 32;
-        for (int step = 0; step < steps; ++step) {
+        if (!kBeyond) fetch(ahead, tid);
+        auto stage = [&](Ahead& next) {
             lds_barrier();
-            {
-                b8 parts[3];
-                if (tid < KD * 4) {
-                    const int tile = tile_of(tid >> 2), to = 17 * (tid & 3) + row_in_tile(tid >> 2);
+            b8 parts[3];
+            if (tid < KD * 4) {
+                const int tile = tile_of(tid >> 2), to = 17 * (tid & 3) + row_in_tile(tid >> 2);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) both = __builtin_fma((double)next_s.v[i], (double)next_ds.v[i], both);
-                    split_signed(next_s.v, tile, parts);
+                for (int i = 0; i < 8; ++i) both = __builtin_fma((double)next.s.v[i], (double)next.ds.v[i], both);
+                split_signed(next.s.v, tile, parts);
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.s[tile][m][to] = parts[m];
-                    split_signed(next_ds.v, tile, parts);
+                for (int m = 0; m < 3; ++m) pool.columns.s[tile][m][to] = parts[m];
+                split_signed(next.ds.v, tile, parts);
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.ds[tile][m][to] = parts[m];
-                }
-                const int tile = tile_of(piece_row);
-                if (half) {
-                    b8 values[NX];
-                    next_values.split(values);
-                    split_signed(next_rows.v, tile, parts);
-#pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.u[tile][m][piece] = parts[m];
-#pragma unroll
-                    for (int m = 0; m < NX; ++m) pool.columns.dy[tile][m][piece] = values[m];
-                } else {
-                    float values[8];
-                    next_values.values(values);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) zv = __builtin_fmaf(next_rows.v[i], values[i], zv);
-                    split8(next_rows.v, parts);
-#pragma unroll
-                    for (int m = 0; m < 3; ++m) pool.columns.z[tile][m][piece] = parts[m];
-                }
+                for (int m = 0; m < 3; ++m) pool.columns.ds[tile][m][to] = parts[m];
             }
+            const int tile = tile_of(piece_row);
+            if (half) {
+                b8 values[NX];
+                next.values.split(values);
+                split_signed(next.rows.v, tile, parts);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) pool.columns.u[tile][m][piece] = parts[m];
+#pragma unroll
+                for (int m = 0; m < NX; ++m) pool.columns.dy[tile][m][piece] = values[m];
+            } else {
+                float values[8];
+                next.values.values(values);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) zv = __builtin_fmaf(next.rows.v[i], values[i], zv);
+                split8(next.rows.v, parts);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) pool.columns.z[tile][m][piece] = parts[m];
+            }
+            ++item;
+            if (NX < 3 && (kBeyond ? item < items : item % steps != 0)) fetch(next, tid);
             lds_barrier();
-            if (step + 1 < steps) fetch(step + 1);
+        };
+        for (int step = 0; step < steps; ++step) {
+            stage(ahead);
             b8 oa[NX], za[3], ua[3];
 #pragma unroll
             for (int m = 0; m < NX; ++m) oa[m] = pool.columns.dy[wave][m][place];
 #pragma unroll
             for (int m = 0; m < 3; ++m) za[m] = pool.columns.z[wave][m][place];
+            auto squares = [&](const auto& of, auto which) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                if (n / 2 <= middle) {
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int n = 2 * decltype(which)::value; n < 2 * decltype(which)::value + 2; ++n) {
                     b8 ub[3];
 #pragma unroll
                     for (int m = 0; m < 3; ++m) ub[m] = pool.columns.u[n][m][place];
-                    square[n] = half ? multiply<2>(za, ub, square[n]) : multiply<2>(oa, ub, square[n]);
+                    square[n] = multiply<2>(of, ub, square[n]);
                 }
+            };
+            if (half) {
+                squares(za, std::integral_constant<int, 0>());
+                if (middle) squares(za, std::integral_constant<int, 1>());
+            } else {
+                squares(oa, std::integral_constant<int, 0>());
+                if (middle) squares(oa, std::integral_constant<int, 1>());
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int m = 0; m < 3; ++m) ua[m] = pool.columns.u[wave][m][place];
@@ -514,61 +529,71 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                 for (int m = 0; m < 3; ++m) part[m] = pool.columns.ds[t][m][place];
                 us[i] = multiply<2>(ua, part, us[i]);
             }
+            // (fp32 has the registers behind the products only)
+            __builtin_amdgcn_sched_barrier(0);
+            if (NX == 3 && item % steps != 0) fetch(ahead, tid);
         }
+        asm volatile("" : "+v"(tid));
+        if (tid < kScalars * kChunk) scalars[tid] = NX < 3 ? early_scalar : scalar();
         lds_barrier();
         int again = lane;
         asm volatile("" : "+v"(again));
         const int row = tile_row(wave, again & 15), mine = tile_row(wave, 4 * (again >> 4));       // of A operands; the first of four of D
-        // the squares, as they are and transposed
-        const float* scalars = w.scalars + vc * kScalars * kChunk;
         const double* sums = (const double*)(scalars + kSums * kChunk);
-        const f4 gamma = *(const f4*)(scalars + kGamma * kChunk + mine), left = *(const f4*)(scalars + kLeft * kChunk + mine);
         const f4 strength = *(const f4*)(scalars + kStrength * kChunk + mine);
-        double mine_sum[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mine_sum[e] = sums[mine + e];
         // (new addresses for every head, as far as the compiler knows: worked out or loaded ahead of the loop they would take all registers)
-        const bf16_t *kt = w.kt + kc * NX * kChunk * KD, *qt = w.qt + kc * NX * kChunk * KD, *kp = w.k + kc * NX * kChunk * KD, *qp = w.q + kc * NX * kChunk * KD;
-        asm volatile("" : "+s"(kt), "+s"(qt), "+s"(kp), "+s"(qp));
+        size_t keys_at = kc * NX * kChunk * KD;
+        asm volatile("" : "+s"(keys_at));
+        const bf16_t *kt = w.kt + keys_at, *qt = w.qt + keys_at, *kp = w.k + keys_at, *qp = w.q + keys_at;
         const bf16_t* own = half ? kp : qp;        // rows of C belong to keys, those of B to queries
-        f4 of_g = {}, of_b = {}, of_end = {};
+        f4 of_strength = {};
         double of_h[4] = {};
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const int column = tile_row(n, again & 15);
-            if (n / 2 <= middle) {
-                f4 inner = {};
+        // the squares, as they are and transposed: two tiles of columns at a time
+        auto squares = [&](auto which, auto second) {
+            constexpr int N0 = 2 * decltype(which)::value;
+            constexpr bool C = decltype(second)::value;
+            constexpr int kSide = NX == 1 && KD == 64 ? 2 : 1;                     // tiles whose inner products are worked out side by side
+            f4 inner[2] = {};
+            auto products = [&](int n0) {
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    b8 xa[NX], kb[NX];
+                    if (NX > 1) __builtin_amdgcn_sched_barrier(0);
+                    b8 xa[NX], kb[kSide][NX];
 #pragma unroll
                     for (int m = 0; m < NX; ++m) {
-                        if constexpr (kKeep) {
-                            xa[m] = kept[half ? 0 : 1][m][wave * KS + s][again];
-                            kb[m] = kept[0][m][n * KS + s][again];
-                        } else {
-                            xa[m] = operand(own + m * kChunk * KD, KS, wave, s, again);
-                            kb[m] = operand(kp + m * kChunk * KD, KS, n, s, again);
+                        if constexpr (kKeep) xa[m] = kept[C ? 0 : 1][m][wave * KS + s][again];
+                        else xa[m] = operand(own + m * kChunk * KD, KS, wave, s, again);
+#pragma unroll
+                        for (int n = 0; n < kSide; ++n) {
+                            if constexpr (kKeep) kb[n][m] = kept[0][m][(N0 + n0 + n) * KS + s][again];
+                            else kb[n][m] = operand(kp + m * kChunk * KD, KS, N0 + n0 + n, s, again);
                         }
                     }
-                    inner = multiply<2>(xa, kb, inner);
+#pragma unroll
+                    for (int n = 0; n < kSide; ++n) inner[n0 + n] = multiply<2>(xa, kb[n], inner[n0 + n]);
                 }
+            };
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                if (n % kSide == 0) products(n);
+                __builtin_amdgcn_sched_barrier(0);
+                const int column = tile_row(N0 + n, again & 15);
                 const double column_sum = sums[column];
-                const f4 own_square = n & 1 ? -square[n] : square[n];
+                const f4 own_square = n & 1 ? -square[N0 + n] : square[N0 + n];
                 f4 f;
                 double of_column = 0.0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float ratio = fast_exp2((float)(mine_sum[e] - column_sum));
+                    const float ratio = fast_exp2((float)(sums[mine + e] - column_sum));
                     const bool below = column < mine + e;
-                    if (half) {
+                    if (C) {
                         const float c = below ? -(ratio * own_square[e]) : 0.0f;
-                        of_b[e] = below ? __builtin_fmaf(c, inner[e], of_b[e]) : of_b[e];
+                        of_strength[e] = below ? __builtin_fmaf(c, inner[n][e], of_strength[e]) : of_strength[e];
                         f[e] = strength[e] * c;
                     } else {
                         f[e] = column <= mine + e ? p.scale * (ratio * own_square[e]) : 0.0f;
                     }
-                    const double product = below ? (double)(f[e] * inner[e]) : 0.0;
+                    const double product = below ? (double)(f[e] * inner[n][e]) : 0.0;
                     of_h[e] += product;
                     of_column += product;
                 }
@@ -579,73 +604,92 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                 split4(f, parts);
 #pragma unroll
                 for (int m = 0; m < RP; ++m) {
-                    *(u2*)&pool.squares.bt[half][m][column][mine] = parts[m];
+                    *(u2*)&pool.squares.bt[C][m][column][mine] = parts[m];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) pool.squares.b[half][m][mine + e][column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+                    for (int e = 0; e < 4; ++e) pool.squares.b[C][m][mine + e][column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
                 }
-            } else if (again < 16) {
-                columns_dg[4 * half + wave][column] = 0.0;
             }
-        }
+        };
+        auto both_squares = [&](auto second) {
+            squares(std::integral_constant<int, 0>(), second);
+            if (middle) {
+                squares(std::integral_constant<int, 1>(), second);
+            } else if (again < 16) {
+                columns_dg[4 * half + wave][tile_row(2, again)] = 0.0;
+                columns_dg[4 * half + wave][tile_row(3, again)] = 0.0;
+            }
+        };
+        if (half) both_squares(std::true_type());
+        else both_squares(std::false_type());
         lds_barrier();
-#pragma unroll
-        for (int i = 0; i < KH; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int t = half * KH + i;
-            // (U's tile of these positions is a negative where the wavefront's number is odd)
-            const f4 of_dy = gamma * p.scale * (i & 1 ? -dq[i] : dq[i]), of_z = gamma * (i & 1 ? -zs[i] : zs[i]);
-            const f4 of_u = left * ((i ^ wave) & 1 ? -us[i] : us[i]);
-            dq_all[i] += of_dy;
-            dk_all[i] += of_u - strength * of_z;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                b8 kb[NX], qb[NX], m1[RP], m2[RP];
+        // what they and the products with the states give the queries and keys
+        f4 of_g = {}, of_end = {};
+        const f4 gamma = *(const f4*)(scalars + kGamma * kChunk + mine), left = *(const f4*)(scalars + kLeft * kChunk + mine);
+        auto finish = [&](auto which) {
+            constexpr int M = decltype(which)::value;
+            int at = again;
+            auto operands = [&](int t, int s, b8 (&kb)[NX], b8 (&qb)[NX]) {
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
                     if constexpr (kKeepTransposed) {
-                        kb[n] = kept_transposed[0][2 * t + s][again];
-                        qb[n] = kept_transposed[1][2 * t + s][again];
+                        kb[n] = kept_transposed[0][2 * t + s][at];
+                        qb[n] = kept_transposed[1][2 * t + s][at];
                     } else {
-                        kb[n] = operand(kt + n * kChunk * KD, 2, t, s, again);
-                        qb[n] = operand(qt + n * kChunk * KD, 2, t, s, again);
+                        kb[n] = operand(kt + n * kChunk * KD, 2, t, s, at);
+                        qb[n] = operand(qt + n * kChunk * KD, 2, t, s, at);
                     }
                 }
-                if (s == middle) {
-                    // the entries of these positions' own keys and queries are a half of this operand
+            };
+            // the rows' steps, then the columns'
+            auto pass = [&](bool turned, int s) {
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("" : "+v"(at));       // (operands are loaded again rather than kept)
+                b8 of_b[RP], of_c[RP];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float k = wave & 1 ? together(kb, 4 + e) : together(kb, e), q = wave & 1 ? together(qb, 4 + e) : together(qb, e);
-                        of_g[e] += __builtin_fmaf(q, of_dy[e], -strength[e] * (k * of_z[e]));
-                        of_b[e] = __builtin_fmaf(-k, of_z[e], of_b[e]);
-                        of_end[e] = __builtin_fmaf(k, of_u[e], of_end[e]);
-                    }
+                for (int m = 0; m < RP; ++m) {
+                    of_b[m] = *(const b8*)&(turned ? pool.squares.bt : pool.squares.b)[0][m][row][32 * s + 8 * (again >> 4)];
+                    of_c[m] = *(const b8*)&(turned ? pool.squares.bt : pool.squares.b)[1][m][row][32 * s + 8 * (again >> 4)];
                 }
-                if (s <= middle) {
 #pragma unroll
-                    for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.b[0][m][row][32 * s + 8 * (again >> 4)];
-                        m2[m] = *(const b8*)&pool.squares.b[1][m][row][32 * s + 8 * (again >> 4)];
+                for (int i = 0; i < KH; ++i) {
+                    if (NX > 1) __builtin_amdgcn_sched_barrier(0);
+                    b8 kb[NX], qb[NX];
+                    operands(half * KH + i, s, kb, qb);
+                    if (!turned && s == M) {
+                        // (U's tile of these positions is a negative where the wavefront's number is odd)
+                        const f4 of_dy = gamma * p.scale * (i & 1 ? -dq[i] : dq[i]), of_z = gamma * (i & 1 ? -zs[i] : zs[i]);
+                        const f4 of_u = left * ((i ^ wave) & 1 ? -us[i] : us[i]);
+                        // the entries of these positions' own keys and queries are a half of an operand
+                        const f4 k = four_of(kb, wave & 1), q = four_of(qb, wave & 1);
+                        of_g += q * of_dy - strength * (k * of_z);
+                        of_strength -= k * of_z;
+                        of_end += k * of_u;
+                        dq_all[i] += of_dy;
+                        dk_all[i] += of_u - strength * of_z;
                     }
-                    dq_all[i] = multiply<RP - 1>(m1, kb, dq_all[i]);
-                    dk_all[i] = multiply<RP - 1>(m2, kb, dk_all[i]);
-                }
-                if (s >= middle) {
-#pragma unroll
-                    for (int m = 0; m < RP; ++m) {
-                        m1[m] = *(const b8*)&pool.squares.bt[0][m][row][32 * s + 8 * (again >> 4)];
-                        m2[m] = *(const b8*)&pool.squares.bt[1][m][row][32 * s + 8 * (again >> 4)];
+                    if (turned) {
+                        f4 more = {};
+                        more = multiply<RP - 1>(of_b, qb, more);
+                        dk_all[i] = multiply<RP - 1>(of_c, kb, dk_all[i]) + more;
+                    } else {
+                        dq_all[i] = multiply<RP - 1>(of_b, kb, dq_all[i]);
+                        dk_all[i] = multiply<RP - 1>(of_c, kb, dk_all[i]);
                     }
-                    dk_all[i] = multiply<RP - 1>(m1, qb, dk_all[i]);
-                    dk_all[i] = multiply<RP - 1>(m2, kb, dk_all[i]);
                 }
-            }
-        }
+            };
+            pass(false, M);
+            if (M) pass(false, 0);
+            pass(true, M);
+            if (!M) pass(true, 1);
+        };
+        if (middle) finish(std::integral_constant<int, 1>());
+        else finish(std::integral_constant<int, 0>());
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             double dg = of_h[e] + (double)of_g[e];
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) dg += __shfl_xor(dg, m);
-            const float db = row_sum(of_b[e]), de = row_sum(of_end[e]);
+            const float db = row_sum(of_strength[e]), de = row_sum(of_end[e]);
             if ((again & 15) == 0) {
                 rows_dg[half][mine + e] = dg;
                 rows_db[half][mine + e] = db;
@@ -655,42 +699,18 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         zv = quad_sum(zv);
         if (!half && (again & 3) == 0) rows_zv[16 * wave + (again >> 2)] = zv;
         for (int m = 32; m; m >>= 1) both += __shfl_xor(both, m);
-        if (lane == 0) waves_end[4 * half + wave] = both;
+        if (again == 0) waves_end[4 * half + wave] = both;
         lds_barrier();
         if (!half && wave == 0) {
-            // gradients of the sums G that end in a position and behind it, and of what is left behind the positions before it
-            const double own_end = (double)rows_end[0][again] + (double)rows_end[1][again];
-            double dg = rows_dg[0][again] + rows_dg[1][again], de = own_end, end = 0.0;
+            // for the next kernel, which sums over positions: the share of a position, of what is left behind it, and of the whole chunk
+            double dg = rows_dg[0][again] + rows_dg[1][again], end = 0.0;
 #pragma unroll
             for (int m = 0; m < 8; ++m) dg -= columns_dg[m][again], end += waves_end[m];
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const double behind = __shfl_down(dg, m), before = __shfl_up(de, m);
-                if (again + m < 64) dg += behind;
-                if (again >= m) de += before;
-            }
-            const float log_decay = (float)(dg + (de - own_end) + (double)scalars[kGamma * kChunk + kChunk - 1] * end);
-            float of_a = 0.0f, of_bias = 0.0f, db = 0.0f;
-            if (again < rows) {
-                of_a = scalars[kStep * kChunk + again] * log_decay;
-                of_bias = a.a[head] * log_decay * scalars[kSlope * kChunk + again];
-                db = rows_zv[again] + (rows_db[0][again] + rows_db[1][again]);
-                if (p.sigmoid) {
-                    // (1 - b is the sigmoid of -beta, and keeps its digits there)
-                    const float raw = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + again) * p.beta_row + head];
-                    db *= sigmoid(raw) * sigmoid(-raw);
-                }
-            }
-            if (again < here) {
-                ddelta[again * p.value_heads + head] = (T)of_bias;
-                dbeta[again * p.value_heads + head] = (T)db;
-            }
-#pragma unroll
-            for (int m = 32; m; m >>= 1) of_a += __shfl_xor(of_a, m), of_bias += __shfl_xor(of_bias, m);
-            if (again == 0) {
-                w.dg[vc * 2] = of_a;
-                w.dg[vc * 2 + 1] = of_bias;
-            }
+            double* out = w.gates + vc * kGates * kChunk;
+            out[kGateRows * kChunk + again] = dg;
+            out[kGateEnds * kChunk + again] = (double)rows_end[0][again] + (double)rows_end[1][again];
+            out[kGateStrengths * kChunk + again] = (double)(rows_zv[again] + (rows_db[0][again] + rows_db[1][again]));
+            out[kGateWhole * kChunk + again] = (double)scalars[kGamma * kChunk + kChunk - 1] * end;
         }
         // (the next head's operands are put where the squares lie behind a barrier of its own)
     }
@@ -698,7 +718,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     for (int i = 0; i < KH; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int column = tile_row(half * KH + i, r), mine = tile_row(wave, 4 * g);
+            const int column = tile_row(half * KH + i, threadIdx.x & 15), mine = tile_row(wave, 4 * (threadIdx.x >> 4 & 3));
             if (mine + e < here && column < p.key_dim) {
                 const long long at = ((at0 + mine + e) * p.key_heads + key_head) * p.key_dim + column;
                 ((T*)a.dq)[at] = (T)dq_all[i][e];
@@ -707,16 +727,63 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         }
 }
 
-// dA and the bias's gradient: the chunks' sums of a head, a wavefront a head, in 64 bits.
-__global__ __launch_bounds__(64) void delta_gates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+// Gradients of delta, beta and, a chunk each, of A and the bias: a wavefront a chunk of a value head, a lane a position.  The logarithm of a decay gets the gradients
+// of the sums G that end in its position and behind it, what is left behind the positions before it, and what the whole chunk shares, in 64 bits.
+template <typename T>
+__global__ __launch_bounds__(kDeltaThreads) void delta_gates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w, long long all)
+{
+    const long long vc = (long long)blockIdx.x * (kDeltaThreads / 64) + (threadIdx.x >> 6);
+    if (vc >= all) return;
+    const int lane = threadIdx.x & 63, chunk = (int)(vc % shape.chunks), head = (int)(vc / shape.chunks % p.value_heads), b = (int)(vc / shape.chunks / p.value_heads);
+    const int t0 = chunk * kChunk, rows = sequence_length(a.lengths, b, p.length) - t0;
+    float of_a = 0.0f, of_bias = 0.0f, db = 0.0f;
+    if (rows > 0) {
+        const double* from = w.gates + vc * kGates * kChunk;
+        const float* scalars = w.scalars + vc * kScalars * kChunk;
+        const double own_end = from[kGateEnds * kChunk + lane];
+        double dg = from[kGateRows * kChunk + lane], de = own_end;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const double behind = __shfl_down(dg, m), before = __shfl_up(de, m);
+            if (lane + m < 64) dg += behind;
+            if (lane >= m) de += before;
+        }
+        const float log_decay = (float)(dg + (de - own_end) + from[kGateWhole * kChunk + lane]);
+        if (lane < rows) {
+            of_a = scalars[kStep * kChunk + lane] * log_decay;
+            of_bias = a.a[head] * log_decay * scalars[kSlope * kChunk + lane];
+            db = (float)from[kGateStrengths * kChunk + lane];
+            if (p.sigmoid) {
+                // (1 - b is the sigmoid of -beta, and keeps its digits there)
+                const float raw = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
+                db *= sigmoid(raw) * sigmoid(-raw);
+            }
+        }
+    }
+    if (t0 + lane < p.length) {
+        const long long at = ((long long)b * p.length + t0 + lane) * p.value_heads + head;
+        ((T*)a.ddelta)[at] = (T)of_bias;
+        ((T*)a.dbeta)[at] = (T)db;
+    }
+    double sum_a = (double)of_a, sum_bias = (double)of_bias;
+#pragma unroll
+    for (int m = 32; m; m >>= 1) sum_a += __shfl_xor(sum_a, m), sum_bias += __shfl_xor(sum_bias, m);
+    if (lane == 0) {
+        w.shares[vc * 2] = sum_a;
+        w.shares[vc * 2 + 1] = sum_bias;
+    }
+}
+
+// The chunks' sums of a head, a wavefront a head, in 64 bits.
+__global__ __launch_bounds__(64) void delta_rates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
     const int head = blockIdx.x, lane = threadIdx.x;
     double of_a = 0.0, of_bias = 0.0;
     for (int b = 0; b < p.batch; ++b)
         for (int c = lane; c < shape.chunks; c += 64) {
-            const float* from = w.dg + (((size_t)b * p.value_heads + head) * shape.chunks + c) * 2;
-            of_a += (double)from[0];
-            of_bias += (double)from[1];
+            const double* from = w.shares + (((size_t)b * p.value_heads + head) * shape.chunks + c) * 2;
+            of_a += from[0];
+            of_bias += from[1];
         }
 #pragma unroll
     for (int m = 32; m; m >>= 1) of_a += __shfl_xor(of_a, m), of_bias += __shfl_xor(of_bias, m);
@@ -737,9 +804,12 @@ hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape&
     constexpr int kMost = sizeof(T) == 4 && KD > 64 ? 1 : 2;
     if (wide) hipLaunchKernelGGL((delta_back_kernel<T, KD, kMost>), dim3((unsigned)sweeps), dim3(kSweepThreads), 0, s, p, a, of, w);
     else hipLaunchKernelGGL((delta_back_kernel<T, KD, 1>), dim3((unsigned)sweeps), dim3(kSweepThreads), 0, s, p, a, of, w);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess || !chunks) return e;
     hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kGradThreads), 0, s, p, a, shape, w);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const long long all = (long long)shape.chunks * p.value_heads * p.batch, blocks = (all + kDeltaThreads / 64 - 1) / (kDeltaThreads / 64);
+    hipLaunchKernelGGL(delta_gates_kernel<T>, dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, shape, w, all);
     return hipGetLastError();
 }
 
@@ -769,7 +839,7 @@ hipError_t launch_delta_grad(const sys_gated_delta_t& p, const DeltaArgs& a, hip
         }
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(delta_gates_kernel, dim3((unsigned)p.value_heads), dim3(64), 0, s, p, a, shape, w);
+    hipLaunchKernelGGL(delta_rates_kernel, dim3((unsigned)p.value_heads), dim3(64), 0, s, p, a, shape, w);
     return hipGetLastError();
 }
 

@@ -196,7 +196,7 @@ struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
     float *s, *ds, *u, *z;             // [columns / 32][padded][32], [columns / 32][64][32]
     float* scalars;                    // [kScalars][64]
-    float* dg;                         // every chunk's share of the gradients of A and the bias
+    double *gates, *shares;            // of a chunk of a value head: [kGates][64]; its share of the gradients of A and the bias
 };
 
 struct DeltaShape {
@@ -209,6 +209,9 @@ struct DeltaShape {
 
 // e^G, e^(G_end - G), b; for gradients the step size and its derivative by delta, and G in 64 bits, to base 2
 enum Scalars { kGamma, kLeft, kStrength, kStep, kSums, kSlope = 6, kScalars };
+
+// Of a position: the gradient of the sum G that ends there, of what is left behind it, of its strength; of all alike
+enum Gates { kGateRows, kGateEnds, kGateStrengths, kGateWhole, kGates };
 
 inline int delta_padded(const sys_gated_delta_t& p) { return p.key_dim <= 64 ? 64 : 128; }
 inline int delta_chunks(const sys_gated_delta_t& p) { return (p.length + kChunk - 1) / kChunk; }
