@@ -81,22 +81,23 @@ def build_host_sanitized(verbose: bool = True, driver: str = "abi_san_driver") -
     san_dir = os.path.join(OBJ, "san")
     newest = max(os.path.getmtime(os.path.join(d, f)) for d in (CSRC, os.path.join(ROOT, "include")) for f in os.listdir(d) if f.endswith(".h"))
     os.makedirs(san_dir, exist_ok=True)
-    objs = []
-    for src in SOURCES:
-        if src in HOST_LOGIC:
-            obj = os.path.join(san_dir, src.replace(".hip", ".o"))
-            objs.append(obj)
-            if os.path.exists(obj) and os.path.getmtime(obj) > max(newest, os.path.getmtime(os.path.join(CSRC, src)), os.path.getmtime(__file__)):
-                continue                           # built for another driver
+
+    def sanitized(src: str) -> str:
+        obj = os.path.join(san_dir, src.replace(".hip", ".o"))
+        if not os.path.exists(obj) or os.path.getmtime(obj) <= max(newest, os.path.getmtime(os.path.join(CSRC, src)), os.path.getmtime(__file__)):
             cmd = ["hipcc", *[f for f in FLAGS if f != "-O3"], "-O1", *SAN_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
             res = subprocess.run(cmd, capture_output=True, text=True)
             if res.returncode != 0:
                 raise RuntimeError(f"hipcc (host sanitizers) failed on {src}:\n{res.stderr}")
-        else:
-            obj = os.path.join(OBJ, src.replace(".hip", ".o"))
-            if not os.path.exists(obj):
-                _compile(src)
-            objs.append(obj)
+        return obj                                 # (else built for another driver)
+
+    def ordinary(src: str) -> str:
+        obj = os.path.join(OBJ, src.replace(".hip", ".o"))
+        if not os.path.exists(obj):
+            _compile(src)
+        return obj
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        objs = list(pool.map(lambda src: sanitized(src) if src in HOST_LOGIC else ordinary(src), SOURCES))
     exe = os.path.join(san_dir, driver)
     driver = os.path.join(ROOT, "tests", driver + ".cpp")
     cmd = ["hipcc", "--offload-arch=gfx950", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined",
