@@ -433,23 +433,30 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         }
     } else if (GRAD) {
         // what the gradients need of it: S before the chunk, and U.  (From wavefronts of their own: loads that were made behind stores wait for them.)
-        for (int c = 0; c < chunks; ++c) {
-            lds_barrier();
+        auto store_state = [&](int c, int i) {
 #pragma unroll
-            for (int i = 0; i < TW; ++i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const f4 of_s = turn_quad(states.numbers(TW * wave + i, n, lane));
-                    *(f4*)(w.s + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = of_s;
-                }
-            lds_barrier();
-            lds_barrier();
+            for (int n = 0; n < NT; ++n) {
+                const f4 of_s = turn_quad(states.numbers(TW * wave + i, n, lane));
+                *(f4*)(w.s + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = of_s;
+            }
+        };
+        auto store_u = [&](int c) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const f4 u = turn_quad(values.numbers(wave, n, lane));
                 *(f4*)(w.u + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = u;
             }
+        };
+        for (int c = 0; c < chunks; ++c) {
+            // (the state stays as it is to the third barrier, U to the second of the next chunk: nobody waits for this)
+            lds_barrier();
+            if (c) store_u(c - 1);
+            if (TW == 1) store_state(c, 0);
+            lds_barrier();
+            if (TW == 2) store_state(c, 0), store_state(c, 1);
+            lds_barrier();
         }
+        if (chunks > 0) store_u(chunks - 1);
     } else {
         // the outputs
         ChunkRows<T> y((const T*)a.y + b * p.y_batch + head * p.value_dim, p.y_row, p.value_dim, 0, p.length);
@@ -476,23 +483,36 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                 }
         };
         if (chunks > 0) fetch_queries(0), fetch_mixed(0);
+        f4 out[NT] = {}, done[NT];
+        auto of_state = [&](int i) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                b8 parts[RP];
+                states.take(i, n, lane, parts);
+                out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
+            }
+        };
+        auto store = [&] {
+            const __amdgpu_buffer_rsrc_t rows = y.buffer();
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)done[n][e]);
+            y.move(1);
+        };
         for (int c = 0; c < chunks; ++c) {
             const int next = c + 1 < chunks ? c + 1 : c;
+            // (the state stays as it is to the third barrier, U to the second of the next chunk: the work is spread so that the other four never wait for it)
             lds_barrier();
-            f4 out[NT] = {};
+            if (c) store();
 #pragma unroll
-            for (int i = 0; i < KS; ++i)
+            for (int i = 0; i < KS / 2; ++i) of_state(i);
+            lds_barrier();
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    b8 parts[RP];
-                    states.take(i, n, lane, parts);
-                    out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
-                }
+            for (int i = KS / 2; i < KS; ++i) of_state(i);
             const f4 gamma = next_gamma * p.scale;
             fetch_queries(next);
             lds_barrier();
-            lds_barrier();
-            const __amdgpu_buffer_rsrc_t rows = y.buffer();
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 f4 o = out[n] * gamma;
@@ -503,12 +523,12 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                         values.take(i, n, lane, parts);
                         o = multiply<RP - 1>(pa[i], parts, o);
                     }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)o[e]);
+                done[n] = o;
+                out[n] = f4{};
             }
-            y.move(1);
             fetch_mixed(next);
         }
+        if (chunks > 0) store();
         T* behind = (T*)a.y + b * p.y_batch + head * p.value_dim;
         for (int t = chunks * kChunk + (int)((threadIdx.x & 255) >> 4); t < p.length; t += kSweepThreads / 32)
 #pragma unroll

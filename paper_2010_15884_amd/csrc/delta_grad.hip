@@ -205,14 +205,13 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
             }
         b8 qta[TW][2][NX], pa[2][3];
         unsigned next_dy[NT][4];
-        f4 next_gamma, next_strength, queries[TW][NT];
+        f4 next_gamma, next_strength;
         auto fetch_outs = [&](int c) {
             const __amdgpu_buffer_rsrc_t rows = dy.buffer();
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) next_dy[n][e] = buffer_load<T>(rows, dy_at[n][e]);
-            dy.move(-1);
             const float* from = w.scalars + (vc + c) * kScalars * kChunk;
             next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
             next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
@@ -224,6 +223,8 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
                     for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.pt + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
                 }
+        };
+        auto fetch_queries = [&](int c) {
 #pragma unroll
             for (int i = 0; i < TW; ++i)
 #pragma unroll
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                 weighted.put_half(wave, n, lane, next_gamma * p.scale * own);
             }
         };
-        auto products = [&] {
+        auto mixed = [&] {                         // P^T dO
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 f4 u[3] = {};
@@ -253,6 +254,11 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                         multiply_apart<2>(pa[i], parts, u);
                     }
                 of_outs[wave][n][lane] = joined(u);
+            }
+        };
+        auto queries = [&] {                       // Q^T (e^G dO)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
                 f4 more[TW][3] = {};
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
@@ -262,43 +268,48 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                     for (int i = 0; i < TW; ++i) multiply_apart<2>(qta[i][m], parts, more[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < TW; ++i) queries[i][n] = joined(more[i]);
+                for (int i = 0; i < TW; ++i) of_queries[TW * wave + i][n][lane] = joined(more[i]);
             }
         };
+        auto store_values = [&](int c, f4 strength) {
+            const __amdgpu_buffer_rsrc_t rows = dv.buffer();
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f4 z = zs[wave][n][lane], values = strength * z;
+                *(f4*)(w.z + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = turn_quad(z);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, dv_at[n][e], (T)values[e]);
+            }
+            dv.move(-1);
+        };
         if (chunks > 0) {
-            fetch_outs(top), fetch_mixed(top);
-            f4 strength = next_strength;
+            fetch_outs(top), fetch_mixed(top), fetch_queries(top);
+            f4 behind_strength = {}, strength = next_strength;
             put_outs();
             lds_barrier();
-            products();
+            mixed();
             for (int c = top; c >= 0; --c) {
                 const int next = c > 0 ? c - 1 : 0;
-                if (c > 0) fetch_outs(next), fetch_mixed(next);        // (a buffer has no lower end: rows before the first chunk must not be asked for)
+                dy.move(next - c);                 // (a buffer has no lower end: rows before the first chunk must not be asked for, it is read twice instead)
+                fetch_outs(next), fetch_mixed(next);
+                // (dS stays as it is to the third barrier, Z to the second of the next chunk: the work is spread so that the other four wait for little of it)
+                lds_barrier();
+                queries();
+                if (c < top) store_values(c + 1, behind_strength);
+                fetch_queries(next);
                 lds_barrier();
 #pragma unroll
                 for (int i = 0; i < TW; ++i)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        of_queries[TW * wave + i][n][lane] = queries[i][n];
+                    for (int n = 0; n < NT; ++n)
                         *(f4*)(w.ds + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) =
                             turn_quad(states.numbers(TW * wave + i, n, lane));
-                    }
+                behind_strength = strength, strength = next_strength;
+                put_outs();
                 lds_barrier();
-                const f4 after = next_strength;
-                if (c > 0) put_outs();
-                lds_barrier();
-                const __amdgpu_buffer_rsrc_t rows = dv.buffer();
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const f4 z = zs[wave][n][lane], values = strength * z;
-                    *(f4*)(w.z + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = turn_quad(z);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) buffer_store<T>(rows, dv_at[n][e], (T)values[e]);
-                }
-                dv.move(-1);
-                strength = after;
-                if (c > 0) products();
+                mixed();
             }
+            store_values(0, behind_strength);
         }
         T* behind = (T*)a.dv + (long long)b * p.length * dv_row + head * p.value_dim;
         for (int t = chunks * kChunk + (int)((threadIdx.x & 255) >> 4); t < p.length; t += kSweepThreads / 32)
