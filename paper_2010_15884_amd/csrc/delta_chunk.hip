@@ -436,14 +436,14 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         auto store_state = [&](int c, int i) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const f4 of_s = turn_quad(states.numbers(TW * wave + i, n, lane));
+                const f4 of_s = turn_quad(signed_rows(states.numbers(TW * wave + i, n, lane), TW * wave + i));
                 *(f4*)(w.s + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = of_s;
             }
         };
         auto store_u = [&](int c) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const f4 u = turn_quad(values.numbers(wave, n, lane));
+                const f4 u = turn_quad(signed_rows(values.numbers(wave, n, lane), wave));
                 *(f4*)(w.u + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = u;
             }
         };

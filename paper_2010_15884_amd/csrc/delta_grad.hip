@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         *(f4*)(w.ds + block_place(vc + c, KD, shape.columns, tile_row(TW * wave + i, 4 * g) + (r & 3), (tile * NT + n) * 16 + (r & ~3))) =
-                            turn_quad(states.numbers(TW * wave + i, n, lane));
+                            turn_quad(signed_rows(states.numbers(TW * wave + i, n, lane), TW * wave + i));
                 behind_strength = strength, strength = next_strength;
                 put_outs();
                 lds_barrier();
@@ -319,14 +319,22 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
     }
 }
 
-// Sum over the 16 lanes that hold a row of D.
-__device__ __forceinline__ float row_sum(float v)
+// Sums over rows of 16 lanes of four values a lane: lane j of a quad gets that of v[j].
+template <int CONTROL>
+__device__ __forceinline__ double dpp(double v)
 {
-    v += dpp<0xB1>(v);
-    v += dpp<0x4E>(v);
-    v += dpp<0x141>(v);
-    v += dpp<0x140>(v);
-    return v;
+    const unsigned long long bits = __builtin_bit_cast(unsigned long long, v);
+    const unsigned low = __builtin_amdgcn_mov_dpp((int)(unsigned)bits, CONTROL, 0xF, 0xF, true), high = __builtin_amdgcn_mov_dpp((int)(unsigned)(bits >> 32), CONTROL, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, (unsigned long long)high << 32 | low);
+}
+template <typename V>
+__device__ __forceinline__ V row_sums(V v0, V v1, V v2, V v3)
+{
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    const V a = (odd ? v1 : v0) + dpp<0xB1>(odd ? v0 : v1), b = (odd ? v3 : v2) + dpp<0xB1>(odd ? v2 : v3);
+    V sum = (high ? b : a) + dpp<0x4E>(high ? a : b);
+    sum += dpp<0x124>(sum);                        // the quad four lanes away, and then the pair of quads eight lanes away
+    return sum + dpp<0x128>(sum);
 }
 
 // The first or the last four numbers of an operand.
@@ -354,17 +362,6 @@ struct EightFloats {
         for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
     }
 };
-
-// The parts of eight numbers, or of their negatives in every other tile.  The matrix cores cut the sums of an instruction off towards minus infinity; with operands whose entries
-// are mostly of one sign, as keys behind an activation are, that adds up over a row and over the positions, and the gradients of A were off by 2e-6 of
-// themselves.  With every other tile of columns negated (and its sums taken back where they are used) it cancels.
-__device__ __forceinline__ void split_signed(const float (&v)[8], int tile, b8 (&out)[3])
-{
-    float with_sign[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) with_sign[i] = tile & 1 ? -v[i] : v[i];
-    split8(with_sign, out);
-}
 
 // A workgroup a chunk of a key head, through the value heads that share it.  Eight wavefronts: wavefront w the positions of tile w % 4 and half w / 4 of the keys' entries; of the
 // squares the first half has B and the second C.  S, dS' and U of 32 value columns at a time are split on their way into LDS, as the operands
@@ -403,7 +400,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         __device__ Pool() {}
     } pool;
     __shared__ float rows_db[2][kChunk], rows_end[2][kChunk], rows_zv[kChunk];
-    __shared__ double rows_dg[2][kChunk], columns_dg[8][kChunk], waves_end[8];
+    __shared__ double rows_dg[2][kChunk], columns_dg[8][kChunk], waves_end[8][4];
     __shared__ __attribute__((aligned(16))) float scalars[kScalars * kChunk];
 
     // K and Q, which all value heads use, as operands and transposed: as many as LDS has room for
@@ -459,9 +456,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         const int lane = tid & 63, place = lane + (lane >> 4);
         const int piece_row = (tid & 255) >> 2, piece = 17 * (tid & 3) + row_in_tile(piece_row);
         auto scalar = [&] { return tid < kScalars * kChunk ? w.scalars[vc * kScalars * kChunk + tid] : 0.0f; };
-        const float early_scalar = NX < 3 ? scalar() : 0.0f;
+        const float early_scalar = NX == 2 ? scalar() : 0.0f;
         f4 dq[KH] = {}, zs[KH] = {}, us[KH] = {}, square[4] = {};
-        double both = 0.0;                         // (<S, dS'> is the sum of key_dim x value_dim terms of either sign, and all positions of the chunk get it)
+        float both = 0.0f;                         // (8 products a lane and step; <S, dS'> is the sum of key_dim x value_dim terms of either sign, and all positions of the chunk get it)
         float zv = 0.0f;
         if (!kBeyond) fetch(ahead, tid);
         auto stage = [&](Ahead& next) {
@@ -470,11 +467,11 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             if (tid < KD * 4) {
                 const int tile = tile_of(tid >> 2), to = 17 * (tid & 3) + row_in_tile(tid >> 2);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) both = __builtin_fma((double)next.s.v[i], (double)next.ds.v[i], both);
-                split_signed(next.s.v, tile, parts);
+                for (int i = 0; i < 8; ++i) both = __builtin_fmaf(next.s.v[i], next.ds.v[i], both);
+                split8(next.s.v, parts);
 #pragma unroll
                 for (int m = 0; m < 3; ++m) pool.columns.s[tile][m][to] = parts[m];
-                split_signed(next.ds.v, tile, parts);
+                split8(next.ds.v, parts);
 #pragma unroll
                 for (int m = 0; m < 3; ++m) pool.columns.ds[tile][m][to] = parts[m];
             }
@@ -482,7 +479,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             if (half) {
                 b8 values[NX];
                 next.values.split(values);
-                split_signed(next.rows.v, tile, parts);
+                split8(next.rows.v, parts);
 #pragma unroll
                 for (int m = 0; m < 3; ++m) pool.columns.u[tile][m][piece] = parts[m];
 #pragma unroll
@@ -545,7 +542,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             if (NX == 3 && item % steps != 0) fetch(ahead, tid);
         }
         asm volatile("" : "+v"(tid));
-        if (tid < kScalars * kChunk) scalars[tid] = NX < 3 ? early_scalar : scalar();
+        if (tid < kScalars * kChunk) scalars[tid] = NX == 2 ? early_scalar : scalar();
         lds_barrier();
         int again = lane;
         asm volatile("" : "+v"(again));
@@ -695,28 +692,27 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         };
         if (middle) finish(std::integral_constant<int, 1>());
         else finish(std::integral_constant<int, 0>());
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            double dg = of_h[e] + (double)of_g[e];
-#pragma unroll
-            for (int m = 1; m < 16; m <<= 1) dg += __shfl_xor(dg, m);
-            const float db = row_sum(of_strength[e]), de = row_sum(of_end[e]);
-            if ((again & 15) == 0) {
-                rows_dg[half][mine + e] = dg;
-                rows_db[half][mine + e] = db;
-                rows_end[half][mine + e] = de;
-            }
+        const double dg_sum = row_sums(of_h[0] + (double)of_g[0], of_h[1] + (double)of_g[1], of_h[2] + (double)of_g[2], of_h[3] + (double)of_g[3]);
+        const float db_sum = row_sums(of_strength[0], of_strength[1], of_strength[2], of_strength[3]), end_sum = row_sums(of_end[0], of_end[1], of_end[2], of_end[3]);
+        if ((again & 15) < 4) {
+            rows_dg[half][mine + (again & 3)] = dg_sum;
+            rows_db[half][mine + (again & 3)] = db_sum;
+            rows_end[half][mine + (again & 3)] = end_sum;
         }
         zv = quad_sum(zv);
         if (!half && (again & 3) == 0) rows_zv[16 * wave + (again >> 2)] = zv;
-        for (int m = 32; m; m >>= 1) both += __shfl_xor(both, m);
-        if (again == 0) waves_end[4 * half + wave] = both;
+        const double of_row = row_sums((double)both, 0.0, 0.0, 0.0);
+        if ((again & 15) == 0) waves_end[4 * half + wave][again >> 4] = of_row;
         lds_barrier();
         if (!half && wave == 0) {
             // for the next kernel, which sums over positions: the share of a position, of what is left behind it, and of the whole chunk
             double dg = rows_dg[0][again] + rows_dg[1][again], end = 0.0;
 #pragma unroll
-            for (int m = 0; m < 8; ++m) dg -= columns_dg[m][again], end += waves_end[m];
+            for (int m = 0; m < 8; ++m) {
+                dg -= columns_dg[m][again];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) end += waves_end[m][i];
+            }
             double* out = w.gates + vc * kGates * kChunk;
             out[kGateRows * kChunk + again] = dg;
             out[kGateEnds * kChunk + again] = (double)rows_end[0][again] + (double)rows_end[1][again];
@@ -725,11 +721,13 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         }
         // (the next head's operands are put where the squares lie behind a barrier of its own)
     }
+    int out_lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(out_lane));
 #pragma unroll
     for (int i = 0; i < KH; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int column = tile_row(half * KH + i, threadIdx.x & 15), mine = tile_row(wave, 4 * (threadIdx.x >> 4 & 3));
+            const int column = tile_row(half * KH + i, out_lane & 15), mine = tile_row(wave, 4 * (out_lane >> 4));
             if (mine + e < here && column < p.key_dim) {
                 const long long at = ((at0 + mine + e) * p.key_heads + key_head) * p.key_dim + column;
                 ((T*)a.dq)[at] = (T)dq_all[i][e];
