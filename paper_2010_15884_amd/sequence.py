@@ -68,6 +68,7 @@ class _EntryPoints:
             f.argtypes, f.restype = [ctypes.c_char_p], ctypes.c_size_t
             setattr(self, name, f)
         self.empty, self.float32 = torch.empty, torch.float32
+        self.empty_like, self.contiguous = torch.empty_like, torch.contiguous_format
         self.stream, self.external = torch.cuda.stream, torch.cuda.ExternalStream
         self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
@@ -198,6 +199,11 @@ def _allocated(t, stream, make):
         return make(_calls.empty, t.device)
     with _calls.stream(_calls.external(int(stream), device=t.device)):
         return make(_calls.empty, t.device)
+
+
+def _like_it(t):
+    """A contiguous tensor of t's shape, type and device (in half the host time of one by shape); None for None."""
+    return None if t is None else _calls.empty_like(t, memory_format=_calls.contiguous)
 
 
 def _run(name, packed, stream, *pointers):
@@ -534,8 +540,7 @@ def sys_head_norm(d_q, d_k=None, d_wq=None, d_wk=None, d_cos=None, d_sin=None, d
     packed, _ = _planned(_heads_plan, (norm, eps, interleaved, False), d_q, d_k, d_wq, d_wk, d_cos, d_sin, d_positions, d_lengths, d_yq, d_yk)
 
     def make(empty, device):
-        like = lambda t, out: out if t is None or out is not None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
-        return like(d_q, d_yq), like(d_k, d_yk)
+        return _like_it(d_q) if d_yq is None else d_yq, _like_it(d_k) if d_yk is None else d_yk
     d_yq, d_yk = _allocated(d_q, stream, make)
     _run("sys_head_norm", packed, stream, d_q.data_ptr(), _ptr(d_k), _ptr(d_wq), _ptr(d_wk), _ptr(d_cos), _ptr(d_sin), _ptr(d_positions),
          _ptr(d_lengths), d_yq.data_ptr(), _ptr(d_yk))
@@ -548,8 +553,7 @@ def sys_head_norm_backward(d_dyq, d_dyk, d_q, d_k=None, d_wq=None, d_wk=None, d_
     packed, floats = _planned(_heads_plan, (norm, eps, interleaved, True), d_q, d_k, d_wq, d_wk, d_cos, d_sin, d_positions, d_lengths, d_dyq, d_dyk)
 
     def make(empty, device):
-        like = lambda t: None if t is None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
-        return like(d_q), like(d_k), like(d_wq), like(d_wk), empty(floats, dtype=_calls.float32, device=device) if floats else None
+        return _like_it(d_q), _like_it(d_k), _like_it(d_wq), _like_it(d_wk), empty(floats, dtype=_calls.float32, device=device) if floats else None
     dq, dk, dwq, dwk, workspace = _allocated(d_q, stream, make)
     _run("sys_head_norm_backward", packed, stream, d_dyq.data_ptr(), _ptr(d_dyk), d_q.data_ptr(), _ptr(d_k), _ptr(d_wq), _ptr(d_wk), _ptr(d_cos),
          _ptr(d_sin), _ptr(d_positions), _ptr(d_lengths), dq.data_ptr(), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(workspace))
@@ -604,7 +608,7 @@ def sys_gated_delta_rule(d_q, d_k, d_v, d_delta, d_A, d_beta, d_delta_bias=None,
     and the states [batch, value_heads, key_dim, value_dim] are float32.  Returns d_y."""
     packed, floats = _planned(_delta_plan, (scale, softplus, sigmoid, False), d_q, d_k, d_v, d_delta, d_A, d_beta, d_delta_bias, d_state, d_lengths, d_y,
                               d_state_out)
-    d_y, workspace = _allocated(d_q, stream, lambda empty, device: (empty(d_v.shape, dtype=d_v.dtype, device=device) if d_y is None else d_y,
+    d_y, workspace = _allocated(d_q, stream, lambda empty, device: (_like_it(d_v) if d_y is None else d_y,
                                                                     empty(floats, dtype=_calls.float32, device=device) if floats else None))
     _run("sys_gated_delta_rule", packed, stream, d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), d_delta.data_ptr(), d_A.data_ptr(), d_beta.data_ptr(),
          _ptr(d_delta_bias), _ptr(d_state), _ptr(d_lengths), d_y.data_ptr(), _ptr(d_state_out), _ptr(workspace))
@@ -618,8 +622,7 @@ def sys_gated_delta_rule_backward(d_dy, d_q, d_k, d_v, d_delta, d_A, d_beta, d_d
                               d_dstate_out)
 
     def make(empty, device):
-        like = lambda t: None if t is None else empty(t.shape, dtype=t.dtype, device=device)  # noqa: E731
-        return (DeltaGradients(like(d_q), like(d_k), like(d_v), like(d_delta), like(d_A), like(d_beta), like(d_delta_bias), like(d_state)),
+        return (DeltaGradients(*[_like_it(t) for t in (d_q, d_k, d_v, d_delta, d_A, d_beta, d_delta_bias, d_state)]),
                 empty(floats, dtype=_calls.float32, device=device) if floats else None)
     g, workspace = _allocated(d_q, stream, make)
     _run("sys_gated_delta_rule_backward", packed, stream, d_dy.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), d_delta.data_ptr(),
@@ -650,7 +653,7 @@ def sys_gated_delta_rule_update(d_q, d_k, d_v, d_delta, d_A, d_beta, d_state, d_
     """One token a request: d_q, d_k [requests, key_heads, key_dim], d_v [requests, value_heads, value_dim], d_delta, d_beta [requests, value_heads], d_state
     float32 [slots, value_heads, key_dim, value_dim], updated in place (or into d_state_out); slots as sys_causal_conv1d_update.  Returns d_y."""
     packed = _planned(_delta_step_plan, (scale, softplus, sigmoid), d_q, d_k, d_v, d_delta, d_A, d_beta, d_delta_bias, d_state, d_slots, d_y, d_state_out)
-    d_y = _allocated(d_q, stream, lambda empty, device: empty(d_v.shape, dtype=d_v.dtype, device=device) if d_y is None else d_y)
+    d_y = _allocated(d_q, stream, lambda empty, device: _like_it(d_v) if d_y is None else d_y)
     _run("sys_gated_delta_rule_update", packed, stream, d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), d_delta.data_ptr(), d_A.data_ptr(),
          d_beta.data_ptr(), _ptr(d_delta_bias), d_state.data_ptr(), _ptr(d_slots), d_y.data_ptr(),
          _ptr(d_state if d_state_out is None else d_state_out))
