@@ -360,22 +360,36 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
     }
 }
 
-// The workgroups' sums of a column, [blocks][2][dim], four columns a workgroup of 64 lanes each.
-__global__ __launch_bounds__(kThreads) void head_norm_join_kernel(sys_head_norm_t p, HeadNormArgs a, int blocks)
+// The workgroups' sums of a column, [blocks][2][dim]: 16 columns a workgroup (64 bytes of a row), 64 lanes a column, joined in a fixed order.
+constexpr int kJoinColumns = 16, kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void head_norm_join_kernel(sys_head_norm_t p, HeadNormArgs a, int blocks)
 {
-    const int column = blockIdx.x * kWavesOf + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (column >= 2 * p.dim) return;
-    void* out = column < p.dim ? a.dwq : a.dwk;
-    if (!out) return;
+    constexpr int kRows = kJoinThreads / kJoinColumns;
+    const int column = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, first = threadIdx.x / kJoinColumns;
+    const bool there = column < 2 * p.dim;
     float v = 0.0f;
-    for (int i = lane; i < blocks; i += 64) v += a.workspace[(size_t)i * 2 * p.dim + column];
-    v = lanes_sum(v, 6);
-    if (lane == 0) store_param(out, column < p.dim ? column : column - p.dim, p.param_dtype, v);
+#pragma unroll 8
+    for (int i = first; i < blocks; i += kRows) v += there ? a.workspace[(size_t)i * 2 * p.dim + column] : 0.0f;
+    // over the four rows of lanes of a wavefront, then over wavefronts
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    __shared__ float sums[kJoinThreads / 64][kJoinColumns];
+    if ((threadIdx.x & 63) < kJoinColumns) sums[threadIdx.x >> 6][threadIdx.x & 63] = v;
+    __syncthreads();
+    if (threadIdx.x >= kJoinColumns || !there) return;
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kJoinThreads / 64; ++i) v += sums[i][threadIdx.x];
+    void* out = column < p.dim ? a.dwq : a.dwk;
+    if (out) store_param(out, column < p.dim ? column : column - p.dim, p.param_dtype, v);
 }
 
 // ---------------------------------------------------------------- launches
 
-constexpr int kGradBlocks = 1024;                  // at most
+// Workgroups of the gradients, at most: as many as the registers of an instance leave resident, so that none starts behind the others.  8192 tokens of 18 heads
+// of 256 in bf16 (V = 8, 199 registers): 51 us with 512, 59 with 768, 58 with 1024, 65 with 256; of 72 (V = 4, 133): 36, 32, 40, 51; of 50 (V = 1, 91): 42, 37, 34, 67.
+constexpr int kGradBlocks = 1024;
+template <int V, int S> constexpr int kResidentBlocks = V * S == 1 ? kGradBlocks : V == 4 ? 768 : 512;
 
 template <int V, int S>
 NormPlan plan_of(const sys_head_norm_t& p, bool grad)
@@ -412,14 +426,14 @@ hipError_t launch_shape(bool grad, const sys_head_norm_t& p, const HeadNormArgs&
         hipLaunchKernelGGL((head_norm_kernel<T, V, S>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, a, n);
         return hipGetLastError();
     }
-    if (blocks > kGradBlocks) blocks = kGradBlocks;
+    if (blocks > kResidentBlocks<V, S>) blocks = kResidentBlocks<V, S>;
     if (blocks) {
         hipLaunchKernelGGL((head_norm_grad_kernel<T, V, S>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, a, n, waves);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (!a.dwq && !a.dwk) return hipSuccess;
-    hipLaunchKernelGGL(head_norm_join_kernel, dim3((unsigned)(2 * p.dim + kWavesOf - 1) / kWavesOf), dim3(kThreads), 0, s, p, a, (int)blocks);
+    hipLaunchKernelGGL(head_norm_join_kernel, dim3((unsigned)(2 * p.dim + kJoinColumns - 1) / kJoinColumns), dim3(kJoinThreads), 0, s, p, a, (int)blocks);
     return hipGetLastError();
 }
 
