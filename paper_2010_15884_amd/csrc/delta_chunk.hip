@@ -26,15 +26,28 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, g = lane >> 4;
     const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks + chunk;
 
-    __shared__ __attribute__((aligned(16))) bf16_t keys[NX][kChunk][kPitch];
-    __shared__ __attribute__((aligned(16))) float am[kChunk][kSide], xm[kChunk][kSide];
+    // X is put where the keys lay
+    __shared__ __attribute__((aligned(16))) union Pool {
+        bf16_t keys[NX][kChunk][kPitch];
+        float x[kChunk][kSide];
+        __device__ Pool() {}
+    } pool;
+    auto& keys = pool.keys;
+    auto& xm = pool.x;
+    __shared__ __attribute__((aligned(16))) float am[kChunk][kSide];
     __shared__ double sums[kChunk];                // of the logarithms of the decays, to base 2
     __shared__ float strengths[kChunk];
 
-    // K into LDS, and the rows of Q that this wavefront works on
+    // what the first wavefront makes the decays of, K into LDS, and the rows of Q that this wavefront works on, as operands have them
     constexpr int kPieces = kChunk * KD / 8 / kDeltaThreads;
     b8 qa[KS][NX];
     {
+        float raw_delta = 0.0f, raw_beta = 0.0f, bias = 0.0f, rate = 0.0f;
+        if (wave == 0 && lane < rows) {
+            raw_delta = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head];
+            raw_beta = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
+        }
+        if (wave == 0) rate = a.a[head], bias = a.delta_bias ? a.delta_bias[head] : 0.0f;
         Eight<T> from_k[kPieces], from_q[KS];
         const ChunkRows<T> k_rows((const T*)a.k + b * p.k_batch + key_head * p.key_dim, p.k_row, p.key_dim, chunk, last);
         const ChunkRows<T> q_rows((const T*)a.q + b * p.q_batch + key_head * p.key_dim, p.q_row, p.key_dim, chunk, last);
@@ -47,9 +60,47 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const int row = 16 * wave + r, at = 32 * s + 8 * g;
+            const int row = tile_row(wave, r), at = 32 * s + 8 * g;
             if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.offset(row, at) : kNowhere);
             else from_q[s].load_each(q_buffer, q_rows.offset(row, at), p.key_dim - at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (wave == 0) {
+            // in 64 bits: what a step size is off by adds up over all positions that a state lives through, and a ratio of decays is the exponential of a small
+            // difference of what may be large sums (with the step sizes of sequence.h, off by up to 8 2^-24, the gradients of A were off by 2e-6 of themselves
+            // after 2048 positions, now 5e-7)
+            double step = 0.0, strength = 0.0, slope = 0.0;
+            if (lane < rows) {
+                step = (double)raw_delta + (double)bias;
+                strength = (double)raw_beta;
+                slope = 1.0;
+                if (p.softplus) {
+                    const double small = exp(-fabs(step)), large = step < 0.0 ? small : 1.0;
+                    slope = large / (1.0 + small);
+                    step = (step < 0.0 ? 0.0 : step) + log1p(small);       // (a NaN comes back with `small`)
+                }
+                if (p.sigmoid) strength = 1.0 / (1.0 + exp(-strength));
+            }
+            // a decay of 2^-10000 is 0 as any smaller one, and leaves the differences behind it their digits (NaN passes)
+            double sum = step * (double)rate * 1.4426950408889634;
+            sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
+    #pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const double other = __shfl_up(sum, m);
+                if (lane >= m) sum += other;
+            }
+            const double end = __shfl(sum, 63);
+            sums[lane] = sum;
+            strengths[lane] = (float)strength;
+            float* out = w.scalars + vc * kScalars * kChunk;
+            out[kGamma * kChunk + lane] = fast_exp2((float)sum);
+            out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
+            out[kStrength * kChunk + lane] = (float)strength;
+            if (GRAD) {
+                out[kStep * kChunk + lane] = (float)step;
+                out[kSlope * kChunk + lane] = (float)slope;
+                ((double*)(out + kSums * kChunk))[lane] = sum;
+            }
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -63,48 +114,9 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         for (int s = 0; s < KS; ++s) {
             from_q[s].split(qa[s]);
             if (first) {
-                const int row = 16 * wave + r;
 #pragma unroll
-                for (int n = 0; n < NX; ++n)
-                    *(b8*)(w.q + (kc * NX + n) * kChunk * KD + ((tile_of(row) * KS + s) * 64 + g * 16 + row_in_tile(row)) * 8) = qa[s][n];
+                for (int n = 0; n < NX; ++n) *(b8*)(w.q + (kc * NX + n) * kChunk * KD + ((wave * KS + s) * 64 + lane) * 8) = qa[s][n];
             }
-        }
-    }
-    if (wave == 0) {
-        // in 64 bits: what a step size is off by adds up over all positions that a state lives through, and a ratio of decays is the exponential of a small
-        // difference of what may be large sums (with the step sizes of sequence.h, off by up to 8 2^-24, the gradients of A were off by 2e-6 of themselves
-        // after 2048 positions, now 5e-7)
-        double step = 0.0, strength = 0.0, slope = 0.0;
-        if (lane < rows) {
-            step = (double)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head] + (a.delta_bias ? (double)a.delta_bias[head] : 0.0);
-            strength = (double)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
-            slope = 1.0;
-            if (p.softplus) {
-                const double small = exp(-fabs(step)), large = step < 0.0 ? small : 1.0;
-                slope = large / (1.0 + small);
-                step = (step < 0.0 ? 0.0 : step) + log1p(small);       // (a NaN comes back with `small`)
-            }
-            if (p.sigmoid) strength = 1.0 / (1.0 + exp(-strength));
-        }
-        // a decay of 2^-10000 is 0 as any smaller one, and leaves the differences behind it their digits (NaN passes)
-        double sum = step * (double)a.a[head] * 1.4426950408889634;
-        sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const double other = __shfl_up(sum, m);
-            if (lane >= m) sum += other;
-        }
-        const double end = __shfl(sum, 63);
-        sums[lane] = sum;
-        strengths[lane] = (float)strength;
-        float* out = w.scalars + vc * kScalars * kChunk;
-        out[kGamma * kChunk + lane] = fast_exp2((float)sum);
-        out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
-        out[kStrength * kChunk + lane] = (float)strength;
-        if (GRAD) {
-            out[kStep * kChunk + lane] = (float)step;
-            out[kSlope * kChunk + lane] = (float)slope;
-            ((double*)(out + kSums * kChunk))[lane] = sum;
         }
     }
     __syncthreads();
@@ -122,23 +134,22 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
             }
         }
     };
-    auto square = [&](auto of, bf16_t* to, bool turned) {
-        constexpr int N = decltype(of)::value;
+    auto square = [&](bf16_t* to, bool turned) {
         for (int i = wave; i < 8; i += kDeltaThreads / 64) {
             const int tile = i / 2, step = i % 2;
             if (turned ? step < tile / 2 : step > tile / 2) continue;
             const int row = tile_row(tile, r), at = 32 * step + 8 * g;
             float v[8];
-            b8 parts[N];
+            b8 parts[3];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = turned ? xm[at + j][row] : xm[row][at + j];
             split8(v, parts);
 #pragma unroll
-            for (int n = 0; n < N; ++n) *(b8*)(to + n * kSquare + (i * 64 + lane) * 8) = parts[n];
+            for (int n = 0; n < 3; ++n) *(b8*)(to + n * kSquare + (i * 64 + lane) * 8) = parts[n];
         }
     };
 
-    // K K^T and Q K^T, rows of this wavefront (as they lie), columns up to its own; scaled and cut to triangles
+    // A from K K^T: rows of this wavefront (as they lie), columns up to its own
     b8 ka[KS][NX];
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -148,26 +159,74 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     float row_strength[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) row_sum[e] = sums[16 * wave + 4 * g + e], row_strength[e] = strengths[16 * wave + 4 * g + e];
-    for (int n = 0; n <= (wave | 1); ++n) {
-        f4 kk = {}, qk = {};
-        if (n <= wave) {
+    for (int n = 0; n <= wave; ++n) {
+        f4 kk = {};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                b8 kb[NX];
+        for (int s = 0; s < KS; ++s) {
+            b8 kb[NX];
 #pragma unroll
-                for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][16 * n + r][32 * s + 8 * g];
-                kk = multiply<2>(ka[s], kb, kk);
-                qk = multiply<2>(qa[s], kb, qk);
-            }
+            for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][16 * n + r][32 * s + 8 * g];
+            kk = multiply<2>(ka[s], kb, kk);
         }
         const int column = 16 * n + r;
         const double column_sum = sums[column];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = 16 * wave + 4 * g + e;
-            const float ratio = fast_exp2((float)(row_sum[e] - column_sum));
-            if (n <= wave) am[row][column] = column < row ? row_strength[e] * (ratio * kk[e]) : 0.0f;
-            xm[row][column] = column <= row ? p.scale * (ratio * qk[e]) : 0.0f;
+            am[row][column] = column < row ? row_strength[e] * (fast_exp2((float)(row_sum[e] - column_sum)) * kk[e]) : 0.0f;
+        }
+    }
+    // P, without the quarter above the diagonal, in the order of its operands as the products leave it: K Q^T, whose columns are queries, gives a lane eight keys of a
+    // row of P in two tiles; for gradients Q K^T gives it four queries of a row of P^T, half an operand
+    if constexpr (GRAD) {
+        const int query = tile_row(wave, 4 * g);
+        double query_sum[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) query_sum[e] = sums[query + e];
+        for (int n = 0; n <= (wave | 1); ++n) {
+            const int key = tile_row(n, r);
+            f4 qk = {};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                b8 kb[NX];
+#pragma unroll
+                for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][key][32 * s + 8 * g];
+                qk = multiply<2>(qa[s], kb, qk);
+            }
+            const double key_sum = sums[key];
+            f4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = key <= query + e ? p.scale * (fast_exp2((float)(query_sum[e] - key_sum)) * qk[e]) : 0.0f;
+            u2 parts[3];
+            split4(v, parts);
+#pragma unroll
+            for (int m = 0; m < 3; ++m) *(u2*)(w.pt + (vc * 3 + m) * kSquare + ((2 * n + (wave >> 1)) * 64 + lane) * 8 + 4 * (wave & 1)) = parts[m];
+        }
+    } else {
+        const int query = tile_row(wave, r);
+        const double query_sum = sums[query];
+        for (int step = 0; step <= wave >> 1; ++step) {
+            float v[8];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f4 qk = {};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    b8 kb[NX];
+#pragma unroll
+                    for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][tile_row(2 * step + n, r)][32 * s + 8 * g];
+                    qk = multiply<2>(kb, qa[s], qk);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = 32 * step + 8 * g + 4 * n + e;
+                    v[4 * n + e] = key <= query ? p.scale * (fast_exp2((float)(query_sum - sums[key])) * qk[e]) : 0.0f;
+                }
+            }
+            b8 parts[RP];
+            split8(v, parts);
+#pragma unroll
+            for (int m = 0; m < RP; ++m) *(b8*)(w.p + (vc * RP + m) * kSquare + ((2 * wave + step) * 64 + lane) * 8) = parts[m];
         }
     }
     if (first) {
@@ -178,21 +237,16 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
                 *(b8*)(w.k + (kc * NX + n) * kChunk * KD + (i * 64 + lane) * 8) = *(const b8*)&keys[n][tile_row(i / KS, r)][32 * (i % KS) + 8 * g];
         transposed(w.kt);
     }
-    __syncthreads();
-    // P (its transpose for gradients) from xm
-    {
-        constexpr int N = GRAD ? 3 : RP;
-        square(std::integral_constant<int, N>(), (GRAD ? w.pt : w.p) + vc * N * kSquare, GRAD);
-    }
     if (GRAD && first) {
         // Q^T the same way as K^T, through its place
+        __syncthreads();
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int n = 0; n < NX; ++n) *(b8*)&keys[n][16 * wave + r][32 * s + 8 * g] = qa[s][n];
+            for (int n = 0; n < NX; ++n) *(b8*)&keys[n][tile_row(wave, r)][32 * s + 8 * g] = qa[s][n];
+        __syncthreads();
+        transposed(w.qt);
     }
-    __syncthreads();
-    if (GRAD && first) transposed(w.qt);
 
     // X: the 16 x 16 blocks on the diagonal by substitution, a column a lane (four times over) ...
     float x[16];
@@ -202,6 +256,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 #pragma unroll
         for (int j = 0; j < i; ++j) x[i] = __builtin_fmaf(-am[16 * wave + i][16 * wave + j], x[j], x[i]);
     }
+    __syncthreads();                               // (all are done with the keys)
     if (g == 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) xm[16 * wave + i][16 * wave + r] = x[i];
@@ -238,8 +293,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 #pragma unroll
         for (int e = 0; e < 4; ++e) xm[16 * i + 4 * g + e][16 * wave + r] = 0.0f;
     __syncthreads();
-    square(std::integral_constant<int, 3>(), w.x + vc * 3 * kSquare, false);
-    if (GRAD) square(std::integral_constant<int, 3>(), w.xt + vc * 3 * kSquare, true);
+    square(w.x + vc * 3 * kSquare, false);
+    if (GRAD) square(w.xt + vc * 3 * kSquare, true);
 }
 
 // ---------------------------------------------------------------- the sweep
@@ -492,19 +547,20 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
                 out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
             }
         };
-        auto store = [&] {
+        auto store = [&](int c) {
             const __amdgpu_buffer_rsrc_t rows = y.buffer();
+            const int left = last - c * kChunk - my_row;               // (behind the sequence 0, also where the state is not finite)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)done[n][e]);
+                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, y_at[n][e], (T)(e < left ? done[n][e] : 0.0f));
             y.move(1);
         };
         for (int c = 0; c < chunks; ++c) {
             const int next = c + 1 < chunks ? c + 1 : c;
             // (the state stays as it is to the third barrier, U to the second of the next chunk: the work is spread so that the other four never wait for it)
             lds_barrier();
-            if (c) store();
+            if (c) store(c - 1);
 #pragma unroll
             for (int i = 0; i < KS / 2; ++i) of_state(i);
             lds_barrier();
@@ -528,7 +584,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
             }
             fetch_mixed(next);
         }
-        if (chunks > 0) store();
+        if (chunks > 0) store(chunks - 1);
         T* behind = (T*)a.y + b * p.y_batch + head * p.value_dim;
         for (int t = chunks * kChunk + (int)((threadIdx.x & 255) >> 4); t < p.length; t += kSweepThreads / 32)
 #pragma unroll

@@ -273,12 +273,13 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         };
         auto store_values = [&](int c, f4 strength) {
             const __amdgpu_buffer_rsrc_t rows = dv.buffer();
+            const int left = last - c * kChunk - my_row;               // (behind the sequence 0, also where a gradient is not finite)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const f4 z = zs[wave][n][lane], values = strength * z;
                 *(f4*)(w.z + block_place(vc + c, kChunk, shape.columns, my_row + (r & 3), (tile * NT + n) * 16 + (r & ~3))) = turn_quad(z);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, dv_at[n][e], (T)values[e]);
+                for (int e = 0; e < 4; ++e) buffer_store<T>(rows, dv_at[n][e], (T)(e < left ? values[e] : 0.0f));
             }
             dv.move(-1);
         };
@@ -730,8 +731,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             const int column = tile_row(half * KH + i, out_lane & 15), mine = tile_row(wave, 4 * (out_lane >> 4));
             if (mine + e < here && column < p.key_dim) {
                 const long long at = ((at0 + mine + e) * p.key_heads + key_head) * p.key_dim + column;
-                ((T*)a.dq)[at] = (T)dq_all[i][e];
-                ((T*)a.dk)[at] = (T)dk_all[i][e];
+                ((T*)a.dq)[at] = (T)(mine + e < rows ? dq_all[i][e] : 0.0f);
+                ((T*)a.dk)[at] = (T)(mine + e < rows ? dk_all[i][e] : 0.0f);
             }
         }
 }

@@ -137,6 +137,18 @@ def test_states_that_are_not_finite_stay_in_their_column():
     assert not torch.isfinite(y[1, 1:, 0, 20]).any() and torch.equal(state[1, 0][:, others], clean_state[1, 0][:, others])
 
 
+@pytest.mark.parametrize("length", [9, 100])
+def test_rows_behind_a_sequence_are_zero_whatever_the_state_is(length):
+    c = _make(78, 3, length, 1, 2, 64, 48, BF16, state=True, lengths=[length - 4, 0, 5])
+    c["state"][:, 0, 3, 7], c["dstate_out"][:, 1, 2, 9] = float("inf"), float("nan")
+    y, _ = _forward(c)
+    grads = _backward(c)
+    for b, n in enumerate([length - 4, 0, 5]):
+        for t in (y, grads.dq, grads.dk, grads.dv, grads.ddelta, grads.dbeta):
+            assert (t[b, n:] == 0).all()
+    assert not torch.isfinite(y[0, :length - 4, 0, 7]).any()
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_operators_in_a_row(dtype):
     """Convolution, norm of queries and keys, delta rule, norm of the results: each of what the one before left, over ragged prompts and one token more."""
