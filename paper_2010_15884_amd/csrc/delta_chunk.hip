@@ -671,6 +671,9 @@ DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a)
     s.chunks = delta_chunks(p);
     s.padded = delta_padded(p);
     s.columns = (p.value_dim + 31) / 32 * 32;
+    // where that leaves half of the CUs or more without a workgroup: 24 chunks of key heads with two value heads of 64 x 100 each in fp32 take 24 us apart, and 4 for
+    // the join of their sums, against 41 one after the other; from half of the CUs on there are no fewer rounds of workgroups to win
+    s.apart = p.value_heads > p.key_heads && 2 * (long long)s.chunks * p.key_heads * p.batch <= kCus;
     return s;
 }
 
@@ -702,6 +705,7 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
         take(of.ds, state);
         take(of.u, rows);
         take(of.z, rows);
+        if (shape.apart) take(of.parts, 2 * value_chunks * kChunk * shape.padded * sizeof(float));
         take(of.gates, value_chunks * kGates * kChunk * sizeof(double));
         take(of.shares, 2 * value_chunks * sizeof(double));
     }

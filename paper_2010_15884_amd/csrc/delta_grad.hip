@@ -373,8 +373,9 @@ template <typename T, int KD>
 __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
     constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KS = KD / 32, KT = KD / 16, KH = KT / 2, kPitch = kChunk + 8;
-    const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, key_head = rest % p.key_heads, b = rest / p.key_heads;
-    const int shared = p.value_heads / p.key_heads;
+    const int shared = shape.apart ? 1 : p.value_heads / p.key_heads, groups = p.value_heads / shared;     // value heads of this workgroup, and groups of them
+    const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, first_head = rest % groups * shared, b = rest / groups;
+    const int key_head = first_head / (p.value_heads / p.key_heads);
     const int t0 = chunk * kChunk, last = sequence_length(a.lengths, b, p.length), rows = last - t0;
     const int tid = threadIdx.x, half = __builtin_amdgcn_readfirstlane(tid >> 8);
     // (the tiles of the second half the other way round: those of later positions have more below the diagonal, and wavefronts four apart share a SIMD)
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     const int here = p.length - t0 < kChunk ? p.length - t0 : kChunk;  // rows of the results
     const long long at0 = (long long)b * p.length + t0;
     if (rows <= 0) {
-        for (int i = tid; i < here * p.key_dim; i += kGradThreads) {
+        for (int i = tid; !shape.apart && i < here * p.key_dim; i += kGradThreads) {
             const long long at = ((at0 + i / p.key_dim) * p.key_heads + key_head) * p.key_dim + i % p.key_dim;
             ((T*)a.dq)[at] = (T)0.0f;
             ((T*)a.dk)[at] = (T)0.0f;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         EightFloats s, ds, rows;
         Eight<T> values;                           // V or dO
     } ahead;
-    int fetch_head = key_head * shared, fetch_step = 0;
+    int fetch_head = first_head, fetch_step = 0;
     auto fetch = [&](Ahead& to, int tid) {
         // pieces of eight: four a row and step; S and dS' by all lanes, Z and V by the first half of them, U and dO by the second
         const size_t vc = ((size_t)b * p.value_heads + fetch_head) * shape.chunks + chunk;
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     };
     if (kBeyond) fetch(ahead, threadIdx.x);
     for (int h = 0, item = 0; h < shared; ++h) {
-        const int head = key_head * shared + h;
+        const int head = first_head + h;
         const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks + chunk;
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));              // (see below)
@@ -724,17 +725,42 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     }
     int out_lane = threadIdx.x & 63;
     asm volatile("" : "+v"(out_lane));
+    float* parts = w.parts + (((size_t)b * p.value_heads + first_head) * shape.chunks + chunk) * 2 * kChunk * KD;
 #pragma unroll
     for (int i = 0; i < KH; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int column = tile_row(half * KH + i, out_lane & 15), mine = tile_row(wave, 4 * (out_lane >> 4));
-            if (mine + e < here && column < p.key_dim) {
+            if (shape.apart) {
+                parts[(mine + e) * KD + column] = dq_all[i][e];
+                parts[(kChunk + mine + e) * KD + column] = dk_all[i][e];
+            } else if (mine + e < here && column < p.key_dim) {
                 const long long at = ((at0 + mine + e) * p.key_heads + key_head) * p.key_dim + column;
                 ((T*)a.dq)[at] = (T)(mine + e < rows ? dq_all[i][e] : 0.0f);
                 ((T*)a.dk)[at] = (T)(mine + e < rows ? dk_all[i][e] : 0.0f);
             }
         }
+}
+
+// Where value heads are apart: dq and dk of a position, the sums over the value heads of a key head, in their order.
+template <typename T>
+__global__ __launch_bounds__(kDeltaThreads) void delta_heads_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+{
+    const int shared = p.value_heads / p.key_heads, b = blockIdx.x / p.length, t = blockIdx.x - b * p.length;
+    const bool there = t < sequence_length(a.lengths, b, p.length);
+    for (int i = threadIdx.x; i < p.key_heads * p.key_dim; i += kDeltaThreads) {
+        const int key_head = i / p.key_dim, column = i - key_head * p.key_dim;
+        float dq = 0.0f, dk = 0.0f;
+        for (int h = 0; there && h < shared; ++h) {
+            const size_t vc = ((size_t)b * p.value_heads + key_head * shared + h) * shape.chunks + t / kChunk;
+            const float* from = w.parts + (vc * 2 * kChunk + t % kChunk) * shape.padded + column;
+            dq += from[0];
+            dk += from[kChunk * shape.padded];
+        }
+        const long long at = (long long)blockIdx.x * p.key_heads * p.key_dim + i;
+        ((T*)a.dq)[at] = (T)dq;
+        ((T*)a.dk)[at] = (T)dk;
+    }
 }
 
 // Gradients of delta, beta and, a chunk each, of A and the bias: a wavefront a chunk of a value head, a lane a position.  The logarithm of a decay gets the gradients
@@ -784,23 +810,29 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_gates_kernel(sys_gated_de
     }
 }
 
-// The chunks' sums of a head, a wavefront a head, in 64 bits.
-__global__ __launch_bounds__(64) void delta_rates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+// The chunks' sums of a head, a workgroup a head, in 64 bits.
+__global__ __launch_bounds__(kDeltaThreads) void delta_rates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    const int head = blockIdx.x, lane = threadIdx.x;
+    const int head = blockIdx.x;
+    const long long all = (long long)p.batch * shape.chunks;
     double of_a = 0.0, of_bias = 0.0;
-    for (int b = 0; b < p.batch; ++b)
-        for (int c = lane; c < shape.chunks; c += 64) {
-            const double* from = w.shares + (((size_t)b * p.value_heads + head) * shape.chunks + c) * 2;
-            of_a += from[0];
-            of_bias += from[1];
-        }
+    for (long long i = threadIdx.x; i < all; i += kDeltaThreads) {
+        const long long b = i / shape.chunks;
+        const double* from = w.shares + ((b * p.value_heads + head) * shape.chunks + (i - b * shape.chunks)) * 2;
+        of_a += from[0];
+        of_bias += from[1];
+    }
 #pragma unroll
     for (int m = 32; m; m >>= 1) of_a += __shfl_xor(of_a, m), of_bias += __shfl_xor(of_bias, m);
-    if (lane == 0) {
-        a.da[head] = (float)of_a;
-        if (a.ddelta_bias) a.ddelta_bias[head] = (float)of_bias;
-    }
+    __shared__ double waves[2][kDeltaThreads / 64];
+    if ((threadIdx.x & 63) == 0) waves[0][threadIdx.x >> 6] = of_a, waves[1][threadIdx.x >> 6] = of_bias;
+    __syncthreads();
+    if (threadIdx.x) return;
+    of_a = of_bias = 0.0;
+#pragma unroll
+    for (int i = 0; i < kDeltaThreads / 64; ++i) of_a += waves[0][i], of_bias += waves[1][i];
+    a.da[head] = (float)of_a;
+    if (a.ddelta_bias) a.ddelta_bias[head] = (float)of_bias;
 }
 
 template <typename T, int KD>
@@ -809,7 +841,7 @@ hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape&
     DeltaShape of = shape;
     const bool wide = delta_wide(p);
     of.tiles = shape.columns / (wide ? 32 : 16);
-    const long long sweeps = (long long)of.tiles * p.value_heads * p.batch, chunks = (long long)shape.chunks * p.key_heads * p.batch;
+    const long long sweeps = (long long)of.tiles * p.value_heads * p.batch, chunks = (long long)shape.chunks * (shape.apart ? p.value_heads : p.key_heads) * p.batch;
     if (sweeps > 0x7fffffffLL || chunks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     constexpr int kMost = sizeof(T) == 4 && KD > 64 ? 1 : 2;
     if (wide) hipLaunchKernelGGL((delta_back_kernel<T, KD, kMost>), dim3((unsigned)sweeps), dim3(kSweepThreads), 0, s, p, a, of, w);
@@ -818,6 +850,10 @@ hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape&
     if (e != hipSuccess || !chunks) return e;
     hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kGradThreads), 0, s, p, a, shape, w);
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (shape.apart) {                             // (fewer chunks than CUs, so positions fit a grid)
+        hipLaunchKernelGGL(delta_heads_kernel<T>, dim3((unsigned)((long long)p.batch * p.length)), dim3(kDeltaThreads), 0, s, p, a, shape, w);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const long long all = (long long)shape.chunks * p.value_heads * p.batch, blocks = (all + kDeltaThreads / 64 - 1) / (kDeltaThreads / 64);
     hipLaunchKernelGGL(delta_gates_kernel<T>, dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, shape, w, all);
     return hipGetLastError();
@@ -849,7 +885,7 @@ hipError_t launch_delta_grad(const sys_gated_delta_t& p, const DeltaArgs& a, hip
         }
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(delta_rates_kernel, dim3((unsigned)p.value_heads), dim3(64), 0, s, p, a, shape, w);
+    hipLaunchKernelGGL(delta_rates_kernel, dim3((unsigned)p.value_heads), dim3(kDeltaThreads), 0, s, p, a, shape, w);
     return hipGetLastError();
 }
 

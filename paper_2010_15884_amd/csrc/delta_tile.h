@@ -201,6 +201,7 @@ struct DeltaPlanes {
     bf16_t *x, *p, *xt, *pt, *k, *q, *kt, *qt;
     float *s, *ds, *u, *z;             // [columns / 32][padded][32], [columns / 32][64][32]
     float* scalars;                    // [kScalars][64]
+    float* parts;                      // where heads are apart, their shares of dq and dk: [2][64][padded]
     double *gates, *shares;            // of a chunk of a value head: [kGates][64]; its share of the gradients of A and the bias
 };
 
@@ -210,6 +211,7 @@ struct DeltaShape {
     int columns;                       // the value dimension rounded up to 32
     int tiles;                         // of columns
     int whole, whole_values;           // rows of q and k, of v and dy may be loaded 16 bytes at a time
+    int apart;                         // gradients of a chunk: a workgroup for each of the value heads of a key head
 };
 
 // e^G, e^(G_end - G), b; for gradients the step size and its derivative by delta, and G in 64 bits, to base 2

@@ -137,6 +137,16 @@ def test_states_that_are_not_finite_stay_in_their_column():
     assert not torch.isfinite(y[1, 1:, 0, 20]).any() and torch.equal(state[1, 0][:, others], clean_state[1, 0][:, others])
 
 
+@pytest.mark.parametrize("dtype,key_dim", [(F32, 64), (F16, 40), (BF16, 128)])
+def test_many_sequences(dtype, key_dim):
+    """More chunks of key heads than CUs: a workgroup goes through the value heads that share keys, instead of one of them."""
+    lengths = [(0, 1, 2, 3)[b % 4] for b in range(150)]
+    lengths[7], lengths[31], lengths[149] = 70, 64, 65
+    c = _make(79, 150, 70, 2, 6, key_dim, 16, dtype, state=True, lengths=lengths)
+    _check_forward(c)
+    _check_gradients(c)
+
+
 @pytest.mark.parametrize("length", [9, 100])
 def test_rows_behind_a_sequence_are_zero_whatever_the_state_is(length):
     c = _make(78, 3, length, 1, 2, 64, 48, BF16, state=True, lengths=[length - 4, 0, 5])
