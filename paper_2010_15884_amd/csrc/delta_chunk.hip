@@ -637,8 +637,10 @@ hipError_t launch(bool is_sweep, const sys_gated_delta_t& p, const DeltaArgs& a,
     }
 }
 
-// Sequences of up to this many positions go a position at a time.
-constexpr int kShort = 16;
+// Whether sequences are so short that they go a position at a time.  12 positions take 17 us so and 14 in chunks where one sequence has 32 heads of 128 x 128 in bf16
+// (8: 12 and 14), 14 and 15 with four of 8 heads of 64 x 128 in fp16; where there are more heads than CUs the chunks' matrices take longer: 16 positions of 16 sequences of
+// 32 heads 43 and 49 (24: 59 and 49), of 64 sequences 128 and 168 (24: 187 and 173), of 32 sequences of 8 heads of 64 x 64 in fp32 18 and 26 (24: 25 and 26).
+bool delta_short(const sys_gated_delta_t& p) { return p.length <= ((long long)p.batch * p.value_heads >= kCus ? 20 : 12); }
 
 }  // namespace
 
@@ -715,12 +717,12 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
 
 size_t delta_workspace(const sys_gated_delta_t& p)
 {
-    return p.length > kShort && p.batch ? delta_planes(p, delta_shape(p), false, nullptr, nullptr) : 0;
+    return !delta_short(p) && p.batch ? delta_planes(p, delta_shape(p), false, nullptr, nullptr) : 0;
 }
 
 hipError_t launch_delta(const sys_gated_delta_t& p, const DeltaArgs& a, hipStream_t s)
 {
-    if (p.length <= kShort) return launch_delta_positions(p, a, s);
+    if (delta_short(p)) return launch_delta_positions(p, a, s);
     const DeltaShape shape = delta_shape(p, &a);
     DeltaPlanes w;
     delta_planes(p, shape, false, a.workspace, &w);

@@ -147,6 +147,11 @@ def test_many_sequences(dtype, key_dim):
     _check_gradients(c)
 
 
+@pytest.mark.parametrize("batch,length", [(1, 12), (1, 13), (64, 20), (64, 21)])
+def test_lengths_between_the_routes(batch, length):
+    _check_forward(_make(80 + length, batch, length, 2, 4, 40, 24, BF16, state=True))
+
+
 @pytest.mark.parametrize("length", [9, 100])
 def test_rows_behind_a_sequence_are_zero_whatever_the_state_is(length):
     c = _make(78, 3, length, 1, 2, 64, 48, BF16, state=True, lengths=[length - 4, 0, 5])
