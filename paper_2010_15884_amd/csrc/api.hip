@@ -302,6 +302,6 @@ const char* sys_projection_name(int projection)
 
 int sys_last_hip_error(void) { return g_last_hip_error; }
 
-int sys_version(void) { return 200; }
+int sys_version(void) { return 300; }
 
 }  // extern "C"

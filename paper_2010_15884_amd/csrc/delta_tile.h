@@ -116,7 +116,7 @@ __device__ __forceinline__ constexpr int row_in_tile(int row) { return 4 * (row 
 
 // Matrices lie in the workspace as the operands that are taken of them: 1 KB a tile of rows and step of 32 columns, where lane l has the eight entries from
 // column 8 (l / 16) on of row l % 16 of the tile.  (Row-major, a load's neighbouring lanes would be in rows of their own: 45 cache accesses an
-// instruction instead of 16, and the addresses' unit was what the sweep waited for: 163 us against 110 for 4096 positions of 32 heads of 128 x 128.)
+// instruction instead of 16, and the addresses' unit was what the sweep waited for: it took half again as long for 4096 positions of 32 heads of 128 x 128.)
 __device__ __forceinline__ b8 operand(const bf16_t* matrix, int steps, int tile, int step, int lane)
 {
     return *(const b8*)(matrix + ((tile * steps + step) * 64 + lane) * 8);

@@ -5,7 +5,8 @@
 // that are turned with each other (or a first and a second half of what is not turned), so that no entry is needed in another lane; a wavefront runs `heads` heads
 // of one token side by side and walks through the rest of them with the next ones' loads in flight: the tables' rows and the weights are
 // loaded once a token.
-// Bound by memory: 16-bit entries cost 4 bytes in the forward pass and some five vector instructions.
+// Bound by memory: 16-bit entries cost 4 bytes in the forward pass and some five vector instructions.  8192 tokens of 36 heads of 128 in bf16 take 32 us (4.9 TB/s, a
+// copy's rate), the gradients of 18 heads of 256 51 us (4.5 TB/s; eight wavefronts a CU hold what is in flight), 32 tokens of 40 heads 4 us, a launch.
 #include "launch.h"
 #include "sequence.h"
 
