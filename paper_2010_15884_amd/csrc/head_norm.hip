@@ -6,7 +6,8 @@
 // of one token side by side and walks through the rest of them with the next ones' loads in flight: the tables' rows and the weights are
 // loaded once a token.
 // Bound by memory: 16-bit entries cost 4 bytes in the forward pass and some five vector instructions.  8192 tokens of 36 heads of 128 in bf16 take 32 us (4.9 TB/s, a
-// copy's rate), the gradients of 18 heads of 256 51 us (4.5 TB/s; eight wavefronts a CU hold what is in flight), 32 tokens of 40 heads 4 us, a launch.
+// copy's rate), the gradients of 18 heads of 256 58 us and 4 for the join of the weights' sums (3.9 TB/s; eight wavefronts a CU, which wait for 59 % of their time and keep the vector
+// units busy for half of it), 32 tokens of 40 heads 4 us, a launch.
 #include "launch.h"
 #include "sequence.h"
 
@@ -294,10 +295,12 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
                         if (slots.turns(i)) angles.turn(p.interleaved, i, -1.0f, z[0][i], z[1][i]);
 #pragma unroll
                         for (int j = 0; j < V; ++j) {
-                            x[0][i][j] = slots.is(i) ? x[0][i][j] : 0.0f;
-                            x[1][i][j] = slots.has_second(i) ? x[1][i][j] : 0.0f;
-                            z[0][i][j] = slots.is(i) ? z[0][i][j] : 0.0f;
-                            z[1][i][j] = slots.has_second(i) ? z[1][i][j] : 0.0f;
+                            if (S > 1 || V == 1) {
+                                x[0][i][j] = slots.is(i) ? x[0][i][j] : 0.0f;
+                                x[1][i][j] = slots.has_second(i) ? x[1][i][j] : 0.0f;
+                                z[0][i][j] = slots.is(i) ? z[0][i][j] : 0.0f;
+                                z[1][i][j] = slots.has_second(i) ? z[1][i][j] : 0.0f;
+                            }
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 sum = __builtin_fmaf(x[h][i][j], x[h][i][j], sum);
@@ -307,6 +310,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_grad_kernel(sys_head_norm_
                     }
                 }
                 fetch(head + at.step);
+                if (S == 1 && V > 1 && !slots.is(0)) sum = dot = 0.0f;  // (a lane without entries has another's, whose products nobody takes)
                 sum = lanes_sum(sum, n.parts_log);
                 dot = lanes_sum(dot, n.parts_log);
                 const float r = 1.0f / __builtin_sqrtf(__builtin_fmaf(sum, share, p.eps));
