@@ -477,7 +477,7 @@ typedef struct {
  *   d_cos, d_sin  [positions, rotary/2] fp32 (where rotary > 0): pair i at position p turns by the angle of row p, column i
  *   d_positions (optional)  [batch, length]: the table's row of each token; one outside 0 .. positions-1 marks a token that is not
  *            there: its rows are 0, and so are its gradients.  Without it position t is row t (length <= positions: SYS_ERR_SIZE).
- *   Rows behind a sequence's length are 0.
+ *   Rows behind a sequence's length are 0.  Squares are summed in fp32: a head with entries beyond 10^18 comes out as 0.
  */
 int sys_head_norm(const sys_head_norm_t *p, const void *d_q, const void *d_k, const void *d_wq, const void *d_wk,
                   const float *d_cos, const float *d_sin, const int *d_positions, const int *d_lengths,
