@@ -751,9 +751,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
 
 // Where value heads are apart: dq and dk of a position, the sums over the value heads of a key head, in their order.
 template <typename T>
-__global__ __launch_bounds__(kDeltaThreads) void delta_heads_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
+__device__ __forceinline__ void sum_heads(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape& shape, const DeltaPlanes& w, int position)
 {
-    const int shared = p.value_heads / p.key_heads, b = blockIdx.x / p.length, t = blockIdx.x - b * p.length;
+    const int shared = p.value_heads / p.key_heads, b = position / p.length, t = position - b * p.length;
     const bool there = t < sequence_length(a.lengths, b, p.length);
     for (int i = threadIdx.x; i < p.key_heads * p.key_dim; i += kDeltaThreads) {
         const int key_head = i / p.key_dim, column = i - key_head * p.key_dim;
@@ -764,7 +764,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_heads_kernel(sys_gated_de
             dq += from[0];
             dk += from[kChunk * shape.padded];
         }
-        const long long at = (long long)blockIdx.x * p.key_heads * p.key_dim + i;
+        const long long at = (long long)position * p.key_heads * p.key_dim + i;
         ((T*)a.dq)[at] = (T)dq;
         ((T*)a.dk)[at] = (T)dk;
     }
@@ -773,8 +773,12 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_heads_kernel(sys_gated_de
 // Gradients of delta, beta and, a chunk each, of A and the bias: a wavefront a chunk of a value head, a lane a position.  The logarithm of a decay gets the gradients
 // of the sums G that end in its position and behind it, what is left behind the positions before it, and what the whole chunk shares, in 64 bits.
 template <typename T>
-__global__ __launch_bounds__(kDeltaThreads) void delta_gates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w, long long all)
+__global__ __launch_bounds__(kDeltaThreads) void delta_gates_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w, long long all, int blocks)
 {
+    if ((int)blockIdx.x >= blocks) {               // (in the same launch: a workgroup a position)
+        sum_heads<T>(p, a, shape, w, blockIdx.x - blocks);
+        return;
+    }
     const long long vc = (long long)blockIdx.x * (kDeltaThreads / 64) + (threadIdx.x >> 6);
     if (vc >= all) return;
     const int lane = threadIdx.x & 63, chunk = (int)(vc % shape.chunks), head = (int)(vc / shape.chunks % p.value_heads), b = (int)(vc / shape.chunks / p.value_heads);
@@ -857,12 +861,9 @@ hipError_t run(const sys_gated_delta_t& p, const DeltaArgs& a, const DeltaShape&
     if (e != hipSuccess || !chunks) return e;
     hipLaunchKernelGGL((delta_grad_kernel<T, KD>), dim3((unsigned)chunks), dim3(kGradThreads), 0, s, p, a, shape, w);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (shape.apart) {                             // (fewer chunks than CUs, so positions fit a grid)
-        hipLaunchKernelGGL(delta_heads_kernel<T>, dim3((unsigned)((long long)p.batch * p.length)), dim3(kDeltaThreads), 0, s, p, a, shape, w);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
     const long long all = (long long)shape.chunks * p.value_heads * p.batch, blocks = (all + kDeltaThreads / 64 - 1) / (kDeltaThreads / 64);
-    hipLaunchKernelGGL(delta_gates_kernel<T>, dim3((unsigned)blocks), dim3(kDeltaThreads), 0, s, p, a, shape, w, all);
+    const long long positions = shape.apart ? (long long)p.batch * p.length : 0;   // (of fewer chunks than CUs)
+    hipLaunchKernelGGL(delta_gates_kernel<T>, dim3((unsigned)(blocks + positions)), dim3(kDeltaThreads), 0, s, p, a, shape, w, all, (int)blocks);
     return hipGetLastError();
 }
 
