@@ -47,8 +47,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     // what the first wavefront makes the decays of, K into LDS, and the rows of Q that this wavefront works on, as operands have them
     constexpr int kPieces = kChunk * KD / 8 / kDeltaThreads;
     b8 qa[KS][NX];
+    float raw_delta = 0.0f, raw_beta = 0.0f, bias = 0.0f, rate = 0.0f;
     {
-        float raw_delta = 0.0f, raw_beta = 0.0f, bias = 0.0f, rate = 0.0f;
         if (wave == 0 && lane < rows) {
             raw_delta = (float)((const T*)a.delta)[b * p.delta_batch + (t0 + lane) * p.delta_row + head];
             raw_beta = (float)((const T*)a.beta)[b * p.beta_batch + (t0 + lane) * p.beta_row + head];
@@ -70,44 +70,6 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
             if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.offset(row, at) : kNowhere);
             else from_q[s].load_each(q_buffer, q_rows.offset(row, at), p.key_dim - at);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (wave == 0) {
-            // in 64 bits: what a step size is off by adds up over all positions that a state lives through, and a ratio of decays is the exponential of a small
-            // difference of what may be large sums (with the step sizes of sequence.h, off by up to 8 2^-24, the gradients of A were off by 2e-6 of themselves
-            // after 2048 positions, now 5e-7)
-            double step = 0.0, strength = 0.0, slope = 0.0;
-            if (lane < rows) {
-                step = (double)raw_delta + (double)bias;
-                strength = (double)raw_beta;
-                slope = 1.0;
-                if (p.softplus) {
-                    const double small = exp(-fabs(step)), large = step < 0.0 ? small : 1.0;
-                    slope = large / (1.0 + small);
-                    step = (step < 0.0 ? 0.0 : step) + log1p(small);       // (a NaN comes back with `small`)
-                }
-                if (p.sigmoid) strength = 1.0 / (1.0 + exp(-strength));
-            }
-            // a decay of 2^-10000 is 0 as any smaller one, and leaves the differences behind it their digits (NaN passes)
-            double sum = step * (double)rate * 1.4426950408889634;
-            sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
-    #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const double other = __shfl_up(sum, m);
-                if (lane >= m) sum += other;
-            }
-            const double end = __shfl(sum, 63);
-            sums[lane] = sum;
-            strengths[lane] = (float)strength;
-            float* out = w.scalars + vc * kScalars * kChunk;
-            out[kGamma * kChunk + lane] = fast_exp2((float)sum);
-            out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
-            out[kStrength * kChunk + lane] = (float)strength;
-            if (GRAD) {
-                out[kStep * kChunk + lane] = (float)step;
-                out[kSlope * kChunk + lane] = (float)slope;
-                ((double*)(out + kSums * kChunk))[lane] = sum;
-            }
-        }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int row = (tid + i * kDeltaThreads) / (KD / 8), at = (tid + i * kDeltaThreads) % (KD / 8) * 8;
@@ -125,7 +87,45 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
             }
         }
     }
-    __syncthreads();
+    lds_barrier();
+    // (beside the other wavefronts' products, of which the first has the fewest)
+    if (wave == 0) {
+        // in 64 bits: what a step size is off by adds up over all positions that a state lives through, and a ratio of decays is the exponential of a small
+        // difference of what may be large sums (with the step sizes of sequence.h, off by up to 8 2^-24, the gradients of A were off by 2e-6 of themselves
+        // after 2048 positions, now 5e-7)
+        double step = 0.0, strength = 0.0, slope = 0.0;
+        if (lane < rows) {
+            step = (double)raw_delta + (double)bias;
+            strength = (double)raw_beta;
+            slope = 1.0;
+            if (p.softplus) {
+                const double small = exp(-fabs(step)), large = step < 0.0 ? small : 1.0;
+                slope = large / (1.0 + small);
+                step = (step < 0.0 ? 0.0 : step) + log1p(small);       // (a NaN comes back with `small`)
+            }
+            if (p.sigmoid) strength = 1.0 / (1.0 + exp(-strength));
+        }
+        // a decay of 2^-10000 is 0 as any smaller one, and leaves the differences behind it their digits (NaN passes)
+        double sum = step * (double)rate * 1.4426950408889634;
+        sum = sum < -10000.0 ? -10000.0 : sum > 10000.0 ? 10000.0 : sum;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const double other = __shfl_up(sum, m);
+            if (lane >= m) sum += other;
+        }
+        const double end = __shfl(sum, 63);
+        sums[lane] = sum;
+        strengths[lane] = (float)strength;
+        float* out = w.scalars + vc * kScalars * kChunk;
+        out[kGamma * kChunk + lane] = fast_exp2((float)sum);
+        out[kLeft * kChunk + lane] = fast_exp2((float)(end - sum));
+        out[kStrength * kChunk + lane] = (float)strength;
+        if (GRAD) {
+            out[kStep * kChunk + lane] = (float)step;
+            out[kSlope * kChunk + lane] = (float)slope;
+            ((double*)(out + kSums * kChunk))[lane] = sum;
+        }
+    }
 
     // A plane's pieces from LDS: K^T (Q^T), eight positions of a column; a square, or its transpose, without the quarter above (below) the diagonal
     auto transposed = [&](bf16_t* to) {
@@ -155,33 +155,48 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         }
     };
 
-    // A from K K^T: rows of this wavefront (as they lie), columns up to its own
-    b8 ka[KS][NX];
+    // K K^T, rows of this wavefront (as they lie), columns up to its own; and K Q^T, whose columns are the wavefront's queries (for gradients Q K^T, whose rows are)
+    f4 kk[4] = {}, qk[4] = {};
+    {
+        b8 ka[KS][NX];
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int n = 0; n < NX; ++n) ka[s][n] = *(const b8*)&keys[n][16 * wave + r][32 * s + 8 * g];
+            for (int n = 0; n < NX; ++n) ka[s][n] = *(const b8*)&keys[n][16 * wave + r][32 * s + 8 * g];
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (n <= (wave | 1)) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    b8 kb[NX];
+                    if (n <= wave) {
+#pragma unroll
+                        for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][16 * n + r][32 * s + 8 * g];
+                        kk[n] = multiply<2>(ka[s], kb, kk[n]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][tile_row(n, r)][32 * s + 8 * g];
+                    qk[n] = GRAD ? multiply<2>(qa[s], kb, qk[n]) : multiply<2>(kb, qa[s], qk[n]);
+                }
+            }
+    }
+    lds_barrier();
+    // A
     double row_sum[4];
     float row_strength[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) row_sum[e] = sums[16 * wave + 4 * g + e], row_strength[e] = strengths[16 * wave + 4 * g + e];
-    for (int n = 0; n <= wave; ++n) {
-        f4 kk = {};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            b8 kb[NX];
+    for (int n = 0; n < 4; ++n)
+        if (n <= wave) {
+            const int column = 16 * n + r;
+            const double column_sum = sums[column];
 #pragma unroll
-            for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][16 * n + r][32 * s + 8 * g];
-            kk = multiply<2>(ka[s], kb, kk);
+            for (int e = 0; e < 4; ++e) {
+                const int row = 16 * wave + 4 * g + e;
+                am[row][column] = column < row ? row_strength[e] * (fast_exp2((float)(row_sum[e] - column_sum)) * kk[n][e]) : 0.0f;
+            }
         }
-        const int column = 16 * n + r;
-        const double column_sum = sums[column];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = 16 * wave + 4 * g + e;
-            am[row][column] = column < row ? row_strength[e] * (fast_exp2((float)(row_sum[e] - column_sum)) * kk[e]) : 0.0f;
-        }
-    }
     // P, without the quarter above the diagonal, in the order of its operands as the products leave it: K Q^T, whose columns are queries, gives a lane eight keys of a
     // row of P in two tiles; for gradients Q K^T gives it four queries of a row of P^T, half an operand
     if constexpr (GRAD) {
@@ -189,20 +204,14 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
         double query_sum[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) query_sum[e] = sums[query + e];
-        for (int n = 0; n <= (wave | 1); ++n) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if (n > (wave | 1)) break;
             const int key = tile_row(n, r);
-            f4 qk = {};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                b8 kb[NX];
-#pragma unroll
-                for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][key][32 * s + 8 * g];
-                qk = multiply<2>(qa[s], kb, qk);
-            }
             const double key_sum = sums[key];
             f4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = key <= query + e ? p.scale * (fast_exp2((float)(query_sum[e] - key_sum)) * qk[e]) : 0.0f;
+            for (int e = 0; e < 4; ++e) v[e] = key <= query + e ? p.scale * (fast_exp2((float)(query_sum[e] - key_sum)) * qk[n][e]) : 0.0f;
             u2 parts[3];
             split4(v, parts);
 #pragma unroll
@@ -211,22 +220,16 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     } else {
         const int query = tile_row(wave, r);
         const double query_sum = sums[query];
-        for (int step = 0; step <= wave >> 1; ++step) {
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            if (step > wave >> 1) break;
             float v[8];
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                f4 qk = {};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    b8 kb[NX];
-#pragma unroll
-                    for (int m = 0; m < NX; ++m) kb[m] = *(const b8*)&keys[m][tile_row(2 * step + n, r)][32 * s + 8 * g];
-                    qk = multiply<2>(kb, qa[s], qk);
-                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = 32 * step + 8 * g + 4 * n + e;
-                    v[4 * n + e] = key <= query ? p.scale * (fast_exp2((float)(query_sum - sums[key])) * qk[e]) : 0.0f;
+                    v[4 * n + e] = key <= query ? p.scale * (fast_exp2((float)(query_sum - sums[key])) * qk[2 * step + n][e]) : 0.0f;
                 }
             }
             b8 parts[RP];
@@ -245,12 +248,12 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     }
     if (GRAD && first) {
         // Q^T the same way as K^T, through its place
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int n = 0; n < NX; ++n) *(b8*)&keys[n][tile_row(wave, r)][32 * s + 8 * g] = qa[s][n];
-        __syncthreads();
+        lds_barrier();
         transposed(w.qt);
     }
 
@@ -262,12 +265,12 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 #pragma unroll
         for (int j = 0; j < i; ++j) x[i] = __builtin_fmaf(-am[16 * wave + i][16 * wave + j], x[j], x[i]);
     }
-    __syncthreads();                               // (all are done with the keys)
+    lds_barrier();                               // (all are done with the keys)
     if (g == 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) xm[16 * wave + i][16 * wave + r] = x[i];
     }
-    __syncthreads();
+    lds_barrier();
     // ... and those below, X_ij = -X_ii (sum_k A_ik X_kj), a column of blocks a wavefront, in fp32
     f4 column[4];
 #pragma unroll
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
     for (int i = 0; i < wave; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) xm[16 * i + 4 * g + e][16 * wave + r] = 0.0f;
-    __syncthreads();
+    lds_barrier();
     square(w.x + vc * 3 * kSquare, false);
     if (GRAD) square(w.xt + vc * 3 * kSquare, true);
 }
