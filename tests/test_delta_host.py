@@ -182,6 +182,46 @@ def test_binding_refuses_before_the_library_is_looked_for(monkeypatch):
             call()
 
 
+@pytest.mark.gpu
+def test_binding_refuses_shapes_types_and_strides():
+    zeros = lambda *s, **how: torch.zeros(s, device="cuda", **how)  # noqa: E731
+    q, k, w, table = zeros(2, 5, 4, 8), zeros(2, 5, 2, 8), zeros(8), zeros(9, 4)
+    positions, lengths = zeros(2, 5, dtype=torch.int32), zeros(2, dtype=torch.int32)
+    ok = dict(d_q=q, d_k=k, d_wq=w, d_wk=w, d_cos=table, d_sin=table, d_positions=positions, d_lengths=lengths)
+    B.sys_head_norm(**ok)
+    for error, change in ((ValueError, dict(d_q=q[0])), (ValueError, dict(d_q=q.transpose(1, 2).contiguous().transpose(1, 2))), (ValueError, dict(d_k=k[:1])),
+                          (TypeError, dict(d_k=k.half())), (ValueError, dict(d_k=zeros(2, 5, 2, 6))), (ValueError, dict(d_wq=w[:7])), (TypeError, dict(d_wq=w.half())),
+                          (ValueError, dict(d_sin=None)), (ValueError, dict(d_sin=table[:8])), (TypeError, dict(d_cos=table.half())), (ValueError, dict(d_cos=None, d_sin=None)),
+                          (ValueError, dict(d_positions=positions[:1])), (TypeError, dict(d_positions=positions.long())), (TypeError, dict(d_lengths=lengths.float())),
+                          (ValueError, dict(d_yq=k)), (KeyError, dict(norm="MAX")), (B.SysconvError, dict(eps=-1.0)), (B.SysconvError, dict(d_yq=q)),
+                          (ValueError, dict(d_k=None)), (TypeError, dict(d_q=q.cpu())), (ValueError, dict(d_q=zeros(2, 5, 4, 16)[..., ::2])),
+                          (B.SysconvError, dict(d_positions=None, d_cos=table[:4].contiguous(), d_sin=table[:4].contiguous()))):
+        with pytest.raises(error):
+            B.sys_head_norm(**dict(ok, **change))
+    with pytest.raises(TypeError):
+        B.sys_head_norm_backward(q, None, **ok)
+    v, gates, A, state = zeros(2, 5, 4, 6), zeros(2, 5, 4), zeros(4), zeros(2, 4, 8, 6)
+    ok = dict(d_q=k, d_k=k, d_v=v, d_delta=gates, d_A=A, d_beta=gates, d_delta_bias=A, d_state=state, d_lengths=lengths)
+    B.sys_gated_delta_rule(**ok)
+    wrong = ((ValueError, dict(d_q=k[0])), (ValueError, dict(d_k=q)), (ValueError, dict(d_v=v[:, :4])), (TypeError, dict(d_v=v.half())), (ValueError, dict(d_delta=gates[..., :3])),
+             (TypeError, dict(d_beta=gates.half())), (TypeError, dict(d_A=A.half())), (ValueError, dict(d_A=A[:3])), (TypeError, dict(d_A=None)),
+             (ValueError, dict(d_delta_bias=A[:3])), (ValueError, dict(d_state=state[:1])), (TypeError, dict(d_state=state.half())), (ValueError, dict(d_lengths=lengths[:1])),
+             (B.SysconvError, dict(d_q=zeros(2, 5, 3, 8), d_k=zeros(2, 5, 3, 8))), (B.SysconvError, dict(d_q=zeros(2, 5, 2, 129), d_k=zeros(2, 5, 2, 129), d_state=None)))
+    for error, change in (*wrong, (ValueError, dict(d_y=v[:1])), (B.SysconvError, dict(d_y=v)), (ValueError, dict(d_state_out=state[:1])), (B.SysconvError, dict(d_state_out=state))):
+        with pytest.raises(error):
+            B.sys_gated_delta_rule(**dict(ok, **change))
+    for error, change in (*wrong, (TypeError, dict(d_dy=v.half())), (ValueError, dict(d_dy=v[:1])), (ValueError, dict(d_dstate_out=state[:1]))):
+        with pytest.raises(error):
+            B.sys_gated_delta_rule_backward(**{**ok, "d_dy": v, **change})
+    ok = dict(d_q=k[:, 0], d_k=k[:, 0], d_v=v[:, 0], d_delta=gates[:, 0], d_A=A, d_beta=gates[:, 0], d_state=state, d_slots=lengths)
+    B.sys_gated_delta_rule_update(**ok)
+    for error, change in ((ValueError, dict(d_q=k)), (ValueError, dict(d_state=state[:, :2])), (TypeError, dict(d_state=state.half())), (TypeError, dict(d_slots=lengths.long())),
+                          (ValueError, dict(d_slots=lengths[:1])), (B.SysconvError, dict(d_slots=None, d_state=state[:1])), (ValueError, dict(d_state_out=state[:1])),
+                          (ValueError, dict(d_y=v)), (B.SysconvError, dict(d_y=v[:, 0]))):
+        with pytest.raises(error):
+            B.sys_gated_delta_rule_update(**dict(ok, **change))
+
+
 # ---------------------------------------------------------------- the references themselves
 
 def _slope(loss, point, key, v, e=1e-5):
