@@ -14,6 +14,9 @@ constexpr unsigned kNowhere = 0xffffff00u;  // offset of a buffer store that is 
 __device__ __forceinline__ void lds_barrier()
 {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    // lgkmcnt(0): the wait that the fence stands for is dropped by the compiler where a loop begins with the barrier and nothing is outstanding when it is entered, also
+    // if its last writes are on the way back
+    __builtin_amdgcn_s_waitcnt(0xc07f);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
