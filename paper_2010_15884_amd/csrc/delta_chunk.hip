@@ -61,14 +61,14 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int row = (tid + i * kDeltaThreads) / (KD / 8), at = (tid + i * kDeltaThreads) % (KD / 8) * 8;
-            if (shape.whole) from_k[i].load(k_buffer, at < p.key_dim ? k_rows.offset(row, at) : kNowhere);
-            else from_k[i].load_each(k_buffer, k_rows.offset(row, at), p.key_dim - at);
+            if (shape.whole) from_k[i].load(k_buffer, at < p.key_dim ? k_rows.place(row, at) : kNowhere);
+            else from_k[i].load_each(k_buffer, k_rows.offset(row, at), row < rows ? p.key_dim - at : 0);
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const int row = tile_row(wave, r), at = 32 * s + 8 * g;
-            if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.offset(row, at) : kNowhere);
-            else from_q[s].load_each(q_buffer, q_rows.offset(row, at), p.key_dim - at);
+            if (shape.whole) from_q[s].load(q_buffer, at < p.key_dim ? q_rows.place(row, at) : kNowhere);
+            else from_q[s].load_each(q_buffer, q_rows.offset(row, at), row < rows ? p.key_dim - at : 0);
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -373,6 +373,12 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         };
         auto fetch_values = [&](int c) {
             const __amdgpu_buffer_rsrc_t rows = v.buffer();
+            if (v.exist < kChunk) {                // (the last chunk: what does not exist there does not behind it)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v_at[n][e] = my_row + e < v.exist ? v_at[n][e] : kNowhere;
+            }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll

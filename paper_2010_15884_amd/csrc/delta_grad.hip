@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) next_dy[n][e] = buffer_load<T>(rows, dy_at[n][e]);
+                for (int e = 0; e < 4; ++e) next_dy[n][e] = buffer_load<T>(rows, my_row + e < dy.exist ? dy_at[n][e] : kNowhere);
             const float* from = w.scalars + (vc + c) * kScalars * kChunk;
             next_gamma = *(const f4*)(from + kGamma * kChunk + my_row);
             next_strength = *(const f4*)(from + kStrength * kChunk + my_row);
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         to.rows.load(plane(half ? w.u : w.z, kChunk), (row * 32 + at) * 4u, fetch_step * kChunk * 128);
         const T* base = half ? (const T*)a.dy + b * p.y_batch : (const T*)a.v + b * p.v_batch;
         const ChunkRows<T> values(base + fetch_head * p.value_dim, half ? p.y_row : p.v_row, p.value_dim, chunk, last);
-        const int left = p.value_dim - 32 * fetch_step - at;
+        const int left = row < rows ? p.value_dim - 32 * fetch_step - at : 0;
         const unsigned offset = values.offset(row, 32 * fetch_step + at);
         if (shape.whole_values) to.values.load(values.buffer(), left > 0 ? offset : kNowhere);
         else to.values.load_each(values.buffer(), offset, left);

@@ -228,18 +228,26 @@ inline int delta_chunks(const sys_gated_delta_t& p) { return (p.length + kChunk 
 
 __device__ __forceinline__ bf16_t as_bf16(unsigned bits) { return __builtin_bit_cast(bf16_t, (unsigned short)bits); }
 
-// Entries of neighbouring positions of a chunk, one column a lane, addressed as a buffer that ends with the last row that exists (zeros behind it).
+// Entries of neighbouring positions of a chunk, one column a lane, addressed as a buffer that ends with the last row that exists.  Rows behind it lie past that end
+// only where rows are no less apart than they are long: inputs may use a row again, or one row's end as another's beginning, and where there is one row the
+// distance to the next may be anything.  So what is read goes by the row's number.
 template <typename T>
 struct ChunkRows {
     T* at;                             // row 0 of the present chunk
     long long left, row;               // bytes to the end of the last row
+    int exist;                         // rows from the present chunk's first one on
     __device__ __forceinline__ ChunkRows(const void* base, long long row_stride, int columns, int chunk, int end)
-        : at((T*)base + chunk * kChunk * row_stride), left(bytes_left(chunk * kChunk, end, row_stride, columns, sizeof(T))), row(row_stride)
+        : at((T*)base + chunk * kChunk * row_stride), left(bytes_left(chunk * kChunk, end, row_stride, columns, sizeof(T))), row(row_stride), exist(end - chunk * kChunk)
     {
     }
-    __device__ __forceinline__ void move(int chunks) { at += chunks * kChunk * row, left -= chunks * kChunk * row * (long long)sizeof(T); }
+    __device__ __forceinline__ void move(int chunks)
+    {
+        at += chunks * kChunk * row, left -= chunks * kChunk * row * (long long)sizeof(T), exist -= chunks * kChunk;
+    }
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, buffer_size(left), 0x00027000); }
     __device__ __forceinline__ unsigned offset(int r, int column) const { return (unsigned)((r * row + column) * (long long)sizeof(T)); }
+    // of an entry that is read: nowhere, which gives 0, if its row does not exist
+    __device__ __forceinline__ unsigned place(int r, int column) const { return r < exist ? offset(r, column) : kNowhere; }
 };
 
 // Eight neighbouring entries of a row on their way into parts.
@@ -251,7 +259,7 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rows, offset, 16 * i, 0));
     }
-    // one by one; those behind the `left` that belong to the row are dropped when they are there (they lie in the buffer or past its end)
+    // one by one; those behind the `left` that belong to the row (none of a row that does not exist) are dropped when they are there (they lie in the buffer or past its end)
     __device__ __forceinline__ void load_each(__amdgpu_buffer_rsrc_t rows, unsigned offset, int left)
     {
         constexpr int kEach = 4 / (int)sizeof(T);
