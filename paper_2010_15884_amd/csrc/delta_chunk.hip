@@ -23,7 +23,7 @@ namespace {
 template <typename T, int KD, bool GRAD>
 __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    constexpr int NX = kInputParts<T>, KS = KD / 32, RP = kResultParts<T>, kPitch = KD + 8, kSide = kChunk + 4;
+    constexpr int NX = kInputParts<T>, KS = KD / 32, kPitch = KD + 8, kSide = kChunk + 4;
     const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, head = rest % p.value_heads, b = rest / p.value_heads;
     const int shared = p.value_heads / p.key_heads, key_head = head / shared;
     const bool first = head % shared == 0;         // of the value heads of a key head: it writes what they have in common
@@ -232,10 +232,10 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
                     v[4 * n + e] = key <= query ? p.scale * (fast_exp2((float)(query_sum - sums[key])) * qk[2 * step + n][e]) : 0.0f;
                 }
             }
-            b8 parts[RP];
+            b8 parts[3];
             split8(v, parts);
 #pragma unroll
-            for (int m = 0; m < RP; ++m) *(b8*)(w.p + (vc * RP + m) * kSquare + ((2 * wave + step) * 64 + lane) * 8) = parts[m];
+            for (int m = 0; m < 3; ++m) *(b8*)(w.p + (vc * 3 + m) * kSquare + ((2 * wave + step) * 64 + lane) * 8) = parts[m];
         }
     }
     if (first) {
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_matrices_kernel(sys_gated
 template <typename T, int KD, int NT, bool GRAD>
 __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void delta_sweep_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64, RP = kResultParts<T>;
+    constexpr int NX = kInputParts<T>, KS = KD / 32, TW = KD / 64;
     constexpr bool kAtOnce = NX * NT <= 2;         // there are registers for all operands of a product
     const unsigned place = xcd_place(blockIdx.x, gridDim.x);
     const int tile = place % shape.tiles, rest = place / shape.tiles, head = rest % p.value_heads, b = rest / p.value_heads;
@@ -327,8 +327,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
     for (int n = 0; n < NT; ++n) column[n] = (tile * NT + n) * 16 + r, there[n] = column[n] < p.value_dim;
 
     __shared__ Operands<KS, 3, NT> states;
-    __shared__ Operands<2, 3, NT> misses, writes;
-    __shared__ Operands<2, GRAD ? 3 : RP, NT> values;
+    __shared__ Operands<2, 3, NT> misses, writes, values;
 
     const size_t vc = ((size_t)b * p.value_heads + head) * shape.chunks, kc = ((size_t)b * p.key_heads + key_head) * shape.chunks;
     // (loads come back in their order: they are made in the order of their use, a chunk ahead, each kind when the one before it has been used up)
@@ -535,7 +534,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) y_at[n][e] = there[n] ? y.offset(my_row + e, column[n]) : kNowhere;
-        b8 qa[KS][NX], pa[2][RP];
+        b8 qa[KS][NX], pa[2][3];
         f4 next_gamma;
         auto fetch_queries = [&](int c) {
 #pragma unroll
@@ -549,7 +548,7 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
             for (int i = 0; i < 2; ++i)
                 if (i < steps) {
 #pragma unroll
-                    for (int n = 0; n < RP; ++n) pa[i][n] = operand(w.p + ((vc + c) * RP + n) * kSquare, 2, wave, i, lane);
+                    for (int n = 0; n < 3; ++n) pa[i][n] = operand(w.p + ((vc + c) * 3 + n) * kSquare, 2, wave, i, lane);
                 }
         };
         if (chunks > 0) fetch_queries(0), fetch_mixed(0);
@@ -557,9 +556,9 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
         auto of_state = [&](int i) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                b8 parts[RP];
+                b8 parts[3];
                 states.take(i, n, lane, parts);
-                out[n] = multiply<RP - 1>(qa[i], parts, out[n]);
+                out[n] = multiply<2>(qa[i], parts, out[n]);
             }
         };
         auto store = [&](int c) {
@@ -590,9 +589,9 @@ __global__ __launch_bounds__(kSweepThreads) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (i < steps) {
-                        b8 parts[RP];
+                        b8 parts[3];
                         values.take(i, n, lane, parts);
-                        o = multiply<RP - 1>(pa[i], parts, o);
+                        o = multiply<2>(pa[i], parts, o);
                     }
                 done[n] = o;
                 out[n] = f4{};
@@ -699,7 +698,7 @@ DeltaShape delta_shape(const sys_gated_delta_t& p, const DeltaArgs* a)
 size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool grad, void* base, DeltaPlanes* w)
 {
     const size_t value_chunks = (size_t)p.batch * p.value_heads * shape.chunks, key_chunks = (size_t)p.batch * p.key_heads * shape.chunks;
-    const size_t input = p.dtype == SYS_F32 ? 3 : p.dtype == SYS_F16 ? 2 : 1, result = p.dtype == SYS_F32 ? 3 : 2;
+    const size_t input = p.dtype == SYS_F32 ? 3 : p.dtype == SYS_F16 ? 2 : 1;
     const size_t keys = key_chunks * input * kChunk * shape.padded * sizeof(bf16_t), square = value_chunks * kSquare * sizeof(bf16_t);
     const size_t begin = ((uintptr_t)base + 255) / 256 * 256;
     size_t at = begin;
@@ -714,7 +713,7 @@ size_t delta_planes(const sys_gated_delta_t& p, const DeltaShape& shape, bool gr
     take(of.kt, keys);
     take(of.scalars, value_chunks * kScalars * kChunk * sizeof(float));
     if (!grad) {
-        take(of.p, result * square);
+        take(of.p, 3 * square);
     } else {
         take(of.xt, 3 * square);
         take(of.pt, 3 * square);
