@@ -651,10 +651,15 @@ hipError_t launch(bool is_sweep, const sys_gated_delta_t& p, const DeltaArgs& a,
     }
 }
 
-// Whether sequences are so short that they go a position at a time.  12 positions take 17 us so and 14 in chunks where one sequence has 32 heads of 128 x 128 in bf16
-// (8: 12 and 14), 14 and 15 with four of 8 heads of 64 x 128 in fp16; where there are more heads than CUs the chunks' matrices take longer: 16 positions of 16 sequences of
-// 32 heads 43 and 49 (24: 59 and 49), of 64 sequences 128 and 168 (24: 187 and 173), of 32 sequences of 8 heads of 64 x 64 in fp32 18 and 26 (24: 25 and 26).
-bool delta_short(const sys_gated_delta_t& p) { return p.length <= ((long long)p.batch * p.value_heads >= kCus ? 20 : 12); }
+// Whether sequences are so short that they go a position at a time, which takes 2 us a position and hardly goes by the state's size, while a chunk's two launches take
+// longer where inputs have more parts.  Us a position at a time and in chunks: one sequence of 32 heads of 128 x 128 in bf16 10 positions 14.9 and 14.2 (8: 12.5 and 14.1, 12:
+// 17.2 and 14.3), in fp16 12 positions 17.1 and 16.5 (14: 19.4 and 16.8), in fp32 16.3 and 19.1 (14: 18.4 and 19.1); of eight heads of 64 x 64 in bf16 10 positions 12.3 and
+// 12.2, in fp16 12 positions 14.2 and 13.0, in fp32 13.8 and 14.1.  Where there are more heads than CUs the chunks' matrices take longer: 20 positions of 8 sequences of 32 heads of
+// 128 x 128 in bf16 32.7 and 35.2 (24: 37.8 and 35.2), of 32 sequences of eight heads of 64 x 64 22.9 and 24.4 (24: 26.7 and 24.5), of 64 sequences of 32 heads 170 and 202 (24: 200 and 203).
+bool delta_short(const sys_gated_delta_t& p)
+{
+    return p.length <= ((long long)p.batch * p.value_heads >= kCus ? 20 : p.dtype == SYS_BF16 ? 10 : 12);
+}
 
 }  // namespace
 
