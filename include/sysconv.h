@@ -519,8 +519,7 @@ typedef struct {
  *   SYS_ERR_UNSUPPORTED  dimensions beyond the limits above, rows further apart than SYS_MAX_DELTA_ROW elements, pointers off their element's alignment
  *   SYS_ERR_SIZE  negative sizes, no heads, key heads that do not divide the value heads, strides of y that make rows overlap
  * Keys are meant to have a length of about one (sys_head_norm, SYS_NORM_L2): with b_t |k_t|^2 > 2 the recurrence itself grows.
- * Products are taken of numbers split into bf16 parts: 24 bits and more of states and whatever leads to outputs or fp32 results, 16 of the
- * squares of a chunk that only lead to 16-bit gradients of q and k.  Sequences of more than some positions are worked on in chunks of 64: a NaN or infinity in q, k, v, delta or beta then reaches all
+ * Products are taken of numbers split into bf16 parts, 24 bits and more of each, and summed in fp32.  Sequences of more than some positions are worked on in chunks of 64: a NaN or infinity in q, k, v, delta or beta then reaches all
  * positions of its chunk, in its head (of v: in its column), as a NaN, and from there what the formula lets it reach; decays below 2^-10000 are 0.
  * Gradients of an infinite or NaN input are of no value in its head.
  */

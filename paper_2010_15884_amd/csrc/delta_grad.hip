@@ -371,15 +371,16 @@ struct EightFloats {
 // A workgroup a chunk of a key head, through the value heads that share it.  Eight wavefronts: wavefront w the positions of tile w % 4 and half w / 4 of the keys' entries; of the
 // squares the first half has B and the second C.  S, dS' and U of 32 value columns at a time are split on their way into LDS, as the operands
 // that all wavefronts need, and <S, dS'> is taken there.
-// A head of 128 x 128 in bf16 is 48 thousand clocks: 17 in products (70 % of them matrix instructions), 17 in splitting what comes from memory and waiting for it, 6 for the
-// squares, 4 for what they give, the rest barriers and sums.  With two parts instead of three in the products it took 10 % less, but the gradients of the rates were off by
-// 2.4e-6 of themselves instead of 3e-7.  One workgroup of eight wavefronts a CU: its operands and K, Q and their transposes fill LDS.
+// A head of 128 x 128 in bf16 is some 50 thousand clocks: 17 in products (70 % of them matrix instructions), 17 in splitting what comes from memory and waiting for it, 6 for the
+// squares, 7 for what they give, the rest barriers and sums.  With two parts instead of three in the products it took 10 % less, but the gradients of the rates were off by
+// 2.4e-6 of themselves instead of 3e-7.  One workgroup of eight wavefronts a CU: its operands and K, Q and their transposes fill LDS, and the squares take turns with their own
+// transposes (with two parts there was room for both, and the launch of 4 x 2048 positions took 200 us instead of 211, but see delta_tile.h).
 constexpr int kGradThreads = 512;
 
 template <typename T, int KD>
 __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delta_t p, DeltaArgs a, DeltaShape shape, DeltaPlanes w)
 {
-    constexpr int NX = kInputParts<T>, RP = kResultParts<T>, KS = KD / 32, KT = KD / 16, KH = KT / 2, kPitch = kChunk + 8;
+    constexpr int NX = kInputParts<T>, KS = KD / 32, KT = KD / 16, KH = KT / 2, kPitch = kChunk + 8;
     const int shared = shape.apart ? 1 : p.value_heads / p.key_heads, groups = p.value_heads / shared;     // value heads of this workgroup, and groups of them
     const int chunk = blockIdx.x % shape.chunks, rest = blockIdx.x / shape.chunks, first_head = rest % groups * shared, b = rest / groups;
     const int key_head = first_head / (p.value_heads / p.key_heads);
@@ -402,7 +403,12 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
 
     constexpr int kBlock = 64 + 4;                 // an operand's pieces, 17 for 16: lanes that write the four pieces of a row meet other banks
     struct Columns { b8 s[KT][3][kBlock], ds[KT][3][kBlock], u[4][3][kBlock], z[4][3][kBlock], dy[4][NX][kBlock]; };
-    struct Squares { bf16_t b[2][RP][kChunk][kPitch], bt[2][RP][kChunk][kPitch]; };            // B and b C, as they are and transposed
+    // B and b C, as they are and transposed: side by side, or one after the other where K and Q take the room
+    constexpr bool kKeep = NX < 3, kKeepTransposed = NX == 1, kAtOnce = !kKeep;
+    struct Squares {
+        bf16_t v[kAtOnce ? 2 : 1][2][3][kChunk][kPitch];
+        f4 numbers[kAtOnce ? 1 : 24][64];          // a tile's lanes: those that the transposed ones are made of
+    };
     __shared__ union Pool {
         Columns columns;
         Squares squares;
@@ -413,7 +419,6 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
     __shared__ __attribute__((aligned(16))) float scalars[kScalars * kChunk];
 
     // K and Q, which all value heads use, as operands and transposed: as many as LDS has room for
-    constexpr bool kKeep = NX < 3, kKeepTransposed = NX == 1;
     __shared__ b8 kept[2][kKeep ? NX : 1][kKeep ? 4 * KS : 1][64], kept_transposed[2][kKeepTransposed ? 4 * KS : 1][64];
     if (kKeep) {
         for (int i = tid; i < NX * 4 * KS * 64; i += kGradThreads) {
@@ -565,6 +570,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         const bf16_t* own = half ? kp : qp;        // rows of C belong to keys, those of B to queries
         f4 of_strength = {};
         double of_h[4] = {};
+        const int my_tiles = 12 * half + (middle ? 4 * (wave - 1) : 2 * wave);     // (two or four a wavefront)
         // the squares, as they are and transposed: two tiles of columns at a time
         auto squares = [&](auto which, auto second) {
             constexpr int N0 = 2 * decltype(which)::value;
@@ -617,15 +623,27 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                 of_column += __shfl_xor(of_column, 16);
                 of_column += __shfl_xor(of_column, 32);
                 if (again < 16) columns_dg[4 * half + wave][column] = of_column;
-                u2 parts[RP];
+                u2 parts[3];
                 split4(f, parts);
 #pragma unroll
-                for (int m = 0; m < RP; ++m) {
-                    *(u2*)&pool.squares.bt[C][m][column][mine] = parts[m];
+                for (int m = 0; m < 3; ++m) {
+                    if constexpr (kAtOnce) *(u2*)&pool.squares.v[1][C][m][column][mine] = parts[m];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) pool.squares.b[C][m][mine + e][column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
+                    for (int e = 0; e < 4; ++e) pool.squares.v[0][C][m][mine + e][column] = as_bf16(parts[m][e / 2] >> 16 * (e & 1));
                 }
+                if constexpr (!kAtOnce) pool.squares.numbers[my_tiles + N0 + n][again] = f;
             }
+        };
+        auto put_transposed = [&] {
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (n < 2 || middle) {
+                    const int column = tile_row(n, again & 15);
+                    u2 parts[3];
+                    split4(pool.squares.numbers[my_tiles + n][again], parts);
+#pragma unroll
+                    for (int m = 0; m < 3; ++m) *(u2*)&pool.squares.v[0][half][m][column][mine] = parts[m];
+                }
         };
         auto both_squares = [&](auto second) {
             squares(std::integral_constant<int, 0>(), second);
@@ -642,9 +660,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
         // what they and the products with the states give the queries and keys
         f4 of_g = {}, of_end = {};
         const f4 gamma = *(const f4*)(scalars + kGamma * kChunk + mine), left = *(const f4*)(scalars + kLeft * kChunk + mine);
-        auto finish = [&](auto which) {
+        int at = again;
+        auto finish = [&](auto which, bool turned) {
             constexpr int M = decltype(which)::value;
-            int at = again;
             auto operands = [&](int t, int s, b8 (&kb)[NX], b8 (&qb)[NX]) {
 #pragma unroll
                 for (int n = 0; n < NX; ++n) {
@@ -661,11 +679,12 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
             auto pass = [&](bool turned, int s) {
                 __builtin_amdgcn_sched_barrier(0);
                 asm volatile("" : "+v"(at));       // (operands are loaded again rather than kept)
-                b8 of_b[RP], of_c[RP];
+                b8 of_b[3], of_c[3];
+                const auto& of = pool.squares.v[turned && kAtOnce];
 #pragma unroll
-                for (int m = 0; m < RP; ++m) {
-                    of_b[m] = *(const b8*)&(turned ? pool.squares.bt : pool.squares.b)[0][m][row][32 * s + 8 * (again >> 4)];
-                    of_c[m] = *(const b8*)&(turned ? pool.squares.bt : pool.squares.b)[1][m][row][32 * s + 8 * (again >> 4)];
+                for (int m = 0; m < 3; ++m) {
+                    of_b[m] = *(const b8*)&of[0][m][row][32 * s + 8 * (again >> 4)];
+                    of_c[m] = *(const b8*)&of[1][m][row][32 * s + 8 * (again >> 4)];
                 }
 #pragma unroll
                 for (int i = 0; i < KH; ++i) {
@@ -686,21 +705,26 @@ __global__ __launch_bounds__(kGradThreads) void delta_grad_kernel(sys_gated_delt
                     }
                     if (turned) {
                         f4 more = {};
-                        more = multiply<RP - 1>(of_b, qb, more);
-                        dk_all[i] = multiply<RP - 1>(of_c, kb, dk_all[i]) + more;
+                        more = multiply<2>(of_b, qb, more);
+                        dk_all[i] = multiply<2>(of_c, kb, dk_all[i]) + more;
                     } else {
-                        dq_all[i] = multiply<RP - 1>(of_b, kb, dq_all[i]);
-                        dk_all[i] = multiply<RP - 1>(of_c, kb, dk_all[i]);
+                        dq_all[i] = multiply<2>(of_b, kb, dq_all[i]);
+                        dk_all[i] = multiply<2>(of_c, kb, dk_all[i]);
                     }
                 }
             };
-            pass(false, M);
-            if (M) pass(false, 0);
-            pass(true, M);
-            if (!M) pass(true, 1);
+            pass(turned, M);
+            if (turned ? !M : M) pass(turned, 1 - M);
         };
-        if (middle) finish(std::integral_constant<int, 1>());
-        else finish(std::integral_constant<int, 0>());
+        if (middle) finish(std::integral_constant<int, 1>(), false);
+        else finish(std::integral_constant<int, 0>(), false);
+        if constexpr (!kAtOnce) {
+            lds_barrier();
+            put_transposed();
+            lds_barrier();
+        }
+        if (middle) finish(std::integral_constant<int, 1>(), true);
+        else finish(std::integral_constant<int, 0>(), true);
         const double dg_sum = row_sums(of_h[0] + (double)of_g[0], of_h[1] + (double)of_g[1], of_h[2] + (double)of_g[2], of_h[3] + (double)of_g[3]);
         const float db_sum = row_sums(of_strength[0], of_strength[1], of_strength[2], of_strength[3]), end_sum = row_sums(of_end[0], of_end[1], of_end[2], of_end[3]);
         if ((again & 15) < 4) {

@@ -9,9 +9,9 @@
 //
 // Precision: v_mfma_f32_16x16x32_bf16 on numbers that are split into bf16 parts, accumulated in fp32.  Inputs in bf16 are one part, in fp16
 // two, in fp32 three, exactly; states, U and what leads to them are three (24 bits), and products of parts i and j are taken up to
-// i + j = 2, so that what is left out is below 2^-24 of the term, as in split_bf16.h.  Outputs in 16 bits are no exception: what a position reads of the state and what its
-// chunk writes cancel where a value is written over a larger one, and with two parts it came out off by 2^-17 of the old value (three cost 3 % of the forward call in bf16,
-// 8 in fp16).  Two parts (16 bits) have the squares B and C behind the gradients of q and k, where these are 16-bit.
+// i + j = 2, so that what is left out is below 2^-24 of the term, as in split_bf16.h.  What only leads to 16-bit results is no exception: what a position reads of the state
+// before its chunk and what the chunk writes cancel where values are written over larger ones, and with two parts outputs and the gradients of q and k came out off by 2^-17 of the
+// old values (three cost 3 % of the forward call in bf16, 8 in fp16, and 2 of the gradients' in bf16).
 // The split keeps fp32's range; infinities in it become NaN, and a NaN reaches all positions of its chunk (0 times NaN).
 //
 // Layout: D of an instruction holds rows 4 (lane / 16) + i of column lane % 16, B takes rows 8 (lane / 16) + j of column lane % 16.
@@ -36,9 +36,6 @@ constexpr int kSquare = kChunk * kChunk;           // elements of X, P
 
 // Parts of an input.
 template <typename T> constexpr int kInputParts = sizeof(T) == 4 ? 3 : std::is_same<T, f16_t>::value ? 2 : 1;
-// Parts of what leads to gradients of q and k of this type alone.
-template <typename T> constexpr int kResultParts = sizeof(T) == 4 ? 3 : 2;
-
 __device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // c += a b, parts whose order is at most MOST, the small ones first.

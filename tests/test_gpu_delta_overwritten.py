@@ -45,3 +45,35 @@ def test_new_values_over_large_ones(dtype, key_dim, value_dim, heads, length):
     error = size(R.wide(y) - want["y"])[0]
     allowed = 2.4e-6 * (sizes / (length * value_dim)).sqrt() + (torch.finfo(dtype).eps / 2) * size(want["y"])[0]
     assert (error <= allowed).all(), (error / allowed).max()
+
+
+@pytest.mark.parametrize("length", [64, 150])
+@pytest.mark.parametrize("key_dim,shared", [(16, 1), (32, 2)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_gradients_of_queries_behind_an_overwritten_state(dtype, key_dim, shared, length):
+    """dq = scale S dy, with S the state behind the position: small where its chunk has written over all that was there, though the state before the chunk was large.
+
+    The first key_dim positions have the unit vectors as keys and strength 1, so that the state behind them has nothing of the old one's m = 3000 a column and entry left.  In
+    the chunk dq is the sum of scale e^G S dy over value_dim columns and of B K, which takes it back: products of numbers of 24 bits (2^-24 of a term, as often up as down)
+    and sums of value_dim and of two times 64 terms (U, B, and B K), whose squares add up to value_dim (m |dy|)^2 / value_dim each, in norm over the entries: sqrt(2 value_dim + 4 * 64) 2^-24
+    m |dy| for the sums and no more for the numbers.  On top of it comes the rounding to the type."""
+    g = torch.Generator(device="cuda").manual_seed(key_dim + length)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    value_dim, heads = 48, 2
+    k = torch.nn.functional.normalize(rand(1, length, heads // shared, key_dim), dim=-1) * 0.99
+    k[0, :key_dim] = torch.eye(key_dim, device="cuda")[:, None]
+    k, q, v = k.to(dtype), rand(1, length, heads // shared, key_dim).to(dtype), rand(1, length, heads, value_dim).to(dtype)
+    dy = rand(1, length, heads, value_dim)
+    dy[0, :key_dim] = 0.0                          # (what was large is not asked for)
+    dy = dy.to(dtype)
+    state = 3000.0 * rand(1, heads, key_dim, value_dim)
+    delta, A = torch.full((1, length, heads), 0.01, device="cuda").to(dtype), torch.zeros(heads, device="cuda")
+    beta = torch.full((1, length, heads), 0.5, device="cuda").to(dtype)
+    beta[0, :key_dim] = 1.0
+    got = B.sys_gated_delta_rule_backward(dy, q, k, v, delta, A, beta, scale=1.0, d_state=state)
+    want = D.gated_delta(q, k, v, delta, A, beta, scale=1.0, softplus=False, sigmoid_beta=False, state=state, dy=dy)["dq"]
+    error = (R.wide(got.dq) - want).norm(dim=3)[0, key_dim:].norm(dim=1)           # of a position, over heads and entries
+    size = R.wide(dy).norm(dim=3)[0, key_dim:].norm(dim=1)
+    allowed = 2 * (2 * value_dim + 4 * 64) ** 0.5 * 2.0 ** -24 * 3000.0 * key_dim ** 0.5 * size + (torch.finfo(dtype).eps / 2) * want[0, key_dim:].flatten(1).norm(dim=1)
+    assert float(want[0, key_dim:].abs().max()) < 100.0
+    assert (error <= allowed).all(), (error / allowed).max()
