@@ -475,8 +475,8 @@ typedef struct {
  *   d_q, d_yq  [batch, length, q_heads, dim];  d_k, d_yk  [batch, length, k_heads, dim] (none with k_heads 0)
  *   d_wq, d_wk (optional)  [dim]
  *   d_cos, d_sin  [positions, rotary/2] fp32 (where rotary > 0): pair i at position p turns by the angle of row p, column i
- *   d_positions (optional)  [batch, length]: the table's row of each token; one outside 0 .. positions-1 marks a token that is not
- *            there: its rows are 0, and so are its gradients.  Without it position t is row t (length <= positions: SYS_ERR_SIZE).
+ *   d_positions (optional; read where rotary > 0)  [batch, length]: the table's row of each token; one outside 0 .. positions-1
+ *            marks a token that is not there: its rows are 0, and so are its gradients.  Without it position t is row t (length <= positions: SYS_ERR_SIZE).
  *   Rows behind a sequence's length are 0.  Squares are summed in fp32: a head with entries beyond 10^18 comes out as 0.
  */
 int sys_head_norm(const sys_head_norm_t *p, const void *d_q, const void *d_k, const void *d_wq, const void *d_wk,
@@ -532,6 +532,9 @@ size_t sys_gated_delta_rule_workspace(const sys_gated_delta_t *p);
  * Its gradients.  d_dy [batch, length, value_heads, value_dim]; d_dstate_out (optional): gradient of state_out.
  * Written, all contiguous: d_dq, d_dk (summed over the value heads of a key head), d_dv, d_ddelta, d_dbeta like their inputs; d_dA, d_ddelta_bias (optional;
  * it needs d_delta_bias) [value_heads] fp32; d_dstate like d_state (optional; it needs d_state).
+ * Workspaces: for every 64 positions of a sequence 50 KiB a value head and 48 (bf16), 96 (fp16) or 144 KiB (fp32) a key head for the forward call,
+ * 268 and 64, 128 or 192 KiB for the gradients, with 128 entries of keys and values: 155 and 630 MB for 4 sequences of 2048 with 8 key heads and 16
+ * value heads in bf16.  Keys of up to 64 entries take half of what a key head has.
  */
 int sys_gated_delta_rule_backward(const sys_gated_delta_t *p, const void *d_dy, const void *d_q, const void *d_k, const void *d_v,
                                   const void *d_delta, const float *d_A, const void *d_beta, const float *d_delta_bias,

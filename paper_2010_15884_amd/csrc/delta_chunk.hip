@@ -5,9 +5,9 @@
 // parts through LDS with three barriers a chunk; operands that do not depend on the state are loaded a chunk ahead.  Four more wavefronts take S and U from LDS
 // and make the outputs of them (or store them for the gradients) in what time the barriers leave.
 //
-// 4096 positions of 16 key heads and 32 value heads of 128 in bf16, 8600 us as torch operators: 42 us + 98 us.  The first launch moves 150 MB at 3.6 TB/s, three workgroups
+// 4096 positions of 16 key heads and 32 value heads of 128 in bf16, 8400 us as torch operators: 132 us (43 + 98 by the profiler).  The first launch moves 162 MB at 3.8 TB/s, three workgroups
 // a CU that load, work and store in turn; each operand that is not stored (the quarter of X and P that is 0) is time.  The second is a chain: 64 chunks of 2900 clocks, 870 + 960 + 820 for the three
-// products and 300 at their barriers, with 590 of matrix instructions in each of the four wavefronts of the chain and 320 beside them.  What is left in a
+// products and 300 at their barriers, with 590 of matrix instructions in each of the four wavefronts of the chain and 450 beside them.  What is left in a
 // phase is reading and writing LDS and the latency of an instruction after the other; U from U and S of the chunk before, one exchange a chunk, would need
 // two more matrices a chunk of the first launch.  With one group of wavefronts for everything the sweep took 107 us for 16 columns (the outputs in the chain's way).
 #include "delta_tile.h"

@@ -13,9 +13,9 @@
 // and what else there is comes from the products with the states: q_i . (e^G S dO)_i + b_i k_i . (-e^G S Z)_i from the position on, E_i k_i . (dS' U_i) up
 // to it, e^(G_end) <S, dS'> for all; sums over the positions of a chunk are in 64 bits.
 //
-// Four sequences of 2048, 8 key heads and 16 value heads of 128 in bf16 (22200 us as torch operators): 50 us for the chunks' matrices, 113 for the sweep forwards,
-// 145 for the one backwards, 210 for the chunks' gradients, 6 + 4 for what gates and rates get.  S, dS', U and Z are 400 MB that are written and read once: the sweep
-// forwards takes 75 us without its stores, and the chunks' gradients read 546 MB at 2.6 TB/s over the launch, more while they go through the columns.
+// Four sequences of 2048, 8 key heads and 16 value heads of 128 in bf16 (22000 us as torch operators): 499 us.  By the profiler, under which they add up to 5 % more, 48 us for the chunks'
+// matrices, 109 for the sweep forwards, 141 for the one backwards, 215 for the chunks' gradients, 6 + 5 for what gates and rates get.  S, dS', U and Z are 400 MB that are written and read once: the sweep
+// forwards takes 75 us without its stores, and the chunks' gradients read 546 MB at 2.5 TB/s over the launch, more while they go through the columns.
 #include "delta_tile.h"
 #include "launch.h"
 

@@ -6,8 +6,8 @@
 // of one token side by side and walks through the rest of them with the next ones' loads in flight: the tables' rows and the weights are
 // loaded once a token.
 // Bound by memory: 16-bit entries cost 4 bytes in the forward pass and some five vector instructions.  8192 tokens of 36 heads of 128 in bf16 take 32 us (4.9 TB/s, a
-// copy's rate), the gradients of 18 heads of 256 58 us and 4 for the join of the weights' sums (3.9 TB/s; eight wavefronts a CU, which wait for 59 % of their time and keep the vector
-// units busy for half of it), 32 tokens of 40 heads 4 us, a launch.
+// copy's rate), the gradients of 18 heads of 256 62 us (56 and 5 for the join of the weights' sums by the profiler; 4.1 TB/s over the first; eight wavefronts a CU, which wait for 59 % of
+// their time and keep the vector units busy for half of it), 32 tokens of 40 heads 4 us, a launch.
 #include "launch.h"
 #include "sequence.h"
 
@@ -391,8 +391,9 @@ __global__ __launch_bounds__(kJoinThreads) void head_norm_join_kernel(sys_head_n
 
 // ---------------------------------------------------------------- launches
 
-// Workgroups of the gradients, at most: as many as the registers of an instance leave resident, so that none starts behind the others.  8192 tokens of 18 heads
-// of 256 in bf16 (V = 8, 199 registers): 51 us with 512, 59 with 768, 58 with 1024, 65 with 256; of 72 (V = 4, 133): 36, 32, 40, 51; of 50 (V = 1, 91): 42, 37, 34, 67.
+// Workgroups of the gradients, at most: as many as the registers of an instance leave resident, so that none starts behind the others.  Whole calls on 8192 tokens, one behind the
+// other, us with 512, 768, 1024 and 256: 18 heads of 256 in bf16 (V = 8, 199 registers) 60, 72, 67, 77; of 36 heads of 128 62, 76, 70, 80; of 72 heads of 72 (V = 4, 133) 105, 92, 112, 166;
+// of 36 heads of 128 in fp32 (V = 4 as well) 97, 99, 111, 111; of 50 heads of 50 (V = 1, 91) 101, 90, 82, 169; of 16 heads of 200 in fp32 (V = 1, S = 4) 93, 107, 96, 133.
 constexpr int kGradBlocks = 1024;
 template <int V, int S> constexpr int kResidentBlocks = V * S == 1 ? kGradBlocks : V == 4 ? 768 : 512;
 
